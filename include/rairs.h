@@ -333,6 +333,128 @@ int rairs_assign(rairs_index_t *h, const float *d_vectors, int64_t n, int n_cand
 int rairs_pq_encode(const float *d_codebook, int d, int M, const float *d_vectors, int64_t n,
                     uint8_t *d_codes, void *hip_stream);
 
+/* ---- the query side of an index that stands: projection and log probabilities ---------------- */
+
+/*
+ * The vectors of an index are embeddings that a model learned; what is tuned while they stay is the
+ * way a query takes to them.  rairs_project puts a batch of rows of many tenants through a projection
+ * that all share and a low-rank adapter of each row's own; rairs_logprob says how probable items are
+ * under a softmax over inner products with a table of vectors, and its backward pass with
+ * rairs_project_backward trains the adapters.
+ *
+ * These calls need no index.  They only enqueue work on `hip_stream`, allocate nothing and read
+ * nothing back; scratch memory is the caller's: `d_ws`, 256-byte aligned, at least as many bytes as the
+ * call's rairs_..._workspace_bytes says (RAIRS_EWORKSPACE otherwise, nothing enqueued), not shared by
+ * calls that may overlap.  Calls with workspaces and outputs of their own may overlap on any streams,
+ * and all of them may be captured into a graph.  Inputs and outputs must not overlap in memory.
+ * Row strides (ld_...) are in elements and at least the row's length.  Results do not depend on the
+ * order in which workgroups run: the same call gives the same bits.
+ */
+enum { RAIRS_F32 = 0, RAIRS_BF16 = 1, RAIRS_U8 = 2 };
+#define RAIRS_MAX_RANK 128          /* of an adapter */
+#define RAIRS_MAX_ADAPTERS 4096
+#define RAIRS_MAX_ROWS (1 << 24)    /* rows of a batch */
+#define RAIRS_MAX_WIDTH 16384       /* d_in, d_out; d of a table's rows */
+#define RAIRS_MAX_TOP 64            /* most probable rows that rairs_logprob returns */
+
+/*
+ * y = W x + scale[a] B[a] (A[a] x): the shared projection and n_adapters low-rank adapters, all of one
+ * rank (adapters of smaller ranks are filled up with zeros), all of type dtype (RAIRS_F32 or
+ * RAIRS_BF16), contiguous device memory.
+ */
+typedef struct {
+    int32_t d_in, d_out, rank, n_adapters, dtype;   /* n_adapters == 0: the shared projection alone */
+    const void *W;           /* [d_out][d_in] */
+    const void *A;           /* [n_adapters][rank][d_in] */
+    const void *B;           /* [n_adapters][d_out][rank] */
+    const float *scale;      /* [n_adapters], or NULL: 1 */
+} rairs_projection_t;
+
+/*
+ *   d_x        device [n] rows of d_in, type dtype
+ *   d_adapter  device [n] int32: the row's adapter; a value outside [0, n_adapters) means none.  Rows of
+ *              an adapter need not be together.  NULL: no row has one
+ *   d_y        device [n] rows of d_out, y_dtype RAIRS_F32 or dtype
+ * Sums are held in fp32; A[a] x enters the second product with 16 or more bits.  n == 0 is a
+ * successful no-op.
+ */
+size_t rairs_project_workspace_bytes(const rairs_projection_t *p, int64_t n);
+int rairs_project(const rairs_projection_t *p, const void *d_x, int64_t ld_x, int64_t n, const int32_t *d_adapter, void *d_y,
+                  int64_t ld_y, int y_dtype, void *d_ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Gradients of rairs_project for d_dy, device [n] rows of d_out, type dtype:
+ *   d_dx  [n] rows of d_in          W^T dy + scale A^T (B^T dy)               (NULL: not wanted)
+ *   d_dA  [n_adapters][rank][d_in]  sum over an adapter's rows of scale (B^T dy) x^T
+ *   d_dB  [n_adapters][d_out][rank] sum over an adapter's rows of scale dy (A x)^T
+ * all of type dtype, d_dA and d_dB both or neither; an adapter without rows gets zeros.  W is shared and
+ * stays: it has no gradient here.  n == 0 writes the zeros of d_dA and d_dB.
+ */
+size_t rairs_project_backward_workspace_bytes(const rairs_projection_t *p, int64_t n);
+int rairs_project_backward(const rairs_projection_t *p, const void *d_x, int64_t ld_x, int64_t n, const int32_t *d_adapter,
+                           const void *d_dy, int64_t ld_dy, void *d_dx, int64_t ld_dx, void *d_dA, void *d_dB, void *d_ws,
+                           size_t ws_bytes, void *hip_stream);
+
+/*
+ * rairs_search of what rairs_project makes of d_x, in one call: d_queries, device [n][d] fp32, receives the
+ * projected rows, which the search then reads (the projection's d_out must be the index's d).  d_ws is
+ * rairs_project's; the search uses the handle's workspace as rairs_search does.
+ */
+int rairs_search_projected(rairs_index_t *h, const rairs_projection_t *p, const void *d_x, int64_t ld_x, int64_t n,
+                           const int32_t *d_adapter, float *d_queries, int k, int nprobe, int refine_k, int64_t *d_out_ids,
+                           float *d_out_dists, void *d_ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * A table of vectors and how it is scored: l_v = scale <q, t_v>, scale > 0 and finite.
+ * d_live: device words, bit v & 31 of word v >> 5 set where a query may see row v; ld_live words from one
+ * query's mask to the next, 0 for a mask that all queries share; NULL: all rows are live.  Rows of the
+ * table that no query sees may hold anything.  V < 2^31 - 64.
+ */
+typedef struct {
+    const void *vectors;     /* device [V] rows of d */
+    int64_t ld, V;
+    int32_t d, dtype;        /* RAIRS_F32, RAIRS_BF16, or RAIRS_U8 */
+    float scale;
+    const uint32_t *d_live;
+    int64_t ld_live;
+} rairs_table_t;
+
+/* The index's own vectors as a table (row v is vector id v; fp32 or bytes, as the device keeps them), scale 1,
+   all rows live: deleted vectors are still there, a mask hides them.  Valid until rairs_free. */
+int rairs_index_table(const rairs_index_t *h, rairs_table_t *out);
+
+/*
+ *   d_q        device [n] rows of d, q_dtype: the table's type (RAIRS_F32 for RAIRS_U8)
+ *   d_targets  device [n] int64: the row whose log probability is asked for; outside [0, V): none
+ *   d_logp     device [n] fp32 log p of the target: 0 without a target, -inf if the mask hides it
+ *   d_lse      device [n] fp32 log sum exp of the live rows' l (-inf if there is none)
+ *   d_entropy  device [n] fp32 -sum p log p (0 without a live row), or NULL
+ *   d_top_ids  device [n][top] int64, d_top_logp [n][top] fp32: the `top` most probable live rows, 0 <=
+ *              top <= RAIRS_MAX_TOP, ordered by (inner product in float64, row id): the larger product
+ *              first, of equal ones the smaller id; missing entries are id -1, -inf.  A query whose
+ *              products are not all finite may get missing entries instead.
+ * Products of fp32 rows are as exact as fp32 sums are.  n == 0 is a successful no-op.
+ */
+size_t rairs_logprob_workspace_bytes(const rairs_table_t *t, int64_t n, int q_dtype, int top);
+int rairs_logprob(const rairs_table_t *t, const void *d_q, int64_t ld_q, int q_dtype, int64_t n, const int64_t *d_targets,
+                  float *d_logp, float *d_lse, float *d_entropy, int top, int64_t *d_top_ids, float *d_top_logp, void *d_ws,
+                  size_t ws_bytes, void *hip_stream);
+
+/*
+ * Gradients of sum_i dlogp[i] logp[i] + dentropy[i] entropy[i] with respect to the queries and the table:
+ *   G[i][v] = scale (dlogp[i] (1[v = target] - p[v]) - dentropy[i] p[v] (log p[v] + entropy[i]))
+ *   d_dq [n] rows of d, the queries' type: G T;   d_dtable [V] rows of d, the table's type: G^T q,
+ * either may be NULL; d_dtable only for tables that are not RAIRS_U8 (zeros in rows that no query sees).
+ *   d_lse, d_entropy  what rairs_logprob wrote; d_dlogp [n] fp32; d_dentropy [n] fp32 or NULL (d_entropy may
+ *                     then be NULL too)
+ * A target that is none or that the mask hides passes no gradient; a row that passes none at all (dlogp
+ * and dentropy 0) may hold anything and gets zeros.
+ */
+size_t rairs_logprob_backward_workspace_bytes(const rairs_table_t *t, int64_t n, int q_dtype, int table_grad);
+int rairs_logprob_backward(const rairs_table_t *t, const void *d_q, int64_t ld_q, int q_dtype, int64_t n, const int64_t *d_targets,
+                           const float *d_lse, const float *d_entropy, const float *d_dlogp, const float *d_dentropy, void *d_dq,
+                           int64_t ld_dq, void *d_dtable, int64_t ld_dtable, void *d_ws, size_t ws_bytes, void *hip_stream);
+
 const char *rairs_last_error(void);
 
 #ifdef __cplusplus

@@ -6,8 +6,10 @@ library is missing, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -26,6 +28,9 @@ EXPORTS = ("rairs_index_upload", "rairs_search", "rairs_free", "rairs_workspace_
            "rairs_scan", "rairs_refine", "rairs_set_scan_mode", "rairs_set_profiling", "rairs_get_stage_ms",
            "rairs_get_stage_ms_mean",
            "rairs_get_dco", "rairs_get_scan_stats", "rairs_scan_kernel_name", "rairs_index_bytes", "rairs_pq_encode", "rairs_assign",
+           "rairs_project", "rairs_project_workspace_bytes", "rairs_project_backward", "rairs_project_backward_workspace_bytes",
+           "rairs_search_projected", "rairs_index_table",
+           "rairs_logprob", "rairs_logprob_workspace_bytes", "rairs_logprob_backward", "rairs_logprob_backward_workspace_bytes",
            "rairs_last_error")
 
 
@@ -64,6 +69,8 @@ def load() -> C.CDLL:
         lib.rairs_last_error.restype = C.c_char_p
         lib.rairs_workspace_bytes.restype = C.c_size_t
         lib.rairs_scan_kernel_name.restype = C.c_char_p
+        for name in ("rairs_project", "rairs_project_backward", "rairs_logprob", "rairs_logprob_backward"):
+            getattr(lib, name + "_workspace_bytes").restype = C.c_size_t
         for name in EXPORTS:
             getattr(lib, name)
         _lib = lib
@@ -107,6 +114,211 @@ def pq_encode(codebook: torch.Tensor, vectors: torch.Tensor, stream=None) -> tor
                                C.c_int64(n), _dev(codes, torch.uint8, "codes") if n else C.c_void_p(0),
                                _stream_ptr(stream)))
     return codes
+
+
+# --- the query side: projection with low-rank adapters, log probabilities -----------------------
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.uint8: 2}
+MAX_TOP = 64
+
+
+class _Projection(C.Structure):
+    _fields_ = [("d_in", C.c_int32), ("d_out", C.c_int32), ("rank", C.c_int32), ("n_adapters", C.c_int32),
+                ("dtype", C.c_int32), ("W", C.c_void_p), ("A", C.c_void_p), ("B", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class _Table(C.Structure):
+    _fields_ = [("vectors", C.c_void_p), ("ld", C.c_int64), ("V", C.c_int64), ("d", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_float), ("d_live", C.c_void_p), ("ld_live", C.c_int64)]
+
+
+@contextlib.contextmanager
+def _on(device, stream):
+    """The device of a call's tensors current, and `stream` the stream that its workspace and results are
+    allocated for (None: the device's current one)."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream()
+        else:
+            with torch.cuda.stream(stream):
+                yield stream
+
+
+def _rows(t: torch.Tensor, name: str, dtype, cols: int, device):
+    """A device matrix whose rows are contiguous (any stride between them): pointer and row stride."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.ndim == 2 and t.dtype == dtype
+            and t.shape[1] == cols and (cols == 1 or t.shape[0] == 0 or t.stride(1) == 1)):
+        raise TypeError(f"{name}: expected a matrix of {dtype} with {cols} contiguous columns on {device}")
+    ld = t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
+    return C.c_void_p(t.data_ptr() if t.numel() else 0), C.c_int64(ld)
+
+
+def _vec(t, name: str, dtype, n: int, device) -> C.c_void_p:
+    if t is None:
+        return C.c_void_p(0)
+    if not (isinstance(t, torch.Tensor) and t.device == device and t.is_cuda and t.dtype == dtype and t.shape == (n,)
+            and t.is_contiguous()):
+        raise TypeError(f"{name}: expected {n} contiguous values of {dtype} on {device}")
+    return C.c_void_p(t.data_ptr() if n else 0)
+
+
+def _workspace(need: int):
+    if need == 0:
+        return None, C.c_void_p(0), C.c_size_t(0)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    return ws, C.c_void_p(ws.data_ptr()), C.c_size_t(need)
+
+
+class Projection:
+    """A projection that all tenants share, W [d_out][d_in], and the low-rank adapters of each, A [n][rank][d_in],
+    B [n][d_out][rank], scale [n] (None: 1): y = W x + scale[a] B[a] (A[a] x).  All of float32 or bfloat16,
+    contiguous on one device; scale is float32.  Holds the tensors, copies nothing."""
+
+    def __init__(self, W: torch.Tensor, A: Optional[torch.Tensor] = None, B: Optional[torch.Tensor] = None,
+                 scale: Optional[torch.Tensor] = None):
+        if W.ndim != 2 or W.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("W must be a matrix of float32 or bfloat16")
+        if (A is None) != (B is None):
+            raise ValueError("A and B: both or neither")
+        self.W, self.A, self.B, self.scale = W, A, B, scale
+        self.d_out, self.d_in = W.shape
+        self.n_adapters, self.rank = (0, 0) if A is None else (A.shape[0], A.shape[1])
+        s = self._s = _Projection()
+        s.d_in, s.d_out, s.rank, s.n_adapters, s.dtype = self.d_in, self.d_out, self.rank, self.n_adapters, DTYPES[W.dtype]
+        s.W = _dev(W, W.dtype, "W")
+        if A is not None:
+            if A.shape != (self.n_adapters, self.rank, self.d_in) or B.shape != (self.n_adapters, self.d_out, self.rank):
+                raise ValueError("A must be [n][rank][d_in] and B [n][d_out][rank]")
+            if A.device != W.device or B.device != W.device:
+                raise TypeError("W, A and B must be on one device")
+            s.A, s.B = _dev(A, W.dtype, "A"), _dev(B, W.dtype, "B")
+            s.scale = _vec(scale, "scale", torch.float32, self.n_adapters, W.device)
+
+    def project(self, x: torch.Tensor, adapter: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                out_dtype=None, stream=None) -> torch.Tensor:
+        """rairs_project: rows [n][d_in] to [n][d_out], float32 (what a search takes) unless out or out_dtype
+        says W's type; adapter [n] int32, a value outside [0, n_adapters) is none."""
+        lib, dev, n = load(), self.W.device, x.shape[0]
+        px, ldx = _rows(x, "x", self.W.dtype, self.d_in, dev)
+        pa = _vec(adapter, "adapter", torch.int32, n, dev)
+        with _on(dev, stream) as st:
+            if out is None:
+                out = torch.empty((n, self.d_out), dtype=out_dtype or torch.float32, device=dev)
+            elif out.shape[0] != n or (out_dtype is not None and out.dtype != out_dtype):
+                raise ValueError("out does not fit")
+            if out.dtype not in DTYPES:
+                raise TypeError(f"out: unsupported type {out.dtype}")
+            py, ldy = _rows(out, "out", out.dtype, self.d_out, dev)
+            need = lib.rairs_project_workspace_bytes(C.byref(self._s), C.c_int64(n))
+            ws, pw, nw = _workspace(need)
+            _check(lib.rairs_project(C.byref(self._s), px, ldx, C.c_int64(n), pa, py, ldy, C.c_int(DTYPES[out.dtype]),
+                                     pw, nw, _stream_ptr(st)))
+        return out
+
+    def backward(self, x: torch.Tensor, adapter: Optional[torch.Tensor], dy: torch.Tensor, x_grad: bool = True,
+                 adapter_grad: bool = True, stream=None):
+        """rairs_project_backward: (dx, dA, dB) for dy [n][d_out] of W's type; None for what is not wanted."""
+        lib, dev, n, t = load(), self.W.device, x.shape[0], self.W.dtype
+        px, ldx = _rows(x, "x", t, self.d_in, dev)
+        pg, ldg = _rows(dy, "dy", t, self.d_out, dev)
+        if dy.shape[0] != n:
+            raise ValueError("dy must have as many rows as x")
+        pa = _vec(adapter, "adapter", torch.int32, n, dev)
+        adapter_grad = adapter_grad and self.n_adapters > 0
+        with _on(dev, stream) as st:
+            dx = torch.empty((n, self.d_in), dtype=t, device=dev) if x_grad else None
+            da = torch.empty_like(self.A) if adapter_grad else None
+            db = torch.empty_like(self.B) if adapter_grad else None
+            need = lib.rairs_project_backward_workspace_bytes(C.byref(self._s), C.c_int64(n))
+            ws, pw, nw = _workspace(need)
+            _check(lib.rairs_project_backward(
+                C.byref(self._s), px, ldx, C.c_int64(n), pa, pg, ldg,
+                C.c_void_p(dx.data_ptr() if x_grad and n else 0), C.c_int64(self.d_in),
+                C.c_void_p(da.data_ptr() if adapter_grad else 0), C.c_void_p(db.data_ptr() if adapter_grad else 0),
+                pw, nw, _stream_ptr(st)))
+        return dx, da, db
+
+
+class LogProb(NamedTuple):
+    logp: torch.Tensor                       # [n] log p of each query's target
+    lse: torch.Tensor                        # [n] log sum exp of its live rows
+    entropy: Optional[torch.Tensor]          # [n]
+    top_ids: Optional[torch.Tensor]          # [n][top] int64
+    top_logp: Optional[torch.Tensor]         # [n][top]
+
+
+def _table(table: torch.Tensor, scale: float, live, n: int):
+    dev = table.device
+    if table.dtype not in DTYPES:
+        raise TypeError(f"table: unsupported type {table.dtype}")
+    if table.ndim != 2:
+        raise TypeError("table must be a matrix")
+    t = _Table()
+    t.vectors, ld = _rows(table, "table", table.dtype, table.shape[1], dev)
+    t.ld, t.V, t.d, t.dtype, t.scale = ld.value, table.shape[0], table.shape[1], DTYPES[table.dtype], scale
+    return _with_mask(t, live, n, dev)
+
+
+def _with_mask(t, live, n: int, dev):
+    if live is not None:
+        words = (t.V + 31) // 32
+        if live.ndim == 1:
+            t.d_live, t.ld_live = _vec(live, "live", torch.int32, words, dev), 0
+        else:
+            if live.shape[0] != n:
+                raise ValueError("live: one mask, or one per query")
+            t.d_live, ld = _rows(live, "live", torch.int32, words, dev)
+            t.ld_live = ld.value
+    return t
+
+
+def _logprob(t, q, targets, top, entropy, stream) -> LogProb:
+    lib, dev, n = load(), q.device, q.shape[0]
+    qt = torch.float32 if t.dtype == DTYPES[torch.uint8] else {v: k for k, v in DTYPES.items()}[t.dtype]
+    pq, ldq = _rows(q, "q", qt, t.d, dev)
+    pt = _vec(targets, "targets", torch.int64, n, dev)
+    with _on(dev, stream) as st:
+        need = lib.rairs_logprob_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(DTYPES[qt]), C.c_int(top))
+        ws, pw, nw = _workspace(need)
+        r = LogProb(torch.empty(n, device=dev), torch.empty(n, device=dev), torch.empty(n, device=dev) if entropy else None,
+                    torch.empty((n, top), dtype=torch.int64, device=dev) if top > 0 else None,
+                    torch.empty((n, top), device=dev) if top > 0 else None)
+        p = [C.c_void_p(x.data_ptr() if x is not None and n else 0) for x in r]
+        _check(lib.rairs_logprob(C.byref(t), pq, ldq, C.c_int(DTYPES[qt]), C.c_int64(n), pt, p[0], p[1], p[2], C.c_int(top), p[3],
+                                 p[4], pw, nw, _stream_ptr(st)))
+    return r
+
+
+def logprob(q: torch.Tensor, table: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, top: int = 0,
+            live: Optional[torch.Tensor] = None, entropy: bool = True, stream=None) -> LogProb:
+    """rairs_logprob: softmax over scale * <q, row> of the table's live rows.  q [n][d] and table [V][d] of
+    float32 or bfloat16 (a uint8 table: float32 queries), rows may be strided; targets [n] int64 (outside
+    [0, V): none); live: int32 words of 32 rows each, [words] for all queries or [n][words]."""
+    return _logprob(_table(table, scale, live, q.shape[0]), q, targets, top, entropy, stream)
+
+
+def logprob_backward(q: torch.Tensor, table: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor,
+                     scale: float = 1.0, live: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                     dentropy: Optional[torch.Tensor] = None, q_grad: bool = True, table_grad: bool = False, stream=None):
+    """rairs_logprob_backward: (dq, dtable) for the gradients dlogp, dentropy [n] of logprob's results; None for
+    what is not wanted.  lse and entropy are logprob's."""
+    lib, dev, n = load(), q.device, q.shape[0]
+    t = _table(table, scale, live, n)
+    qt = torch.float32 if table.dtype == torch.uint8 else table.dtype
+    pq, ldq = _rows(q, "q", qt, t.d, dev)
+    f = [_vec(x, name, torch.float32, n, dev) for x, name in
+         ((lse, "lse"), (entropy, "entropy"), (dlogp, "dlogp"), (dentropy, "dentropy"))]
+    pt = _vec(targets, "targets", torch.int64, n, dev)
+    with _on(dev, stream) as st:
+        need = lib.rairs_logprob_backward_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(DTYPES[qt]), C.c_int(int(table_grad)))
+        ws, pw, nw = _workspace(need)
+        dq = torch.empty((n, t.d), dtype=qt, device=dev) if q_grad else None
+        dt = torch.empty((t.V, t.d), dtype=table.dtype, device=dev) if table_grad else None
+        _check(lib.rairs_logprob_backward(
+            C.byref(t), pq, ldq, C.c_int(DTYPES[qt]), C.c_int64(n), pt, f[0], f[1], f[2], f[3],
+            C.c_void_p(dq.data_ptr() if q_grad and n else 0), C.c_int64(t.d),
+            C.c_void_p(dt.data_ptr() if table_grad else 0), C.c_int64(t.d), pw, nw, _stream_ptr(st)))
+    return dq, dt
 
 
 def host_struct(hx):
@@ -242,6 +454,35 @@ class Index:
             C.c_int(nprobe), C.c_int(refine_k), _dev(out_ids, torch.int64, "out_ids"),
             _dev(out_dists, torch.float32, "out_dists"), _stream_ptr(stream), C.byref(g)))
         return SearchGraph(self._lib, g, (queries, out_ids, out_dists))
+
+    # --- the query side -------------------------------------------------------------------
+    def search_projected(self, projection: Projection, x: torch.Tensor, adapter, k: int, nprobe: int, refine_k: int,
+                         stream=None):
+        """rairs_search_projected: rows [n][d_in] through the projection and into the search; returns ids,
+        distances and the queries that were searched with [n][d]."""
+        n, dev = x.shape[0], projection.W.device
+        px, ldx = _rows(x, "x", projection.W.dtype, projection.d_in, dev)
+        pa = _vec(adapter, "adapter", torch.int32, n, dev)
+        with _on(dev, stream) as st:
+            self._reserve(n, nprobe, refine_k)
+            ids = torch.empty((n, k), dtype=torch.int64, device=dev)
+            dists = torch.empty((n, k), dtype=torch.float32, device=dev)
+            q = torch.empty((n, self.d), dtype=torch.float32, device=dev)
+            need = self._lib.rairs_project_workspace_bytes(C.byref(projection._s), C.c_int64(n))
+            ws, pw, nw = _workspace(need)
+            _check(self._lib.rairs_search_projected(
+                self._h, C.byref(projection._s), px, ldx, C.c_int64(n), pa, C.c_void_p(q.data_ptr() if n else 0), C.c_int(k),
+                C.c_int(nprobe), C.c_int(refine_k), C.c_void_p(ids.data_ptr() if n else 0),
+                C.c_void_p(dists.data_ptr() if n else 0), pw, nw, _stream_ptr(st)))
+        return ids, dists, q
+
+    def logprob(self, q: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, top: int = 0, live=None,
+                entropy: bool = True, stream=None) -> LogProb:
+        """logprob over the index's own vectors (rairs_index_table): float32 queries, targets are vector ids."""
+        t = _Table()
+        _check(self._lib.rairs_index_table(self._h, C.byref(t)))
+        t.scale = scale
+        return _logprob(_with_mask(t, live, q.shape[0], q.device), q, targets, top, entropy, stream)
 
     # --- stages ---------------------------------------------------------------------------
     def coarse(self, queries: torch.Tensor, nprobe: int, stream=None):

@@ -1,0 +1,99 @@
+// Products of a few rows with many: a wave takes 16 PT of the many rows and all of the few, and both
+// operands go from memory straight into the matrix instruction's registers.  The many rows are read
+// once, which is what bounds these calls; the few come from the caches.  A lane holds 16 bytes of a row
+// per load, so that four lanes read 64 consecutive bytes of it, and the four loads in flight a line.
+//
+// bf16 rows use the 16 x 16 x 32 instruction, fp32 rows the fp32 one (16 x 16 x 4: 64 operations a cycle
+// and SIMD are enough next to memory for up to 64 rows), byte rows are widened to fp32.  The order in
+// which the summed dimension is taken does not matter to the instruction as long as both operands
+// agree: lane group g takes values g CH .. g CH + CH - 1 of a step.
+#pragma once
+#include "rowprod.h"
+
+template <int PT_, int QT_>
+struct FewTile {
+    static constexpr int PT = PT_, QT = QT_;
+};
+
+template <class S>
+struct FewLoad {                    // values per lane and step, by the type of the many rows
+    static constexpr int CH = 16 / sizeof(S);
+};
+
+template <class S, int CH>
+struct FewFrag {
+    S e[CH];
+};
+
+// CH values of a row from k on, zero from d on
+template <class S, int CH, bool VEC>
+static __device__ __forceinline__ FewFrag<S, CH> few_load(const S *row, int k, int d)
+{
+    FewFrag<S, CH> f;
+    if (VEC && k <= d - CH) {
+#pragma unroll
+        for (int w = 0; w < CH * (int)sizeof(S) / 16; w++) {
+            const v4u x = *(const v4u *)(row + k + w * (16 / sizeof(S)));
+            __builtin_memcpy(&f.e[w * (16 / sizeof(S))], &x, 16);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < CH; e++) f.e[e] = k + e < d ? row[k + e] : (S)0;
+    }
+    return f;
+}
+
+template <int CH>
+static __device__ __forceinline__ v4f few_mfma(const FewFrag<__bf16, CH> &a, const FewFrag<__bf16, CH> &b, v4f c)
+{
+    v8bf x, y;
+    __builtin_memcpy(&x, a.e, 16);
+    __builtin_memcpy(&y, b.e, 16);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+}
+template <class S, int CH>
+static __device__ __forceinline__ v4f few_mfma(const FewFrag<S, CH> &a, const FewFrag<float, CH> &b, v4f c)
+{
+#pragma unroll
+    for (int e = 0; e < CH; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32((float)a.e[e], b.e[e], c, 0, 0, 0);
+    return c;
+}
+
+// one step: 4 CH values of every row, from value k on for this lane
+template <class S, class Q, int PT, int QT, bool VEC, bool NORM>
+static __device__ __forceinline__ void few_step(const S *const (&prow)[PT], const Q *const (&qrow)[QT], int k, int d, v4f (&acc)[PT][QT],
+                                                float (&nrm)[PT])
+{
+    constexpr int CH = FewLoad<S>::CH;
+    FewFrag<S, CH> a[PT];
+    FewFrag<Q, CH> b[QT];
+#pragma unroll
+    for (int i = 0; i < PT; i++) a[i] = few_load<S, CH, VEC>(prow[i], k, d);
+#pragma unroll
+    for (int j = 0; j < QT; j++) b[j] = few_load<Q, CH, VEC>(qrow[j], k, d);
+#pragma unroll
+    for (int i = 0; i < PT; i++) {
+#pragma unroll
+        for (int j = 0; j < QT; j++) acc[i][j] = few_mfma(a[i], b[j], acc[i][j]);
+        if constexpr (NORM) {
+#pragma unroll
+            for (int e = 0; e < CH; e++) nrm[i] = fmaf((float)a[i].e[e], (float)a[i].e[e], nrm[i]);
+        }
+    }
+}
+
+// acc += rows prow (many) times rows qrow (few) over the steps [s0, s1); prow/qrow: this lane's rows
+// (p tile i: row lane & 15 of it).  NORM: nrm[i] collects this lane's part of |p row|^2.
+template <class S, class Q, int PT, int QT, bool VEC, bool NORM>
+static __device__ __forceinline__ void few_dot(const S *const (&prow)[PT], const Q *const (&qrow)[QT], int s0, int s1, int d, int lane,
+                                               v4f (&acc)[PT][QT], float (&nrm)[PT])
+{
+    constexpr int STEP = 4 * FewLoad<S>::CH;
+    const int off = (lane >> 4) * FewLoad<S>::CH, whole = VEC ? (d / STEP < s1 ? d / STEP : s1) : s0;
+    int s = s0;
+    // (the bound that few_load compares with is the step's own end here: no comparison is left)
+#pragma unroll 4
+    for (; s < whole; s++) few_step<S, Q, PT, QT, VEC, NORM>(prow, qrow, s * STEP + off, 0x7FFFFFFF, acc, nrm);
+#pragma unroll 1
+    for (; s < s1; s++) few_step<S, Q, PT, QT, VEC, NORM>(prow, qrow, s * STEP + off, d, acc, nrm);
+}

@@ -1,0 +1,880 @@
+// Log probabilities of a table's rows under a softmax over inner products, and their gradients.
+//
+// One pass over the logits l = scale <q, t_v>, which are never written: a wave that has a tile's products
+// in registers folds them into a running maximum m, s = sum 2^(z - m) and e = sum 2^(z - m) (z - m) with
+// z = l log2(e), and leaves one {m, s, e} per query and run of table rows ("part").  From them
+//     lse = ln 2 (m + log2 s),     entropy = ln 2 (log2 s - e / s).
+// For the most probable rows it also leaves the largest product of every 16 rows ("group"): a row among
+// the K best lies in a group whose maximum is at least the K-th best maximum less what the sums can be
+// off by, so those groups, little more than K of them, are all that is scored again in float64, which
+// orders rows whose fp32 products are too close to tell apart.
+#include "fewrows.h"
+#include "query_ops.h"
+
+#define LOG2E 1.4426950408889634f
+#define LN2 0.6931471805599453f
+#define NEG_INF (-__builtin_huge_valf())
+
+// ---- statistics of a tile ----------------------------------------------------------------------------
+
+struct StatsArgs {
+    int64_t n, V;
+    float c;                        // scale log2(e)
+    const uint32_t *live;
+    int64_t ld_live;
+    const int64_t *targets;
+    float4 *parts;                  // [n][nparts] {m, s, e, 0}; m: the largest product itself, not times c
+    int64_t nparts;
+    float *gmax;                    // [n][ngroups], or null
+    int64_t ngroups;                // 4 per 64 rows: group 4 b + h holds rows 64 b + 16 i + 4 h + r
+    int per;                        // groups per part (the last may have fewer)
+    float *zt;                      // [n] the target's product
+};
+
+// 2^x for x <= 0 (a result below 2^-126 may be flushed)
+static __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <int QT>
+struct StatsState {
+    float m[QT], s[QT], e[QT];
+    __device__ __forceinline__ void begin()
+    {
+#pragma unroll
+        for (int j = 0; j < QT; j++) { m[j] = NEG_INF; s[j] = 0.0f; e[j] = 0.0f; }
+    }
+    // sums relative to a maximum m0, brought to m1 >= m0
+    static __device__ __forceinline__ void rebase(float &s, float &e, float m0, float m1, float c)
+    {
+        if (m0 == m1) return;
+        if (m0 == NEG_INF) { s = 0.0f; e = 0.0f; return; }
+        const float d = m0 * c - m1 * c, f = exp2_fast(d);
+        e = f * fmaf(s, fmaxf(d, -1e4f), e);
+        s *= f;
+    }
+    // a tile's products: rows p0 + 16 i + 4 (lane >> 4) + r, queries q0 + 16 j + (lane & 15); acc is
+    // overwritten (-inf where the mask hides a row)
+    template <int PT>
+    __device__ __forceinline__ void tile(const StatsArgs &a, v4f (&acc)[PT][QT], int64_t p0, int64_t q0, int lane)
+    {
+        const int h = lane >> 4;
+        const bool ragged = p0 + 16 * PT > a.V;                       // uniform
+#pragma unroll
+        for (int j = 0; j < QT; j++) {
+            const int64_t q = q0 + 16 * j + (lane & 15);
+            const bool in = q < a.n;
+            const int64_t row = in ? q : a.n - 1;
+            // the target's product, by the lane that has it
+            const int64_t dp = a.targets[row] - p0;
+            if (in && dp >= 0 && dp < 16 * PT && (((int)dp >> 2) & 3) == h) {
+#pragma unroll
+                for (int i = 0; i < PT; i++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++)
+                        if ((int)dp == 16 * i + 4 * h + r) a.zt[row] = acc[i][j][r];
+            }
+            if (a.live || ragged) {
+#pragma unroll
+                for (int i = 0; i < PT; i++) {
+                    const int64_t p = p0 + 16 * i;                    // (a multiple of 16: within one word of the mask)
+                    uint32_t bits = 0;
+                    if (p < a.V) {
+                        bits = a.live ? a.live[row * a.ld_live + (p >> 5)] >> ((p & 31) + 4 * h) : 0xFu;
+                        const int64_t left = a.V - p - 4 * h;
+                        bits &= left >= 4 ? 0xFu : left <= 0 ? 0u : (1u << left) - 1u;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; r++)
+                        if (!((bits >> r) & 1u)) acc[i][j][r] = NEG_INF;
+                }
+            }
+            float top = NEG_INF;
+#pragma unroll
+            for (int b = 0; b < PT; b += 4) {
+                float g = NEG_INF;
+#pragma unroll
+                for (int i = b; i < b + 4 && i < PT; i++)
+                    g = fmaxf(fmaxf(g, fmaxf(acc[i][j][0], acc[i][j][1])), fmaxf(acc[i][j][2], acc[i][j][3]));
+                const int64_t group = (p0 / 64 + b / 4) * 4 + h;
+                if (a.gmax && in && group < a.ngroups) a.gmax[row * a.ngroups + group] = g;
+                top = fmaxf(top, g);
+            }
+            const float m1 = fmaxf(m[j], top);
+            rebase(s[j], e[j], m[j], m1, a.c);
+            m[j] = m1;
+            const float mc = m1 == NEG_INF ? 0.0f : m1 * a.c;
+#pragma unroll
+            for (int i = 0; i < PT; i++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const float t = fmaf(acc[i][j][r], a.c, -mc), x = exp2_fast(t);
+                    s[j] += x;
+                    e[j] = fmaf(x, fmaxf(t, -1e4f), e[j]);
+                }
+        }
+    }
+    __device__ __forceinline__ void end(const StatsArgs &a, int64_t part, int64_t q0, int lane)
+    {
+#pragma unroll
+        for (int j = 0; j < QT; j++) {
+            float top = fmaxf(m[j], __shfl_xor(m[j], 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            rebase(s[j], e[j], m[j], top, a.c);
+            float ss = s[j] + __shfl_xor(s[j], 16), ee = e[j] + __shfl_xor(e[j], 16);
+            ss += __shfl_xor(ss, 32);
+            ee += __shfl_xor(ee, 32);
+            const int64_t q = q0 + 16 * j + (lane & 15);
+            if (q < a.n && lane < 16) a.parts[q * a.nparts + part] = make_float4(top, ss, ee, 0.0f);
+        }
+    }
+};
+
+struct StatsEpi {
+    StatsArgs a;
+    template <class T>
+    __device__ __forceinline__ void operator()(RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
+    {
+        StatsState<T::QT> st;
+        st.begin();
+        st.tile(a, acc.v, p0, q0, lane);
+        if (p0 < a.V) st.end(a, p0 / (16 * T::PT), q0, lane);
+    }
+};
+
+// Largest squared norm of the live rows, one value per workgroup (what the margin of the selection needs).
+template <class S>
+__global__ __launch_bounds__(WG) void table_norm_kernel(const S *__restrict__ t, int64_t ld, int64_t V, int d, const uint32_t *__restrict__ live,
+                                                        int vec, float *__restrict__ out)
+{
+    __shared__ float best[WG / 64];
+    constexpr int CH = FewLoad<S>::CH;
+    const int lane = threadIdx.x & 63, sub = lane & 15;
+    float most = 0.0f;
+    // four rows per wave, 16 lanes each
+    for (int64_t v0 = ((int64_t)blockIdx.x * (WG / 64) + (threadIdx.x >> 6)) * 4; v0 < V; v0 += (int64_t)gridDim.x * WG / 16) {
+        const int64_t v = v0 + (lane >> 4);
+        float x = 0.0f;
+        if (v < V && (!live || ((live[v >> 5] >> (v & 31)) & 1u)))
+            for (int k = sub * CH; k < d; k += 16 * CH) {
+                const FewFrag<S, CH> f = vec ? few_load<S, CH, true>(t + v * ld, k, d) : few_load<S, CH, false>(t + v * ld, k, d);
+#pragma unroll
+                for (int e = 0; e < CH; e++) x = fmaf((float)f.e[e], (float)f.e[e], x);
+            }
+        x += lane_xor8(x);
+        x += lane_xor4(x);
+        x += lane_xor2(x);
+        x += lane_xor1(x);
+        most = fmaxf(most, x);
+    }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    if (lane == 0) best[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) out[blockIdx.x] = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
+}
+
+// words of the masks of all queries, or-ed: rows that any query sees
+__global__ __launch_bounds__(WG) void any_live_kernel(const uint32_t *__restrict__ live, int64_t ld, int64_t n, int64_t words,
+                                                      uint32_t *__restrict__ out)
+{
+    const int64_t w = (int64_t)blockIdx.x * WG + threadIdx.x;
+    if (w >= words) return;
+    uint32_t x = 0;
+    for (int64_t i = 0; i < n; i++) x |= live[i * ld + w];
+    out[w] = x;
+}
+
+// ---- a few queries: the table's rows straight from memory -------------------------------------------
+
+struct FewStatsArgs {
+    StatsArgs st;
+    const void *table, *q;
+    int64_t ldt, ldq;
+    int d, rounds;                  // rounds of 64 rows per wave: a part
+    const uint32_t *any_live;
+    float *xmax;                    // [nparts] largest squared norm of a part's rows, or null
+};
+
+template <class S, class Q, int QT, bool VEC, bool NORM>
+__global__ __launch_bounds__(WG) void few_stats_kernel(FewStatsArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t part = (int64_t)blockIdx.x * (WG / 64) + (threadIdx.x >> 6);
+    if (part >= a.st.nparts) return;
+    const Q *qrow[QT];
+#pragma unroll
+    for (int j = 0; j < QT; j++) {
+        int64_t q = 16 * j + (lane & 15);
+        q = q < a.st.n ? q : a.st.n - 1;
+        qrow[j] = (const Q *)a.q + q * a.ldq;
+    }
+    const int steps = (a.d + 4 * FewLoad<S>::CH - 1) / (4 * FewLoad<S>::CH);
+    StatsState<QT> st;
+    st.begin();
+    float most = 0.0f;
+    for (int r = 0; r < a.rounds; r++) {
+        const int64_t p0 = (part * a.rounds + r) * 64;
+        if (p0 >= a.st.V) break;
+        const S *prow[4];
+        v4f acc[4][QT];
+        float nrm[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            int64_t p = p0 + 16 * i + (lane & 15);
+            p = p < a.st.V ? p : a.st.V - 1;
+            prow[i] = (const S *)a.table + p * a.ldt;
+            nrm[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < QT; j++) acc[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        few_dot<S, Q, 4, QT, VEC, NORM>(prow, qrow, 0, steps, a.d, lane, acc, nrm);
+        if constexpr (NORM) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                float x = nrm[i] + __shfl_xor(nrm[i], 16);
+                x += __shfl_xor(x, 32);
+                const int64_t p = p0 + 16 * i + (lane & 15);
+                if (p < a.st.V && (!a.any_live || ((a.any_live[p >> 5] >> (p & 31)) & 1u))) most = fmaxf(most, x);
+            }
+        }
+        st.tile(a.st, acc, p0, 0, lane);
+    }
+    st.end(a.st, part, 0, lane);
+    if constexpr (NORM) {
+        most = fmaxf(most, lane_xor8(most));
+        most = fmaxf(most, lane_xor4(most));
+        most = fmaxf(most, lane_xor2(most));
+        most = fmaxf(most, lane_xor1(most));
+        if (lane == 0) a.xmax[part] = most;
+    }
+}
+
+// ---- joining the parts, and the most probable rows --------------------------------------------------
+
+struct FinishArgs {
+    StatsArgs st;
+    const void *table, *q;
+    int64_t ldt, ldq;
+    int d, qvec, tvec;
+    float scale;
+    float slack;                    // relative error of a product against |q||t|
+    const float *xmax;
+    int64_t nxmax;
+    float *logp, *lse, *entropy;
+    int top;
+    int64_t *top_ids;
+    float *top_logp;
+};
+
+#define FIN_GROUPS 2048             // groups of the open parts that fit LDS
+#define FIN_BATCH 32                // groups scored at a time
+
+struct FinishShared {
+    float red[4][4];
+    float lane_max[WG];
+    double val[FIN_BATCH * 16 + RAIRS_MAX_TOP];
+    uint32_t id[FIN_BATCH * 16 + RAIRS_MAX_TOP];
+    double best[RAIRS_MAX_TOP];
+    uint32_t best_id[RAIRS_MAX_TOP];
+    uint32_t take[FIN_BATCH];
+    float gval[FIN_GROUPS];
+    uint32_t gid[FIN_GROUPS];
+    int count, nbest, wcnt[WG / 64];
+};
+
+// a lower bound of the k-th largest of all threads' values: the k-th largest of their maxima
+static __device__ __forceinline__ float kth_thread_max(FinishShared &sh, float mine, int k)
+{
+    const int tid = threadIdx.x;
+    __syncthreads();
+    sh.lane_max[tid] = mine;
+    if (tid == 0) sh.red[0][0] = NEG_INF;
+    __syncthreads();
+    int above = 0;
+    for (int i = 0; i < WG; i++) {
+        const float x = sh.lane_max[i];
+        above += x > mine || (x == mine && i < tid) ? 1 : 0;
+    }
+    if (above == k - 1) sh.red[0][0] = mine;
+    __syncthreads();
+    return sh.red[0][0];
+}
+
+// <q, t> in float64 by 16 lanes; the order of the sum depends on d alone, so equal rows get equal values
+template <class S, class Q>
+static __device__ __forceinline__ double dot_exact(const S *t, const Q *q, int d, int sub, int tvec, int qvec)
+{
+    constexpr int CH = FewLoad<S>::CH;
+    double x = 0.0;
+    for (int k = sub * CH; k < d; k += 16 * CH) {
+        const FewFrag<S, CH> f = tvec ? few_load<S, CH, true>(t, k, d) : few_load<S, CH, false>(t, k, d);
+        const FewFrag<Q, CH> g = qvec ? few_load<Q, CH, true>(q, k, d) : few_load<Q, CH, false>(q, k, d);
+#pragma unroll
+        for (int e = 0; e < CH; e++) x = fma((double)(float)f.e[e], (double)(float)g.e[e], x);
+    }
+    for (int s = 8; s > 0; s >>= 1) x += __shfl_xor(x, s);
+    return x;
+}
+
+// scores the `cnt` groups in sh.take and merges their rows into sh.best
+template <class S, class Q>
+static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishShared &sh, int64_t row, int cnt)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & 15, quarter = lane >> 4;
+    const Q *q = (const Q *)a.q + row * a.ldq;
+    for (int it = wave; it < cnt * 4; it += WG / 64) {
+        const uint32_t g = sh.take[it >> 2];
+        const int64_t v = (int64_t)(g >> 2) * 64 + 16 * (it & 3) + 4 * (g & 3) + quarter;
+        const bool in = v < a.st.V && (!a.st.live || ((a.st.live[row * a.st.ld_live + (v >> 5)] >> (v & 31)) & 1u));
+        const double x = dot_exact<S, Q>((const S *)a.table + (in ? v : 0) * a.ldt, q, a.d, sub, a.tvec, a.qvec);
+        if (sub == 0) {
+            const int slot = it * 4 + quarter;
+            const bool ok = in && x == x;
+            sh.val[slot] = ok ? x : 0.0;
+            sh.id[slot] = ok ? (uint32_t)v : 0xFFFFFFFFu;
+        }
+    }
+    const int old = sh.nbest, total = cnt * 16 + old;
+    if (tid < old) {
+        sh.val[cnt * 16 + tid] = sh.best[tid];
+        sh.id[cnt * 16 + tid] = sh.best_id[tid];
+    }
+    if (tid == 0) sh.count = 0;
+    __syncthreads();
+    for (int i = tid; i < total; i += WG) {
+        const double x = sh.val[i];
+        const uint32_t id = sh.id[i];
+        if (id == 0xFFFFFFFFu) continue;
+        int rank = 0;
+        for (int j = 0; j < total && rank < a.top; j++) {
+            const uint32_t idj = sh.id[j];
+            rank += idj != 0xFFFFFFFFu && (sh.val[j] > x || (sh.val[j] == x && idj < id)) ? 1 : 0;
+        }
+        if (rank < a.top) {
+            sh.best[rank] = x;
+            sh.best_id[rank] = id;
+            atomicAdd(&sh.count, 1);
+        }
+    }
+    __syncthreads();
+    if (tid == 0) sh.nbest = sh.count;
+    __syncthreads();
+}
+
+template <class S, class Q>
+__global__ __launch_bounds__(WG) void logprob_finish_kernel(FinishArgs a)
+{
+    __shared__ FinishShared sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x;
+    const float4 *parts = a.st.parts + row * a.st.nparts;
+    const float c = a.st.c;
+    float m = NEG_INF, s = 0.0f, e = 0.0f;
+    for (int64_t i = tid; i < a.st.nparts; i += WG) {
+        float4 p = parts[i];
+        const float m1 = fmaxf(m, p.x);
+        StatsState<1>::rebase(s, e, m, m1, c);
+        StatsState<1>::rebase(p.y, p.z, p.x, m1, c);
+        s += p.y;
+        e += p.z;
+        m = m1;
+    }
+    const float mine = m;
+    float top = m;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+    if (lane == 0) sh.red[wave][0] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(sh.red[0][0], sh.red[1][0]), fmaxf(sh.red[2][0], sh.red[3][0]));
+    StatsState<1>::rebase(s, e, m, top, c);
+    // |q|^2 and the table's largest squared norm, for the margin
+    float q2 = 0.0f, x2 = 0.0f;
+    if (a.top) {
+        const Q *q = (const Q *)a.q + row * a.ldq;
+        for (int k = tid; k < a.d; k += WG) q2 = fmaf((float)q[k], (float)q[k], q2);
+        for (int64_t i = tid; i < a.nxmax; i += WG) x2 = fmaxf(x2, a.xmax[i]);
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+        s += __shfl_xor(s, x);
+        e += __shfl_xor(e, x);
+        q2 += __shfl_xor(q2, x);
+        x2 = fmaxf(x2, __shfl_xor(x2, x));
+    }
+    __syncthreads();
+    if (lane == 0) { sh.red[wave][0] = s; sh.red[wave][1] = e; sh.red[wave][2] = q2; sh.red[wave][3] = x2; }
+    __syncthreads();
+    s = (sh.red[0][0] + sh.red[1][0]) + (sh.red[2][0] + sh.red[3][0]);
+    e = (sh.red[0][1] + sh.red[1][1]) + (sh.red[2][1] + sh.red[3][1]);
+    q2 = (sh.red[0][2] + sh.red[1][2]) + (sh.red[2][2] + sh.red[3][2]);
+    x2 = fmaxf(fmaxf(sh.red[0][3], sh.red[1][3]), fmaxf(sh.red[2][3], sh.red[3][3]));
+    const bool empty = top == NEG_INF && s == 0.0f;
+    const float mc = top * c, logs = log2f(s);
+    if (tid == 0) {
+        a.lse[row] = empty ? NEG_INF : (mc + logs) * LN2;
+        if (a.entropy) a.entropy[row] = empty ? 0.0f : fmaxf((logs - e / s) * LN2, 0.0f);
+        const int64_t t = a.st.targets[row];
+        float lp = 0.0f;
+        if (t >= 0 && t < a.st.V) {
+            const bool seen = !a.st.live || ((a.st.live[row * a.st.ld_live + (t >> 5)] >> (t & 31)) & 1u);
+            lp = seen ? (fmaf(a.st.zt[row], c, -mc) - logs) * LN2 : NEG_INF;
+        }
+        a.logp[row] = lp;
+    }
+    if (a.top == 0) return;
+
+    // what a product may be off by, twice; not finite: nothing can be told apart
+    const float eps = a.slack * sqrtf(q2) * sqrtf(x2) * 1.0001f;
+    if (tid == 0) sh.nbest = 0;
+    __syncthreads();
+    if (!empty && eps < 1e38f) {                                      // uniform
+        float thr = kth_thread_max(sh, mine, a.top) - 2.0f * eps;
+        // the groups of the parts that reach it
+        const int per = a.st.per;
+        const float *gmax = a.st.gmax + row * a.st.ngroups;
+        if (tid == 0) sh.count = 0;
+        __syncthreads();
+        for (int64_t i = tid; i < a.st.nparts; i += WG)
+            if (parts[i].x >= thr && parts[i].x > NEG_INF) {
+                const int at = atomicAdd(&sh.count, 1);
+                if (at < FIN_GROUPS) sh.gid[at] = (uint32_t)i;
+            }
+        __syncthreads();
+        const int nopen = sh.count;
+        __syncthreads();
+        if ((int64_t)nopen * per <= FIN_GROUPS) {
+            // list their groups, tighten the bound, and score what reaches it
+            uint32_t part_of[(FIN_GROUPS + WG - 1) / WG];
+            const int slots = nopen * per;
+#pragma unroll
+            for (int u = 0; u < FIN_GROUPS / WG; u++) {
+                const int i = u * WG + tid;
+                part_of[u] = i < slots ? sh.gid[i / per] : 0u;
+            }
+            __syncthreads();
+            float most = NEG_INF;
+#pragma unroll
+            for (int u = 0; u < FIN_GROUPS / WG; u++) {
+                const int i = u * WG + tid;
+                if (i < slots) {
+                    const int64_t g = (int64_t)part_of[u] * per + i % per;
+                    const float x = g < a.st.ngroups ? gmax[g] : NEG_INF;
+                    sh.gval[i] = x;
+                    sh.gid[i] = (uint32_t)g;
+                    most = fmaxf(most, x);
+                }
+            }
+            thr = fmaxf(thr, kth_thread_max(sh, most, a.top) - 2.0f * eps);
+            for (int i0 = 0; i0 < slots; i0 += WG) {
+                const int i = i0 + tid;
+                bool want = i < slots && sh.gval[i] >= thr && sh.gval[i] > NEG_INF;
+                for (;;) {
+                    // rows that cannot reach the K-th best so far are left out
+                    if (sh.nbest == a.top && want && (double)sh.gval[i] + (double)eps < sh.best[a.top - 1]) want = false;
+                    const unsigned long long b = __ballot(want);
+                    if (lane == 0) sh.wcnt[wave] = __popcll(b);
+                    __syncthreads();
+                    int at = __popcll(b & ((1ull << lane) - 1ull)), total = 0;
+                    for (int w = 0; w < WG / 64; w++) {
+                        at += w < wave ? sh.wcnt[w] : 0;
+                        total += sh.wcnt[w];
+                    }
+                    if (total == 0) break;
+                    if (want && at < FIN_BATCH) {
+                        sh.take[at] = sh.gid[i];
+                        want = false;
+                    }
+                    __syncthreads();
+                    finish_batch<S, Q>(a, sh, row, total < FIN_BATCH ? total : FIN_BATCH);
+                }
+                __syncthreads();
+            }
+        } else {
+            // so many equal products that the list does not hold them: all groups in order of their rows,
+            // so that one that can only equal the K-th best comes too late to displace it
+            for (int64_t g0 = 0; g0 < a.st.ngroups; g0 += WG) {
+                const int64_t g = g0 + tid;
+                const float x = g < a.st.ngroups ? gmax[g] : NEG_INF;
+                bool want = x >= thr && x > NEG_INF;
+                for (;;) {
+                    // (a group's rows lie within its block of 64: whole blocks before it are done, so an
+                    // equal product in it has a larger id than any held from those; within the block ids cross)
+                    if (sh.nbest == a.top && want) {
+                        const double k = sh.best[a.top - 1], up = (double)x + (double)eps;
+                        if (up < k || (up == k && (int64_t)(sh.best_id[a.top - 1] >> 6) < (g >> 2))) want = false;
+                    }
+                    const unsigned long long b = __ballot(want);
+                    if (lane == 0) sh.wcnt[wave] = __popcll(b);
+                    __syncthreads();
+                    int at = __popcll(b & ((1ull << lane) - 1ull)), total = 0;
+                    for (int w = 0; w < WG / 64; w++) {
+                        at += w < wave ? sh.wcnt[w] : 0;
+                        total += sh.wcnt[w];
+                    }
+                    if (total == 0) break;
+                    if (want && at < FIN_BATCH) {
+                        sh.take[at] = (uint32_t)g;
+                        want = false;
+                    }
+                    __syncthreads();
+                    finish_batch<S, Q>(a, sh, row, total < FIN_BATCH ? total : FIN_BATCH);
+                }
+                __syncthreads();
+            }
+        }
+    }
+    __syncthreads();
+    if (tid < a.top) {
+        const bool have = tid < sh.nbest;
+        a.top_ids[row * a.top + tid] = have ? (int64_t)sh.best_id[tid] : -1;
+        a.top_logp[row * a.top + tid] =
+            have ? (float)(sh.best[tid] * (double)a.scale - ((double)mc + (double)logs) * 0.6931471805599453) : NEG_INF;
+    }
+}
+
+// ---- gradient of the logits --------------------------------------------------------------------------
+
+struct GradArgs {
+    int64_t n, V, v0;               // the product's columns are rows v0 .. V - 1 of the table
+    int64_t vc, npad;               // columns of g, of gt
+    float scale;
+    const uint32_t *live;
+    int64_t ld_live;
+    const int64_t *targets;
+    const float *lse, *entropy, *dlogp, *dentropy;
+    __bf16 *g, *gt;                 // [n][vc], [vc][npad]; either null
+    int64_t gpiece, gtpiece;
+};
+
+// G = scale (dlogp (1[v = t] - p) - dentropy p (log p + H)) in registers, rounded to bf16 once (bf16
+// rows: half a step of 2^-9 beside the operands' own) or kept in three pieces (fp32), written for the
+// products with the table (rows of queries) and with the queries (rows of the table).
+template <int NP>
+struct GradEpi {
+    GradArgs a;
+    template <class T>
+    __device__ __forceinline__ void operator()(RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
+    {
+        if (p0 >= a.vc) return;
+        const int h = lane >> 4;
+#pragma unroll
+        for (int j = 0; j < T::QT; j++) {
+            const int64_t q = q0 + 16 * j + (lane & 15);
+            if (q >= a.npad) continue;
+            const bool in = q < a.n;
+            const int64_t row = in ? q : a.n - 1;
+            const int64_t t = a.targets[row];
+            const uint32_t *live = a.live ? a.live + row * a.ld_live : nullptr;
+            const bool seen = t >= 0 && t < a.V && (!live || ((live[t >> 5] >> (t & 31)) & 1u));
+            const float da = in && seen ? a.dlogp[row] * a.scale : 0.0f;
+            const float db = in && a.dentropy ? a.dentropy[row] * a.scale : 0.0f;
+            const float H = db != 0.0f ? a.entropy[row] : 0.0f;
+            const float lse = a.lse[row];
+            const bool dead = da == 0.0f && db == 0.0f;
+#pragma unroll
+            for (int i = 0; i < T::PT; i++) {
+                const int64_t p = p0 + 16 * i + 4 * h, v = a.v0 + p;
+                if (p >= a.vc) continue;
+                uint32_t bits = 0;
+                if (!dead && v < a.V) {
+                    bits = live ? live[v >> 5] >> (v & 31) : 0xFu;
+                    const int64_t left = a.V - v;
+                    bits &= left >= 4 ? 0xFu : (1u << left) - 1u;
+                }
+                __bf16 o[NP][4];
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    // (log p in natural units: scale times the product is exact inside the sum, which log2(e) is not)
+                    const float x = fmaf(acc.v[i][j][r], a.scale, -lse), pr = exp2_fast(x * LOG2E);
+                    const float one = v + r == t ? 1.0f : 0.0f;
+                    float g = da * (one - pr) - db * pr * (fmaxf(x, -1e4f) + H);
+                    g = (bits >> r) & 1u ? g : 0.0f;
+                    o[0][r] = (__bf16)g;
+                    if constexpr (NP == 3) {
+                        const float g1 = g - (float)o[0][r];
+                        o[1][r] = (__bf16)g1;
+                        o[2][r] = (__bf16)(g1 - (float)o[1][r]);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < NP; u++) {
+                    if (a.g && in) *(v4bf *)(a.g + u * a.gpiece + q * a.vc + p) = (v4bf){o[u][0], o[u][1], o[u][2], o[u][3]};
+                    if (a.gt)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) a.gt[u * a.gtpiece + (p + r) * a.npad + q] = o[u][r];
+                }
+            }
+        }
+    }
+};
+
+// bit i: row i passes a gradient
+__global__ __launch_bounds__(WG) void active_rows_kernel(int64_t n, int64_t V, const int64_t *__restrict__ targets,
+                                                         const uint32_t *__restrict__ live, int64_t ld_live, const float *__restrict__ dlogp,
+                                                         const float *__restrict__ dentropy, uint32_t *__restrict__ out)
+{
+    const int64_t i = (int64_t)blockIdx.x * WG + threadIdx.x;
+    bool on = false;
+    if (i < n) {
+        const int64_t t = targets[i];
+        const bool seen = t >= 0 && t < V && (!live || ((live[i * ld_live + (t >> 5)] >> (t & 31)) & 1u));
+        on = (seen && dlogp[i] != 0.0f) || (dentropy && dentropy[i] != 0.0f);
+    }
+    const unsigned long long b = __ballot(on);
+    const int lane = threadIdx.x & 63;
+    if ((lane & 31) == 0 && i < n) out[i >> 5] = (uint32_t)(b >> lane);
+}
+
+// sums of the splits, in their order
+__global__ __launch_bounds__(WG) void join_splits_kernel(const float *__restrict__ part, int splits, int64_t n, int64_t cols, void *__restrict__ out,
+                                                         int64_t ld, int bf16_out)
+{
+    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x, total = n * cols;
+    if (t >= total) return;
+    float x = 0.0f;
+    for (int s = 0; s < splits; s++) x += part[s * total + t];
+    const int64_t r = t / cols, o = r * ld + (t - r * cols);
+    if (bf16_out) ((__bf16 *)out)[o] = (__bf16)x;
+    else ((float *)out)[o] = x;
+}
+
+__global__ __launch_bounds__(WG) void clear_rows_kernel(void *out, int64_t n, int64_t cols, int64_t ld, int width)
+{
+    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x;
+    if (t >= n * cols) return;
+    const int64_t r = t / cols, o = r * ld + (t - r * cols);
+    if (width == 4) ((float *)out)[o] = 0.0f;
+    else ((uint16_t *)out)[o] = 0;
+}
+
+// ---- launches ----------------------------------------------------------------------------------------
+
+#define FEW_ROWS 64                 // up to here the table's rows go straight into registers
+
+typedef RowTile<4, 4, 2, 2> LogTile;
+
+int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, __bf16 *room, RowOperand &out,
+                  hipStream_t s)
+{
+    const int64_t kpad = pad_to(cols, ROWPROD_K);
+    out.rows = rows;
+    out.perm = nullptr;
+    if (!live && rows_lie_right(src, dtype, ld, cols)) {
+        out.p = (const __bf16 *)src;
+        out.ld = ld;
+        out.piece = 0;
+        return RAIRS_OK;
+    }
+    out.p = room;
+    out.ld = kpad;
+    out.piece = rows * kpad;
+    return rairs_launch_pack_rows(src, dtype, ld, rows, cols, live, room, kpad, s);
+}
+
+static int lies_vec(const void *p, int dtype, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * dtype_width(dtype) % 16 == 0; }
+
+static const uint32_t *any_live(const LogprobArgs &a, uint32_t *room, hipStream_t s, int *rc)
+{
+    if (!a.live || a.ld_live == 0) return a.live;
+    const int64_t words = (a.V + 31) / 32;
+    hipLaunchKernelGGL(any_live_kernel, dim3((unsigned)((words + WG - 1) / WG)), dim3(WG), 0, s, a.live, a.ld_live, a.n, words, room);
+    if (hipGetLastError() != hipSuccess) {
+        rairs_set_error("launch failed");
+        *rc = RAIRS_EHIP;
+    }
+    return room;
+}
+
+#define NORM_WGS 1024
+
+template <class S, class Q, bool VEC, bool NORM>
+static void few_stats_launch(const FewStatsArgs &fa, hipStream_t s)
+{
+    const dim3 grid((unsigned)((fa.st.nparts + WG / 64 - 1) / (WG / 64)));
+    if (fa.st.n <= 16) hipLaunchKernelGGL((few_stats_kernel<S, Q, 1, VEC, NORM>), grid, dim3(WG), 0, s, fa);
+    else if (fa.st.n <= 32) hipLaunchKernelGGL((few_stats_kernel<S, Q, 2, VEC, NORM>), grid, dim3(WG), 0, s, fa);
+    else hipLaunchKernelGGL((few_stats_kernel<S, Q, 4, VEC, NORM>), grid, dim3(WG), 0, s, fa);
+}
+
+template <class S, class Q>
+static int few_stats(const FewStatsArgs &fa, bool vec, bool norm, hipStream_t s)
+{
+    if (vec && norm) few_stats_launch<S, Q, true, true>(fa, s);
+    else if (vec) few_stats_launch<S, Q, true, false>(fa, s);
+    else if (norm) few_stats_launch<S, Q, false, true>(fa, s);
+    else few_stats_launch<S, Q, false, false>(fa, s);
+    RAIRS_HIP(hipGetLastError());
+    return RAIRS_OK;
+}
+
+int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
+{
+    const bool few = a.n <= FEW_ROWS;
+    const int64_t blocks = (a.V + 63) / 64;
+    // a few rounds of 64 rows per wave where there are waves enough for every SIMD without
+    const int rounds = few ? (int)(blocks / 4096 < 1 ? 1 : blocks / 4096 > 16 ? 16 : blocks / 4096) : 1;
+    const int64_t unit = few ? 64 * rounds : 16 * LogTile::PT, nparts = (a.V + unit - 1) / unit;
+    const int64_t ngroups = blocks * 4, kpad = pad_to(a.d, ROWPROD_K);
+    Carve w(ws);
+    StatsArgs st = {};
+    st.n = a.n; st.V = a.V; st.c = a.scale * LOG2E; st.live = a.live; st.ld_live = a.ld_live; st.targets = a.targets;
+    st.parts = w.take<float4>(a.n * nparts);
+    st.nparts = nparts;
+    st.gmax = a.top ? w.take<float>(a.n * ngroups) : nullptr;
+    st.ngroups = ngroups;
+    st.per = (int)(unit / 16);
+    st.zt = w.take<float>(a.n);
+    const int64_t nx = few ? nparts : NORM_WGS;
+    float *xmax = w.take<float>(nx);
+    uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
+    // (packed whether they need it or not, so that the size does not depend on where the rows lie)
+    __bf16 *qroom = few ? nullptr : w.take<__bf16>(pack_room(a.qtype, a.n, kpad));
+    __bf16 *troom = few ? nullptr : w.take<__bf16>(pack_room(a.ttype, a.V, kpad));
+    if (bytes) *bytes = w.used;
+    if (!ws) return RAIRS_OK;
+
+    int rc = RAIRS_OK;
+    const uint32_t *seen_by_any = any_live(a, seen, s, &rc);
+    if (rc) return rc;
+    if (few) {
+        FewStatsArgs fa = {st, a.table, a.q, a.ldt, a.ldq, a.d, rounds, seen_by_any, xmax};
+        const bool vec = lies_vec(a.table, a.ttype, a.ldt) && lies_vec(a.q, a.qtype, a.ldq);
+        rc = a.ttype == RAIRS_BF16 ? few_stats<__bf16, __bf16>(fa, vec, a.top != 0, s)
+             : a.ttype == RAIRS_F32 ? few_stats<float, float>(fa, vec, a.top != 0, s)
+                                    : few_stats<uint8_t, float>(fa, vec, a.top != 0, s);
+        if (rc) return rc;
+    } else {
+        if (a.top) {
+            const int vec = lies_vec(a.table, a.ttype, a.ldt);
+            if (a.ttype == RAIRS_BF16)
+                hipLaunchKernelGGL(table_norm_kernel<__bf16>, dim3(NORM_WGS), dim3(WG), 0, s, (const __bf16 *)a.table, a.ldt, a.V, a.d, seen_by_any, vec, xmax);
+            else if (a.ttype == RAIRS_F32)
+                hipLaunchKernelGGL(table_norm_kernel<float>, dim3(NORM_WGS), dim3(WG), 0, s, (const float *)a.table, a.ldt, a.V, a.d, seen_by_any, vec, xmax);
+            else
+                hipLaunchKernelGGL(table_norm_kernel<uint8_t>, dim3(NORM_WGS), dim3(WG), 0, s, (const uint8_t *)a.table, a.ldt, a.V, a.d, seen_by_any, vec, xmax);
+            RAIRS_HIP(hipGetLastError());
+        }
+        RowProd rp = {};
+        rowprod_pieces(rp, dtype_pieces(a.ttype), dtype_pieces(a.qtype));
+        rp.ksteps = (int)(kpad / ROWPROD_K);
+        if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, qroom, rp.Q, s))) return rc;
+        if ((rc = rairs_operand(a.table, a.ttype, a.ldt, a.V, a.d, nullptr, troom, rp.P, s))) return rc;
+        if ((rc = rowprod_launch<LogTile>(rp, StatsEpi{st}, s))) return rc;
+    }
+    FinishArgs f = {};
+    f.st = st;
+    f.table = a.table; f.q = a.q; f.ldt = a.ldt; f.ldq = a.ldq; f.d = a.d;
+    f.qvec = lies_vec(a.q, a.qtype, a.ldq);
+    f.tvec = lies_vec(a.table, a.ttype, a.ldt);
+    f.scale = a.scale;
+    // every addition may round (or cut) at 2^-23 of a partial sum, which |q||t| bounds; the products of pieces that are
+    // left out, and the smaller ones' sums, are covered by the rest
+    f.slack = (1.1f * a.d + 64.0f) * 1.1920929e-7f;
+    f.xmax = xmax;
+    f.nxmax = nx;
+    f.logp = a.logp; f.lse = a.lse; f.entropy = a.entropy;
+    f.top = a.top; f.top_ids = a.top_ids; f.top_logp = a.top_logp;
+    if (a.ttype == RAIRS_BF16) hipLaunchKernelGGL((logprob_finish_kernel<__bf16, __bf16>), dim3((unsigned)a.n), dim3(WG), 0, s, f);
+    else if (a.ttype == RAIRS_F32) hipLaunchKernelGGL((logprob_finish_kernel<float, float>), dim3((unsigned)a.n), dim3(WG), 0, s, f);
+    else hipLaunchKernelGGL((logprob_finish_kernel<uint8_t, float>), dim3((unsigned)a.n), dim3(WG), 0, s, f);
+    RAIRS_HIP(hipGetLastError());
+    return RAIRS_OK;
+}
+
+// G is made for as many of the table's rows at a time as 128 MB of it hold, half of the last-level
+// cache: it is written once and read once for each product.
+#define GRAD_CHUNK_BYTES (128ll << 20)
+
+int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
+{
+    const int np = dtype_pieces(a.qtype), tp = dtype_pieces(a.ttype);
+    const int64_t kpad = pad_to(a.d, ROWPROD_K), npad = pad_to(a.n, ROWPROD_K);
+    const bool need_dt = a.dtable != nullptr, need_dq = a.dq != nullptr;
+    int64_t vc = GRAD_CHUNK_BYTES / (2 * np * npad) / 1024 * 1024;
+    vc = vc < 1024 ? 1024 : vc;
+    const int64_t chunks = (a.V + vc - 1) / vc;
+    vc = pad_to((a.V + chunks - 1) / chunks, ROWPROD_K);              // of about one size
+    // workgroups for the queries' product: its sum over the chunk is cut so that there are about two for every CU
+    const int64_t tiles = ((a.d + LogTile::BP - 1) / LogTile::BP) * ((a.n + LogTile::BQ - 1) / LogTile::BQ);
+    int splits = (int)(512 / tiles < 1 ? 1 : 512 / tiles);
+    const int64_t most = vc / 512 < 1 ? 1 : vc / 512;
+    if (splits > most) splits = (int)most;
+    Carve w(ws);
+    __bf16 *qroom = w.take<__bf16>(pack_room(a.qtype, a.n, kpad));
+    __bf16 *troom = w.take<__bf16>(pack_room(a.ttype, vc, kpad));
+    __bf16 *tcols = need_dq ? w.take<__bf16>((int64_t)a.d * vc * tp) : nullptr;
+    __bf16 *qcols = need_dt ? w.take<__bf16>((int64_t)a.d * npad * np) : nullptr;
+    __bf16 *g = need_dq ? w.take<__bf16>(a.n * vc * np) : nullptr;
+    __bf16 *gt = need_dt ? w.take<__bf16>(vc * npad * np) : nullptr;
+    float *sums = need_dq ? w.take<float>((int64_t)splits * a.n * a.d) : nullptr;
+    uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
+    uint32_t *active = need_dt ? w.take<uint32_t>((a.n + 31) / 32) : nullptr;
+    if (bytes) *bytes = w.used;
+    if (!ws) return RAIRS_OK;
+
+    int rc = RAIRS_OK;
+    const uint32_t *seen_by_any = any_live(a, seen, s, &rc);
+    if (rc) return rc;
+    RowOperand Q = {};
+    if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, qroom, Q, s))) return rc;
+    if (need_dt) {
+        hipLaunchKernelGGL(active_rows_kernel, dim3((unsigned)((a.n + WG - 1) / WG)), dim3(WG), 0, s, a.n, a.V, a.targets, a.live, a.ld_live,
+                           a.dlogp, a.dentropy, active);
+        RAIRS_HIP(hipGetLastError());
+        if ((rc = rairs_launch_pack_cols(a.q, a.qtype, a.ldq, 0, 1, a.n, a.d, active, nullptr, qcols, npad, 0, a.d * npad, s))) return rc;
+    }
+    for (int64_t v0 = 0; v0 < a.V; v0 += vc) {
+        const int64_t rows = a.V - v0 < vc ? a.V - v0 : vc, cpad = pad_to(rows, ROWPROD_K);
+        const char *t = (const char *)a.table + v0 * a.ldt * dtype_width(a.ttype);
+        RowProd rp = {};
+        rowprod_pieces(rp, tp, np);
+        rp.ksteps = (int)(kpad / ROWPROD_K);
+        rp.Q = Q;
+        if ((rc = rairs_operand(t, a.ttype, a.ldt, rows, a.d, nullptr, troom, rp.P, s))) return rc;
+        GradArgs ga = {};
+        ga.n = a.n; ga.V = a.V; ga.v0 = v0; ga.vc = cpad; ga.npad = npad;
+        ga.scale = a.scale;
+        ga.live = a.live; ga.ld_live = a.ld_live; ga.targets = a.targets;
+        ga.lse = a.lse_in; ga.entropy = a.entropy_in; ga.dlogp = a.dlogp; ga.dentropy = a.dentropy;
+        ga.g = g; ga.gt = gt;
+        ga.gpiece = a.n * cpad; ga.gtpiece = cpad * npad;
+        rc = np == 3 ? rowprod_launch<LogTile>(rp, GradEpi<3>{ga}, s) : rowprod_launch<LogTile>(rp, GradEpi<1>{ga}, s);
+        if (rc) return rc;
+        if (need_dq) {
+            // (rows that nobody sees are zero here: their G is zero, and they may hold anything)
+            if ((rc = rairs_launch_pack_cols(t, a.ttype, a.ldt, 0, 1, rows, a.d, seen_by_any ? seen_by_any + v0 / 32 : nullptr, nullptr, tcols,
+                                             cpad, 0, a.d * cpad, s)))
+                return rc;
+            RowProd dp = {};
+            rowprod_pieces(dp, tp, np);
+            dp.P = RowOperand{tcols, cpad, a.d * cpad, a.d, nullptr};
+            dp.Q = RowOperand{g, cpad, a.n * cpad, a.n, nullptr};
+            dp.ksteps = (int)(cpad / ROWPROD_K);
+            dp.splits = splits;
+            StoreEpi e = {sums, a.d, a.n * a.d, a.d, a.n, nullptr, 0, v0 > 0};
+            if ((rc = rowprod_launch<LogTile>(dp, e, s))) return rc;
+        }
+        if (need_dt) {
+            RowProd dp = {};
+            rowprod_pieces(dp, np, np);
+            dp.P = RowOperand{qcols, npad, a.d * npad, a.d, nullptr};
+            dp.Q = RowOperand{gt, npad, cpad * npad, rows, nullptr};
+            dp.ksteps = (int)(npad / ROWPROD_K);
+            StoreEpi e = {(char *)a.dtable + v0 * a.lddt * dtype_width(a.ttype), a.lddt, 0, a.d, rows, nullptr, a.ttype == RAIRS_BF16, 0};
+            if ((rc = rowprod_launch<LogTile>(dp, e, s))) return rc;
+        }
+    }
+    if (need_dq) {
+        hipLaunchKernelGGL(join_splits_kernel, dim3((unsigned)((a.n * a.d + WG - 1) / WG)), dim3(WG), 0, s, sums, splits, a.n, (int64_t)a.d, a.dq,
+                           a.lddq, (int)(a.qtype == RAIRS_BF16));
+        RAIRS_HIP(hipGetLastError());
+    }
+    return RAIRS_OK;
+}
+
+int rairs_launch_clear_rows(void *out, int64_t n, int64_t cols, int64_t ld, int dtype, hipStream_t s)
+{
+    if (n == 0 || cols == 0) return RAIRS_OK;
+    hipLaunchKernelGGL(clear_rows_kernel, dim3((unsigned)((n * cols + WG - 1) / WG)), dim3(WG), 0, s, out, n, cols, ld, dtype_width(dtype));
+    RAIRS_HIP(hipGetLastError());
+    return RAIRS_OK;
+}

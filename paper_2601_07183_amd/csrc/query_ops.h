@@ -1,0 +1,76 @@
+// The operators on the query side of an index: internal declarations of their translation units.
+#pragma once
+#include "rowprod.h"
+
+static inline int dtype_width(int dtype) { return dtype == RAIRS_F32 ? 4 : dtype == RAIRS_BF16 ? 2 : 1; }
+static inline int dtype_pieces(int dtype) { return dtype == RAIRS_F32 ? 3 : 1; }
+static inline int64_t pad_to(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+// Hands out 256-byte aligned parts of a workspace; without one it only counts.
+struct Carve {
+    char *base;
+    size_t used;
+    explicit Carve(void *p) : base((char *)p), used(0) {}
+    template <class X>
+    X *take(int64_t count)
+    {
+        X *p = base ? (X *)(base + used) : nullptr;
+        used += ((size_t)count * sizeof(X) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+// rows of a matrix as bf16 pieces with rows of kpad values, zero from `cols` on (and where live says so)
+int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, __bf16 *dst,
+                           int64_t kpad, hipStream_t s);
+// the same, transposed: dst[c][r] = src[perm ? perm[r] : r][c], zero for r in [rows, rpad)
+int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t src_batch, int64_t batches, int64_t rows, int64_t cols,
+                           const uint32_t *live, const int32_t *perm, __bf16 *dst, int64_t rpad, int64_t dst_batch, int64_t piece,
+                           hipStream_t s);
+
+// A matrix as an operand of rowprod: bf16 rows that lie right already are taken where they are, others
+// are packed into `room` (pack_room elements of it).
+static inline bool rows_lie_right(const void *p, int dtype, int64_t ld, int64_t cols)
+{
+    return dtype == RAIRS_BF16 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % ROWPROD_K == 0;
+}
+static inline int64_t pack_room(int dtype, int64_t rows, int64_t cols) { return rows * pad_to(cols, ROWPROD_K) * dtype_pieces(dtype); }
+int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, __bf16 *room, RowOperand &out,
+                  hipStream_t s);
+
+struct LogprobArgs {
+    const void *q, *table;
+    int qtype, ttype;
+    int64_t ldq, ldt, n, V;
+    int d;
+    float scale;
+    const uint32_t *live;
+    int64_t ld_live;
+    const int64_t *targets;
+    // forward
+    float *logp, *lse, *entropy;
+    int top;
+    int64_t *top_ids;
+    float *top_logp;
+    // backward
+    const float *lse_in, *entropy_in, *dlogp, *dentropy;
+    void *dq, *dtable;
+    int64_t lddq, lddt;
+};
+// (with ws null both only count the bytes they need)
+int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s);
+int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s);
+
+int rairs_launch_clear_rows(void *out, int64_t n, int64_t cols, int64_t ld, int dtype, hipStream_t s);
+
+struct ProjectArgs {
+    rairs_projection_t p;
+    const void *x, *dy;
+    int64_t ldx, lddy, n;
+    const int32_t *adapter;
+    void *y, *dx, *da, *db;
+    int64_t ldy, lddx;
+    int ytype;
+};
+int rairs_run_project(const ProjectArgs &a, void *ws, size_t *bytes, hipStream_t s);
+int rairs_run_project_backward(const ProjectArgs &a, void *ws, size_t *bytes, hipStream_t s);
