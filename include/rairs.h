@@ -405,7 +405,7 @@ int rairs_search_projected(rairs_index_t *h, const rairs_projection_t *p, const 
                            float *d_out_dists, void *d_ws, size_t ws_bytes, void *hip_stream);
 
 /*
- * A table of vectors and how it is scored: l_v = scale <q, t_v>, scale > 0 and finite.
+ * A table of vectors and how it is scored: l_v = scale <q, t_v>, scale within [1e-30, 1e30].
  * d_live: device words, bit v & 31 of word v >> 5 set where a query may see row v; ld_live words from one
  * query's mask to the next, 0 for a mask that all queries share; NULL: all rows are live.  Rows of the
  * table that no query sees may hold anything.  V < 2^31 - 64.
@@ -432,7 +432,8 @@ int rairs_index_table(const rairs_index_t *h, rairs_table_t *out);
  *   d_top_ids  device [n][top] int64, d_top_logp [n][top] fp32: the `top` most probable live rows, 0 <=
  *              top <= RAIRS_MAX_TOP, ordered by (inner product in float64, row id): the larger product
  *              first, of equal ones the smaller id; missing entries are id -1, -inf.  A query whose
- *              products are not all finite may get missing entries instead.
+ *              products are not all finite, or whose or whose table's squared norms are not in fp32, may get
+ *              missing entries instead.
  * Products of fp32 rows are as exact as fp32 sums are.  n == 0 is a successful no-op.
  */
 size_t rairs_logprob_workspace_bytes(const rairs_table_t *t, int64_t n, int q_dtype, int top);

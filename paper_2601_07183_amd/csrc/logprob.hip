@@ -4,16 +4,22 @@
 // in registers folds them into a running maximum m, s = sum 2^(z - m) and e = sum 2^(z - m) (z - m) with
 // z = l log2(e), and leaves one {m, s, e} per query and run of table rows ("part").  From them
 //     lse = ln 2 (m + log2 s),     entropy = ln 2 (log2 s - e / s).
-// For the most probable rows it also leaves the largest product of every 16 rows ("group"): a row among
-// the K best lies in a group whose maximum is at least the K-th best maximum less what the sums can be
-// off by, so those groups, little more than K of them, are all that is scored again in float64, which
-// orders rows whose fp32 products are too close to tell apart.
+// For the most probable rows it also leaves the largest products of every 16 (or 64) rows ("group"): a row
+// among the K best lies in a group whose maximum is at least the K-th best maximum less what the sums can
+// be off by.  Groups of 16 also say which row the maximum is, in the value's last four bits, and what the
+// second largest product is, so that little more than K rows are scored again in float64, which orders
+// rows whose fp32 products are too close to tell apart.
+#include <algorithm>
+
 #include "fewrows.h"
 #include "query_ops.h"
 
 #define LOG2E 1.4426950408889634f
 #define LN2 0.6931471805599453f
 #define NEG_INF (-__builtin_huge_valf())
+// the product of a row that the mask hides: finite, and none of its last bits set, so that bits written
+// into it make it smaller
+#define HIDDEN (-0x1.2cecp+126f)
 
 // ---- statistics of a tile ----------------------------------------------------------------------------
 
@@ -24,35 +30,42 @@ struct StatsArgs {
     int64_t ld_live;
     const int64_t *targets;
     float4 *parts;                  // [n][nparts] {m, s, e, 0}; m: the largest product itself, not times c
-    int64_t nparts;
-    float *gmax;                    // [n][ngroups], or null
-    int64_t ngroups;                // 4 per 64 rows: group 4 b + h holds rows 64 b + 16 i + 4 h + r
-    int per;                        // groups per part (the last may have fewer)
+    int nparts;
+    float *gmax;                    // [n][ngroups] {largest, second} or, wide, the largest alone; or null
+    int64_t ngroups;
+    int wide;                       // group 4 b + h holds rows 64 b + 16 i + 4 h + r; wide: group b, all 64 of them
     float *zt;                      // [n] the target's product
 };
 
 // 2^x for x <= 0 (a result below 2^-126 may be flushed)
 static __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <int QT>
+// sums relative to a maximum m0, brought to m1 >= m0
+static __device__ __forceinline__ void rebase(float &s, float &e, float m0, float m1, float c)
+{
+    if (m0 == m1) return;
+    if (m0 == HIDDEN) { s = 0.0f; e = 0.0f; return; }
+    const float d = m0 * c - m1 * c, f = exp2_fast(d);
+    e = f * fmaf(s, fmaxf(d, -1e4f), e);
+    s *= f;
+}
+
+// ENT: e is wanted too.  TOP: the groups' maxima are, 1 wide, 2 with their rows (0: none).
+template <int QT, bool ENT, int TOP>
 struct StatsState {
     float m[QT], s[QT], e[QT];
-    __device__ __forceinline__ void begin()
+    int32_t target[QT];             // the query's target, -1: none (V is below 2^31)
+    __device__ __forceinline__ void begin(const StatsArgs &a, int64_t q0, int lane)
     {
 #pragma unroll
-        for (int j = 0; j < QT; j++) { m[j] = NEG_INF; s[j] = 0.0f; e[j] = 0.0f; }
-    }
-    // sums relative to a maximum m0, brought to m1 >= m0
-    static __device__ __forceinline__ void rebase(float &s, float &e, float m0, float m1, float c)
-    {
-        if (m0 == m1) return;
-        if (m0 == NEG_INF) { s = 0.0f; e = 0.0f; return; }
-        const float d = m0 * c - m1 * c, f = exp2_fast(d);
-        e = f * fmaf(s, fmaxf(d, -1e4f), e);
-        s *= f;
+        for (int j = 0; j < QT; j++) {
+            m[j] = HIDDEN; s[j] = 0.0f; e[j] = 0.0f;
+            const int64_t q = q0 + 16 * j + (lane & 15), t = q < a.n ? a.targets[q] : -1;
+            target[j] = t >= 0 && t < a.V ? (int32_t)t : -1;
+        }
     }
     // a tile's products: rows p0 + 16 i + 4 (lane >> 4) + r, queries q0 + 16 j + (lane & 15); acc is
-    // overwritten (-inf where the mask hides a row)
+    // overwritten (HIDDEN where the mask hides a row)
     template <int PT>
     __device__ __forceinline__ void tile(const StatsArgs &a, v4f (&acc)[PT][QT], int64_t p0, int64_t q0, int lane)
     {
@@ -62,17 +75,19 @@ struct StatsState {
         for (int j = 0; j < QT; j++) {
             const int64_t q = q0 + 16 * j + (lane & 15);
             const bool in = q < a.n;
-            const int64_t row = in ? q : a.n - 1;
             // the target's product, by the lane that has it
-            const int64_t dp = a.targets[row] - p0;
-            if (in && dp >= 0 && dp < 16 * PT && (((int)dp >> 2) & 3) == h) {
+            const uint32_t dp = (uint32_t)target[j] - (uint32_t)p0;
+            if (__any(target[j] >= 0 && dp < 16 * PT)) {              // (seldom)
+                if (target[j] >= 0 && dp < 16 * PT && ((dp >> 2) & 3) == (uint32_t)h) {
 #pragma unroll
-                for (int i = 0; i < PT; i++)
+                    for (int i = 0; i < PT; i++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++)
-                        if ((int)dp == 16 * i + 4 * h + r) a.zt[row] = acc[i][j][r];
+                        for (int r = 0; r < 4; r++)
+                            if ((int)dp == 16 * i + 4 * h + r) a.zt[q] = acc[i][j][r];
+                }
             }
             if (a.live || ragged) {
+                const int64_t row = in ? q : a.n - 1;
 #pragma unroll
                 for (int i = 0; i < PT; i++) {
                     const int64_t p = p0 + 16 * i;                    // (a multiple of 16: within one word of the mask)
@@ -84,35 +99,57 @@ struct StatsState {
                     }
 #pragma unroll
                     for (int r = 0; r < 4; r++)
-                        if (!((bits >> r) & 1u)) acc[i][j][r] = NEG_INF;
+                        if (!((bits >> r) & 1u)) acc[i][j][r] = HIDDEN;
                 }
             }
-            float top = NEG_INF;
+            float top = HIDDEN;
 #pragma unroll
             for (int b = 0; b < PT; b += 4) {
-                float g = NEG_INF;
+                const int64_t blk = p0 / 64 + b / 4;
+                float g = HIDDEN, g2 = HIDDEN;
+                if constexpr (TOP == 2) {
 #pragma unroll
-                for (int i = b; i < b + 4 && i < PT; i++)
-                    g = fmaxf(fmaxf(g, fmaxf(acc[i][j][0], acc[i][j][1])), fmaxf(acc[i][j][2], acc[i][j][3]));
-                const int64_t group = (p0 / 64 + b / 4) * 4 + h;
-                if (a.gmax && in && group < a.ngroups) a.gmax[row * a.ngroups + group] = g;
+                    for (int i = b; i < b + 4; i++)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) {
+                            const float x = __uint_as_float((__float_as_uint(acc[i][j][r]) & ~15u) | (uint32_t)(4 * (i - b) + r));
+                            g2 = __builtin_amdgcn_fmed3f(g, g2, x);
+                            g = fmaxf(g, x);
+                        }
+                    if (in && blk * 4 < a.ngroups) *(float2 *)(a.gmax + (q * a.ngroups + blk * 4 + h) * 2) = make_float2(g, g2);
+                } else {
+#pragma unroll
+                    for (int i = b; i < b + 4; i++)
+                        g = fmaxf(fmaxf(g, fmaxf(acc[i][j][0], acc[i][j][1])), fmaxf(acc[i][j][2], acc[i][j][3]));
+                    if constexpr (TOP == 1) {
+                        float w = fmaxf(g, __shfl_xor(g, 16));
+                        w = fmaxf(w, __shfl_xor(w, 32));
+                        if (in && h == 0 && blk < a.ngroups) a.gmax[q * a.ngroups + blk] = w;
+                    }
+                }
                 top = fmaxf(top, g);
             }
-            const float m1 = fmaxf(m[j], top);
-            rebase(s[j], e[j], m[j], m1, a.c);
-            m[j] = m1;
-            const float mc = m1 == NEG_INF ? 0.0f : m1 * a.c;
+            if (__any(top > m[j])) {                                  // (ever more seldom)
+                const float m1 = fmaxf(m[j], top);
+                rebase(s[j], e[j], m[j], m1, a.c);
+                m[j] = m1;
+            }
+            const float mc = m[j] == HIDDEN ? 0.0f : m[j] * a.c;
+            float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
             for (int i = 0; i < PT; i++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
                     const float t = fmaf(acc[i][j][r], a.c, -mc), x = exp2_fast(t);
-                    s[j] += x;
-                    e[j] = fmaf(x, fmaxf(t, -1e4f), e[j]);
+                    if (r & 1) s1 += x;
+                    else s0 += x;
+                    if constexpr (ENT) e[j] = fmaf(x, fmaxf(t, -1e4f), e[j]);
                 }
+            s[j] += s0 + s1;
+            __builtin_amdgcn_sched_barrier(0);                        // (one query's values at a time in registers)
         }
     }
-    __device__ __forceinline__ void end(const StatsArgs &a, int64_t part, int64_t q0, int lane)
+    __device__ __forceinline__ void end(const StatsArgs &a, int part, int64_t q0, int lane)
     {
 #pragma unroll
         for (int j = 0; j < QT; j++) {
@@ -128,15 +165,24 @@ struct StatsState {
     }
 };
 
+template <bool ENT, int TOP>
 struct StatsEpi {
     StatsArgs a;
     template <class T>
-    __device__ __forceinline__ void operator()(RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
+    struct State {
+        StatsState<T::QT, ENT, TOP> s;
+    };
+    template <class T>
+    __device__ __forceinline__ void begin(State<T> &st, int64_t q0, int lane) const { st.s.begin(a, q0, lane); }
+    template <class T>
+    __device__ __forceinline__ void tile(State<T> &st, RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
     {
-        StatsState<T::QT> st;
-        st.begin();
-        st.tile(a, acc.v, p0, q0, lane);
-        if (p0 < a.V) st.end(a, p0 / (16 * T::PT), q0, lane);
+        if constexpr (T::PT % 4 == 0) st.s.tile(a, acc.v, p0, q0, lane);
+    }
+    template <class T>
+    __device__ __forceinline__ void end(State<T> &st, int run, int wp, int64_t q0, int lane) const
+    {
+        st.s.end(a, run * T::WP + wp, q0, lane);
     }
 };
 
@@ -198,7 +244,7 @@ template <class S, class Q, int QT, bool VEC, bool NORM>
 __global__ __launch_bounds__(WG) void few_stats_kernel(FewStatsArgs a)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t part = (int64_t)blockIdx.x * (WG / 64) + (threadIdx.x >> 6);
+    const int part = blockIdx.x * (WG / 64) + (threadIdx.x >> 6);
     if (part >= a.st.nparts) return;
     const Q *qrow[QT];
 #pragma unroll
@@ -208,11 +254,11 @@ __global__ __launch_bounds__(WG) void few_stats_kernel(FewStatsArgs a)
         qrow[j] = (const Q *)a.q + q * a.ldq;
     }
     const int steps = (a.d + 4 * FewLoad<S>::CH - 1) / (4 * FewLoad<S>::CH);
-    StatsState<QT> st;
-    st.begin();
+    StatsState<QT, true, NORM ? 2 : 0> st;
+    st.begin(a.st, 0, lane);
     float most = 0.0f;
     for (int r = 0; r < a.rounds; r++) {
-        const int64_t p0 = (part * a.rounds + r) * 64;
+        const int64_t p0 = ((int64_t)part * a.rounds + r) * 64;
         if (p0 >= a.st.V) break;
         const S *prow[4];
         v4f acc[4][QT];
@@ -254,145 +300,203 @@ struct FinishArgs {
     StatsArgs st;
     const void *table, *q;
     int64_t ldt, ldq;
-    int d, qvec, tvec;
+    int d, vec;
     float scale;
     float slack;                    // relative error of a product against |q||t|
     const float *xmax;
-    int64_t nxmax;
+    int nxmax;
     float *logp, *lse, *entropy;
     int top;
     int64_t *top_ids;
     float *top_logp;
 };
 
-#define FIN_GROUPS 2048             // groups of the open parts that fit LDS
-#define FIN_BATCH 32                // groups scored at a time
+#define FIN_LIST 1024               // rows (wide: groups) that reach the bound that fit LDS
+#define FIN_ITEMS 1024              // rows to score at a time
 
 struct FinishShared {
-    float red[4][4];
-    float lane_max[WG];
-    double val[FIN_BATCH * 16 + RAIRS_MAX_TOP];
-    uint32_t id[FIN_BATCH * 16 + RAIRS_MAX_TOP];
+    float red[16][4];
+    float kth_in[256];
+    float kth_out;
+    double val[FIN_ITEMS + RAIRS_MAX_TOP];
+    uint32_t id[FIN_ITEMS + RAIRS_MAX_TOP];
     double best[RAIRS_MAX_TOP];
     uint32_t best_id[RAIRS_MAX_TOP];
-    uint32_t take[FIN_BATCH];
-    float gval[FIN_GROUPS];
-    uint32_t gid[FIN_GROUPS];
-    int count, nbest, wcnt[WG / 64];
+    uint32_t take[FIN_ITEMS];
+    float lval[FIN_LIST];
+    uint32_t lid[FIN_LIST];
+    int count, nbest, wcnt[16];
 };
 
-// a lower bound of the k-th largest of all threads' values: the k-th largest of their maxima
-static __device__ __forceinline__ float kth_thread_max(FinishShared &sh, float mine, int k)
+// rows of an entry of the lists: the row itself, a group of 16 or one of 64
+enum { ENTRY_ROW = 1, ENTRY_GROUP = 16, ENTRY_WIDE = 64 };
+static __device__ __forceinline__ int64_t entry_row(uint32_t entry, int member, int kind)
+{
+    return kind == ENTRY_ROW    ? (int64_t)entry
+           : kind == ENTRY_WIDE ? (int64_t)entry * 64 + member
+                                : (int64_t)(entry >> 2) * 64 + 16 * (member >> 2) + 4 * (entry & 3) + (member & 3);
+}
+
+// a lower bound of the k-th largest (k <= 64) of all threads' values: the k-th largest of the maxima of 256 sets
+template <int NT>
+static __device__ __forceinline__ float kth_set_max(FinishShared &sh, float mine, int k)
 {
     const int tid = threadIdx.x;
+#pragma unroll
+    for (int x = 1; x < NT / 256; x <<= 1) mine = fmaxf(mine, __shfl_xor(mine, x));
     __syncthreads();
-    sh.lane_max[tid] = mine;
-    if (tid == 0) sh.red[0][0] = NEG_INF;
+    if (tid % (NT / 256) == 0) sh.kth_in[tid / (NT / 256)] = mine;
+    if (tid == 0) sh.kth_out = NEG_INF;
     __syncthreads();
-    int above = 0;
-    for (int i = 0; i < WG; i++) {
-        const float x = sh.lane_max[i];
-        above += x > mine || (x == mine && i < tid) ? 1 : 0;
+    if (tid < 256) {
+        const float x = sh.kth_in[tid];
+        int above = 0;
+#pragma unroll 8
+        for (int i = 0; i < 256; i += 4) {
+            const v4f y = *(const v4f *)&sh.kth_in[i];
+#pragma unroll
+            for (int u = 0; u < 4; u++) above += y[u] > x || (y[u] == x && i + u < tid) ? 1 : 0;
+        }
+        if (above == k - 1) sh.kth_out = x;
     }
-    if (above == k - 1) sh.red[0][0] = mine;
     __syncthreads();
-    return sh.red[0][0];
+    return sh.kth_out;
 }
 
 // <q, t> in float64 by 16 lanes; the order of the sum depends on d alone, so equal rows get equal values
-template <class S, class Q>
-static __device__ __forceinline__ double dot_exact(const S *t, const Q *q, int d, int sub, int tvec, int qvec)
+template <class S, class Q, bool VEC>
+static __device__ __forceinline__ double dot_exact(const S *t, const Q *q, int d, int sub)
 {
-    constexpr int CH = FewLoad<S>::CH;
+    constexpr int CH = FewLoad<S>::CH, AHEAD = 16 / CH;
     double x = 0.0;
+#pragma unroll AHEAD
     for (int k = sub * CH; k < d; k += 16 * CH) {
-        const FewFrag<S, CH> f = tvec ? few_load<S, CH, true>(t, k, d) : few_load<S, CH, false>(t, k, d);
-        const FewFrag<Q, CH> g = qvec ? few_load<Q, CH, true>(q, k, d) : few_load<Q, CH, false>(q, k, d);
+        const FewFrag<S, CH> f = few_load<S, CH, VEC>(t, k, d);
+        const FewFrag<Q, CH> g = few_load<Q, CH, VEC>(q, k, d);
 #pragma unroll
         for (int e = 0; e < CH; e++) x = fma((double)(float)f.e[e], (double)(float)g.e[e], x);
     }
+#pragma unroll
     for (int s = 8; s > 0; s >>= 1) x += __shfl_xor(x, s);
     return x;
 }
 
-// scores the `cnt` groups in sh.take and merges their rows into sh.best
-template <class S, class Q>
-static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishShared &sh, int64_t row, int cnt)
+// scores the rows of the `cnt` entries in sh.take and merges those of at least `floor` into sh.best
+template <class S, class Q, int NT>
+static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishShared &sh, int64_t row, int cnt, int kind, double floor)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & 15, quarter = lane >> 4;
     const Q *q = (const Q *)a.q + row * a.ldq;
-    for (int it = wave; it < cnt * 4; it += WG / 64) {
-        const uint32_t g = sh.take[it >> 2];
-        const int64_t v = (int64_t)(g >> 2) * 64 + 16 * (it & 3) + 4 * (g & 3) + quarter;
-        const bool in = v < a.st.V && (!a.st.live || ((a.st.live[row * a.st.ld_live + (v >> 5)] >> (v & 31)) & 1u));
-        const double x = dot_exact<S, Q>((const S *)a.table + (in ? v : 0) * a.ldt, q, a.d, sub, a.tvec, a.qvec);
-        if (sub == 0) {
-            const int slot = it * 4 + quarter;
-            const bool ok = in && x == x;
-            sh.val[slot] = ok ? x : 0.0;
-            sh.id[slot] = ok ? (uint32_t)v : 0xFFFFFFFFu;
+    const int old = sh.nbest;
+    if (tid < old) {
+        sh.val[tid] = sh.best[tid];
+        sh.id[tid] = sh.best_id[tid];
+    }
+    if (tid == 0) sh.count = old;
+    __syncthreads();
+    const int items = cnt * kind;
+#pragma unroll 1
+    for (int i0 = wave * 4; i0 < items; i0 += NT / 16) {              // four rows per wave, 16 lanes each
+        const int i = i0 + quarter, ic = i < items ? i : items - 1;
+        const int64_t v = entry_row(sh.take[ic / kind], ic % kind, kind);
+        const bool in = i < items && v < a.st.V && (!a.st.live || ((a.st.live[row * a.st.ld_live + (v >> 5)] >> (v & 31)) & 1u));
+        const S *t = (const S *)a.table + (in ? v : 0) * a.ldt;
+        const double x = a.vec ? dot_exact<S, Q, true>(t, q, a.d, sub) : dot_exact<S, Q, false>(t, q, a.d, sub);
+        if (sub == 0 && in && x >= floor) {                           // (not a NaN either)
+            const int slot = atomicAdd(&sh.count, 1);
+            sh.val[slot] = x;
+            sh.id[slot] = (uint32_t)v;
         }
     }
-    const int old = sh.nbest, total = cnt * 16 + old;
-    if (tid < old) {
-        sh.val[cnt * 16 + tid] = sh.best[tid];
-        sh.id[cnt * 16 + tid] = sh.best_id[tid];
-    }
-    if (tid == 0) sh.count = 0;
     __syncthreads();
-    for (int i = tid; i < total; i += WG) {
+    const int total = sh.count;
+#pragma unroll 1
+    for (int i = tid; i < total; i += NT) {
         const double x = sh.val[i];
         const uint32_t id = sh.id[i];
-        if (id == 0xFFFFFFFFu) continue;
         int rank = 0;
-        for (int j = 0; j < total && rank < a.top; j++) {
-            const uint32_t idj = sh.id[j];
-            rank += idj != 0xFFFFFFFFu && (sh.val[j] > x || (sh.val[j] == x && idj < id)) ? 1 : 0;
-        }
+        for (int j = 0; j < total; j++) rank += sh.val[j] > x || (sh.val[j] == x && sh.id[j] < id) ? 1 : 0;
         if (rank < a.top) {
             sh.best[rank] = x;
             sh.best_id[rank] = id;
-            atomicAdd(&sh.count, 1);
         }
     }
-    __syncthreads();
-    if (tid == 0) sh.nbest = sh.count;
+    if (tid == 0) sh.nbest = total < a.top ? total : a.top;
     __syncthreads();
 }
 
-template <class S, class Q>
-__global__ __launch_bounds__(WG) void logprob_finish_kernel(FinishArgs a)
+// the entries with want set, FIN_ITEMS rows at a time, until none is left (drop() is asked again before each time)
+template <class S, class Q, int NT, class Drop>
+static __device__ __forceinline__ void finish_entries(const FinishArgs &a, FinishShared &sh, int64_t row, bool want, uint32_t entry, int kind,
+                                                      double floor, const Drop &drop)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, most = FIN_ITEMS / kind;
+    for (;;) {
+        if (want && drop()) want = false;
+        const unsigned long long b = __ballot(want);
+        if (lane == 0) sh.wcnt[wave] = __popcll(b);
+        __syncthreads();
+        int at = __popcll(b & ((1ull << lane) - 1ull)), total = 0;
+        for (int w = 0; w < NT / 64; w++) {
+            at += w < wave ? sh.wcnt[w] : 0;
+            total += sh.wcnt[w];
+        }
+        if (want && at < most) {
+            sh.take[at] = entry;
+            want = false;
+        }
+        __syncthreads();
+        if (total == 0) return;                                       // uniform
+        finish_batch<S, Q, NT>(a, sh, row, total < most ? total : most, kind, floor);
+    }
+}
+
+template <class S, class Q, int NT>
+__global__ __launch_bounds__(NT, 4) void logprob_finish_kernel(FinishArgs a)
 {
     __shared__ FinishShared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row = blockIdx.x;
     const float4 *parts = a.st.parts + row * a.st.nparts;
     const float c = a.st.c;
-    float m = NEG_INF, s = 0.0f, e = 0.0f;
-    for (int64_t i = tid; i < a.st.nparts; i += WG) {
+    float m = HIDDEN, s = 0.0f, e = 0.0f;
+    for (int i = tid; i < a.st.nparts; i += NT) {
         float4 p = parts[i];
         const float m1 = fmaxf(m, p.x);
-        StatsState<1>::rebase(s, e, m, m1, c);
-        StatsState<1>::rebase(p.y, p.z, p.x, m1, c);
+        rebase(s, e, m, m1, c);
+        rebase(p.y, p.z, p.x, m1, c);
         s += p.y;
         e += p.z;
         m = m1;
     }
-    const float mine = m;
+    // |q|^2 and the table's largest squared norm, for the margin; and the groups' maxima
+    float q2 = 0.0f, x2 = 0.0f, most = HIDDEN;
+    bool zero = true;
+    const float *gmax = a.st.gmax + row * a.st.ngroups * (a.st.wide ? 1 : 2);
+    if (a.top) {
+        const Q *q = (const Q *)a.q + row * a.ldq;
+        for (int k = tid; k < a.d; k += NT) {
+            const float x = (float)q[k];
+            q2 = fmaf(x, x, q2);
+            zero = zero && x == 0.0f;
+        }
+        for (int i = tid; i < a.nxmax; i += NT) x2 = fmaxf(x2, a.xmax[i]);
+        if (a.st.wide) {
+#pragma unroll 8
+            for (int64_t g = tid; g < a.st.ngroups; g += NT) most = fmaxf(most, gmax[g]);
+        } else {
+#pragma unroll 8
+            for (int64_t g = tid; g < a.st.ngroups; g += NT) most = fmaxf(most, gmax[2 * g]);
+        }
+    }
     float top = m;
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
     if (lane == 0) sh.red[wave][0] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(sh.red[0][0], sh.red[1][0]), fmaxf(sh.red[2][0], sh.red[3][0]));
-    StatsState<1>::rebase(s, e, m, top, c);
-    // |q|^2 and the table's largest squared norm, for the margin
-    float q2 = 0.0f, x2 = 0.0f;
-    if (a.top) {
-        const Q *q = (const Q *)a.q + row * a.ldq;
-        for (int k = tid; k < a.d; k += WG) q2 = fmaf((float)q[k], (float)q[k], q2);
-        for (int64_t i = tid; i < a.nxmax; i += WG) x2 = fmaxf(x2, a.xmax[i]);
-    }
+    top = sh.red[0][0];
+    for (int w = 1; w < NT / 64; w++) top = fmaxf(top, sh.red[w][0]);
+    rebase(s, e, m, top, c);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) {
         s += __shfl_xor(s, x);
@@ -403,11 +507,14 @@ __global__ __launch_bounds__(WG) void logprob_finish_kernel(FinishArgs a)
     __syncthreads();
     if (lane == 0) { sh.red[wave][0] = s; sh.red[wave][1] = e; sh.red[wave][2] = q2; sh.red[wave][3] = x2; }
     __syncthreads();
-    s = (sh.red[0][0] + sh.red[1][0]) + (sh.red[2][0] + sh.red[3][0]);
-    e = (sh.red[0][1] + sh.red[1][1]) + (sh.red[2][1] + sh.red[3][1]);
-    q2 = (sh.red[0][2] + sh.red[1][2]) + (sh.red[2][2] + sh.red[3][2]);
-    x2 = fmaxf(fmaxf(sh.red[0][3], sh.red[1][3]), fmaxf(sh.red[2][3], sh.red[3][3]));
-    const bool empty = top == NEG_INF && s == 0.0f;
+    s = e = q2 = x2 = 0.0f;
+    for (int w = 0; w < NT / 64; w++) {
+        s += sh.red[w][0];
+        e += sh.red[w][1];
+        q2 += sh.red[w][2];
+        x2 = fmaxf(x2, sh.red[w][3]);
+    }
+    const bool empty = top == HIDDEN && s == 0.0f;
     const float mc = top * c, logs = log2f(s);
     if (tid == 0) {
         a.lse[row] = empty ? NEG_INF : (mc + logs) * LN2;
@@ -419,106 +526,67 @@ __global__ __launch_bounds__(WG) void logprob_finish_kernel(FinishArgs a)
             lp = seen ? (fmaf(a.st.zt[row], c, -mc) - logs) * LN2 : NEG_INF;
         }
         a.logp[row] = lp;
+        sh.nbest = 0;
+        sh.count = 0;
     }
     if (a.top == 0) return;
 
-    // what a product may be off by, twice; not finite: nothing can be told apart
-    const float eps = a.slack * sqrtf(q2) * sqrtf(x2) * 1.0001f;
-    if (tid == 0) sh.nbest = 0;
-    __syncthreads();
+    // what a product may be off by (components whose squares underflow, and a group's row in the last bits of a
+    // denormal, have terms of their own); not finite: nothing can be told apart
+    const float under = sqrtf((float)a.d) * 1.1e-19f;
+    const float eps = a.slack * (sqrtf(q2) + under) * (sqrtf(x2) + under) * 1.0001f + 4e-44f;
+    const bool zeros = __syncthreads_and(zero);                       // a query of zeros: every product is 0
     if (!empty && eps < 1e38f) {                                      // uniform
-        float thr = kth_thread_max(sh, mine, a.top) - 2.0f * eps;
-        // the groups of the parts that reach it
-        const int per = a.st.per;
-        const float *gmax = a.st.gmax + row * a.st.ngroups;
-        if (tid == 0) sh.count = 0;
-        __syncthreads();
-        for (int64_t i = tid; i < a.st.nparts; i += WG)
-            if (parts[i].x >= thr && parts[i].x > NEG_INF) {
-                const int at = atomicAdd(&sh.count, 1);
-                if (at < FIN_GROUPS) sh.gid[at] = (uint32_t)i;
-            }
-        __syncthreads();
-        const int nopen = sh.count;
-        __syncthreads();
-        if ((int64_t)nopen * per <= FIN_GROUPS) {
-            // list their groups, tighten the bound, and score what reaches it
-            uint32_t part_of[(FIN_GROUPS + WG - 1) / WG];
-            const int slots = nopen * per;
-#pragma unroll
-            for (int u = 0; u < FIN_GROUPS / WG; u++) {
-                const int i = u * WG + tid;
-                part_of[u] = i < slots ? sh.gid[i / per] : 0u;
-            }
-            __syncthreads();
-            float most = NEG_INF;
-#pragma unroll
-            for (int u = 0; u < FIN_GROUPS / WG; u++) {
-                const int i = u * WG + tid;
-                if (i < slots) {
-                    const int64_t g = (int64_t)part_of[u] * per + i % per;
-                    const float x = g < a.st.ngroups ? gmax[g] : NEG_INF;
-                    sh.gval[i] = x;
-                    sh.gid[i] = (uint32_t)g;
-                    most = fmaxf(most, x);
+        const float thr = kth_set_max<NT>(sh, most, a.top) - 2.0f * eps;
+        // exact products of the K best are at least this
+        const double floor = (double)thr + (double)eps * 0.999;
+        if (most >= thr && most > HIDDEN)
+            for (int64_t g = tid; g < a.st.ngroups; g += NT) {
+                if (a.st.wide) {
+                    const float x = gmax[g];
+                    if (x >= thr && x > HIDDEN) {
+                        const int at = atomicAdd(&sh.count, 1);
+                        if (at < FIN_LIST) {
+                            sh.lval[at] = x;
+                            sh.lid[at] = (uint32_t)g;
+                        }
+                    }
+                } else {
+                    const float2 x = *(const float2 *)(gmax + 2 * g);
+                    if (x.x >= thr && x.x > HIDDEN) {
+                        // the group's best row alone, or all of its rows if another may reach the bound too
+                        const int rows = x.y >= thr ? 16 : 1, at = atomicAdd(&sh.count, rows);
+                        for (int u = 0; u < rows && at + u < FIN_LIST; u++) {
+                            sh.lval[at + u] = x.x;
+                            sh.lid[at + u] = (uint32_t)entry_row((uint32_t)g, rows == 1 ? (int)(__float_as_uint(x.x) & 15u) : u, ENTRY_GROUP);
+                        }
+                    }
                 }
             }
-            thr = fmaxf(thr, kth_thread_max(sh, most, a.top) - 2.0f * eps);
-            for (int i0 = 0; i0 < slots; i0 += WG) {
+        __syncthreads();
+        const int found = sh.count;
+        __syncthreads();
+        if (found <= FIN_LIST) {
+            for (int i0 = 0; i0 < found; i0 += NT) {
                 const int i = i0 + tid;
-                bool want = i < slots && sh.gval[i] >= thr && sh.gval[i] > NEG_INF;
-                for (;;) {
-                    // rows that cannot reach the K-th best so far are left out
-                    if (sh.nbest == a.top && want && (double)sh.gval[i] + (double)eps < sh.best[a.top - 1]) want = false;
-                    const unsigned long long b = __ballot(want);
-                    if (lane == 0) sh.wcnt[wave] = __popcll(b);
-                    __syncthreads();
-                    int at = __popcll(b & ((1ull << lane) - 1ull)), total = 0;
-                    for (int w = 0; w < WG / 64; w++) {
-                        at += w < wave ? sh.wcnt[w] : 0;
-                        total += sh.wcnt[w];
-                    }
-                    if (total == 0) break;
-                    if (want && at < FIN_BATCH) {
-                        sh.take[at] = sh.gid[i];
-                        want = false;
-                    }
-                    __syncthreads();
-                    finish_batch<S, Q>(a, sh, row, total < FIN_BATCH ? total : FIN_BATCH);
-                }
-                __syncthreads();
+                const float x = i < found ? sh.lval[i] : HIDDEN;
+                // (an entry that cannot reach the K-th best so far is left out)
+                finish_entries<S, Q, NT>(a, sh, row, i < found, i < found ? sh.lid[i] : 0u, a.st.wide ? ENTRY_WIDE : ENTRY_ROW, floor, [&]() {
+                    return sh.nbest == a.top && (double)x + (double)eps < sh.best[a.top - 1];
+                });
             }
         } else {
-            // so many equal products that the list does not hold them: all groups in order of their rows,
-            // so that one that can only equal the K-th best comes too late to displace it
-            for (int64_t g0 = 0; g0 < a.st.ngroups; g0 += WG) {
+            // so many equal products that the list does not hold them: all groups in order of their blocks of 64
+            // rows, so that a block whose rows can only equal the K-th best comes too late to displace it
+            for (int64_t g0 = 0; g0 < a.st.ngroups; g0 += NT) {
                 const int64_t g = g0 + tid;
-                const float x = g < a.st.ngroups ? gmax[g] : NEG_INF;
-                bool want = x >= thr && x > NEG_INF;
-                for (;;) {
-                    // (a group's rows lie within its block of 64: whole blocks before it are done, so an
-                    // equal product in it has a larger id than any held from those; within the block ids cross)
-                    if (sh.nbest == a.top && want) {
-                        const double k = sh.best[a.top - 1], up = (double)x + (double)eps;
-                        if (up < k || (up == k && (int64_t)(sh.best_id[a.top - 1] >> 6) < (g >> 2))) want = false;
-                    }
-                    const unsigned long long b = __ballot(want);
-                    if (lane == 0) sh.wcnt[wave] = __popcll(b);
-                    __syncthreads();
-                    int at = __popcll(b & ((1ull << lane) - 1ull)), total = 0;
-                    for (int w = 0; w < WG / 64; w++) {
-                        at += w < wave ? sh.wcnt[w] : 0;
-                        total += sh.wcnt[w];
-                    }
-                    if (total == 0) break;
-                    if (want && at < FIN_BATCH) {
-                        sh.take[at] = (uint32_t)g;
-                        want = false;
-                    }
-                    __syncthreads();
-                    finish_batch<S, Q>(a, sh, row, total < FIN_BATCH ? total : FIN_BATCH);
-                }
-                __syncthreads();
+                const float x = g < a.st.ngroups ? gmax[a.st.wide ? g : 2 * g] : HIDDEN;
+                const int64_t blk = a.st.wide ? g : g >> 2;
+                finish_entries<S, Q, NT>(a, sh, row, x >= thr && x > HIDDEN, (uint32_t)g, a.st.wide ? ENTRY_WIDE : ENTRY_GROUP, floor, [&]() {
+                    if (sh.nbest < a.top) return false;
+                    const double k = sh.best[a.top - 1], up = zeros ? 0.0 : (double)x + (double)eps;
+                    return up < k || (up == k && (int64_t)(sh.best_id[a.top - 1] >> 6) < blk);
+                });
             }
         }
     }
@@ -552,41 +620,62 @@ template <int NP>
 struct GradEpi {
     GradArgs a;
     template <class T>
-    __device__ __forceinline__ void operator()(RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
+    struct State {
+        float da[T::QT], db[T::QT], H[T::QT], lse[T::QT];
+        int32_t target[T::QT];      // from the chunk's first row on, or far below it
+    };
+    template <class T>
+    __device__ __forceinline__ void begin(State<T> &st, int64_t q0, int lane) const
+    {
+#pragma unroll
+        for (int j = 0; j < T::QT; j++) {
+            const int64_t q = q0 + 16 * j + (lane & 15);
+            const bool in = q < a.n;
+            const int64_t row = in ? q : a.n - 1, t = a.targets[row];
+            const bool seen = t >= 0 && t < a.V && (!a.live || ((a.live[row * a.ld_live + (t >> 5)] >> (t & 31)) & 1u));
+            st.da[j] = in && seen ? a.dlogp[row] * a.scale : 0.0f;
+            st.db[j] = in && a.dentropy ? a.dentropy[row] * a.scale : 0.0f;
+            st.H[j] = st.db[j] != 0.0f ? a.entropy[row] : 0.0f;
+            st.lse[j] = a.lse[row];
+            st.target[j] = seen ? (int32_t)(t - a.v0) : -0x7FFFFFFF;
+        }
+    }
+    template <class T>
+    __device__ __forceinline__ void end(State<T> &, int, int, int64_t, int) const {}
+    template <class T>
+    __device__ __forceinline__ void tile(State<T> &st, RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
     {
         if (p0 >= a.vc) return;
         const int h = lane >> 4;
+        const bool checked = a.live || a.v0 + p0 + 16 * T::PT > a.V;  // uniform: a mask, or the table's end
 #pragma unroll
         for (int j = 0; j < T::QT; j++) {
             const int64_t q = q0 + 16 * j + (lane & 15);
             if (q >= a.npad) continue;
             const bool in = q < a.n;
-            const int64_t row = in ? q : a.n - 1;
-            const int64_t t = a.targets[row];
-            const uint32_t *live = a.live ? a.live + row * a.ld_live : nullptr;
-            const bool seen = t >= 0 && t < a.V && (!live || ((live[t >> 5] >> (t & 31)) & 1u));
-            const float da = in && seen ? a.dlogp[row] * a.scale : 0.0f;
-            const float db = in && a.dentropy ? a.dentropy[row] * a.scale : 0.0f;
-            const float H = db != 0.0f ? a.entropy[row] : 0.0f;
-            const float lse = a.lse[row];
+            const float da = st.da[j], db = st.db[j], H = st.H[j], lse = st.lse[j];
             const bool dead = da == 0.0f && db == 0.0f;
 #pragma unroll
             for (int i = 0; i < T::PT; i++) {
                 const int64_t p = p0 + 16 * i + 4 * h, v = a.v0 + p;
                 if (p >= a.vc) continue;
-                uint32_t bits = 0;
-                if (!dead && v < a.V) {
-                    bits = live ? live[v >> 5] >> (v & 31) : 0xFu;
-                    const int64_t left = a.V - v;
-                    bits &= left >= 4 ? 0xFu : (1u << left) - 1u;
+                uint32_t bits = dead ? 0u : 0xFu;
+                if (checked && !dead) {
+                    bits = 0;
+                    if (v < a.V) {
+                        bits = a.live ? a.live[(in ? q : 0) * a.ld_live + (v >> 5)] >> (v & 31) : 0xFu;
+                        const int64_t left = a.V - v;
+                        bits &= left >= 4 ? 0xFu : (1u << left) - 1u;
+                    }
                 }
                 __bf16 o[NP][4];
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
                     // (log p in natural units: scale times the product is exact inside the sum, which log2(e) is not)
                     const float x = fmaf(acc.v[i][j][r], a.scale, -lse), pr = exp2_fast(x * LOG2E);
-                    const float one = v + r == t ? 1.0f : 0.0f;
-                    float g = da * (one - pr) - db * pr * (fmaxf(x, -1e4f) + H);
+                    const float one = (int)p + r == st.target[j] ? 1.0f : 0.0f;
+                    float g = da * (one - pr);
+                    if (a.dentropy) g -= db * pr * (fmaxf(x, -1e4f) + H);
                     g = (bits >> r) & 1u ? g : 0.0f;
                     o[0][r] = (__bf16)g;
                     if constexpr (NP == 3) {
@@ -650,26 +739,6 @@ __global__ __launch_bounds__(WG) void clear_rows_kernel(void *out, int64_t n, in
 
 #define FEW_ROWS 64                 // up to here the table's rows go straight into registers
 
-typedef RowTile<4, 4, 2, 2> LogTile;
-
-int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, __bf16 *room, RowOperand &out,
-                  hipStream_t s)
-{
-    const int64_t kpad = pad_to(cols, ROWPROD_K);
-    out.rows = rows;
-    out.perm = nullptr;
-    if (!live && rows_lie_right(src, dtype, ld, cols)) {
-        out.p = (const __bf16 *)src;
-        out.ld = ld;
-        out.piece = 0;
-        return RAIRS_OK;
-    }
-    out.p = room;
-    out.ld = kpad;
-    out.piece = rows * kpad;
-    return rairs_launch_pack_rows(src, dtype, ld, rows, cols, live, room, kpad, s);
-}
-
 static int lies_vec(const void *p, int dtype, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * dtype_width(dtype) % 16 == 0; }
 
 static const uint32_t *any_live(const LogprobArgs &a, uint32_t *room, hipStream_t s, int *rc)
@@ -706,24 +775,54 @@ static int few_stats(const FewStatsArgs &fa, bool vec, bool norm, hipStream_t s)
     return RAIRS_OK;
 }
 
+// A product of fp32 sums may be off by: every addition may round (or cut) at 2^-23 of a partial sum, which
+// |q||t| bounds; the 64 covers the products of pieces that are left out and the smaller ones' sums, and the
+// last term the bits that say which row of a group it is.
+static float product_slack(int d) { return (1.1f * (float)d + 64.0f) * 1.1920929e-7f + 1.9073486e-6f; }
+
+template <class S, class Q>
+static int finish_launch(const FinishArgs &f, hipStream_t s)
+{
+    // few rows: as many waves on each as there can be, since a row's groups are scored by one workgroup
+    if (f.st.n <= FEW_ROWS) hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 1024>), dim3((unsigned)f.st.n), dim3(1024), 0, s, f);
+    else hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 256>), dim3((unsigned)f.st.n), dim3(256), 0, s, f);
+    RAIRS_HIP(hipGetLastError());
+    return RAIRS_OK;
+}
+
+template <bool ENT, int TOP>
+static int stats_launch(RowProd &rp, const StatsArgs &st, bool large, int64_t prun, hipStream_t s)
+{
+    return large ? rowprod_launch<TileL>(rp, StatsEpi<ENT, TOP>{st}, s, (int)prun) : rowprod_launch<TileM>(rp, StatsEpi<ENT, TOP>{st}, s, (int)prun);
+}
+
 int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
 {
     const bool few = a.n <= FEW_ROWS;
-    const int64_t blocks = (a.V + 63) / 64;
+    const int64_t blocks = (a.V + 63) / 64, kpad = pad_to(a.d, ROWPROD_K);
     // a few rounds of 64 rows per wave where there are waves enough for every SIMD without
     const int rounds = few ? (int)(blocks / 4096 < 1 ? 1 : blocks / 4096 > 16 ? 16 : blocks / 4096) : 1;
-    const int64_t unit = few ? 64 * rounds : 16 * LogTile::PT, nparts = (a.V + unit - 1) / unit;
-    const int64_t ngroups = blocks * 4, kpad = pad_to(a.d, ROWPROD_K);
+    // runs of p tiles: as long as about two workgroups (four of the smaller tile) for every CU are left
+    const bool large = rowprod_size(a.V, a.n) == 2;
+    const int64_t ptiles = large ? (a.V + TileL::BP - 1) / TileL::BP : (a.V + TileM::BP - 1) / TileM::BP;
+    const int64_t qtiles = large ? (a.n + TileL::BQ - 1) / TileL::BQ : (a.n + TileM::BQ - 1) / TileM::BQ;
+    const int64_t prun = few ? 1 : std::max<int64_t>(1, std::min<int64_t>(64, ptiles * qtiles / (large ? 512 : 1024)));
+    const int nparts = (int)(few ? (blocks + rounds - 1) / rounds : (ptiles + prun - 1) / prun * 2);     // (both tiles: two waves along P)
+    // Groups of 16 rows or of 64.  Per query, the smaller ones cost two more operations a row and 8 bytes for 16 rows
+    // instead of 4 for 64, about 0.14 ps times V; the larger ones 64 rows of the table for each of the `top`, at about
+    // 6 TB/s.  (A few queries: the vector units have nothing else to do.)
+    const int wide = !few && a.V > 76ll * a.top * a.d * dtype_width(a.ttype);
+    const int64_t ngroups = wide ? blocks : blocks * 4;
     Carve w(ws);
     StatsArgs st = {};
     st.n = a.n; st.V = a.V; st.c = a.scale * LOG2E; st.live = a.live; st.ld_live = a.ld_live; st.targets = a.targets;
     st.parts = w.take<float4>(a.n * nparts);
     st.nparts = nparts;
-    st.gmax = a.top ? w.take<float>(a.n * ngroups) : nullptr;
+    st.gmax = a.top ? w.take<float>(a.n * ngroups * (wide ? 1 : 2)) : nullptr;
     st.ngroups = ngroups;
-    st.per = (int)(unit / 16);
+    st.wide = wide;
     st.zt = w.take<float>(a.n);
-    const int64_t nx = few ? nparts : NORM_WGS;
+    const int nx = few ? nparts : NORM_WGS;
     float *xmax = w.take<float>(nx);
     uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
     // (packed whether they need it or not, so that the size does not depend on where the rows lie)
@@ -758,26 +857,25 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
         rp.ksteps = (int)(kpad / ROWPROD_K);
         if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, qroom, rp.Q, s))) return rc;
         if ((rc = rairs_operand(a.table, a.ttype, a.ldt, a.V, a.d, nullptr, troom, rp.P, s))) return rc;
-        if ((rc = rowprod_launch<LogTile>(rp, StatsEpi{st}, s))) return rc;
+        const bool ent = a.entropy != nullptr;
+        if (a.top == 0) rc = ent ? stats_launch<true, 0>(rp, st, large, prun, s) : stats_launch<false, 0>(rp, st, large, prun, s);
+        else if (wide) rc = ent ? stats_launch<true, 1>(rp, st, large, prun, s) : stats_launch<false, 1>(rp, st, large, prun, s);
+        else rc = ent ? stats_launch<true, 2>(rp, st, large, prun, s) : stats_launch<false, 2>(rp, st, large, prun, s);
+        if (rc) return rc;
     }
     FinishArgs f = {};
     f.st = st;
     f.table = a.table; f.q = a.q; f.ldt = a.ldt; f.ldq = a.ldq; f.d = a.d;
-    f.qvec = lies_vec(a.q, a.qtype, a.ldq);
-    f.tvec = lies_vec(a.table, a.ttype, a.ldt);
+    f.vec = lies_vec(a.q, a.qtype, a.ldq) && lies_vec(a.table, a.ttype, a.ldt);
     f.scale = a.scale;
-    // every addition may round (or cut) at 2^-23 of a partial sum, which |q||t| bounds; the products of pieces that are
-    // left out, and the smaller ones' sums, are covered by the rest
-    f.slack = (1.1f * a.d + 64.0f) * 1.1920929e-7f;
+    f.slack = product_slack(a.d);
     f.xmax = xmax;
     f.nxmax = nx;
     f.logp = a.logp; f.lse = a.lse; f.entropy = a.entropy;
     f.top = a.top; f.top_ids = a.top_ids; f.top_logp = a.top_logp;
-    if (a.ttype == RAIRS_BF16) hipLaunchKernelGGL((logprob_finish_kernel<__bf16, __bf16>), dim3((unsigned)a.n), dim3(WG), 0, s, f);
-    else if (a.ttype == RAIRS_F32) hipLaunchKernelGGL((logprob_finish_kernel<float, float>), dim3((unsigned)a.n), dim3(WG), 0, s, f);
-    else hipLaunchKernelGGL((logprob_finish_kernel<uint8_t, float>), dim3((unsigned)a.n), dim3(WG), 0, s, f);
-    RAIRS_HIP(hipGetLastError());
-    return RAIRS_OK;
+    return a.ttype == RAIRS_BF16 ? finish_launch<__bf16, __bf16>(f, s)
+           : a.ttype == RAIRS_F32 ? finish_launch<float, float>(f, s)
+                                  : finish_launch<uint8_t, float>(f, s);
 }
 
 // G is made for as many of the table's rows at a time as 128 MB of it hold, half of the last-level
@@ -794,7 +892,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     const int64_t chunks = (a.V + vc - 1) / vc;
     vc = pad_to((a.V + chunks - 1) / chunks, ROWPROD_K);              // of about one size
     // workgroups for the queries' product: its sum over the chunk is cut so that there are about two for every CU
-    const int64_t tiles = ((a.d + LogTile::BP - 1) / LogTile::BP) * ((a.n + LogTile::BQ - 1) / LogTile::BQ);
+    const int64_t tiles = ((a.d + TileM::BP - 1) / TileM::BP) * ((a.n + TileM::BQ - 1) / TileM::BQ);
     int splits = (int)(512 / tiles < 1 ? 1 : 512 / tiles);
     const int64_t most = vc / 512 < 1 ? 1 : vc / 512;
     if (splits > most) splits = (int)most;
@@ -837,7 +935,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         ga.lse = a.lse_in; ga.entropy = a.entropy_in; ga.dlogp = a.dlogp; ga.dentropy = a.dentropy;
         ga.g = g; ga.gt = gt;
         ga.gpiece = a.n * cpad; ga.gtpiece = cpad * npad;
-        rc = np == 3 ? rowprod_launch<LogTile>(rp, GradEpi<3>{ga}, s) : rowprod_launch<LogTile>(rp, GradEpi<1>{ga}, s);
+        rc = np == 3 ? rowprod_launch_any(rp, GradEpi<3>{ga}, s) : rowprod_launch_any(rp, GradEpi<1>{ga}, s);
         if (rc) return rc;
         if (need_dq) {
             // (rows that nobody sees are zero here: their G is zero, and they may hold anything)
@@ -851,7 +949,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
             dp.ksteps = (int)(cpad / ROWPROD_K);
             dp.splits = splits;
             StoreEpi e = {sums, a.d, a.n * a.d, a.d, a.n, nullptr, 0, v0 > 0};
-            if ((rc = rowprod_launch<LogTile>(dp, e, s))) return rc;
+            if ((rc = rowprod_launch_any(dp, e, s))) return rc;
         }
         if (need_dt) {
             RowProd dp = {};
@@ -860,7 +958,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
             dp.Q = RowOperand{gt, npad, cpad * npad, rows, nullptr};
             dp.ksteps = (int)(npad / ROWPROD_K);
             StoreEpi e = {(char *)a.dtable + v0 * a.lddt * dtype_width(a.ttype), a.lddt, 0, a.d, rows, nullptr, a.ttype == RAIRS_BF16, 0};
-            if ((rc = rowprod_launch<LogTile>(dp, e, s))) return rc;
+            if ((rc = rowprod_launch_any(dp, e, s))) return rc;
         }
     }
     if (need_dq) {

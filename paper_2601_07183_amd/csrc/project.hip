@@ -15,8 +15,6 @@
 #define UNIT_ROWS 16                // rows of one adapter that one workgroup multiplies by A
 #define CHUNK_ROWS 128              // rows of one adapter in one partial sum of its gradient
 
-typedef RowTile<4, 4, 2, 2> ProjTile;
-
 // ---- rows in order of their adapter ------------------------------------------------------------------
 
 struct SortView {
@@ -441,20 +439,19 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     RowProd rp = {};
     rowprod_pieces(rp, np, np);
     rp.ksteps = (int)(pad_to(p.d_in, ROWPROD_K) / ROWPROD_K);
+    if (use && (rc = sort_launch(sv, s))) return rc;
     if ((rc = rairs_operand(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, wroom, rp.P, s))) return rc;
-    if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, nullptr, xroom, rp.Q, s))) return rc;
+    if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, xroom, rp.Q, s))) return rc;
     if (use) {
-        if ((rc = sort_launch(sv, s))) return rc;
         ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side};
         const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
         const int64_t units = max_units(g.n, p.n_adapters, UNIT_ROWS);
         if ((rc = p.dtype == RAIRS_BF16 ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s))) return rc;
         if ((rc = pack_side_launch(p.B, p.dtype, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, p.n_adapters, side, bp, zero, s))) return rc;
-        rp.Q.perm = sv.perm;
         rp.ad = AdapterPart{up, bp, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.y, g.ldy, 0, p.d_out, g.n, use ? sv.perm : nullptr, g.ytype == RAIRS_BF16, 0};
-    return rowprod_launch<ProjTile>(rp, e, s);
+    return use ? rowprod_launch_any<true>(rp, e, s) : rowprod_launch_any(rp, e, s);
 }
 
 // ---- backward ------------------------------------------------------------------------------------------
@@ -599,12 +596,11 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     rp.ksteps = (int)(opad / ROWPROD_K);
     if ((rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, 0, 1, p.d_out, p.d_in, nullptr, nullptr, wt, opad, 0, p.d_in * opad, s))) return rc;
     rp.P = RowOperand{wt, opad, p.d_in * opad, p.d_in, nullptr};
-    if ((rc = rairs_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, nullptr, yroom, rp.Q, s))) return rc;
+    if ((rc = rairs_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, yroom, rp.Q, s))) return rc;
     if (use) {
         if ((rc = pack_side_launch(p.A, p.dtype, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, na, side, ap, zero, s))) return rc;
-        rp.Q.perm = sv.perm;
         rp.ad = AdapterPart{vp, ap, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.dx, g.lddx, 0, p.d_in, g.n, use ? sv.perm : nullptr, bf, 0};
-    return rowprod_launch<ProjTile>(rp, e, s);
+    return use ? rowprod_launch_any<true>(rp, e, s) : rowprod_launch_any(rp, e, s);
 }

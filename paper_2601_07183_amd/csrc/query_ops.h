@@ -21,7 +21,8 @@ struct Carve {
 };
 
 // rows of a matrix as bf16 pieces with rows of kpad values, zero from `cols` on (and where live says so)
-int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, __bf16 *dst,
+// (perm: row r is src's row perm[r])
+int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *dst,
                            int64_t kpad, hipStream_t s);
 // the same, transposed: dst[c][r] = src[perm ? perm[r] : r][c], zero for r in [rows, rpad)
 int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t src_batch, int64_t batches, int64_t rows, int64_t cols,
@@ -29,13 +30,14 @@ int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t src_b
                            hipStream_t s);
 
 // A matrix as an operand of rowprod: bf16 rows that lie right already are taken where they are, others
-// are packed into `room` (pack_room elements of it).
+// are packed into `room` (pack_room elements of it).  With a permutation (the product's row r is row
+// perm[r]) rows are packed in its order, or, if a 32-bit offset reaches them all, taken through it.
 static inline bool rows_lie_right(const void *p, int dtype, int64_t ld, int64_t cols)
 {
-    return dtype == RAIRS_BF16 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % ROWPROD_K == 0;
+    return dtype == RAIRS_BF16 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld < (1 << 22) && cols % ROWPROD_K == 0;
 }
 static inline int64_t pack_room(int dtype, int64_t rows, int64_t cols) { return rows * pad_to(cols, ROWPROD_K) * dtype_pieces(dtype); }
-int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, __bf16 *room, RowOperand &out,
+int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *room, RowOperand &out,
                   hipStream_t s);
 
 struct LogprobArgs {

@@ -44,17 +44,14 @@ static __device__ __forceinline__ bool row_live(const uint32_t *live, int64_t r)
 
 template <class S, int NP>
 __global__ __launch_bounds__(WG) void pack_rows_kernel(const S *__restrict__ src, int64_t ld, int64_t rows, int64_t cols,
-                                                       const uint32_t *__restrict__ live, int vec, __bf16 *__restrict__ dst,
+                                                       const int32_t *__restrict__ perm, int vec, __bf16 *__restrict__ dst,
                                                        int64_t kpad, int64_t piece)
 {
     const int64_t per = kpad / 8, total = rows * per;
     for (int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x; t < total; t += (int64_t)gridDim.x * WG) {
         const int64_t r = t / per, i0 = (t - r * per) * 8;
         float x[8];
-        if (row_live(live, r)) load8(src + r * ld, i0, cols, vec, x);
-        else
-#pragma unroll
-            for (int e = 0; e < 8; e++) x[e] = 0.0f;
+        load8(src + (perm ? (int64_t)perm[r] : r) * ld, i0, cols, vec, x);
         v8bf o[NP];
 #pragma unroll
         for (int e = 0; e < 8; e++) {
@@ -110,7 +107,7 @@ static int is_vec(const void *p, int64_t ld, int64_t batch, int width)
     return (uintptr_t)p % a == 0 && ld * width % a == 0 && batch * width % a == 0;
 }
 
-int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, __bf16 *dst,
+int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *dst,
                            int64_t kpad, hipStream_t s)
 {
     if (rows == 0) return RAIRS_OK;
@@ -118,11 +115,11 @@ int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows,
     const dim3 grid((unsigned)(want < 8192 ? want : 8192));
     const int vec = is_vec(src, ld, 0, dtype_width(dtype));
     if (dtype == RAIRS_F32)
-        hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, live, vec, dst, kpad, piece);
+        hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, perm, vec, dst, kpad, piece);
     else if (dtype == RAIRS_BF16)
-        hipLaunchKernelGGL((pack_rows_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, live, vec, dst, kpad, piece);
+        hipLaunchKernelGGL((pack_rows_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, perm, vec, dst, kpad, piece);
     else
-        hipLaunchKernelGGL((pack_rows_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, live, vec, dst, kpad, piece);
+        hipLaunchKernelGGL((pack_rows_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, perm, vec, dst, kpad, piece);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
@@ -148,4 +145,23 @@ int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t src_b
         RAIRS_HIP(hipGetLastError());
     }
     return RAIRS_OK;
+}
+
+int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *room, RowOperand &out,
+                  hipStream_t s)
+{
+    const int64_t kpad = pad_to(cols, ROWPROD_K);
+    out.rows = rows;
+    out.perm = nullptr;
+    if (rows_lie_right(src, dtype, ld, cols) && (!perm || rows * ld < (1ll << 31))) {
+        out.p = (const __bf16 *)src;
+        out.ld = ld;
+        out.piece = 0;
+        out.perm = perm;
+        return RAIRS_OK;
+    }
+    out.p = room;
+    out.ld = kpad;
+    out.piece = rows * kpad;
+    return rairs_launch_pack_rows(src, dtype, ld, rows, cols, perm, room, kpad, s);
 }

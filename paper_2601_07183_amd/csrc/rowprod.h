@@ -22,13 +22,13 @@ typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
 
 #define ROWPROD_K 64                // values of a row in LDS at a time
 
-// Rows of bf16 pieces: value k of piece i of row r at p[i * piece + r * ld + k]; ld a multiple of 8,
-// p 16-byte aligned, k up to a multiple of ROWPROD_K readable (zero beyond the row).
+// Rows of bf16 pieces: value k of piece i of row r at p[i * piece + r * ld + k]; ld a multiple of 8, below
+// 2^22, p 16-byte aligned, k up to a multiple of ROWPROD_K readable (zero beyond the row).
 struct RowOperand {
     const __bf16 *p;
     int64_t ld, piece;
     int64_t rows;
-    const int32_t *perm;            // row r of the product is row perm[r] here (null: r)
+    const int32_t *perm;            // Q only: row r of the product is row perm[r] here (null: r); then rows * ld below 2^31
 };
 
 // The part of a sum that depends on the row's adapter: rows are sorted by adapter, a tile runs over
@@ -48,7 +48,8 @@ struct RowProd {
     uint8_t sp[6], sq[6];           // piece of P and of Q of each
     int ksteps;                     // steps of ROWPROD_K per product
     int splits;                     // workgroups that share a tile's sum
-    int ptiles, qtiles;
+    int ptiles, qtiles;             // tiles, and workgroups along P: each takes prun tiles
+    int prun, pruns;
     AdapterPart ad;
 };
 
@@ -65,10 +66,10 @@ static inline void rowprod_pieces(RowProd &a, int np, int nq)
         }
 }
 
-// PT x QT tiles of 16 x 16 per wave, WP x WQ waves.
-template <int PT_, int QT_, int WP_, int WQ_>
+// PT x QT tiles of 16 x 16 per wave, WP x WQ waves; registers for MINW waves per SIMD.
+template <int PT_, int QT_, int WP_, int WQ_, int MINW_ = 2>
 struct RowTile {
-    static constexpr int PT = PT_, QT = QT_, WP = WP_, WQ = WQ_, NT = 64 * WP * WQ;
+    static constexpr int PT = PT_, QT = QT_, WP = WP_, WQ = WQ_, NT = 64 * WP * WQ, MINW = MINW_;
     static constexpr int BP = 16 * PT * WP, BQ = 16 * QT * WQ;
     static constexpr int LP = BP * 8 / NT, LQ = BQ * 8 / NT;          // 16-byte loads per thread and step
     static constexpr int BYTES = (BP + BQ) * 128;                     // of one LDS buffer
@@ -77,23 +78,36 @@ struct RowTile {
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
+// The tile of a product: the largest that still gives every CU a workgroup.  Large tiles need less of
+// the caches per product (256 x 256: a step's 64 KB for 2,048 cycles of products, 128 x 128: 32 KB for 512).
+typedef RowTile<8, 4, 2, 4> TileL;  // 256 x 256
+typedef RowTile<4, 4, 2, 2> TileM;  // 128 x 128
+typedef RowTile<2, 2, 2, 2> TileS;  // 64 x 64
+static inline int rowprod_size(int64_t p, int64_t q)
+{
+    if (((p + 255) / 256) * ((q + 255) / 256) >= 200) return 2;
+    if (((p + 127) / 128) * ((q + 127) / 128) >= 200) return 1;
+    return 0;
+}
+
 template <class T>
 struct RowAcc {
     v4f v[T::PT][T::QT];
 };
 
-// one step's 16-byte chunks of both operands, straight into LDS
+// one step's 16-byte chunks of both operands, straight into LDS: a row's place is a 32-bit offset from an
+// address that the workgroup shares
 template <class T>
-static __device__ __forceinline__ void rowprod_fetch(char *buf, const __bf16 *const (&pp)[T::LP], const __bf16 *const (&qp)[T::LQ],
-                                                     int64_t op, int64_t oq, int wave)
+static __device__ __forceinline__ void rowprod_fetch(char *buf, const char *pb, const uint32_t (&po)[T::LP], const char *qb,
+                                                     const uint32_t (&qo)[T::LQ], int wave)
 {
 #pragma unroll
     for (int i = 0; i < T::LP; i++)
-        __builtin_amdgcn_global_load_lds((global_void *)(pp[i] + op), (lds_void *)(buf + (i * T::NT + wave * 64) * 16), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_void *)(pb + po[i]), (lds_void *)(buf + (i * T::NT + wave * 64) * 16), 16, 0, 0);
 #pragma unroll
     for (int i = 0; i < T::LQ; i++)
-        __builtin_amdgcn_global_load_lds((global_void *)(qp[i] + oq), (lds_void *)(buf + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16,
-                                         0, 0);
+        __builtin_amdgcn_global_load_lds((global_void *)(qb + qo[i]), (lds_void *)(buf + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16, 0,
+                                         0);
 }
 
 // every load into LDS of this wave has landed, then every wave's
@@ -103,6 +117,9 @@ static __device__ __forceinline__ void rowprod_landed()
     __syncthreads();
 }
 
+// (the operand that more products follow each other with stays: the longer side's tiles in the inner loop.
+// 128,000 x 4096 x 1024 at 256 x 256: 885 us so, 922 with the loops the other way round; with both halves'
+// operands fetched first, or products and fetches interleaved by hand, 960 to 1,025)
 template <class T>
 static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int wq, int lane, RowAcc<T> &acc)
 {
@@ -115,122 +132,162 @@ static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int
 #pragma unroll
         for (int j = 0; j < T::QT; j++) b[j] = *(const v8bf *)(buf + T::BP * 128 + (wq * T::QT + j) * 2048 + slot);
 #pragma unroll
-        for (int i = 0; i < T::PT; i++)
-#pragma unroll
-            for (int j = 0; j < T::QT; j++) acc.v[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc.v[i][j], 0, 0, 0);
+        for (int x = 0; x < T::PT * T::QT; x++) {
+            const int i = T::PT >= T::QT ? x % T::PT : x / T::QT, j = T::PT >= T::QT ? x / T::PT : x % T::QT;
+            acc.v[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc.v[i][j], 0, 0, 0);
+        }
     }
 }
 
-// Workgroup's tile: neighbouring workgroups of one XCD (they are handed out round robin over the
-// eight) take the q tiles of the same p tile one after the other, so that its rows come from that
+// A workgroup's run of p tiles: neighbouring workgroups of one XCD (they are handed out round robin over
+// the eight) take the q tiles of the same run one after the other, so that its rows come from that
 // XCD's L2 cache after the first.
-static __device__ __forceinline__ bool rowprod_tile(const RowProd &a, int &pt, int &qt, int &split)
+static __device__ __forceinline__ bool rowprod_tile(const RowProd &a, int &run, int &qt, int &split)
 {
-    const uint32_t total = (uint32_t)(a.ptiles * a.qtiles * a.splits), per = (total + 7) / 8;
+    const uint32_t total = (uint32_t)(a.pruns * a.qtiles * a.splits), per = (total + 7) / 8;
     const uint32_t id = (blockIdx.x % 8) * per + blockIdx.x / 8;
     if (blockIdx.x / 8 >= per || id >= total) return false;
     qt = (int)(id % a.qtiles);
-    pt = (int)(id / a.qtiles % a.ptiles);
-    split = (int)(id / (a.qtiles * a.ptiles));
+    run = (int)(id / a.qtiles % a.pruns);
+    split = (int)(id / (a.qtiles * a.pruns));
     return true;
 }
 static inline unsigned rowprod_grid(const RowProd &a)
 {
-    const uint32_t total = (uint32_t)(a.ptiles * a.qtiles * a.splits);
+    const uint32_t total = (uint32_t)(a.pruns * a.qtiles * a.splits);
     return (total + 7) / 8 * 8;
 }
 
-// The epilogue is called as epi(acc, p0, q0, lane, split): lane l holds, for its tiles (i, j), rows
-// q0 + 16 j + (l & 15) and columns p0 + 16 i + 4 (l >> 4) + 0..3.
-template <class T, class Epi>
-__global__ __launch_bounds__(T::NT) void rowprod_kernel(RowProd a, Epi epi)
+// offsets of a tile's rows from its first one, `ld` elements apart; rows beyond the last of `rows` read it
+// (they are computed, not stored)
+template <class T, int L>
+static __device__ __forceinline__ void rowprod_rows(int64_t r0, int64_t rows, int64_t ld, int tid, uint32_t (&o)[L])
+{
+    const uint32_t chunk = ((tid & 7) ^ ((tid >> 3) & 7)) * 16, last = (uint32_t)(rows - 1 - r0 < 0x7FFFFFFF ? rows - 1 - r0 : 0x7FFFFFFF);
+#pragma unroll
+    for (int i = 0; i < L; i++) {
+        const uint32_t r = i * (T::NT / 8) + (tid >> 3);              // (NT / 8 is a multiple of 8: chunk is the same for every load)
+        o[i] = (r < last ? r : last) * (uint32_t)(ld * 2) + chunk;
+    }
+}
+
+// A workgroup takes a q tile and a run of p tiles one after the other; the loads of a tile's first step
+// are under way while the tile before it is finished.  The epilogue keeps a state of its own over the
+// run: epi.begin(state, q0, lane), epi.tile(state, acc, p0, q0, lane, split) per tile, epi.end(state, run, wp,
+// q0, lane): lane l holds, for its tiles (i, j), rows q0 + 16 j + (l & 15) and columns p0 + 16 i +
+// 4 (l >> 4) + 0..3.
+template <class T, class Epi, bool ADAPT>
+__global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi epi)
 {
     extern __shared__ __align__(16) char rowprod_lds[];
-    int pt, qt, split;
-    if (!rowprod_tile(a, pt, qt, split)) return;
+    int run, qt, split;
+    if (!rowprod_tile(a, run, qt, split)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wp = wave % T::WP, wq = wave / T::WP;
-    const int64_t p0 = (int64_t)pt * T::BP, q0 = (int64_t)qt * T::BQ;
+    const int t0 = run * a.prun, t1 = min(t0 + a.prun, a.ptiles);
+    const int64_t q0 = (int64_t)qt * T::BQ, qw = q0 + wq * (16 * T::QT);
 
-    const int chunk = ((tid & 7) ^ ((tid >> 3) & 7)) * 8;             // (NT / 8 is a multiple of 8: the same for every load)
-    const __bf16 *pp[T::LP], *qp[T::LQ];
+    uint32_t po[T::LP], qo[T::LQ];
+    rowprod_rows<T>((int64_t)t0 * T::BP, a.P.rows, a.P.ld, tid, po);
+    const char *pb = (const char *)(a.P.p + (int64_t)t0 * T::BP * a.P.ld), *qb = (const char *)a.Q.p;
+    if (a.Q.perm) {
+        const uint32_t chunk = ((tid & 7) ^ ((tid >> 3) & 7)) * 16;
 #pragma unroll
-    for (int i = 0; i < T::LP; i++) {
-        int64_t r = p0 + i * (T::NT / 8) + (tid >> 3);
-        r = r < a.P.rows ? r : a.P.rows - 1;                          // (rows beyond the last: computed, not stored)
-        if (a.P.perm) r = a.P.perm[r];
-        pp[i] = a.P.p + r * a.P.ld + chunk;
+        for (int i = 0; i < T::LQ; i++) {
+            const int64_t r = q0 + i * (T::NT / 8) + (tid >> 3);
+            qo[i] = (uint32_t)a.Q.perm[r < a.Q.rows ? r : a.Q.rows - 1] * (uint32_t)(a.Q.ld * 2) + chunk;
+        }
+    } else {
+        rowprod_rows<T>(q0, a.Q.rows, a.Q.ld, tid, qo);
+        qb += q0 * a.Q.ld * 2;
     }
-#pragma unroll
-    for (int i = 0; i < T::LQ; i++) {
-        int64_t r = q0 + i * (T::NT / 8) + (tid >> 3);
-        r = r < a.Q.rows ? r : a.Q.rows - 1;
-        if (a.Q.perm) r = a.Q.perm[r];
-        qp[i] = a.Q.p + r * a.Q.ld + chunk;
-    }
-    RowAcc<T> acc;
-#pragma unroll
-    for (int i = 0; i < T::PT; i++)
-#pragma unroll
-        for (int j = 0; j < T::QT; j++) acc.v[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
-
     const int steps = a.nseg * a.ksteps;
     const int s0 = (int)((int64_t)steps * split / a.splits), s1 = (int)((int64_t)steps * (split + 1) / a.splits);
     char *b0 = rowprod_lds, *b1 = rowprod_lds + T::BYTES;
-    if (s0 < s1) {
-        int seg = s0 / a.ksteps, k = s0 % a.ksteps;
-        rowprod_fetch<T>(b0, pp, qp, a.sp[seg] * a.P.piece + k * ROWPROD_K, a.sq[seg] * a.Q.piece + k * ROWPROD_K, wave);
-        rowprod_landed();
-        for (int s = s0; s < s1; s++) {
-            if (s + 1 < s1) {
-                if (++k == a.ksteps) { k = 0; seg++; }
-                rowprod_fetch<T>(b1, pp, qp, a.sp[seg] * a.P.piece + k * ROWPROD_K, a.sq[seg] * a.Q.piece + k * ROWPROD_K, wave);
-            }
+    int seg = s0 / a.ksteps, k = s0 % a.ksteps;
+    auto fetch = [&](char *buf) {
+        rowprod_fetch<T>(buf, pb + (a.sp[seg] * a.P.piece + k * ROWPROD_K) * 2, po, qb + (a.sq[seg] * a.Q.piece + k * ROWPROD_K) * 2, qo, wave);
+    };
+    fetch(b0);
+    typename Epi::template State<T> state;
+    epi.begin(state, qw, lane);
+    rowprod_landed();
+    for (int t = t0; t < t1; t++) {
+        RowAcc<T> acc;
+#pragma unroll
+        for (int i = 0; i < T::PT; i++)
+#pragma unroll
+            for (int j = 0; j < T::QT; j++) acc.v[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = s0; s < s1 - 1; s++) {
+            if (++k == a.ksteps) { k = 0; seg++; }
+            fetch(b1);
             rowprod_step<T>(b0, wp, wq, lane, acc);
             rowprod_landed();
-            char *t = b0; b0 = b1; b1 = t;
+            char *x = b0; b0 = b1; b1 = x;
         }
-    }
-    if (a.ad.kpad) {                                                  // uniform
-        const int64_t qend = q0 + T::BQ < a.Q.rows ? q0 + T::BQ : a.Q.rows;
-        for (int64_t pos = q0; pos < qend;) {
-            const int ad = a.ad.of_row[pos];
-            if (ad < 0) break;                                        // rows without an adapter are the last
-            pos = a.ad.end[ad];
+        seg = s0 / a.ksteps;
+        k = s0 % a.ksteps;
+        if (t + 1 < t1) {
+            pb += (int64_t)T::BP * a.P.ld * 2;
+            if (t + 2 == a.ptiles) rowprod_rows<T>((int64_t)(t + 1) * T::BP, a.P.rows, a.P.ld, tid, po);
+            fetch(b1);
+        }
+        rowprod_step<T>(b0, wp, wq, lane, acc);
+        char *x = b0; b0 = b1; b1 = x;
+        const int64_t p0 = (int64_t)t * T::BP;
+        if constexpr (ADAPT) {                                        // (a run is one tile)
+            const int64_t qend = q0 + T::BQ < a.Q.rows ? q0 + T::BQ : a.Q.rows;
+            for (int64_t pos = q0; pos < qend;) {
+                const int ad = a.ad.of_row[pos];
+                if (ad < 0) break;                                    // rows without an adapter are the last
+                pos = a.ad.end[ad];
+                rowprod_rows<T>(p0, a.P.rows, a.ad.kpad, tid, po);
+                rowprod_rows<T>(q0, a.Q.rows, a.ad.kpad, tid, qo);
+                const char *bb = (const char *)(a.ad.b + ((int64_t)ad * a.P.rows + p0) * a.ad.kpad), *ub = (const char *)(a.ad.u + q0 * a.ad.kpad);
+                for (int kk = 0; kk < a.ad.kpad; kk += ROWPROD_K) {
+                    rowprod_landed();                                 // (the buffer is free: every wave is past the last step)
 #pragma unroll
-            for (int i = 0; i < T::LP; i++) {
-                int64_t r = p0 + i * (T::NT / 8) + (tid >> 3);
-                r = r < a.P.rows ? r : a.P.rows - 1;
-                pp[i] = a.ad.b + ((int64_t)ad * a.P.rows + r) * a.ad.kpad + chunk;
-            }
+                    for (int i = 0; i < T::LP; i++)
+                        __builtin_amdgcn_global_load_lds((global_void *)(bb + po[i] + kk * 2), (lds_void *)(b0 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
 #pragma unroll
-            for (int i = 0; i < T::LQ; i++) {
-                int64_t r = q0 + i * (T::NT / 8) + (tid >> 3);
-                r = r < a.Q.rows ? r : a.Q.rows - 1;
-                qp[i] = (a.ad.of_row[r] == ad ? a.ad.u + r * a.ad.kpad : a.ad.zero) + chunk;
-            }
-            for (int k = 0; k < a.ad.kpad; k += ROWPROD_K) {
-                rowprod_fetch<T>(b0, pp, qp, k, k, wave);
-                rowprod_landed();
-                rowprod_step<T>(b0, wp, wq, lane, acc);
-                rowprod_landed();
+                    for (int i = 0; i < T::LQ; i++) {
+                        const int64_t r = q0 + i * (T::NT / 8) + (tid >> 3);
+                        const char *src = a.ad.of_row[r < a.Q.rows ? r : a.Q.rows - 1] == ad ? ub + qo[i] : (const char *)a.ad.zero;
+                        __builtin_amdgcn_global_load_lds((global_void *)(src + kk * 2), (lds_void *)(b0 + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
+                    }
+                    rowprod_landed();
+                    rowprod_step<T>(b0, wp, wq, lane, acc);
+                }
             }
         }
+        epi.tile(state, acc, p0 + wp * (16 * T::PT), qw, lane, split);
+        rowprod_landed();
     }
-    epi(acc, p0 + wp * (16 * T::PT), q0 + wq * (16 * T::QT), lane, split);
+    epi.end(state, run, wp, qw, lane);
 }
 
-template <class T, class Epi>
-static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s)
+// `prun`: p tiles that a workgroup takes one after the other
+template <class T, bool ADAPT = false, class Epi>
+static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 1)
 {
     a.ptiles = (int)((a.P.rows + T::BP - 1) / T::BP);
     a.qtiles = (int)((a.Q.rows + T::BQ - 1) / T::BQ);
+    a.prun = prun;
+    a.pruns = (a.ptiles + prun - 1) / prun;
     if (a.splits < 1) a.splits = 1;
-    auto kern = rowprod_kernel<T, Epi>;
+    auto kern = rowprod_kernel<T, Epi, ADAPT>;
     RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * T::BYTES));
     hipLaunchKernelGGL(kern, dim3(rowprod_grid(a)), dim3(T::NT), 2 * T::BYTES, s, a, epi);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
+}
+
+// the same with the tile chosen by rowprod_size
+template <bool ADAPT = false, class Epi>
+static int rowprod_launch_any(RowProd &a, const Epi &epi, hipStream_t s)
+{
+    const int size = rowprod_size(a.P.rows, a.Q.rows * (a.splits > 1 ? a.splits : 1));
+    return size == 2 ? rowprod_launch<TileL, ADAPT>(a, epi, s) : size == 1 ? rowprod_launch<TileM, ADAPT>(a, epi, s) : rowprod_launch<TileS, ADAPT>(a, epi, s);
 }
 
 // ---- epilogues -------------------------------------------------------------------------------------
@@ -243,15 +300,29 @@ struct StoreEpi {
     const int32_t *perm;            // row r goes to row perm[r] (null: r)
     int bf16_out, add;              // add (fp32 only): onto what is there
     template <class T>
-    __device__ __forceinline__ void operator()(const RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int split) const
+    struct State {
+        int64_t row[T::QT];         // of the output, -1: none
+    };
+    template <class T>
+    __device__ __forceinline__ void begin(State<T> &st, int64_t q0, int lane) const
+    {
+#pragma unroll
+        for (int j = 0; j < T::QT; j++) {
+            const int64_t q = q0 + 16 * j + (lane & 15);
+            st.row[j] = q >= nq ? -1 : perm ? perm[q] : q;
+        }
+    }
+    template <class T>
+    __device__ __forceinline__ void end(State<T> &, int, int, int64_t, int) const {}
+    template <class T>
+    __device__ __forceinline__ void tile(State<T> &st, const RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int split) const
     {
         // four values at once where every row starts on a multiple of four elements
         const bool four = ld % 4 == 0 && (bf16_out ? ((uintptr_t)out & 7) == 0 : ((uintptr_t)out & 15) == 0) && split_stride % 4 == 0;
 #pragma unroll
         for (int j = 0; j < T::QT; j++) {
-            const int64_t q = q0 + 16 * j + (lane & 15);
-            if (q >= nq) continue;
-            const int64_t row = (perm ? perm[q] : q) * ld + split * split_stride;
+            if (st.row[j] < 0) continue;
+            const int64_t row = st.row[j] * ld + split * split_stride;
 #pragma unroll
             for (int i = 0; i < T::PT; i++) {
                 const int64_t p = p0 + 16 * i + 4 * (lane >> 4);

@@ -95,7 +95,7 @@ def test_project_backward_refuses(kw, code, says):
 @pytest.mark.parametrize("change,code,says", [
     (dict(dtype=3), EINVAL, "type"), (dict(dtype=1), EINVAL, "queries of type"), (dict(d=0), EINVAL, "d="), (dict(V=0), EINVAL, "row"),
     (dict(d=20_000, ld=20_000), EUNSUPPORTED, "limit"), (dict(V=1 << 31), EUNSUPPORTED, "V="), (dict(scale=0.0), EINVAL, "scale"),
-    (dict(scale=-1.0), EINVAL, "scale"), (dict(scale=float("inf")), EINVAL, "scale"), (dict(scale=float("nan")), EINVAL, "scale"),
+    (dict(scale=-1.0), EINVAL, "scale"), (dict(scale=float("inf")), EINVAL, "scale"), (dict(scale=1e-31), EINVAL, "scale"), (dict(scale=2e30), EINVAL, "scale"), (dict(scale=float("nan")), EINVAL, "scale"),
     (dict(ld_live=31, d_live=P), EINVAL, "ld_live"), (dict(ld_live=-1), EINVAL, "ld_live"), (dict(ld_live=40), EINVAL, "without a mask"),
     (dict(vectors=None), EINVAL, "vectors"), (dict(ld=63), EINVAL, "stride"),
 ])
