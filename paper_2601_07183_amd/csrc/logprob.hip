@@ -24,21 +24,28 @@
 // ---- statistics of a tile ----------------------------------------------------------------------------
 
 struct StatsArgs {
-    int64_t n, V;
+    int n, V;
     float c;                        // scale log2(e)
     const uint32_t *live;
     int64_t ld_live;
     const int64_t *targets;
     float4 *parts;                  // [n][nparts] {m, s, e, 0}; m: the largest product itself, not times c
     int nparts;
-    float *gmax;                    // [n][ngroups] {largest, second} or, wide, the largest alone; or null
-    int64_t ngroups;
-    int wide;                       // group 4 b + h holds rows 64 b + 16 i + 4 h + r; wide: group b, all 64 of them
+    // Groups of block b (rows 64 b .. 64 b + 63): [b][n][4] {largest, second} of rows 64 b + 16 i + 4 h + r for h = 0..3
+    // (a wave's store is one run of memory), or, wide, [n][b] the largest of all (a sixteenth of that; a query's are
+    // read in one run)
+    float *gmax;
+    int nblocks;
+    int wide;
     float *zt;                      // [n] the target's product
 };
 
 // 2^x for x <= 0 (a result below 2^-126 may be flushed)
 static __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The larger value, a NaN if there is one.  (The instruction for it takes values as they come out of the
+// matrix cores; fmaxf's has each quieted by an instruction of its own first.)
+static __device__ __forceinline__ float max_of(float x, float y) { return __builtin_elementwise_maximum(x, y); }
 
 // sums relative to a maximum m0, brought to m1 >= m0
 static __device__ __forceinline__ void rebase(float &s, float &e, float m0, float m1, float c)
@@ -55,46 +62,49 @@ template <int QT, bool ENT, int TOP>
 struct StatsState {
     float m[QT], s[QT], e[QT];
     int32_t target[QT];             // the query's target, -1: none (V is below 2^31)
-    __device__ __forceinline__ void begin(const StatsArgs &a, int64_t q0, int lane)
+    __device__ __forceinline__ void begin(const StatsArgs &a, int q0, int lane)
     {
 #pragma unroll
         for (int j = 0; j < QT; j++) {
             m[j] = HIDDEN; s[j] = 0.0f; e[j] = 0.0f;
-            const int64_t q = q0 + 16 * j + (lane & 15), t = q < a.n ? a.targets[q] : -1;
+            const int q = q0 + 16 * j + (lane & 15);
+            const int64_t t = q < a.n ? a.targets[q] : -1;
             target[j] = t >= 0 && t < a.V ? (int32_t)t : -1;
         }
     }
     // a tile's products: rows p0 + 16 i + 4 (lane >> 4) + r, queries q0 + 16 j + (lane & 15); acc is
     // overwritten (HIDDEN where the mask hides a row)
     template <int PT>
-    __device__ __forceinline__ void tile(const StatsArgs &a, v4f (&acc)[PT][QT], int64_t p0, int64_t q0, int lane)
+    __device__ __forceinline__ void tile(const StatsArgs &a, v4f (&acc)[PT][QT], int p0, int q0, int lane)
     {
         const int h = lane >> 4;
         const bool ragged = p0 + 16 * PT > a.V;                       // uniform
 #pragma unroll
         for (int j = 0; j < QT; j++) {
-            const int64_t q = q0 + 16 * j + (lane & 15);
+            const int q = q0 + 16 * j + (lane & 15);
             const bool in = q < a.n;
             // the target's product, by the lane that has it
-            const uint32_t dp = (uint32_t)target[j] - (uint32_t)p0;
-            if (__any(target[j] >= 0 && dp < 16 * PT)) {              // (seldom)
+            const uint32_t dp = (uint32_t)(target[j] - p0);           // (no target: far out)
+            if (__any(dp < 16 * PT && target[j] >= 0)) {              // (seldom)
+                uint32_t at = dp - 4 * h;                             // 16 i + r in that lane
+                asm volatile("" : "+v"(at));                          // (the comparisons stay in here)
                 if (target[j] >= 0 && dp < 16 * PT && ((dp >> 2) & 3) == (uint32_t)h) {
 #pragma unroll
                     for (int i = 0; i < PT; i++)
 #pragma unroll
                         for (int r = 0; r < 4; r++)
-                            if ((int)dp == 16 * i + 4 * h + r) a.zt[q] = acc[i][j][r];
+                            if (at == (uint32_t)(16 * i + r)) a.zt[q] = acc[i][j][r];
                 }
             }
             if (a.live || ragged) {
-                const int64_t row = in ? q : a.n - 1;
+                const uint32_t *live = a.live ? a.live + (in ? q : 0) * a.ld_live : nullptr;
 #pragma unroll
                 for (int i = 0; i < PT; i++) {
-                    const int64_t p = p0 + 16 * i;                    // (a multiple of 16: within one word of the mask)
+                    const int p = p0 + 16 * i;                        // (a multiple of 16: within one word of the mask)
                     uint32_t bits = 0;
                     if (p < a.V) {
-                        bits = a.live ? a.live[row * a.ld_live + (p >> 5)] >> ((p & 31) + 4 * h) : 0xFu;
-                        const int64_t left = a.V - p - 4 * h;
+                        bits = live ? live[p >> 5] >> ((p & 31) + 4 * h) : 0xFu;
+                        const int left = a.V - p - 4 * h;
                         bits &= left >= 4 ? 0xFu : left <= 0 ? 0u : (1u << left) - 1u;
                     }
 #pragma unroll
@@ -105,7 +115,7 @@ struct StatsState {
             float top = HIDDEN;
 #pragma unroll
             for (int b = 0; b < PT; b += 4) {
-                const int64_t blk = p0 / 64 + b / 4;
+                const int blk = p0 / 64 + b / 4;                      // uniform
                 float g = HIDDEN, g2 = HIDDEN;
                 if constexpr (TOP == 2) {
 #pragma unroll
@@ -114,23 +124,26 @@ struct StatsState {
                         for (int r = 0; r < 4; r++) {
                             const float x = __uint_as_float((__float_as_uint(acc[i][j][r]) & ~15u) | (uint32_t)(4 * (i - b) + r));
                             g2 = __builtin_amdgcn_fmed3f(g, g2, x);
-                            g = fmaxf(g, x);
+                            g = max_of(g, x);
                         }
-                    if (in && blk * 4 < a.ngroups) *(float2 *)(a.gmax + (q * a.ngroups + blk * 4 + h) * 2) = make_float2(g, g2);
+                    if (blk < a.nblocks) {
+                        float2 *to = (float2 *)a.gmax + ((int64_t)blk * a.n + q0 + 16 * j) * 4;
+                        if (in) to[4 * (lane & 15) + h] = make_float2(g, g2);
+                    }
                 } else {
 #pragma unroll
                     for (int i = b; i < b + 4; i++)
-                        g = fmaxf(fmaxf(g, fmaxf(acc[i][j][0], acc[i][j][1])), fmaxf(acc[i][j][2], acc[i][j][3]));
+                        g = max_of(max_of(max_of(g, acc[i][j][0]), acc[i][j][1]), max_of(acc[i][j][2], acc[i][j][3]));
                     if constexpr (TOP == 1) {
                         float w = fmaxf(g, __shfl_xor(g, 16));
                         w = fmaxf(w, __shfl_xor(w, 32));
-                        if (in && h == 0 && blk < a.ngroups) a.gmax[q * a.ngroups + blk] = w;
+                        if (in && h == 0 && blk < a.nblocks) a.gmax[(int64_t)q * a.nblocks + blk] = w;
                     }
                 }
-                top = fmaxf(top, g);
+                top = max_of(top, g);
             }
-            if (__any(top > m[j])) {                                  // (ever more seldom)
-                const float m1 = fmaxf(m[j], top);
+            if (__any(!(top <= m[j]))) {                              // (ever more seldom)
+                const float m1 = max_of(m[j], top);
                 rebase(s[j], e[j], m[j], m1, a.c);
                 m[j] = m1;
             }
@@ -149,7 +162,7 @@ struct StatsState {
             __builtin_amdgcn_sched_barrier(0);                        // (one query's values at a time in registers)
         }
     }
-    __device__ __forceinline__ void end(const StatsArgs &a, int part, int64_t q0, int lane)
+    __device__ __forceinline__ void end(const StatsArgs &a, int part, int q0, int lane)
     {
 #pragma unroll
         for (int j = 0; j < QT; j++) {
@@ -159,8 +172,8 @@ struct StatsState {
             float ss = s[j] + __shfl_xor(s[j], 16), ee = e[j] + __shfl_xor(e[j], 16);
             ss += __shfl_xor(ss, 32);
             ee += __shfl_xor(ee, 32);
-            const int64_t q = q0 + 16 * j + (lane & 15);
-            if (q < a.n && lane < 16) a.parts[q * a.nparts + part] = make_float4(top, ss, ee, 0.0f);
+            const int q = q0 + 16 * j + (lane & 15);
+            if (q < a.n && lane < 16) a.parts[(int64_t)q * a.nparts + part] = make_float4(top, ss, ee, 0.0f);
         }
     }
 };
@@ -173,16 +186,16 @@ struct StatsEpi {
         StatsState<T::QT, ENT, TOP> s;
     };
     template <class T>
-    __device__ __forceinline__ void begin(State<T> &st, int64_t q0, int lane) const { st.s.begin(a, q0, lane); }
+    __device__ __forceinline__ void begin(State<T> &st, int64_t q0, int lane) const { st.s.begin(a, (int)q0, lane); }
     template <class T>
     __device__ __forceinline__ void tile(State<T> &st, RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
     {
-        if constexpr (T::PT % 4 == 0) st.s.tile(a, acc.v, p0, q0, lane);
+        st.s.tile(a, acc.v, (int)p0, (int)q0, lane);
     }
     template <class T>
     __device__ __forceinline__ void end(State<T> &st, int run, int wp, int64_t q0, int lane) const
     {
-        st.s.end(a, run * T::WP + wp, q0, lane);
+        st.s.end(a, run * T::WP + wp, (int)q0, lane);
     }
 };
 
@@ -249,8 +262,7 @@ __global__ __launch_bounds__(WG) void few_stats_kernel(FewStatsArgs a)
     const Q *qrow[QT];
 #pragma unroll
     for (int j = 0; j < QT; j++) {
-        int64_t q = 16 * j + (lane & 15);
-        q = q < a.st.n ? q : a.st.n - 1;
+        const int q = min(16 * j + (lane & 15), a.st.n - 1);
         qrow[j] = (const Q *)a.q + q * a.ldq;
     }
     const int steps = (a.d + 4 * FewLoad<S>::CH - 1) / (4 * FewLoad<S>::CH);
@@ -258,16 +270,14 @@ __global__ __launch_bounds__(WG) void few_stats_kernel(FewStatsArgs a)
     st.begin(a.st, 0, lane);
     float most = 0.0f;
     for (int r = 0; r < a.rounds; r++) {
-        const int64_t p0 = ((int64_t)part * a.rounds + r) * 64;
+        const int p0 = (part * a.rounds + r) * 64;
         if (p0 >= a.st.V) break;
         const S *prow[4];
         v4f acc[4][QT];
         float nrm[4];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            int64_t p = p0 + 16 * i + (lane & 15);
-            p = p < a.st.V ? p : a.st.V - 1;
-            prow[i] = (const S *)a.table + p * a.ldt;
+            prow[i] = (const S *)a.table + (int64_t)min(p0 + 16 * i + (lane & 15), a.st.V - 1) * a.ldt;
             nrm[i] = 0.0f;
 #pragma unroll
             for (int j = 0; j < QT; j++) acc[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
@@ -278,7 +288,7 @@ __global__ __launch_bounds__(WG) void few_stats_kernel(FewStatsArgs a)
             for (int i = 0; i < 4; i++) {
                 float x = nrm[i] + __shfl_xor(nrm[i], 16);
                 x += __shfl_xor(x, 32);
-                const int64_t p = p0 + 16 * i + (lane & 15);
+                const int p = p0 + 16 * i + (lane & 15);
                 if (p < a.st.V && (!a.any_live || ((a.any_live[p >> 5] >> (p & 31)) & 1u))) most = fmaxf(most, x);
             }
         }
@@ -311,22 +321,47 @@ struct FinishArgs {
     float *top_logp;
 };
 
-#define FIN_LIST 1024               // rows (wide: groups) that reach the bound that fit LDS
-#define FIN_ITEMS 1024              // rows to score at a time
-
+// A query is finished by a team of threads: a wave of its own in a large batch, a workgroup of 16 waves if
+// there are few queries and one has to be done soon.  Lists in LDS are per team.
+template <int NT>
 struct FinishShared {
-    float red[16][4];
-    float kth_in[256];
-    float kth_out;
-    double val[FIN_ITEMS + RAIRS_MAX_TOP];
-    uint32_t id[FIN_ITEMS + RAIRS_MAX_TOP];
+    static constexpr int LIST = NT == 64 ? 384 : 1024;    // rows (wide: groups) that reach the bound
+    static constexpr int ITEMS = NT == 64 ? 256 : 1024;   // rows to score at a time
+    double val[ITEMS + RAIRS_MAX_TOP];
     double best[RAIRS_MAX_TOP];
+    uint32_t id[ITEMS + RAIRS_MAX_TOP];
     uint32_t best_id[RAIRS_MAX_TOP];
-    uint32_t take[FIN_ITEMS];
-    float lval[FIN_LIST];
-    uint32_t lid[FIN_LIST];
+    uint32_t take[ITEMS];
+    float lval[LIST];
+    uint32_t lid[LIST];
+    float kth_in[NT == 64 ? 4 : 256];
+    float red[16];
+    float kth_out;
     int count, nbest, wcnt[16];
 };
+
+template <int NT>
+static __device__ __forceinline__ void team_sync()
+{
+    if constexpr (NT == 64) wave_lds_sync();
+    else __syncthreads();
+}
+
+// f over the team's values, in every thread
+template <int NT, class F>
+static __device__ __forceinline__ float team_fold(FinishShared<NT> &sh, float x, const F &f)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) x = f(x, __shfl_xor(x, o));
+    if constexpr (NT > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = sh.red[0];
+        for (int w = 1; w < NT / 64; w++) x = f(x, sh.red[w]);
+    }
+    return x;
+}
 
 // rows of an entry of the lists: the row itself, a group of 16 or one of 64
 enum { ENTRY_ROW = 1, ENTRY_GROUP = 16, ENTRY_WIDE = 64 };
@@ -337,30 +372,45 @@ static __device__ __forceinline__ int64_t entry_row(uint32_t entry, int member, 
                                 : (int64_t)(entry >> 2) * 64 + 16 * (member >> 2) + 4 * (entry & 3) + (member & 3);
 }
 
-// a lower bound of the k-th largest (k <= 64) of all threads' values: the k-th largest of the maxima of 256 sets
+// A lower bound of the k-th largest (k <= 64) of the values of which most[0..3] are a thread's maxima of four
+// sets: the k-th largest of the maxima of 256 sets.  A wave finds it bit by bit; a workgroup joins the sets of
+// its threads to 256 and counts.
 template <int NT>
-static __device__ __forceinline__ float kth_set_max(FinishShared &sh, float mine, int k)
+static __device__ __forceinline__ float kth_set_max(FinishShared<NT> &sh, const float (&most)[4], int k, int tid)
 {
-    const int tid = threadIdx.x;
+    if constexpr (NT == 64) {
+        uint32_t key[4], cut = 0;
 #pragma unroll
-    for (int x = 1; x < NT / 256; x <<= 1) mine = fmaxf(mine, __shfl_xor(mine, x));
-    __syncthreads();
-    if (tid % (NT / 256) == 0) sh.kth_in[tid / (NT / 256)] = mine;
-    if (tid == 0) sh.kth_out = NEG_INF;
-    __syncthreads();
-    if (tid < 256) {
-        const float x = sh.kth_in[tid];
-        int above = 0;
-#pragma unroll 8
-        for (int i = 0; i < 256; i += 4) {
-            const v4f y = *(const v4f *)&sh.kth_in[i];
+        for (int u = 0; u < 4; u++) key[u] = f32_key(most[u]);
+        for (int bit = 31; bit >= 0; bit--) {
+            const uint32_t cand = cut | (1u << bit);
+            int n = 0;
 #pragma unroll
-            for (int u = 0; u < 4; u++) above += y[u] > x || (y[u] == x && i + u < tid) ? 1 : 0;
+            for (int u = 0; u < 4; u++) n += __popcll(__ballot(key[u] >= cand));
+            if (n >= k) cut = cand;
         }
-        if (above == k - 1) sh.kth_out = x;
+        return key_f32(cut);
+    } else {
+        float mine = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+#pragma unroll
+        for (int x = 1; x < NT / 256; x <<= 1) mine = fmaxf(mine, __shfl_xor(mine, x));
+        __syncthreads();
+        if (tid % (NT / 256) == 0) sh.kth_in[tid / (NT / 256)] = mine;
+        __syncthreads();
+        if (tid < 256) {
+            const float x = sh.kth_in[tid];
+            int above = 0;
+#pragma unroll 8
+            for (int i = 0; i < 256; i += 4) {
+                const v4f y = *(const v4f *)&sh.kth_in[i];
+#pragma unroll
+                for (int u = 0; u < 4; u++) above += y[u] > x || (y[u] == x && i + u < tid) ? 1 : 0;
+            }
+            if (above == k - 1) sh.kth_out = x;
+        }
+        __syncthreads();
+        return sh.kth_out;
     }
-    __syncthreads();
-    return sh.kth_out;
 }
 
 // <q, t> in float64 by 16 lanes; the order of the sum depends on d alone, so equal rows get equal values
@@ -383,9 +433,10 @@ static __device__ __forceinline__ double dot_exact(const S *t, const Q *q, int d
 
 // scores the rows of the `cnt` entries in sh.take and merges those of at least `floor` into sh.best
 template <class S, class Q, int NT>
-static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishShared &sh, int64_t row, int cnt, int kind, double floor)
+static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishShared<NT> &sh, int64_t row, int tid, int cnt, int kind,
+                                                    double floor)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & 15, quarter = lane >> 4;
+    const int lane = tid & 63, wave = tid >> 6, sub = lane & 15, quarter = lane >> 4;
     const Q *q = (const Q *)a.q + row * a.ldq;
     const int old = sh.nbest;
     if (tid < old) {
@@ -393,7 +444,7 @@ static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishS
         sh.id[tid] = sh.best_id[tid];
     }
     if (tid == 0) sh.count = old;
-    __syncthreads();
+    team_sync<NT>();
     const int items = cnt * kind;
 #pragma unroll 1
     for (int i0 = wave * 4; i0 < items; i0 += NT / 16) {              // four rows per wave, 16 lanes each
@@ -408,7 +459,7 @@ static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishS
             sh.id[slot] = (uint32_t)v;
         }
     }
-    __syncthreads();
+    team_sync<NT>();
     const int total = sh.count;
 #pragma unroll 1
     for (int i = tid; i < total; i += NT) {
@@ -422,98 +473,65 @@ static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishS
         }
     }
     if (tid == 0) sh.nbest = total < a.top ? total : a.top;
-    __syncthreads();
+    team_sync<NT>();
 }
 
-// the entries with want set, FIN_ITEMS rows at a time, until none is left (drop() is asked again before each time)
+// the entries with want set, ITEMS rows at a time, until none is left (drop() is asked again before each time)
 template <class S, class Q, int NT, class Drop>
-static __device__ __forceinline__ void finish_entries(const FinishArgs &a, FinishShared &sh, int64_t row, bool want, uint32_t entry, int kind,
-                                                      double floor, const Drop &drop)
+static __device__ __forceinline__ void finish_entries(const FinishArgs &a, FinishShared<NT> &sh, int64_t row, int tid, bool want,
+                                                      uint32_t entry, int kind, double floor, const Drop &drop)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, most = FIN_ITEMS / kind;
+    const int lane = tid & 63, wave = tid >> 6, most = FinishShared<NT>::ITEMS / kind;
     for (;;) {
         if (want && drop()) want = false;
         const unsigned long long b = __ballot(want);
-        if (lane == 0) sh.wcnt[wave] = __popcll(b);
-        __syncthreads();
-        int at = __popcll(b & ((1ull << lane) - 1ull)), total = 0;
-        for (int w = 0; w < NT / 64; w++) {
-            at += w < wave ? sh.wcnt[w] : 0;
-            total += sh.wcnt[w];
+        int at = __popcll(b & ((1ull << lane) - 1ull)), total = __popcll(b);
+        if constexpr (NT > 64) {
+            if (lane == 0) sh.wcnt[wave] = total;
+            __syncthreads();
+            total = 0;
+            for (int w = 0; w < NT / 64; w++) {
+                at += w < wave ? sh.wcnt[w] : 0;
+                total += sh.wcnt[w];
+            }
         }
         if (want && at < most) {
             sh.take[at] = entry;
             want = false;
         }
-        __syncthreads();
-        if (total == 0) return;                                       // uniform
-        finish_batch<S, Q, NT>(a, sh, row, total < most ? total : most, kind, floor);
+        team_sync<NT>();
+        if (total == 0) return;                                       // (the same in every thread)
+        finish_batch<S, Q, NT>(a, sh, row, tid, total < most ? total : most, kind, floor);
     }
 }
 
-template <class S, class Q, int NT>
-__global__ __launch_bounds__(NT, 4) void logprob_finish_kernel(FinishArgs a)
+// NT threads per query, `TEAMS` queries per workgroup
+template <class S, class Q, int NT, int TEAMS>
+__global__ __launch_bounds__(NT * TEAMS, 4) void logprob_finish_kernel(FinishArgs a)
 {
-    __shared__ FinishShared sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = blockIdx.x;
+    __shared__ FinishShared<NT> shared[TEAMS];
+    FinishShared<NT> &sh = shared[threadIdx.x / NT];
+    const int tid = threadIdx.x % NT;
+    const int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / NT;
+    if (row >= a.st.n) return;                                        // (teams of a workgroup do not wait for each other)
+    const auto largest = [](float x, float y) { return fmaxf(x, y); };
+    const auto sum = [](float x, float y) { return x + y; };
     const float4 *parts = a.st.parts + row * a.st.nparts;
     const float c = a.st.c;
     float m = HIDDEN, s = 0.0f, e = 0.0f;
     for (int i = tid; i < a.st.nparts; i += NT) {
         float4 p = parts[i];
-        const float m1 = fmaxf(m, p.x);
+        const float m1 = max_of(m, p.x);
         rebase(s, e, m, m1, c);
         rebase(p.y, p.z, p.x, m1, c);
         s += p.y;
         e += p.z;
         m = m1;
     }
-    // |q|^2 and the table's largest squared norm, for the margin; and the groups' maxima
-    float q2 = 0.0f, x2 = 0.0f, most = HIDDEN;
-    bool zero = true;
-    const float *gmax = a.st.gmax + row * a.st.ngroups * (a.st.wide ? 1 : 2);
-    if (a.top) {
-        const Q *q = (const Q *)a.q + row * a.ldq;
-        for (int k = tid; k < a.d; k += NT) {
-            const float x = (float)q[k];
-            q2 = fmaf(x, x, q2);
-            zero = zero && x == 0.0f;
-        }
-        for (int i = tid; i < a.nxmax; i += NT) x2 = fmaxf(x2, a.xmax[i]);
-        if (a.st.wide) {
-#pragma unroll 8
-            for (int64_t g = tid; g < a.st.ngroups; g += NT) most = fmaxf(most, gmax[g]);
-        } else {
-#pragma unroll 8
-            for (int64_t g = tid; g < a.st.ngroups; g += NT) most = fmaxf(most, gmax[2 * g]);
-        }
-    }
-    float top = m;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-    if (lane == 0) sh.red[wave][0] = top;
-    __syncthreads();
-    top = sh.red[0][0];
-    for (int w = 1; w < NT / 64; w++) top = fmaxf(top, sh.red[w][0]);
+    const float top = team_fold(sh, m, [](float x, float y) { return max_of(x, y); });
     rebase(s, e, m, top, c);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-        s += __shfl_xor(s, x);
-        e += __shfl_xor(e, x);
-        q2 += __shfl_xor(q2, x);
-        x2 = fmaxf(x2, __shfl_xor(x2, x));
-    }
-    __syncthreads();
-    if (lane == 0) { sh.red[wave][0] = s; sh.red[wave][1] = e; sh.red[wave][2] = q2; sh.red[wave][3] = x2; }
-    __syncthreads();
-    s = e = q2 = x2 = 0.0f;
-    for (int w = 0; w < NT / 64; w++) {
-        s += sh.red[w][0];
-        e += sh.red[w][1];
-        q2 += sh.red[w][2];
-        x2 = fmaxf(x2, sh.red[w][3]);
-    }
+    s = team_fold(sh, s, sum);
+    e = team_fold(sh, e, sum);
     const bool empty = top == HIDDEN && s == 0.0f;
     const float mc = top * c, logs = log2f(s);
     if (tid == 0) {
@@ -531,66 +549,83 @@ __global__ __launch_bounds__(NT, 4) void logprob_finish_kernel(FinishArgs a)
     }
     if (a.top == 0) return;
 
+    // |q|^2 and the table's largest squared norm, for the margin; and the groups' maxima
+    float q2 = 0.0f, x2 = 0.0f, zero = 1.0f;
+    const Q *q = (const Q *)a.q + row * a.ldq;
+    for (int k = tid; k < a.d; k += NT) {
+        const float x = (float)q[k];
+        q2 = fmaf(x, x, q2);
+        zero = x == 0.0f ? zero : 0.0f;
+    }
+    for (int i = tid; i < a.nxmax; i += NT) x2 = fmaxf(x2, a.xmax[i]);
+    q2 = team_fold(sh, q2, sum);
+    x2 = team_fold(sh, x2, largest);
+    zero = team_fold(sh, zero, [](float x, float y) { return x * y; });
     // what a product may be off by (components whose squares underflow, and a group's row in the last bits of a
     // denormal, have terms of their own); not finite: nothing can be told apart
     const float under = sqrtf((float)a.d) * 1.1e-19f;
     const float eps = a.slack * (sqrtf(q2) + under) * (sqrtf(x2) + under) * 1.0001f + 4e-44f;
-    const bool zeros = __syncthreads_and(zero);                       // a query of zeros: every product is 0
-    if (!empty && eps < 1e38f) {                                      // uniform
-        const float thr = kth_set_max<NT>(sh, most, a.top) - 2.0f * eps;
+    const bool zeros = zero != 0.0f;                                  // a query of zeros: every product is 0
+
+    // entry i of the query's groups: block i >> shift, its part i & 3 if it has four
+    const int shift = a.st.wide ? 0 : 2, ngroups = a.st.nblocks << shift;
+    const auto group_at = [&](int i) {
+        return a.st.wide ? a.st.gmax + row * a.st.nblocks + i : a.st.gmax + ((((int64_t)(i >> 2) * a.st.n + row) << 2) + (i & 3)) * 2;
+    };
+    float most[4] = {HIDDEN, HIDDEN, HIDDEN, HIDDEN};
+    {
+        int i = tid;
+        for (; i + 3 * NT < ngroups; i += 4 * NT) {
+#pragma unroll
+            for (int u = 0; u < 4; u++) most[u] = fmaxf(most[u], *group_at(i + u * NT));
+        }
+        for (; i < ngroups; i += NT) most[0] = fmaxf(most[0], *group_at(i));
+    }
+    if (!empty && eps < 1e38f) {                                      // (the same in every thread)
+        const float thr = kth_set_max<NT>(sh, most, a.top, tid) - 2.0f * eps;
         // exact products of the K best are at least this
         const double floor = (double)thr + (double)eps * 0.999;
-        if (most >= thr && most > HIDDEN)
-            for (int64_t g = tid; g < a.st.ngroups; g += NT) {
-                if (a.st.wide) {
-                    const float x = gmax[g];
-                    if (x >= thr && x > HIDDEN) {
-                        const int at = atomicAdd(&sh.count, 1);
-                        if (at < FIN_LIST) {
-                            sh.lval[at] = x;
-                            sh.lid[at] = (uint32_t)g;
-                        }
-                    }
-                } else {
-                    const float2 x = *(const float2 *)(gmax + 2 * g);
-                    if (x.x >= thr && x.x > HIDDEN) {
-                        // the group's best row alone, or all of its rows if another may reach the bound too
-                        const int rows = x.y >= thr ? 16 : 1, at = atomicAdd(&sh.count, rows);
-                        for (int u = 0; u < rows && at + u < FIN_LIST; u++) {
-                            sh.lval[at + u] = x.x;
-                            sh.lid[at + u] = (uint32_t)entry_row((uint32_t)g, rows == 1 ? (int)(__float_as_uint(x.x) & 15u) : u, ENTRY_GROUP);
-                        }
-                    }
+        const float mine = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+        if (mine >= thr && mine > HIDDEN)
+            for (int i = tid; i < ngroups; i += NT) {
+                const float *g = group_at(i);
+                const float x = *g;
+                if (!(x >= thr && x > HIDDEN)) continue;
+                // the group's best row alone, or all of its rows if another may reach the bound too; wide: the group
+                const int rows = !a.st.wide && g[1] >= thr ? 16 : 1, at = atomicAdd(&sh.count, rows);
+                for (int u = 0; u < rows && at + u < FinishShared<NT>::LIST; u++) {
+                    sh.lval[at + u] = x;
+                    sh.lid[at + u] = a.st.wide ? (uint32_t)i
+                                               : (uint32_t)entry_row((uint32_t)i, rows == 1 ? (int)(__float_as_uint(x) & 15u) : u, ENTRY_GROUP);
                 }
             }
-        __syncthreads();
+        team_sync<NT>();
         const int found = sh.count;
-        __syncthreads();
-        if (found <= FIN_LIST) {
+        team_sync<NT>();
+        if (found <= FinishShared<NT>::LIST) {
             for (int i0 = 0; i0 < found; i0 += NT) {
                 const int i = i0 + tid;
                 const float x = i < found ? sh.lval[i] : HIDDEN;
                 // (an entry that cannot reach the K-th best so far is left out)
-                finish_entries<S, Q, NT>(a, sh, row, i < found, i < found ? sh.lid[i] : 0u, a.st.wide ? ENTRY_WIDE : ENTRY_ROW, floor, [&]() {
+                finish_entries<S, Q, NT>(a, sh, row, tid, i < found, i < found ? sh.lid[i] : 0u, a.st.wide ? ENTRY_WIDE : ENTRY_ROW, floor, [&]() {
                     return sh.nbest == a.top && (double)x + (double)eps < sh.best[a.top - 1];
                 });
             }
         } else {
             // so many equal products that the list does not hold them: all groups in order of their blocks of 64
             // rows, so that a block whose rows can only equal the K-th best comes too late to displace it
-            for (int64_t g0 = 0; g0 < a.st.ngroups; g0 += NT) {
-                const int64_t g = g0 + tid;
-                const float x = g < a.st.ngroups ? gmax[a.st.wide ? g : 2 * g] : HIDDEN;
-                const int64_t blk = a.st.wide ? g : g >> 2;
-                finish_entries<S, Q, NT>(a, sh, row, x >= thr && x > HIDDEN, (uint32_t)g, a.st.wide ? ENTRY_WIDE : ENTRY_GROUP, floor, [&]() {
+            for (int i0 = 0; i0 < ngroups; i0 += NT) {
+                const int i = i0 + tid;
+                const float x = i < ngroups ? *group_at(i) : HIDDEN;
+                finish_entries<S, Q, NT>(a, sh, row, tid, x >= thr && x > HIDDEN, (uint32_t)i, a.st.wide ? ENTRY_WIDE : ENTRY_GROUP, floor, [&]() {
                     if (sh.nbest < a.top) return false;
                     const double k = sh.best[a.top - 1], up = zeros ? 0.0 : (double)x + (double)eps;
-                    return up < k || (up == k && (int64_t)(sh.best_id[a.top - 1] >> 6) < blk);
+                    return up < k || (up == k && (int)(sh.best_id[a.top - 1] >> 6) < i >> shift);
                 });
             }
         }
     }
-    __syncthreads();
+    team_sync<NT>();
     if (tid < a.top) {
         const bool have = tid < sh.nbest;
         a.top_ids[row * a.top + tid] = have ? (int64_t)sh.best_id[tid] : -1;
@@ -783,17 +818,16 @@ static float product_slack(int d) { return (1.1f * (float)d + 64.0f) * 1.1920929
 template <class S, class Q>
 static int finish_launch(const FinishArgs &f, hipStream_t s)
 {
-    // few rows: as many waves on each as there can be, since a row's groups are scored by one workgroup
-    if (f.st.n <= FEW_ROWS) hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 1024>), dim3((unsigned)f.st.n), dim3(1024), 0, s, f);
-    else hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 256>), dim3((unsigned)f.st.n), dim3(256), 0, s, f);
+    if (f.st.n <= FEW_ROWS) hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 1024, 1>), dim3((unsigned)f.st.n), dim3(1024), 0, s, f);
+    else hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 64, 4>), dim3((unsigned)((f.st.n + 3) / 4)), dim3(256), 0, s, f);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
 
 template <bool ENT, int TOP>
-static int stats_launch(RowProd &rp, const StatsArgs &st, bool large, int64_t prun, hipStream_t s)
+static int stats_launch(RowProd &rp, const StatsArgs &st, bool large, int prun, hipStream_t s)
 {
-    return large ? rowprod_launch<TileL>(rp, StatsEpi<ENT, TOP>{st}, s, (int)prun) : rowprod_launch<TileM>(rp, StatsEpi<ENT, TOP>{st}, s, (int)prun);
+    return large ? rowprod_launch<TileL>(rp, StatsEpi<ENT, TOP>{st}, s, prun) : rowprod_launch<TileM>(rp, StatsEpi<ENT, TOP>{st}, s, prun);
 }
 
 int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
@@ -802,24 +836,25 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     const int64_t blocks = (a.V + 63) / 64, kpad = pad_to(a.d, ROWPROD_K);
     // a few rounds of 64 rows per wave where there are waves enough for every SIMD without
     const int rounds = few ? (int)(blocks / 4096 < 1 ? 1 : blocks / 4096 > 16 ? 16 : blocks / 4096) : 1;
-    // runs of p tiles: as long as about two workgroups (four of the smaller tile) for every CU are left
     const bool large = rowprod_size(a.V, a.n) == 2;
     const int64_t ptiles = large ? (a.V + TileL::BP - 1) / TileL::BP : (a.V + TileM::BP - 1) / TileM::BP;
     const int64_t qtiles = large ? (a.n + TileL::BQ - 1) / TileL::BQ : (a.n + TileM::BQ - 1) / TileM::BQ;
-    const int64_t prun = few ? 1 : std::max<int64_t>(1, std::min<int64_t>(64, ptiles * qtiles / (large ? 512 : 1024)));
+    // (a start costs a few microseconds, a tile 27 at K = 1024 and 256 x 256; one workgroup of the large tile fits
+    // a CU, two of the smaller)
+    const double ksum = (double)kpad * (dtype_pieces(a.ttype) * dtype_pieces(a.qtype) == 9 ? 6 : dtype_pieces(a.qtype));
+    const int prun = few ? 1 : rowprod_run(ptiles, qtiles, large ? 256 : 512, 100.0 / (ksum + 200.0), 64);
     const int nparts = (int)(few ? (blocks + rounds - 1) / rounds : (ptiles + prun - 1) / prun * 2);     // (both tiles: two waves along P)
     // Groups of 16 rows or of 64.  Per query, the smaller ones cost two more operations a row and 8 bytes for 16 rows
     // instead of 4 for 64, about 0.14 ps times V; the larger ones 64 rows of the table for each of the `top`, at about
     // 6 TB/s.  (A few queries: the vector units have nothing else to do.)
     const int wide = !few && a.V > 76ll * a.top * a.d * dtype_width(a.ttype);
-    const int64_t ngroups = wide ? blocks : blocks * 4;
     Carve w(ws);
     StatsArgs st = {};
-    st.n = a.n; st.V = a.V; st.c = a.scale * LOG2E; st.live = a.live; st.ld_live = a.ld_live; st.targets = a.targets;
+    st.n = (int)a.n; st.V = (int)a.V; st.c = a.scale * LOG2E; st.live = a.live; st.ld_live = a.ld_live; st.targets = a.targets;
     st.parts = w.take<float4>(a.n * nparts);
     st.nparts = nparts;
-    st.gmax = a.top ? w.take<float>(a.n * ngroups * (wide ? 1 : 2)) : nullptr;
-    st.ngroups = ngroups;
+    st.gmax = a.top ? w.take<float>(a.n * blocks * (wide ? 1 : 8)) : nullptr;
+    st.nblocks = (int)blocks;
     st.wide = wide;
     st.zt = w.take<float>(a.n);
     const int nx = few ? nparts : NORM_WGS;

@@ -160,8 +160,8 @@ static SideBySide side_by_side(int upieces, int bpieces, int r)
     x.r = r;
     x.kpad = (int)pad_to(x.np * r, ROWPROD_K);
     for (int t = 0; t < rp.nseg; t++) {
-        x.pb[t] = rp.sp[t];
-        x.pu[t] = rp.sq[t];
+        x.pb[t] = (rp.sp >> (4 * t)) & 15;
+        x.pu[t] = (rp.sq >> (4 * t)) & 15;
     }
     return x;
 }

@@ -45,7 +45,7 @@ struct AdapterPart {
 struct RowProd {
     RowOperand P, Q;
     int nseg;                       // products of pieces
-    uint8_t sp[6], sq[6];           // piece of P and of Q of each
+    uint32_t sp, sq;                // piece of P and of Q of each, four bits a product
     int ksteps;                     // steps of ROWPROD_K per product
     int splits;                     // workgroups that share a tile's sum
     int ptiles, qtiles;             // tiles, and workgroups along P: each takes prun tiles
@@ -56,12 +56,13 @@ struct RowProd {
 static inline void rowprod_pieces(RowProd &a, int np, int nq)
 {
     a.nseg = 0;
+    a.sp = a.sq = 0;
     for (int s = (np - 1) + (nq - 1); s >= 0; s--)                   // the smallest products first
         for (int i = np - 1; i >= 0; i--) {
             const int j = s - i;
             if (j < 0 || j >= nq || s > (np > nq ? np : nq) - 1) continue;
-            a.sp[a.nseg] = (uint8_t)i;
-            a.sq[a.nseg] = (uint8_t)j;
+            a.sp |= (uint32_t)i << (4 * a.nseg);
+            a.sq |= (uint32_t)j << (4 * a.nseg);
             a.nseg++;
         }
 }
@@ -117,11 +118,13 @@ static __device__ __forceinline__ void rowprod_landed()
     __syncthreads();
 }
 
-// (the operand that more products follow each other with stays: the longer side's tiles in the inner loop.
-// 128,000 x 4096 x 1024 at 256 x 256: 885 us so, 922 with the loops the other way round; with both halves'
-// operands fetched first, or products and fetches interleaved by hand, 960 to 1,025)
-template <class T>
-static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int wq, int lane, RowAcc<T> &acc)
+// One step's products.  The operand that more products follow each other with stays: the longer side's tiles
+// are the inner loop.  `fetch`, the next step's loads, is issued in the middle of the first half's products,
+// where the operand reads of that half are out of its way.  128,000 x 4096 x 1024 at 256 x 256: 854 us so, 859
+// with the loads first, 922 with the loops the other way round; with both halves' operands read first, or
+// products and reads interleaved by hand, 960 to 1,025.
+template <class T, class F>
+static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int wq, int lane, RowAcc<T> &acc, const F &fetch)
 {
 #pragma unroll
     for (int kk = 0; kk < 2; kk++) {
@@ -133,6 +136,11 @@ static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int
         for (int j = 0; j < T::QT; j++) b[j] = *(const v8bf *)(buf + T::BP * 128 + (wq * T::QT + j) * 2048 + slot);
 #pragma unroll
         for (int x = 0; x < T::PT * T::QT; x++) {
+            if (kk == 0 && x == T::PT * T::QT / 2) {
+                __builtin_amdgcn_sched_barrier(0);
+                fetch();
+                __builtin_amdgcn_sched_barrier(0);
+            }
             const int i = T::PT >= T::QT ? x % T::PT : x / T::QT, j = T::PT >= T::QT ? x / T::PT : x % T::QT;
             acc.v[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc.v[i][j], 0, 0, 0);
         }
@@ -206,7 +214,8 @@ __global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi 
     char *b0 = rowprod_lds, *b1 = rowprod_lds + T::BYTES;
     int seg = s0 / a.ksteps, k = s0 % a.ksteps;
     auto fetch = [&](char *buf) {
-        rowprod_fetch<T>(buf, pb + (a.sp[seg] * a.P.piece + k * ROWPROD_K) * 2, po, qb + (a.sq[seg] * a.Q.piece + k * ROWPROD_K) * 2, qo, wave);
+        const int64_t ps = (a.sp >> (4 * seg)) & 15, qs = (a.sq >> (4 * seg)) & 15;
+        rowprod_fetch<T>(buf, pb + (ps * a.P.piece + k * ROWPROD_K) * 2, po, qb + (qs * a.Q.piece + k * ROWPROD_K) * 2, qo, wave);
     };
     fetch(b0);
     typename Epi::template State<T> state;
@@ -218,22 +227,23 @@ __global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi 
         for (int i = 0; i < T::PT; i++)
 #pragma unroll
             for (int j = 0; j < T::QT; j++) acc.v[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = s0; s < s1 - 1; s++) {
-            if (++k == a.ksteps) { k = 0; seg++; }
-            fetch(b1);
-            rowprod_step<T>(b0, wp, wq, lane, acc);
-            rowprod_landed();
+        for (int s = s0; s < s1; s++) {
+            bool more = true;                                         // uniform, as all of this
+            if (s + 1 < s1) {
+                if (++k == a.ksteps) { k = 0; seg++; }
+            } else {
+                seg = s0 / a.ksteps;
+                k = s0 % a.ksteps;
+                more = t + 1 < t1;
+                pb += (int64_t)T::BP * a.P.ld * 2;
+                if (more && t + 2 == a.ptiles) rowprod_rows<T>((int64_t)(t + 1) * T::BP, a.P.rows, a.P.ld, tid, po);
+            }
+            rowprod_step<T>(b0, wp, wq, lane, acc, [&]() {
+                if (more) fetch(b1);
+            });
+            if (s + 1 < s1) rowprod_landed();
             char *x = b0; b0 = b1; b1 = x;
         }
-        seg = s0 / a.ksteps;
-        k = s0 % a.ksteps;
-        if (t + 1 < t1) {
-            pb += (int64_t)T::BP * a.P.ld * 2;
-            if (t + 2 == a.ptiles) rowprod_rows<T>((int64_t)(t + 1) * T::BP, a.P.rows, a.P.ld, tid, po);
-            fetch(b1);
-        }
-        rowprod_step<T>(b0, wp, wq, lane, acc);
-        char *x = b0; b0 = b1; b1 = x;
         const int64_t p0 = (int64_t)t * T::BP;
         if constexpr (ADAPT) {                                        // (a run is one tile)
             const int64_t qend = q0 + T::BQ < a.Q.rows ? q0 + T::BQ : a.Q.rows;
@@ -256,7 +266,7 @@ __global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi 
                         __builtin_amdgcn_global_load_lds((global_void *)(src + kk * 2), (lds_void *)(b0 + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
                     }
                     rowprod_landed();
-                    rowprod_step<T>(b0, wp, wq, lane, acc);
+                    rowprod_step<T>(b0, wp, wq, lane, acc, []() {});
                 }
             }
         }
@@ -264,6 +274,20 @@ __global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi 
         rowprod_landed();
     }
     epi.end(state, run, wp, qw, lane);
+}
+
+// p tiles that a workgroup takes one after the other, at most `most`: what the last round of workgroups leaves
+// idle against the start of each (about `start` tiles' time), with room for `slots` workgroups at once
+static inline int rowprod_run(int64_t ptiles, int64_t qtiles, int slots, double start, int most)
+{
+    int best = 1;
+    double least = 1e300;
+    for (int r = 1; r <= most && r <= ptiles; r++) {
+        const int64_t wgs = (ptiles + r - 1) / r * qtiles;
+        const double t = (double)((wgs + slots - 1) / slots) * (r + start);
+        if (t < least) { least = t; best = r; }
+    }
+    return best;
 }
 
 // `prun`: p tiles that a workgroup takes one after the other
