@@ -36,7 +36,7 @@ struct StatsArgs {
     // read in one run)
     float *gmax;
     int nblocks;
-    int wide;
+    int wide, wstride;              // (a query's run is filled up to a multiple of four values)
     float *zt;                      // [n] the target's product
 };
 
@@ -46,6 +46,20 @@ static __device__ __forceinline__ float exp2_fast(float x) { return __builtin_am
 // The larger value, a NaN if there is one.  (The instruction for it takes values as they come out of the
 // matrix cores; fmaxf's has each quieted by an instruction of its own first.)
 static __device__ __forceinline__ float max_of(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
+// The largest of the four lanes that hold the same query (lane & 15), in each of them: registers' halves are swapped
+// between copies of a value, so that each step is one maximum (written as instructions, with the idle slots
+// that the compiler puts around its own; four trips through the LDS crossbar per query took a fifth of the
+// epilogue's time).
+static __device__ __forceinline__ float max_of_four(float x)
+{
+    float y = x;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(x), "+v"(y));
+    x = max_of(x, y);
+    y = x;
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\ts_nop 1" : "+v"(x), "+v"(y));
+    return max_of(x, y);
+}
 
 // sums relative to a maximum m0, brought to m1 >= m0
 static __device__ __forceinline__ void rebase(float &s, float &e, float m0, float m1, float c)
@@ -135,9 +149,8 @@ struct StatsState {
                     for (int i = b; i < b + 4; i++)
                         g = max_of(max_of(max_of(g, acc[i][j][0]), acc[i][j][1]), max_of(acc[i][j][2], acc[i][j][3]));
                     if constexpr (TOP == 1) {
-                        float w = fmaxf(g, __shfl_xor(g, 16));
-                        w = fmaxf(w, __shfl_xor(w, 32));
-                        if (in && h == 0 && blk < a.nblocks) a.gmax[(int64_t)q * a.nblocks + blk] = w;
+                        const float w = max_of_four(g);
+                        if (in && h == 0 && blk < a.nblocks) a.gmax[(int64_t)q * a.wstride + blk] = w;
                     }
                 }
                 top = max_of(top, g);
@@ -254,7 +267,7 @@ struct FewStatsArgs {
 };
 
 template <class S, class Q, int QT, bool VEC, bool NORM>
-__global__ __launch_bounds__(WG) void few_stats_kernel(FewStatsArgs a)
+__global__ __launch_bounds__(WG, QT == 1 ? 4 : QT == 2 ? 3 : 2) void few_stats_kernel(FewStatsArgs a)
 {
     const int lane = threadIdx.x & 63;
     const int part = blockIdx.x * (WG / 64) + (threadIdx.x >> 6);
@@ -272,24 +285,31 @@ __global__ __launch_bounds__(WG) void few_stats_kernel(FewStatsArgs a)
     for (int r = 0; r < a.rounds; r++) {
         const int p0 = (part * a.rounds + r) * 64;
         if (p0 >= a.st.V) break;
-        const S *prow[4];
+        // 32 rows at a time: twice the waves on a SIMD, so that some load while others multiply
         v4f acc[4][QT];
-        float nrm[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            prow[i] = (const S *)a.table + (int64_t)min(p0 + 16 * i + (lane & 15), a.st.V - 1) * a.ldt;
-            nrm[i] = 0.0f;
+        for (int half = 0; half < 2; half++) {
+            const S *prow[2];
+            v4f part[2][QT];
+            float nrm[2];
 #pragma unroll
-            for (int j = 0; j < QT; j++) acc[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
-        }
-        few_dot<S, Q, 4, QT, VEC, NORM>(prow, qrow, 0, steps, a.d, lane, acc, nrm);
-        if constexpr (NORM) {
+            for (int i = 0; i < 2; i++) {
+                prow[i] = (const S *)a.table + (int64_t)min(p0 + 32 * half + 16 * i + (lane & 15), a.st.V - 1) * a.ldt;
+                nrm[i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                float x = nrm[i] + __shfl_xor(nrm[i], 16);
-                x += __shfl_xor(x, 32);
-                const int p = p0 + 16 * i + (lane & 15);
-                if (p < a.st.V && (!a.any_live || ((a.any_live[p >> 5] >> (p & 31)) & 1u))) most = fmaxf(most, x);
+                for (int j = 0; j < QT; j++) part[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            few_dot<S, Q, 2, QT, VEC, NORM>(prow, qrow, 0, steps, a.d, lane, part, nrm);
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+#pragma unroll
+                for (int j = 0; j < QT; j++) acc[2 * half + i][j] = part[i][j];
+                if constexpr (NORM) {
+                    float x = nrm[i] + __shfl_xor(nrm[i], 16);
+                    x += __shfl_xor(x, 32);
+                    const int p = p0 + 32 * half + 16 * i + (lane & 15);
+                    if (p < a.st.V && (!a.any_live || ((a.any_live[p >> 5] >> (p & 31)) & 1u))) most = fmaxf(most, x);
+                }
             }
         }
         st.tile(a.st, acc, p0, 0, lane);
@@ -311,6 +331,7 @@ struct FinishArgs {
     const void *table, *q;
     int64_t ldt, ldq;
     int d, vec;
+    int dot_lanes;                  // lanes that share a row's float64 product
     float scale;
     float slack;                    // relative error of a product against |q||t|
     const float *xmax;
@@ -334,7 +355,7 @@ struct FinishShared {
     uint32_t take[ITEMS];
     float lval[LIST];
     uint32_t lid[LIST];
-    float kth_in[NT == 64 ? 4 : 256];
+    float kth_in[256];
     float red[16];
     float kth_out;
     int count, nbest, wcnt[16];
@@ -373,15 +394,26 @@ static __device__ __forceinline__ int64_t entry_row(uint32_t entry, int member, 
 }
 
 // A lower bound of the k-th largest (k <= 64) of the values of which most[0..3] are a thread's maxima of four
-// sets: the k-th largest of the maxima of 256 sets.  A wave finds it bit by bit; a workgroup joins the sets of
-// its threads to 256 and counts.
+// sets: the k-th largest of the maxima of 256 sets, found bit by bit.
 template <int NT>
 static __device__ __forceinline__ float kth_set_max(FinishShared<NT> &sh, const float (&most)[4], int k, int tid)
 {
-    if constexpr (NT == 64) {
+    float set[4] = {most[0], most[1], most[2], most[3]};
+    if constexpr (NT > 64) {                                          // NT / 256 threads' values to a set, for the first wave
+        float mine = fmaxf(fmaxf(set[0], set[1]), fmaxf(set[2], set[3]));
+#pragma unroll
+        for (int x = 1; x < NT / 256; x <<= 1) mine = fmaxf(mine, __shfl_xor(mine, x));
+        __syncthreads();
+        if (tid % (NT / 256) == 0) sh.kth_in[tid / (NT / 256)] = mine;
+        __syncthreads();
+        if (tid < 64)
+#pragma unroll
+            for (int u = 0; u < 4; u++) set[u] = sh.kth_in[tid + 64 * u];
+    }
+    if (NT == 64 || tid < 64) {
         uint32_t key[4], cut = 0;
 #pragma unroll
-        for (int u = 0; u < 4; u++) key[u] = f32_key(most[u]);
+        for (int u = 0; u < 4; u++) key[u] = f32_key(set[u]);
         for (int bit = 31; bit >= 0; bit--) {
             const uint32_t cand = cut | (1u << bit);
             int n = 0;
@@ -389,46 +421,41 @@ static __device__ __forceinline__ float kth_set_max(FinishShared<NT> &sh, const 
             for (int u = 0; u < 4; u++) n += __popcll(__ballot(key[u] >= cand));
             if (n >= k) cut = cand;
         }
-        return key_f32(cut);
-    } else {
-        float mine = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-#pragma unroll
-        for (int x = 1; x < NT / 256; x <<= 1) mine = fmaxf(mine, __shfl_xor(mine, x));
-        __syncthreads();
-        if (tid % (NT / 256) == 0) sh.kth_in[tid / (NT / 256)] = mine;
-        __syncthreads();
-        if (tid < 256) {
-            const float x = sh.kth_in[tid];
-            int above = 0;
-#pragma unroll 8
-            for (int i = 0; i < 256; i += 4) {
-                const v4f y = *(const v4f *)&sh.kth_in[i];
-#pragma unroll
-                for (int u = 0; u < 4; u++) above += y[u] > x || (y[u] == x && i + u < tid) ? 1 : 0;
-            }
-            if (above == k - 1) sh.kth_out = x;
-        }
-        __syncthreads();
-        return sh.kth_out;
+        if (tid == 0) sh.kth_out = key_f32(cut);
     }
+    team_sync<NT>();
+    return sh.kth_out;
 }
 
-// <q, t> in float64 by 16 lanes; the order of the sum depends on d alone, so equal rows get equal values
+template <class S>
+struct DotLoad {                    // values per lane and step (eight bytes: sixteen and their float64 values are too many registers)
+    static constexpr int CH = sizeof(S) == 1 ? 8 : 16 / sizeof(S);
+};
+
+// <q, t> in float64 for four rows at once by `lanes` lanes (1 to 16), whose own place is `sub`; the order of a
+// sum depends on d alone, so equal rows get equal values
 template <class S, class Q, bool VEC>
-static __device__ __forceinline__ double dot_exact(const S *t, const Q *q, int d, int sub)
+static __device__ __forceinline__ void dot_exact(const S *const (&t)[4], const Q *q, int d, int sub, int lanes, double (&x)[4])
 {
-    constexpr int CH = FewLoad<S>::CH, AHEAD = 16 / CH;
-    double x = 0.0;
-#pragma unroll AHEAD
-    for (int k = sub * CH; k < d; k += 16 * CH) {
-        const FewFrag<S, CH> f = few_load<S, CH, VEC>(t, k, d);
+    constexpr int CH = DotLoad<S>::CH;
+#pragma unroll
+    for (int u = 0; u < 4; u++) x[u] = 0.0;
+#pragma unroll 1
+    for (int k = sub * CH; k < d; k += lanes * CH) {
+        FewFrag<S, CH> f[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) f[u] = few_load<S, CH, VEC>(t[u], k, d);
         const FewFrag<Q, CH> g = few_load<Q, CH, VEC>(q, k, d);
 #pragma unroll
-        for (int e = 0; e < CH; e++) x = fma((double)(float)f.e[e], (double)(float)g.e[e], x);
-    }
+        for (int e = 0; e < CH; e++) {
+            const double y = (double)(float)g.e[e];
 #pragma unroll
-    for (int s = 8; s > 0; s >>= 1) x += __shfl_xor(x, s);
-    return x;
+            for (int u = 0; u < 4; u++) x[u] = fma((double)(float)f[u].e[e], y, x[u]);
+        }
+    }
+    for (int s = lanes >> 1; s > 0; s >>= 1)
+#pragma unroll
+        for (int u = 0; u < 4; u++) x[u] += __shfl_xor(x[u], s);
 }
 
 // scores the rows of the `cnt` entries in sh.take and merges those of at least `floor` into sh.best
@@ -436,7 +463,7 @@ template <class S, class Q, int NT>
 static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishShared<NT> &sh, int64_t row, int tid, int cnt, int kind,
                                                     double floor)
 {
-    const int lane = tid & 63, wave = tid >> 6, sub = lane & 15, quarter = lane >> 4;
+    const int lane = tid & 63, wave = tid >> 6, lanes = a.dot_lanes, sub = lane & (lanes - 1), at = lane / lanes, rows = 64 / lanes;
     const Q *q = (const Q *)a.q + row * a.ldq;
     const int old = sh.nbest;
     if (tid < old) {
@@ -447,17 +474,27 @@ static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishS
     team_sync<NT>();
     const int items = cnt * kind;
 #pragma unroll 1
-    for (int i0 = wave * 4; i0 < items; i0 += NT / 16) {              // four rows per wave, 16 lanes each
-        const int i = i0 + quarter, ic = i < items ? i : items - 1;
-        const int64_t v = entry_row(sh.take[ic / kind], ic % kind, kind);
-        const bool in = i < items && v < a.st.V && (!a.st.live || ((a.st.live[row * a.st.ld_live + (v >> 5)] >> (v & 31)) & 1u));
-        const S *t = (const S *)a.table + (in ? v : 0) * a.ldt;
-        const double x = a.vec ? dot_exact<S, Q, true>(t, q, a.d, sub) : dot_exact<S, Q, false>(t, q, a.d, sub);
-        if (sub == 0 && in && x >= floor) {                           // (not a NaN either)
-            const int slot = atomicAdd(&sh.count, 1);
-            sh.val[slot] = x;
-            sh.id[slot] = (uint32_t)v;
+    for (int i0 = wave * 4 * rows; i0 < items; i0 += NT / 16 * rows) {        // four times 64 / lanes rows per wave
+        const S *t[4];
+        int64_t v[4];
+        double x[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int i = i0 + u * rows + at, ic = i < items ? i : items - 1;
+            v[u] = entry_row(sh.take[ic / kind], ic % kind, kind);
+            const bool in = i < items && v[u] < a.st.V && (!a.st.live || ((a.st.live[row * a.st.ld_live + (v[u] >> 5)] >> (v[u] & 31)) & 1u));
+            v[u] = in ? v[u] : -1;
+            t[u] = (const S *)a.table + (in ? v[u] : 0) * a.ldt;
         }
+        if (a.vec) dot_exact<S, Q, true>(t, q, a.d, sub, lanes, x);
+        else dot_exact<S, Q, false>(t, q, a.d, sub, lanes, x);
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+            if (sub == 0 && v[u] >= 0 && x[u] >= floor) {             // (not a NaN either)
+                const int slot = atomicAdd(&sh.count, 1);
+                sh.val[slot] = x[u];
+                sh.id[slot] = (uint32_t)v[u];
+            }
     }
     team_sync<NT>();
     const int total = sh.count;
@@ -507,7 +544,7 @@ static __device__ __forceinline__ void finish_entries(const FinishArgs &a, Finis
 
 // NT threads per query, `TEAMS` queries per workgroup
 template <class S, class Q, int NT, int TEAMS>
-__global__ __launch_bounds__(NT * TEAMS, 4) void logprob_finish_kernel(FinishArgs a)
+__global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_kernel(FinishArgs a)
 {
     __shared__ FinishShared<NT> shared[TEAMS];
     FinishShared<NT> &sh = shared[threadIdx.x / NT];
@@ -557,6 +594,7 @@ __global__ __launch_bounds__(NT * TEAMS, 4) void logprob_finish_kernel(FinishArg
         q2 = fmaf(x, x, q2);
         zero = x == 0.0f ? zero : 0.0f;
     }
+#pragma unroll 8
     for (int i = tid; i < a.nxmax; i += NT) x2 = fmaxf(x2, a.xmax[i]);
     q2 = team_fold(sh, q2, sum);
     x2 = team_fold(sh, x2, largest);
@@ -569,28 +607,68 @@ __global__ __launch_bounds__(NT * TEAMS, 4) void logprob_finish_kernel(FinishArg
 
     // entry i of the query's groups: block i >> shift, its part i & 3 if it has four
     const int shift = a.st.wide ? 0 : 2, ngroups = a.st.nblocks << shift;
+    const float *wmax = a.st.gmax + row * a.st.wstride;
     const auto group_at = [&](int i) {
-        return a.st.wide ? a.st.gmax + row * a.st.nblocks + i : a.st.gmax + ((((int64_t)(i >> 2) * a.st.n + row) << 2) + (i & 3)) * 2;
+        return a.st.wide ? wmax + i : a.st.gmax + ((((int64_t)(i >> 2) * a.st.n + row) << 2) + (i & 3)) * 2;
+    };
+    // All of them, up to 32 values at a time, by a body that is straight-line code to begin with (a load whose use is
+    // behind a branch is moved there, and loads then wait for one another).
+    const auto each_group = [&](const auto &body) {
+        if (a.st.wide) {
+            const int fours = (ngroups + 3) / 4;
+            for (int i0 = tid; i0 < fours; i0 += 8 * NT) {
+                v4f x[8];
+#pragma unroll
+                for (int u = 0; u < 8; u++) x[u] = *(const v4f *)(wmax + 4 * min(i0 + u * NT, fours - 1));
+                float y[32];
+#pragma unroll
+                for (int u = 0; u < 32; u++) y[u] = 4 * (i0 + (u >> 2) * NT) + (u & 3) < ngroups ? x[u >> 2][u & 3] : HIDDEN;
+                body(y, [&](int u) { return 4 * (i0 + (u >> 2) * NT) + (u & 3); });
+            }
+        } else {
+            for (int i0 = tid; i0 < ngroups; i0 += 16 * NT) {
+                float y[32];
+#pragma unroll
+                for (int u = 0; u < 16; u++) y[u] = *group_at(min(i0 + u * NT, ngroups - 1));
+#pragma unroll
+                for (int u = 0; u < 16; u++) y[u] = i0 + u * NT < ngroups ? y[u] : HIDDEN;
+#pragma unroll
+                for (int u = 16; u < 32; u++) y[u] = HIDDEN;
+                body(y, [&](int u) { return i0 + u * NT; });
+            }
+        }
     };
     float most[4] = {HIDDEN, HIDDEN, HIDDEN, HIDDEN};
-    {
-        int i = tid;
-        for (; i + 3 * NT < ngroups; i += 4 * NT) {
+    each_group([&](const float (&y)[32], const auto &) {
 #pragma unroll
-            for (int u = 0; u < 4; u++) most[u] = fmaxf(most[u], *group_at(i + u * NT));
-        }
-        for (; i < ngroups; i += NT) most[0] = fmaxf(most[0], *group_at(i));
-    }
+        for (int u = 0; u < 32; u++) most[u & 3] = fmaxf(most[u & 3], y[u]);
+    });
     if (!empty && eps < 1e38f) {                                      // (the same in every thread)
         const float thr = kth_set_max<NT>(sh, most, a.top, tid) - 2.0f * eps;
         // exact products of the K best are at least this
         const double floor = (double)thr + (double)eps * 0.999;
         const float mine = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
         if (mine >= thr && mine > HIDDEN)
-            for (int i = tid; i < ngroups; i += NT) {
+            each_group([&](const float (&y)[32], const auto &index) {
+                uint32_t hits = 0;
+#pragma unroll
+                for (int u = 0; u < 32; u++) hits |= y[u] >= thr && y[u] > HIDDEN ? 1u << u : 0u;
+                while (hits) {
+                    const int i = index(__ffs(hits) - 1), at = atomicAdd(&sh.count, 1);
+                    hits &= hits - 1;
+                    if (at < FinishShared<NT>::ITEMS) sh.id[at] = (uint32_t)i;
+                }
+            });
+        team_sync<NT>();
+        const int groups = sh.count;
+        team_sync<NT>();
+        if (tid == 0) sh.count = groups <= FinishShared<NT>::ITEMS ? 0 : FinishShared<NT>::LIST + 1;
+        team_sync<NT>();
+        if (groups <= FinishShared<NT>::ITEMS)
+            for (int u0 = tid; u0 < groups; u0 += NT) {
+                const int i = (int)sh.id[u0];
                 const float *g = group_at(i);
-                const float x = *g;
-                if (!(x >= thr && x > HIDDEN)) continue;
+                const float x = g[0];
                 // the group's best row alone, or all of its rows if another may reach the bound too; wide: the group
                 const int rows = !a.st.wide && g[1] >= thr ? 16 : 1, at = atomicAdd(&sh.count, rows);
                 for (int u = 0; u < rows && at + u < FinishShared<NT>::LIST; u++) {
@@ -816,8 +894,10 @@ static int few_stats(const FewStatsArgs &fa, bool vec, bool norm, hipStream_t s)
 static float product_slack(int d) { return (1.1f * (float)d + 64.0f) * 1.1920929e-7f + 1.9073486e-6f; }
 
 template <class S, class Q>
-static int finish_launch(const FinishArgs &f, hipStream_t s)
+static int finish_launch(FinishArgs &f, hipStream_t s)
 {
+    f.dot_lanes = 1;
+    while (f.dot_lanes < 16 && f.dot_lanes * DotLoad<S>::CH < f.d) f.dot_lanes *= 2;
     if (f.st.n <= FEW_ROWS) hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 1024, 1>), dim3((unsigned)f.st.n), dim3(1024), 0, s, f);
     else hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 64, 4>), dim3((unsigned)((f.st.n + 3) / 4)), dim3(256), 0, s, f);
     RAIRS_HIP(hipGetLastError());
@@ -834,8 +914,9 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
 {
     const bool few = a.n <= FEW_ROWS;
     const int64_t blocks = (a.V + 63) / 64, kpad = pad_to(a.d, ROWPROD_K);
-    // a few rounds of 64 rows per wave where there are waves enough for every SIMD without
-    const int rounds = few ? (int)(blocks / 4096 < 1 ? 1 : blocks / 4096 > 16 ? 16 : blocks / 4096) : 1;
+    // rounds of 64 rows per wave, up to 16, for 4,096 waves (four a SIMD) or a multiple
+    const int64_t fills = (blocks + 16 * 4096 - 1) / (16 * 4096);
+    const int rounds = few ? (int)((blocks + fills * 4096 - 1) / (fills * 4096)) : 1;
     const bool large = rowprod_size(a.V, a.n) == 2;
     const int64_t ptiles = large ? (a.V + TileL::BP - 1) / TileL::BP : (a.V + TileM::BP - 1) / TileM::BP;
     const int64_t qtiles = large ? (a.n + TileL::BQ - 1) / TileL::BQ : (a.n + TileM::BQ - 1) / TileM::BQ;
@@ -853,7 +934,8 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     st.n = (int)a.n; st.V = (int)a.V; st.c = a.scale * LOG2E; st.live = a.live; st.ld_live = a.ld_live; st.targets = a.targets;
     st.parts = w.take<float4>(a.n * nparts);
     st.nparts = nparts;
-    st.gmax = a.top ? w.take<float>(a.n * blocks * (wide ? 1 : 8)) : nullptr;
+    st.wstride = (int)pad_to(blocks, 4);
+    st.gmax = a.top ? w.take<float>(wide ? a.n * st.wstride : a.n * blocks * 8) : nullptr;
     st.nblocks = (int)blocks;
     st.wide = wide;
     st.zt = w.take<float>(a.n);
@@ -863,6 +945,7 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     // (packed whether they need it or not, so that the size does not depend on where the rows lie)
     __bf16 *qroom = few ? nullptr : w.take<__bf16>(pack_room(a.qtype, a.n, kpad));
     __bf16 *troom = few ? nullptr : w.take<__bf16>(pack_room(a.ttype, a.V, kpad));
+    uint32_t *piece_flags = w.take<uint32_t>(2);
     if (bytes) *bytes = w.used;
     if (!ws) return RAIRS_OK;
 
@@ -890,8 +973,12 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
         RowProd rp = {};
         rowprod_pieces(rp, dtype_pieces(a.ttype), dtype_pieces(a.qtype));
         rp.ksteps = (int)(kpad / ROWPROD_K);
-        if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, qroom, rp.Q, s))) return rc;
-        if ((rc = rairs_operand(a.table, a.ttype, a.ldt, a.V, a.d, nullptr, troom, rp.P, s))) return rc;
+        // (queries of byte vectors are whole numbers as a rule, whose lower pieces are zero: packing them says so, and
+        // the products of those pieces are left out)
+        const bool flags = a.ttype == RAIRS_U8;
+        if ((rc = rairs_operand(a.table, a.ttype, a.ldt, a.V, a.d, nullptr, troom, rp.P, s, flags ? piece_flags : nullptr, true))) return rc;
+        if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, qroom, rp.Q, s, flags ? piece_flags : nullptr, false))) return rc;
+        if (flags) rp.Q.pieces_there = piece_flags;
         const bool ent = a.entropy != nullptr;
         if (a.top == 0) rc = ent ? stats_launch<true, 0>(rp, st, large, prun, s) : stats_launch<false, 0>(rp, st, large, prun, s);
         else if (wide) rc = ent ? stats_launch<true, 1>(rp, st, large, prun, s) : stats_launch<false, 1>(rp, st, large, prun, s);
@@ -979,8 +1066,8 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
                 return rc;
             RowProd dp = {};
             rowprod_pieces(dp, tp, np);
-            dp.P = RowOperand{tcols, cpad, a.d * cpad, a.d, nullptr};
-            dp.Q = RowOperand{g, cpad, a.n * cpad, a.n, nullptr};
+            dp.P = RowOperand{tcols, cpad, a.d * cpad, a.d, nullptr, nullptr};
+            dp.Q = RowOperand{g, cpad, a.n * cpad, a.n, nullptr, nullptr};
             dp.ksteps = (int)(cpad / ROWPROD_K);
             dp.splits = splits;
             StoreEpi e = {sums, a.d, a.n * a.d, a.d, a.n, nullptr, 0, v0 > 0};
@@ -989,8 +1076,8 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         if (need_dt) {
             RowProd dp = {};
             rowprod_pieces(dp, np, np);
-            dp.P = RowOperand{qcols, npad, a.d * npad, a.d, nullptr};
-            dp.Q = RowOperand{gt, npad, cpad * npad, rows, nullptr};
+            dp.P = RowOperand{qcols, npad, a.d * npad, a.d, nullptr, nullptr};
+            dp.Q = RowOperand{gt, npad, cpad * npad, rows, nullptr, nullptr};
             dp.ksteps = (int)(npad / ROWPROD_K);
             StoreEpi e = {(char *)a.dtable + v0 * a.lddt * dtype_width(a.ttype), a.lddt, 0, a.d, rows, nullptr, a.ttype == RAIRS_BF16, 0};
             if ((rc = rowprod_launch_any(dp, e, s))) return rc;

@@ -21,9 +21,10 @@ struct Carve {
 };
 
 // rows of a matrix as bf16 pieces with rows of kpad values, zero from `cols` on (and where live says so)
-// (perm: row r is src's row perm[r])
+// (perm: row r is src's row perm[r]; flags[i], if given: cleared if `clear`, else set if piece i + 1 of any value is
+// not zero)
 int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *dst,
-                           int64_t kpad, hipStream_t s);
+                           int64_t kpad, hipStream_t s, uint32_t *flags = nullptr, bool clear = false);
 // the same, transposed: dst[c][r] = src[perm ? perm[r] : r][c], zero for r in [rows, rpad)
 int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t src_batch, int64_t batches, int64_t rows, int64_t cols,
                            const uint32_t *live, const int32_t *perm, __bf16 *dst, int64_t rpad, int64_t dst_batch, int64_t piece,
@@ -38,7 +39,7 @@ static inline bool rows_lie_right(const void *p, int dtype, int64_t ld, int64_t 
 }
 static inline int64_t pack_room(int dtype, int64_t rows, int64_t cols) { return rows * pad_to(cols, ROWPROD_K) * dtype_pieces(dtype); }
 int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *room, RowOperand &out,
-                  hipStream_t s);
+                  hipStream_t s, uint32_t *flags = nullptr, bool clear = false);
 
 struct LogprobArgs {
     const void *q, *table;

@@ -45,8 +45,10 @@ static __device__ __forceinline__ bool row_live(const uint32_t *live, int64_t r)
 template <class S, int NP>
 __global__ __launch_bounds__(WG) void pack_rows_kernel(const S *__restrict__ src, int64_t ld, int64_t rows, int64_t cols,
                                                        const int32_t *__restrict__ perm, int vec, __bf16 *__restrict__ dst,
-                                                       int64_t kpad, int64_t piece)
+                                                       int64_t kpad, int64_t piece, uint32_t *__restrict__ flags, int clear)
 {
+    if (flags && clear && blockIdx.x == 0 && threadIdx.x < 2) flags[threadIdx.x] = 0;
+    uint32_t there = 0;
     const int64_t per = kpad / 8, total = rows * per;
     for (int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x; t < total; t += (int64_t)gridDim.x * WG) {
         const int64_t r = t / per, i0 = (t - r * per) * 8;
@@ -59,9 +61,15 @@ __global__ __launch_bounds__(WG) void pack_rows_kernel(const S *__restrict__ src
             split_pieces<NP>(x[e], pc);
 #pragma unroll
             for (int u = 0; u < NP; u++) o[u][e] = pc[u];
+#pragma unroll
+            for (int u = 1; u < NP; u++) there |= (float)pc[u] != 0.0f ? 1u << (u - 1) : 0u;
         }
 #pragma unroll
         for (int u = 0; u < NP; u++) *(v8bf *)(dst + u * piece + r * kpad + i0) = o[u];
+    }
+    if (NP > 1 && flags && !clear) {
+        if (__any(there & 1u) && (threadIdx.x & 63) == 0) flags[0] = 1;      // (all that do write the same)
+        if (__any(there & 2u) && (threadIdx.x & 63) == 0) flags[1] = 1;
     }
 }
 
@@ -108,18 +116,21 @@ static int is_vec(const void *p, int64_t ld, int64_t batch, int width)
 }
 
 int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *dst,
-                           int64_t kpad, hipStream_t s)
+                           int64_t kpad, hipStream_t s, uint32_t *flags, bool clear)
 {
     if (rows == 0) return RAIRS_OK;
     const int64_t piece = rows * kpad, want = (rows * (kpad / 8) + WG - 1) / WG;
     const dim3 grid((unsigned)(want < 8192 ? want : 8192));
     const int vec = is_vec(src, ld, 0, dtype_width(dtype));
     if (dtype == RAIRS_F32)
-        hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, perm, vec, dst, kpad, piece);
+        hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, perm, vec, dst, kpad, piece, flags,
+                           (int)clear);
     else if (dtype == RAIRS_BF16)
-        hipLaunchKernelGGL((pack_rows_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, perm, vec, dst, kpad, piece);
+        hipLaunchKernelGGL((pack_rows_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, perm, vec, dst, kpad, piece, flags,
+                           (int)clear);
     else
-        hipLaunchKernelGGL((pack_rows_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, perm, vec, dst, kpad, piece);
+        hipLaunchKernelGGL((pack_rows_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, perm, vec, dst, kpad, piece, flags,
+                           (int)clear);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
@@ -148,11 +159,12 @@ int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t src_b
 }
 
 int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *room, RowOperand &out,
-                  hipStream_t s)
+                  hipStream_t s, uint32_t *flags, bool clear)
 {
     const int64_t kpad = pad_to(cols, ROWPROD_K);
     out.rows = rows;
     out.perm = nullptr;
+    out.pieces_there = nullptr;
     if (rows_lie_right(src, dtype, ld, cols) && (!perm || rows * ld < (1ll << 31))) {
         out.p = (const __bf16 *)src;
         out.ld = ld;
@@ -163,5 +175,5 @@ int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t 
     out.p = room;
     out.ld = kpad;
     out.piece = rows * kpad;
-    return rairs_launch_pack_rows(src, dtype, ld, rows, cols, perm, room, kpad, s);
+    return rairs_launch_pack_rows(src, dtype, ld, rows, cols, perm, room, kpad, s, flags, clear);
 }

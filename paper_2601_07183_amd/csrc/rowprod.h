@@ -29,6 +29,7 @@ struct RowOperand {
     int64_t ld, piece;
     int64_t rows;
     const int32_t *perm;            // Q only: row r of the product is row perm[r] here (null: r); then rows * ld below 2^31
+    const uint32_t *pieces_there;   // Q only: word i is 0 if piece i + 1 is zero everywhere (null: not known)
 };
 
 // The part of a sum that depends on the row's adapter: rows are sorted by adapter, a tile runs over
@@ -209,12 +210,26 @@ __global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi 
         rowprod_rows<T>(q0, a.Q.rows, a.Q.ld, tid, qo);
         qb += q0 * a.Q.ld * 2;
     }
-    const int steps = a.nseg * a.ksteps;
+    uint32_t sp = a.sp, sq = a.sq;
+    int nseg = a.nseg;
+    if (a.Q.pieces_there) {
+        const uint32_t there = 1u | (a.Q.pieces_there[0] ? 2u : 0u) | (a.Q.pieces_there[1] ? 4u : 0u);
+        sp = sq = 0;
+        nseg = 0;
+        for (int i = 0; i < a.nseg; i++) {
+            const uint32_t u = (a.sp >> (4 * i)) & 15, v = (a.sq >> (4 * i)) & 15;
+            if (!((there >> v) & 1u)) continue;
+            sp |= u << (4 * nseg);
+            sq |= v << (4 * nseg);
+            nseg++;
+        }
+    }
+    const int steps = nseg * a.ksteps;
     const int s0 = (int)((int64_t)steps * split / a.splits), s1 = (int)((int64_t)steps * (split + 1) / a.splits);
     char *b0 = rowprod_lds, *b1 = rowprod_lds + T::BYTES;
     int seg = s0 / a.ksteps, k = s0 % a.ksteps;
     auto fetch = [&](char *buf) {
-        const int64_t ps = (a.sp >> (4 * seg)) & 15, qs = (a.sq >> (4 * seg)) & 15;
+        const int64_t ps = (sp >> (4 * seg)) & 15, qs = (sq >> (4 * seg)) & 15;
         rowprod_fetch<T>(buf, pb + (ps * a.P.piece + k * ROWPROD_K) * 2, po, qb + (qs * a.Q.piece + k * ROWPROD_K) * 2, qo, wave);
     };
     fetch(b0);

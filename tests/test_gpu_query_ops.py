@@ -287,6 +287,8 @@ LOGPROBS = [
     (17, 1000, 96, 20, "shared"), (33, 3001, 100, 50, "rows"), (64, 127, 7, 4, None), (3, 700, 40, 8, "none"),
     (65, 129, 64, 10, None), (70, 1000, 65, 64, "shared"), (100, 2047, 128, 0, "rows"), (130, 300, 1000, 7, None),
     (200, 64, 32, 5, "none"), (300, 5000, 72, 20, "rows"), (129, 1, 64, 2, None), (4, 300_000, 24, 10, None), (128, 40_000, 32, 33, "shared"),
+    # large tiles and wide groups
+    (300, 60_000, 24, 2, None), (260, 51_300, 100, 1, "shared"), (257, 70_001, 64, 0, None), (520, 30_011, 200, 12, "rows"),
 ]
 
 
@@ -318,6 +320,21 @@ def test_logprob_strided_rows(n, pad, offset, tt):
     q, table, targets, scale, _ = logprob_data(n, 333, 40, tt, 8)
     r = binding.logprob(strided(q, pad, offset), strided(table, pad, offset), targets.cuda(), scale=scale, top=9)
     check_logprob(r, exact_logprob(q, table, targets, scale, None, 9), 333, 9)
+
+
+@pytest.mark.parametrize("n", [20, 300])
+@pytest.mark.parametrize("part", ["half", "fine", "one"])
+def test_logprob_of_bytes_and_queries_that_are_not_whole(n, part):
+    # queries whose second, or second and third bf16 piece is there, in all rows or in one value alone
+    q, table, targets, scale, _ = logprob_data(n, 700, 40, U8, 17)
+    if part == "half":
+        q += 0.5
+    elif part == "fine":
+        q += torch.rand(q.shape, generator=gen(3))
+    else:
+        q[n - 1, 39] += 1.0 / 3.0
+    r = binding.logprob(q.cuda(), table.cuda(), targets.cuda(), scale=scale, top=9)
+    check_logprob(r, exact_logprob(q, table, targets, scale, None, 9), 700, 9)
 
 
 @pytest.mark.parametrize("tt", [F32, BF16])
