@@ -432,30 +432,30 @@ struct DotLoad {                    // values per lane and step (eight bytes: si
     static constexpr int CH = sizeof(S) == 1 ? 8 : 16 / sizeof(S);
 };
 
-// <q, t> in float64 for four rows at once by `lanes` lanes (1 to 16), whose own place is `sub`; the order of a
+// <q, t> in float64 for U rows at once by `lanes` lanes (1 to 16), whose own place is `sub`; the order of a
 // sum depends on d alone, so equal rows get equal values
-template <class S, class Q, bool VEC>
-static __device__ __forceinline__ void dot_exact(const S *const (&t)[4], const Q *q, int d, int sub, int lanes, double (&x)[4])
+template <class S, class Q, bool VEC, int U>
+static __device__ __forceinline__ void dot_exact(const S *const (&t)[U], const Q *q, int d, int sub, int lanes, double (&x)[U])
 {
     constexpr int CH = DotLoad<S>::CH;
 #pragma unroll
-    for (int u = 0; u < 4; u++) x[u] = 0.0;
+    for (int u = 0; u < U; u++) x[u] = 0.0;
 #pragma unroll 1
     for (int k = sub * CH; k < d; k += lanes * CH) {
-        FewFrag<S, CH> f[4];
+        FewFrag<S, CH> f[U];
 #pragma unroll
-        for (int u = 0; u < 4; u++) f[u] = few_load<S, CH, VEC>(t[u], k, d);
+        for (int u = 0; u < U; u++) f[u] = few_load<S, CH, VEC>(t[u], k, d);
         const FewFrag<Q, CH> g = few_load<Q, CH, VEC>(q, k, d);
 #pragma unroll
         for (int e = 0; e < CH; e++) {
             const double y = (double)(float)g.e[e];
 #pragma unroll
-            for (int u = 0; u < 4; u++) x[u] = fma((double)(float)f[u].e[e], y, x[u]);
+            for (int u = 0; u < U; u++) x[u] = fma((double)(float)f[u].e[e], y, x[u]);
         }
     }
     for (int s = lanes >> 1; s > 0; s >>= 1)
 #pragma unroll
-        for (int u = 0; u < 4; u++) x[u] += __shfl_xor(x[u], s);
+        for (int u = 0; u < U; u++) x[u] += __shfl_xor(x[u], s);
 }
 
 // scores the rows of the `cnt` entries in sh.take and merges those of at least `floor` into sh.best
@@ -473,13 +473,14 @@ static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishS
     if (tid == 0) sh.count = old;
     team_sync<NT>();
     const int items = cnt * kind;
+    constexpr int U = sizeof(S) == 1 && NT == 64 ? 8 : 4;             // (a workgroup of 16 waves has half a wave's registers each)
 #pragma unroll 1
-    for (int i0 = wave * 4 * rows; i0 < items; i0 += NT / 16 * rows) {        // four times 64 / lanes rows per wave
-        const S *t[4];
-        int64_t v[4];
-        double x[4];
+    for (int i0 = wave * U * rows; i0 < items; i0 += NT / 64 * U * rows) {    // U times 64 / lanes rows per wave
+        const S *t[U];
+        int64_t v[U];
+        double x[U];
 #pragma unroll
-        for (int u = 0; u < 4; u++) {
+        for (int u = 0; u < U; u++) {
             const int i = i0 + u * rows + at, ic = i < items ? i : items - 1;
             v[u] = entry_row(sh.take[ic / kind], ic % kind, kind);
             const bool in = i < items && v[u] < a.st.V && (!a.st.live || ((a.st.live[row * a.st.ld_live + (v[u] >> 5)] >> (v[u] & 31)) & 1u));
@@ -489,7 +490,7 @@ static __device__ __forceinline__ void finish_batch(const FinishArgs &a, FinishS
         if (a.vec) dot_exact<S, Q, true>(t, q, a.d, sub, lanes, x);
         else dot_exact<S, Q, false>(t, q, a.d, sub, lanes, x);
 #pragma unroll
-        for (int u = 0; u < 4; u++)
+        for (int u = 0; u < U; u++)
             if (sub == 0 && v[u] >= 0 && x[u] >= floor) {             // (not a NaN either)
                 const int slot = atomicAdd(&sh.count, 1);
                 sh.val[slot] = x[u];
@@ -611,54 +612,68 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
     const auto group_at = [&](int i) {
         return a.st.wide ? wmax + i : a.st.gmax + ((((int64_t)(i >> 2) * a.st.n + row) << 2) + (i & 3)) * 2;
     };
-    // All of them, up to 32 values at a time, by a body that is straight-line code to begin with (a load whose use is
-    // behind a branch is moved there, and loads then wait for one another).
-    const auto each_group = [&](const auto &body) {
-        if (a.st.wide) {
-            const int fours = (ngroups + 3) / 4;
-            for (int i0 = tid; i0 < fours; i0 += 8 * NT) {
-                v4f x[8];
+    // A thread's groups are four sets; of each it keeps the largest value, where that is, and the second largest.
+    // (loads first, then straight-line code: a load whose use is behind a branch is moved there, and loads then wait
+    // for one another)
+    float most[4] = {HIDDEN, HIDDEN, HIDDEN, HIDDEN}, second[4] = {HIDDEN, HIDDEN, HIDDEN, HIDDEN};
+    int where[4] = {0, 0, 0, 0};
+    const auto keep = [&](int set, float x, int i) {
+        second[set] = __builtin_amdgcn_fmed3f(most[set], second[set], x);
+        where[set] = x > most[set] ? i : where[set];
+        most[set] = fmaxf(most[set], x);
+    };
+    // place k of set u of this thread
+    const auto group_of = [&](int u, int k) { return a.st.wide ? 4 * (tid + k * NT) + u : tid + (u + 4 * k) * NT; };
+    if (a.st.wide) {
+        const int fours = (ngroups + 3) / 4;
+        for (int k = 0; tid + k * NT < fours; k += 8) {
+            v4f x[8];
 #pragma unroll
-                for (int u = 0; u < 8; u++) x[u] = *(const v4f *)(wmax + 4 * min(i0 + u * NT, fours - 1));
-                float y[32];
+            for (int u = 0; u < 8; u++) x[u] = *(const v4f *)(wmax + 4 * min(tid + (k + u) * NT, fours - 1));
 #pragma unroll
-                for (int u = 0; u < 32; u++) y[u] = 4 * (i0 + (u >> 2) * NT) + (u & 3) < ngroups ? x[u >> 2][u & 3] : HIDDEN;
-                body(y, [&](int u) { return 4 * (i0 + (u >> 2) * NT) + (u & 3); });
-            }
-        } else {
-            for (int i0 = tid; i0 < ngroups; i0 += 16 * NT) {
-                float y[32];
+            for (int u = 0; u < 8; u++)
 #pragma unroll
-                for (int u = 0; u < 16; u++) y[u] = *group_at(min(i0 + u * NT, ngroups - 1));
+                for (int e = 0; e < 4; e++) keep(e, group_of(e, k + u) < ngroups ? x[u][e] : HIDDEN, group_of(e, k + u));
+        }
+    } else {
+        for (int k = 0; tid + 4 * k * NT < ngroups; k += 4) {
+            float x[16];
 #pragma unroll
-                for (int u = 0; u < 16; u++) y[u] = i0 + u * NT < ngroups ? y[u] : HIDDEN;
+            for (int u = 0; u < 16; u++) x[u] = *group_at(min(group_of(u & 3, k + (u >> 2)), ngroups - 1));
 #pragma unroll
-                for (int u = 16; u < 32; u++) y[u] = HIDDEN;
-                body(y, [&](int u) { return i0 + u * NT; });
+            for (int u = 0; u < 16; u++) {
+                const int i = group_of(u & 3, k + (u >> 2));
+                keep(u & 3, i < ngroups ? x[u] : HIDDEN, i);
             }
         }
-    };
-    float most[4] = {HIDDEN, HIDDEN, HIDDEN, HIDDEN};
-    each_group([&](const float (&y)[32], const auto &) {
-#pragma unroll
-        for (int u = 0; u < 32; u++) most[u & 3] = fmaxf(most[u & 3], y[u]);
-    });
+    }
     if (!empty && eps < 1e38f) {                                      // (the same in every thread)
         const float thr = kth_set_max<NT>(sh, most, a.top, tid) - 2.0f * eps;
         // exact products of the K best are at least this
         const double floor = (double)thr + (double)eps * 0.999;
-        const float mine = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-        if (mine >= thr && mine > HIDDEN)
-            each_group([&](const float (&y)[32], const auto &index) {
+        const auto note = [&](int i) {
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < FinishShared<NT>::ITEMS) sh.id[at] = (uint32_t)i;
+        };
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            if (!(most[u] >= thr && most[u] > HIDDEN)) continue;
+            note(where[u]);
+            if (!(second[u] >= thr && second[u] > HIDDEN)) continue;
+            // (seldom: two of a set)
+            for (int k = 0; group_of(u, k) < ngroups; k += 8) {
+                float x[8];
+#pragma unroll
+                for (int w = 0; w < 8; w++) x[w] = *group_at(min(group_of(u, k + w), ngroups - 1));
                 uint32_t hits = 0;
 #pragma unroll
-                for (int u = 0; u < 32; u++) hits |= y[u] >= thr && y[u] > HIDDEN ? 1u << u : 0u;
-                while (hits) {
-                    const int i = index(__ffs(hits) - 1), at = atomicAdd(&sh.count, 1);
-                    hits &= hits - 1;
-                    if (at < FinishShared<NT>::ITEMS) sh.id[at] = (uint32_t)i;
+                for (int w = 0; w < 8; w++) {
+                    const int i = group_of(u, k + w);
+                    hits |= i < ngroups && i != where[u] && x[w] >= thr && x[w] > HIDDEN ? 1u << w : 0u;
                 }
-            });
+                for (; hits; hits &= hits - 1) note(group_of(u, k + __ffs(hits) - 1));
+            }
+        }
         team_sync<NT>();
         const int groups = sh.count;
         team_sync<NT>();
@@ -715,8 +730,8 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
 // ---- gradient of the logits --------------------------------------------------------------------------
 
 struct GradArgs {
-    int64_t n, V, v0;               // the product's columns are rows v0 .. V - 1 of the table
-    int64_t vc, npad;               // columns of g, of gt
+    int n, V, v0;                   // the product's columns are rows v0 .. V - 1 of the table
+    int vc, npad;                   // columns of g, of gt
     float scale;
     const uint32_t *live;
     int64_t ld_live;
@@ -728,8 +743,10 @@ struct GradArgs {
 
 // G = scale (dlogp (1[v = t] - p) - dentropy p (log p + H)) in registers, rounded to bf16 once (bf16
 // rows: half a step of 2^-9 beside the operands' own) or kept in three pieces (fp32), written for the
-// products with the table (rows of queries) and with the queries (rows of the table).
-template <int NP>
+// products with the table (rows of queries) and with the queries (rows of the table).  Both sum over what
+// they have in common with the operand beside them, so their columns lie in the order that a wave holds
+// them in (ORDER_TABLE, ORDER_QUERIES): a lane's values are 32 or 8 bytes in a row, the lanes of a row 128.
+template <int NP, bool ENT>
 struct GradEpi {
     GradArgs a;
     template <class T>
@@ -742,68 +759,102 @@ struct GradEpi {
     {
 #pragma unroll
         for (int j = 0; j < T::QT; j++) {
-            const int64_t q = q0 + 16 * j + (lane & 15);
+            const int q = (int)q0 + 16 * j + (lane & 15);
             const bool in = q < a.n;
-            const int64_t row = in ? q : a.n - 1, t = a.targets[row];
+            const int row = in ? q : a.n - 1;
+            const int64_t t = a.targets[row];
             const bool seen = t >= 0 && t < a.V && (!a.live || ((a.live[row * a.ld_live + (t >> 5)] >> (t & 31)) & 1u));
             st.da[j] = in && seen ? a.dlogp[row] * a.scale : 0.0f;
-            st.db[j] = in && a.dentropy ? a.dentropy[row] * a.scale : 0.0f;
-            st.H[j] = st.db[j] != 0.0f ? a.entropy[row] : 0.0f;
+            st.db[j] = ENT && in ? a.dentropy[row] * a.scale : 0.0f;
+            st.H[j] = ENT && st.db[j] != 0.0f ? a.entropy[row] : 0.0f;
             st.lse[j] = a.lse[row];
-            st.target[j] = seen ? (int32_t)(t - a.v0) : -0x7FFFFFFF;
+            st.target[j] = in && seen ? (int32_t)(t - a.v0) : -0x7FFFFFFF;
         }
     }
     template <class T>
     __device__ __forceinline__ void end(State<T> &, int, int, int64_t, int) const {}
     template <class T>
-    __device__ __forceinline__ void tile(State<T> &st, RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
+    __device__ __forceinline__ void tile(State<T> &st, RowAcc<T> &acc, int64_t p0l, int64_t q0l, int lane, int) const
     {
-        if (p0 >= a.vc) return;
-        const int h = lane >> 4;
+        static_assert(T::QT == 4 && T::PT % 4 == 0, "a wave has whole groups of 64");
+        const int p0 = (int)p0l, q0 = (int)q0l, h = lane >> 4, c = lane & 15;
+        if (p0 >= a.vc || q0 >= a.npad) return;                       // uniform
         const bool checked = a.live || a.v0 + p0 + 16 * T::PT > a.V;  // uniform: a mask, or the table's end
 #pragma unroll
-        for (int j = 0; j < T::QT; j++) {
-            const int64_t q = q0 + 16 * j + (lane & 15);
-            if (q >= a.npad) continue;
-            const bool in = q < a.n;
-            const float da = st.da[j], db = st.db[j], H = st.H[j], lse = st.lse[j];
-            const bool dead = da == 0.0f && db == 0.0f;
+        for (int b = 0; b < T::PT / 4; b++) {                         // 64 rows of the table
+            if (p0 + 64 * b >= a.vc) break;
 #pragma unroll
-            for (int i = 0; i < T::PT; i++) {
-                const int64_t p = p0 + 16 * i + 4 * h, v = a.v0 + p;
-                if (p >= a.vc) continue;
-                uint32_t bits = dead ? 0u : 0xFu;
-                if (checked && !dead) {
-                    bits = 0;
-                    if (v < a.V) {
-                        bits = a.live ? a.live[(in ? q : 0) * a.ld_live + (v >> 5)] >> (v & 31) : 0xFu;
-                        const int64_t left = a.V - v;
-                        bits &= left >= 4 ? 0xFu : (1u << left) - 1u;
+            for (int j = 0; j < 4; j++) {
+                const int q = q0 + 16 * j + c;
+                const bool in = q < a.n;
+                const float da = st.da[j], db = st.db[j], lse = st.lse[j];
+                const bool dead = da == 0.0f && db == 0.0f;
+                const uint32_t dp = (uint32_t)(st.target[j] - p0 - 64 * b);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    v4f &x = acc.v[4 * b + i][j];
+                    const v4f z = x;
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        // (log p in natural units: scale times the product is exact inside the sum, which log2(e) is not)
+                        const float lp = fmaf(z[r], a.scale, -lse), pr = exp2_fast(lp * LOG2E);
+                        float g = -da * pr;
+                        if constexpr (ENT) g -= db * pr * (fmaxf(lp, -1e4f) + st.H[j]);
+                        x[r] = g;
                     }
-                }
-                __bf16 o[NP][4];
+                    if (__any(dp >= (uint32_t)(16 * i) && dp < (uint32_t)(16 * i + 16))) {   // (seldom)
+                        uint32_t at = dp - 16 * i - 4 * h;
+                        asm volatile("" : "+v"(at));
 #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    // (log p in natural units: scale times the product is exact inside the sum, which log2(e) is not)
-                    const float x = fmaf(acc.v[i][j][r], a.scale, -lse), pr = exp2_fast(x * LOG2E);
-                    const float one = (int)p + r == st.target[j] ? 1.0f : 0.0f;
-                    float g = da * (one - pr);
-                    if (a.dentropy) g -= db * pr * (fmaxf(x, -1e4f) + H);
-                    g = (bits >> r) & 1u ? g : 0.0f;
-                    o[0][r] = (__bf16)g;
-                    if constexpr (NP == 3) {
-                        const float g1 = g - (float)o[0][r];
-                        o[1][r] = (__bf16)g1;
-                        o[2][r] = (__bf16)(g1 - (float)o[1][r]);
+                        for (int r = 0; r < 4; r++)
+                            if (at == (uint32_t)r) {
+                                const float lp = fmaf(z[r], a.scale, -lse), pr = exp2_fast(lp * LOG2E);
+                                float g = da * (1.0f - pr);
+                                if constexpr (ENT) g -= db * pr * (fmaxf(lp, -1e4f) + st.H[j]);
+                                x[r] = g;
+                            }
                     }
-                }
+                    uint32_t bits = dead ? 0u : 0xFu;
+                    if (checked) {
+                        const int v = a.v0 + p0 + 64 * b + 16 * i + 4 * h, left = a.V - v;
+                        if (left < 4) bits &= left <= 0 ? 0u : (1u << left) - 1u;
+                        if (a.live && left > 0) bits &= a.live[(in ? q : 0) * a.ld_live + (v >> 5)] >> (v & 31);
+                    }
 #pragma unroll
-                for (int u = 0; u < NP; u++) {
-                    if (a.g && in) *(v4bf *)(a.g + u * a.gpiece + q * a.vc + p) = (v4bf){o[u][0], o[u][1], o[u][2], o[u][3]};
-                    if (a.gt)
-#pragma unroll
-                        for (int r = 0; r < 4; r++) a.gt[u * a.gtpiece + (p + r) * a.npad + q] = o[u][r];
+                    for (int r = 0; r < 4; r++) x[r] = (bits >> r) & 1u ? x[r] : 0.0f;
                 }
+            }
+            // pieces, one after the other: rounded off what is left
+#pragma unroll
+            for (int u = 0; u < NP; u++) {
+                v4bf o[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) {
+                            o[i][j][r] = (__bf16)acc.v[4 * b + i][j][r];
+                            if (u + 1 < NP) acc.v[4 * b + i][j][r] -= (float)o[i][j][r];
+                        }
+                if (a.g)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const int q = q0 + 16 * j + c;
+                        __bf16 *to = a.g + u * a.gpiece + (int64_t)q * a.vc + p0 + 64 * b + 16 * h;
+                        if (q < a.n) {
+                            *(v8bf *)to = __builtin_shufflevector(o[0][j], o[1][j], 0, 1, 2, 3, 4, 5, 6, 7);
+                            *(v8bf *)(to + 8) = __builtin_shufflevector(o[2][j], o[3][j], 0, 1, 2, 3, 4, 5, 6, 7);
+                        }
+                    }
+                if (a.gt)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+#pragma unroll
+                        for (int r = 0; r < 4; r++) {
+                            __bf16 *to = a.gt + u * a.gtpiece + (int64_t)(p0 + 64 * b + 16 * i + 4 * h + r) * a.npad + q0 + 4 * c;
+                            *(v4bf *)to = (v4bf){o[i][0][r], o[i][1][r], o[i][2][r], o[i][3][r]};
+                        }
             }
         }
     }
@@ -826,17 +877,22 @@ __global__ __launch_bounds__(WG) void active_rows_kernel(int64_t n, int64_t V, c
     if ((lane & 31) == 0 && i < n) out[i >> 5] = (uint32_t)(b >> lane);
 }
 
-// sums of the splits, in their order
-__global__ __launch_bounds__(WG) void join_splits_kernel(const float *__restrict__ part, int splits, int64_t n, int64_t cols, void *__restrict__ out,
-                                                         int64_t ld, int bf16_out)
+// sums of the splits, in their order; rows of dpad values, a multiple of four
+__global__ __launch_bounds__(WG) void join_splits_kernel(const float *__restrict__ part, int splits, int64_t n, int cols, int dpad,
+                                                         void *__restrict__ out, int64_t ld, int bf16_out)
 {
-    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x, total = n * cols;
-    if (t >= total) return;
-    float x = 0.0f;
-    for (int s = 0; s < splits; s++) x += part[s * total + t];
-    const int64_t r = t / cols, o = r * ld + (t - r * cols);
-    if (bf16_out) ((__bf16 *)out)[o] = (__bf16)x;
-    else ((float *)out)[o] = x;
+    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x, total = n * dpad;
+    if (t * 4 >= total) return;
+    v4f x = *(const v4f *)(part + t * 4);
+    for (int s = 1; s < splits; s++) x += *(const v4f *)(part + s * total + t * 4);
+    const int64_t r = t * 4 / dpad, o = r * ld;
+    const int c = (int)(t * 4 - r * dpad);
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        if (c + e < cols) {
+            if (bf16_out) ((__bf16 *)out)[o + c + e] = (__bf16)x[e];
+            else ((float *)out)[o + c + e] = x[e];
+        }
 }
 
 __global__ __launch_bounds__(WG) void clear_rows_kernel(void *out, int64_t n, int64_t cols, int64_t ld, int width)
@@ -907,7 +963,7 @@ static int finish_launch(FinishArgs &f, hipStream_t s)
 template <bool ENT, int TOP>
 static int stats_launch(RowProd &rp, const StatsArgs &st, bool large, int prun, hipStream_t s)
 {
-    return large ? rowprod_launch<TileL>(rp, StatsEpi<ENT, TOP>{st}, s, prun) : rowprod_launch<TileM>(rp, StatsEpi<ENT, TOP>{st}, s, prun);
+    return large ? rowprod_launch<TileL>(rp, StatsEpi<ENT, TOP>{st}, s, prun) : rowprod_launch<TileW>(rp, StatsEpi<ENT, TOP>{st}, s, prun);
 }
 
 int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
@@ -918,10 +974,10 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     const int64_t fills = (blocks + 16 * 4096 - 1) / (16 * 4096);
     const int rounds = few ? (int)((blocks + fills * 4096 - 1) / (fills * 4096)) : 1;
     const bool large = rowprod_size(a.V, a.n) == 2;
-    const int64_t ptiles = large ? (a.V + TileL::BP - 1) / TileL::BP : (a.V + TileM::BP - 1) / TileM::BP;
-    const int64_t qtiles = large ? (a.n + TileL::BQ - 1) / TileL::BQ : (a.n + TileM::BQ - 1) / TileM::BQ;
-    // (a start costs a few microseconds, a tile 27 at K = 1024 and 256 x 256; one workgroup of the large tile fits
-    // a CU, two of the smaller)
+    const int64_t ptiles = large ? (a.V + TileL::BP - 1) / TileL::BP : (a.V + TileW::BP - 1) / TileW::BP;
+    const int64_t qtiles = large ? (a.n + TileL::BQ - 1) / TileL::BQ : (a.n + TileW::BQ - 1) / TileW::BQ;
+    // (a start costs a few microseconds, a tile 27 at K = 1024 and 256 x 256; one workgroup of the large tile
+    // fits a CU, two of the smaller)
     const double ksum = (double)kpad * (dtype_pieces(a.ttype) * dtype_pieces(a.qtype) == 9 ? 6 : dtype_pieces(a.qtype));
     const int prun = few ? 1 : rowprod_run(ptiles, qtiles, large ? 256 : 512, 100.0 / (ksum + 200.0), 64);
     const int nparts = (int)(few ? (blocks + rounds - 1) / rounds : (ptiles + prun - 1) / prun * 2);     // (both tiles: two waves along P)
@@ -1000,24 +1056,33 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
                                   : finish_launch<uint8_t, float>(f, s);
 }
 
-// G is made for as many of the table's rows at a time as 128 MB of it hold, half of the last-level
-// cache: it is written once and read once for each product.
-#define GRAD_CHUNK_BYTES (128ll << 20)
+// G is made for as many of the table's rows at a time as 1 GB of it hold.  (In pieces of 128 MB, which the last-level
+// cache would keep, 4,095 x 65,537 x 1024 took 2.5 ms instead of 1.9: five launches of each product that fill the card
+// less well, and partial sums read again each time.)
+#define GRAD_CHUNK_BYTES (1ll << 30)
+
+template <int NP, bool ENT>
+static int grad_launch(RowProd &rp, const GradArgs &ga, hipStream_t s)
+{
+    return rowprod_size(rp.P.rows, rp.Q.rows) == 2 ? rowprod_launch<TileL>(rp, GradEpi<NP, ENT>{ga}, s) : rowprod_launch<TileW>(rp, GradEpi<NP, ENT>{ga}, s);
+}
 
 int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
 {
     const int np = dtype_pieces(a.qtype), tp = dtype_pieces(a.ttype);
-    const int64_t kpad = pad_to(a.d, ROWPROD_K), npad = pad_to(a.n, ROWPROD_K);
+    const int64_t kpad = pad_to(a.d, ROWPROD_K), npad = pad_to(a.n, ROWPROD_K), dpad = pad_to(a.d, 4);
     const bool need_dt = a.dtable != nullptr, need_dq = a.dq != nullptr;
     int64_t vc = GRAD_CHUNK_BYTES / (2 * np * npad) / 1024 * 1024;
     vc = vc < 1024 ? 1024 : vc;
     const int64_t chunks = (a.V + vc - 1) / vc;
     vc = pad_to((a.V + chunks - 1) / chunks, ROWPROD_K);              // of about one size
-    // workgroups for the queries' product: its sum over the chunk is cut so that there are about two for every CU
-    const int64_t tiles = ((a.d + TileM::BP - 1) / TileM::BP) * ((a.n + TileM::BQ - 1) / TileM::BQ);
-    int splits = (int)(512 / tiles < 1 ? 1 : 512 / tiles);
-    const int64_t most = vc / 512 < 1 ? 1 : vc / 512;
-    if (splits > most) splits = (int)most;
+    // the queries' product: its sum over the chunk is cut so that there are workgroups for every CU, of large tiles if
+    // pieces of 2,048 rows (of the small tiles' 512) are enough for that
+    const int64_t tl = rowprod_tiles(a.d, a.n, 256), tm = rowprod_tiles(a.d, a.n, 128), ts = rowprod_tiles(a.d, a.n, 64);
+    int64_t splits = (256 + tl - 1) / tl;
+    if (splits > vc / 2048) splits = std::min((256 + tm - 1) / tm, vc / 1024);
+    if (splits * tm < 160) splits = std::min((512 + ts - 1) / ts, vc / 512);
+    if (splits < 1) splits = 1;
     Carve w(ws);
     __bf16 *qroom = w.take<__bf16>(pack_room(a.qtype, a.n, kpad));
     __bf16 *troom = w.take<__bf16>(pack_room(a.ttype, vc, kpad));
@@ -1025,7 +1090,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     __bf16 *qcols = need_dt ? w.take<__bf16>((int64_t)a.d * npad * np) : nullptr;
     __bf16 *g = need_dq ? w.take<__bf16>(a.n * vc * np) : nullptr;
     __bf16 *gt = need_dt ? w.take<__bf16>(vc * npad * np) : nullptr;
-    float *sums = need_dq ? w.take<float>((int64_t)splits * a.n * a.d) : nullptr;
+    float *sums = need_dq ? w.take<float>(splits * a.n * dpad) : nullptr;
     uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
     uint32_t *active = need_dt ? w.take<uint32_t>((a.n + 31) / 32) : nullptr;
     if (bytes) *bytes = w.used;
@@ -1040,7 +1105,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         hipLaunchKernelGGL(active_rows_kernel, dim3((unsigned)((a.n + WG - 1) / WG)), dim3(WG), 0, s, a.n, a.V, a.targets, a.live, a.ld_live,
                            a.dlogp, a.dentropy, active);
         RAIRS_HIP(hipGetLastError());
-        if ((rc = rairs_launch_pack_cols(a.q, a.qtype, a.ldq, 0, 1, a.n, a.d, active, nullptr, qcols, npad, 0, a.d * npad, s))) return rc;
+        if ((rc = rairs_launch_pack_cols(a.q, a.qtype, a.ldq, a.n, a.d, active, ORDER_QUERIES, qcols, npad, s))) return rc;
     }
     for (int64_t v0 = 0; v0 < a.V; v0 += vc) {
         const int64_t rows = a.V - v0 < vc ? a.V - v0 : vc, cpad = pad_to(rows, ROWPROD_K);
@@ -1051,26 +1116,27 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         rp.Q = Q;
         if ((rc = rairs_operand(t, a.ttype, a.ldt, rows, a.d, nullptr, troom, rp.P, s))) return rc;
         GradArgs ga = {};
-        ga.n = a.n; ga.V = a.V; ga.v0 = v0; ga.vc = cpad; ga.npad = npad;
+        ga.n = (int)a.n; ga.V = (int)a.V; ga.v0 = (int)v0; ga.vc = (int)cpad; ga.npad = (int)npad;
         ga.scale = a.scale;
         ga.live = a.live; ga.ld_live = a.ld_live; ga.targets = a.targets;
         ga.lse = a.lse_in; ga.entropy = a.entropy_in; ga.dlogp = a.dlogp; ga.dentropy = a.dentropy;
         ga.g = g; ga.gt = gt;
         ga.gpiece = a.n * cpad; ga.gtpiece = cpad * npad;
-        rc = np == 3 ? rowprod_launch_any(rp, GradEpi<3>{ga}, s) : rowprod_launch_any(rp, GradEpi<1>{ga}, s);
+        const bool ent = a.dentropy != nullptr;
+        if (np == 3) rc = ent ? grad_launch<3, true>(rp, ga, s) : grad_launch<3, false>(rp, ga, s);
+        else rc = ent ? grad_launch<1, true>(rp, ga, s) : grad_launch<1, false>(rp, ga, s);
         if (rc) return rc;
         if (need_dq) {
             // (rows that nobody sees are zero here: their G is zero, and they may hold anything)
-            if ((rc = rairs_launch_pack_cols(t, a.ttype, a.ldt, 0, 1, rows, a.d, seen_by_any ? seen_by_any + v0 / 32 : nullptr, nullptr, tcols,
-                                             cpad, 0, a.d * cpad, s)))
+            if ((rc = rairs_launch_pack_cols(t, a.ttype, a.ldt, rows, a.d, seen_by_any ? seen_by_any + v0 / 32 : nullptr, ORDER_TABLE, tcols, cpad, s)))
                 return rc;
             RowProd dp = {};
             rowprod_pieces(dp, tp, np);
             dp.P = RowOperand{tcols, cpad, a.d * cpad, a.d, nullptr, nullptr};
             dp.Q = RowOperand{g, cpad, a.n * cpad, a.n, nullptr, nullptr};
             dp.ksteps = (int)(cpad / ROWPROD_K);
-            dp.splits = splits;
-            StoreEpi e = {sums, a.d, a.n * a.d, a.d, a.n, nullptr, 0, v0 > 0};
+            dp.splits = (int)splits;
+            StoreEpi e = {sums, dpad, a.n * dpad, a.d, a.n, nullptr, 0, v0 > 0};
             if ((rc = rowprod_launch_any(dp, e, s))) return rc;
         }
         if (need_dt) {
@@ -1084,8 +1150,8 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         }
     }
     if (need_dq) {
-        hipLaunchKernelGGL(join_splits_kernel, dim3((unsigned)((a.n * a.d + WG - 1) / WG)), dim3(WG), 0, s, sums, splits, a.n, (int64_t)a.d, a.dq,
-                           a.lddq, (int)(a.qtype == RAIRS_BF16));
+        hipLaunchKernelGGL(join_splits_kernel, dim3((unsigned)((a.n * dpad / 4 + WG - 1) / WG)), dim3(WG), 0, s, sums, (int)splits, a.n, a.d,
+                           (int)dpad, a.dq, a.lddq, (int)(a.qtype == RAIRS_BF16));
         RAIRS_HIP(hipGetLastError());
     }
     return RAIRS_OK;

@@ -594,7 +594,7 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     RowProd rp = {};
     rowprod_pieces(rp, np, np);
     rp.ksteps = (int)(opad / ROWPROD_K);
-    if ((rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, 0, 1, p.d_out, p.d_in, nullptr, nullptr, wt, opad, 0, p.d_in * opad, s))) return rc;
+    if ((rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, ORDER_SAME, wt, opad, s))) return rc;
     rp.P = RowOperand{wt, opad, p.d_in * opad, p.d_in, nullptr, nullptr};
     if ((rc = rairs_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, yroom, rp.Q, s))) return rc;
     if (use) {

@@ -25,10 +25,11 @@ struct Carve {
 // not zero)
 int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *dst,
                            int64_t kpad, hipStream_t s, uint32_t *flags = nullptr, bool clear = false);
-// the same, transposed: dst[c][r] = src[perm ? perm[r] : r][c], zero for r in [rows, rpad)
-int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t src_batch, int64_t batches, int64_t rows, int64_t cols,
-                           const uint32_t *live, const int32_t *perm, __bf16 *dst, int64_t rpad, int64_t dst_batch, int64_t piece,
-                           hipStream_t s);
+// the same, transposed: dst[c][place of r] = src[r][c], zero for r in [rows, rpad) and where live says so; rows keep
+// their places (order 0), or change them among their 64 as the gradient of the logits does (rowpack.hip)
+enum { ORDER_SAME = 0, ORDER_TABLE = 1, ORDER_QUERIES = 2 };
+int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, int order, __bf16 *dst,
+                           int64_t rpad, hipStream_t s);
 
 // A matrix as an operand of rowprod: bf16 rows that lie right already are taken where they are, others
 // are packed into `room` (pack_room elements of it).  With a permutation (the product's row r is row

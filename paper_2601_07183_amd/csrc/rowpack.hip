@@ -73,29 +73,34 @@ __global__ __launch_bounds__(WG) void pack_rows_kernel(const S *__restrict__ src
     }
 }
 
-// 64 x 64 tiles turned through LDS: dst[c][r] = src[perm[r]][c], rows from `rows` to rpad zero.  A
-// batch of matrices lies on grid z.
+// 64 x 64 tiles turned through LDS: dst[c][r] = src[r][c], rows from `rows` to rpad zero.  `order`: the place of
+// a row among its 64 (the order of a sum's terms does not matter as long as both operands keep it; gradients of
+// logits are written in the orders that a wave holds them in): 0 its own; 1: row 16 i + 4 h + r at 16 h + 4 i + r;
+// 2: row 16 j + c at 4 c + j.
+static __device__ __forceinline__ int place_of(int r, int order)
+{
+    return order == 0 ? r : order == 1 ? 16 * ((r >> 2) & 3) + 4 * (r >> 4) + (r & 3) : 4 * (r & 15) + (r >> 4);
+}
+
 template <class S, int NP>
-__global__ __launch_bounds__(WG) void pack_cols_kernel(const S *__restrict__ src, int64_t ld, int64_t src_batch, int64_t rows, int64_t cols,
-                                                       const uint32_t *__restrict__ live, const int32_t *__restrict__ perm, int vec,
-                                                       __bf16 *__restrict__ dst, int64_t rpad, int64_t dst_batch, int64_t piece)
+__global__ __launch_bounds__(WG) void pack_cols_kernel(const S *__restrict__ src, int64_t ld, int64_t rows, int64_t cols,
+                                                       const uint32_t *__restrict__ live, int order, int vec,
+                                                       __bf16 *__restrict__ dst, int64_t rpad, int64_t piece)
 {
     __shared__ __bf16 tile[NP][64][72];                  // [piece][column][row], rows of 144 bytes
     const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
-    src += blockIdx.z * src_batch;
-    dst += blockIdx.z * dst_batch;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
         const int t = threadIdx.x + h * WG, r = t >> 3, i0 = (t & 7) * 8;
         float x[8];
         const bool in = r0 + r < rows && row_live(live, r0 + r);
-        if (in) load8(src + (perm ? (int64_t)perm[r0 + r] : r0 + r) * ld, c0 + i0, cols, vec, x);
+        if (in) load8(src + (r0 + r) * ld, c0 + i0, cols, vec, x);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             __bf16 pc[NP];
             split_pieces<NP>(in ? x[e] : 0.0f, pc);
 #pragma unroll
-            for (int u = 0; u < NP; u++) tile[u][i0 + e][r] = pc[u];
+            for (int u = 0; u < NP; u++) tile[u][i0 + e][place_of(r, order)] = pc[u];
         }
     }
     __syncthreads();
@@ -109,10 +114,10 @@ __global__ __launch_bounds__(WG) void pack_cols_kernel(const S *__restrict__ src
     }
 }
 
-static int is_vec(const void *p, int64_t ld, int64_t batch, int width)
+static int is_vec(const void *p, int64_t ld, int width)
 {
     const int64_t a = width == 1 ? 8 : 16;
-    return (uintptr_t)p % a == 0 && ld * width % a == 0 && batch * width % a == 0;
+    return (uintptr_t)p % a == 0 && ld * width % a == 0;
 }
 
 int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *dst,
@@ -121,7 +126,7 @@ int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows,
     if (rows == 0) return RAIRS_OK;
     const int64_t piece = rows * kpad, want = (rows * (kpad / 8) + WG - 1) / WG;
     const dim3 grid((unsigned)(want < 8192 ? want : 8192));
-    const int vec = is_vec(src, ld, 0, dtype_width(dtype));
+    const int vec = is_vec(src, ld, dtype_width(dtype));
     if (dtype == RAIRS_F32)
         hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, perm, vec, dst, kpad, piece, flags,
                            (int)clear);
@@ -135,26 +140,20 @@ int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows,
     return RAIRS_OK;
 }
 
-int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t src_batch, int64_t batches, int64_t rows, int64_t cols,
-                           const uint32_t *live, const int32_t *perm, __bf16 *dst, int64_t rpad, int64_t dst_batch, int64_t piece,
-                           hipStream_t s)
+int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, int order, __bf16 *dst,
+                           int64_t rpad, hipStream_t s)
 {
     if (cols == 0 || rpad == 0) return RAIRS_OK;
-    const int vec = is_vec(src, ld, src_batch, dtype_width(dtype));
-    for (int64_t b0 = 0; b0 < batches; b0 += 32768) {                 // (grid z ends at 65,535)
-        const int64_t nb = batches - b0 < 32768 ? batches - b0 : 32768;
-        const dim3 grid((unsigned)((rpad + 63) / 64), (unsigned)((cols + 63) / 64), (unsigned)nb);
-        if (dtype == RAIRS_F32)
-            hipLaunchKernelGGL((pack_cols_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src + b0 * src_batch, ld, src_batch, rows, cols,
-                               live, perm, vec, dst + b0 * dst_batch, rpad, dst_batch, piece);
-        else if (dtype == RAIRS_BF16)
-            hipLaunchKernelGGL((pack_cols_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src + b0 * src_batch, ld, src_batch, rows,
-                               cols, live, perm, vec, dst + b0 * dst_batch, rpad, dst_batch, piece);
-        else
-            hipLaunchKernelGGL((pack_cols_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src + b0 * src_batch, ld, src_batch, rows,
-                               cols, live, perm, vec, dst + b0 * dst_batch, rpad, dst_batch, piece);
-        RAIRS_HIP(hipGetLastError());
-    }
+    const int vec = is_vec(src, ld, dtype_width(dtype));
+    const int64_t piece = cols * rpad;
+    const dim3 grid((unsigned)((rpad + 63) / 64), (unsigned)((cols + 63) / 64));
+    if (dtype == RAIRS_F32)
+        hipLaunchKernelGGL((pack_cols_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, live, order, vec, dst, rpad, piece);
+    else if (dtype == RAIRS_BF16)
+        hipLaunchKernelGGL((pack_cols_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, live, order, vec, dst, rpad, piece);
+    else
+        hipLaunchKernelGGL((pack_cols_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, live, order, vec, dst, rpad, piece);
+    RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
 

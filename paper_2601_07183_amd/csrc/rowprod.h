@@ -7,8 +7,8 @@
 // ones first (what is left out is below 2^-23 |P||Q|).  A piece list is only a longer sum, so bf16
 // rows, fp32 rows and byte rows share one kernel.
 //
-// A workgroup stages 64 values of each of its rows in LDS, two buffers, fetched straight into LDS by
-// 16-byte loads.  Such a load writes lane l's bytes at base + 16 l, so the order in LDS is chosen by
+// A workgroup stages 64 values of each of its rows in LDS, fetched straight into LDS by 16-byte loads into a ring
+// of two buffers (large tiles, whose products take longer than a load) or four (small ones).  Such a load writes lane l's bytes at base + 16 l, so the order in LDS is chosen by
 // the address that each lane reads: slot s of row r holds the row's 16-byte chunk s ^ (r & 7), which
 // keeps a global access 128 bytes long and the operand reads (16 rows, one chunk) free of bank conflicts.
 #pragma once
@@ -68,10 +68,10 @@ static inline void rowprod_pieces(RowProd &a, int np, int nq)
         }
 }
 
-// PT x QT tiles of 16 x 16 per wave, WP x WQ waves; registers for MINW waves per SIMD.
-template <int PT_, int QT_, int WP_, int WQ_, int MINW_ = 2>
+// PT x QT tiles of 16 x 16 per wave, WP x WQ waves; a ring of ST buffers.
+template <int PT_, int QT_, int WP_, int WQ_, int ST_>
 struct RowTile {
-    static constexpr int PT = PT_, QT = QT_, WP = WP_, WQ = WQ_, NT = 64 * WP * WQ, MINW = MINW_;
+    static constexpr int PT = PT_, QT = QT_, WP = WP_, WQ = WQ_, NT = 64 * WP * WQ, ST = ST_;
     static constexpr int BP = 16 * PT * WP, BQ = 16 * QT * WQ;
     static constexpr int LP = BP * 8 / NT, LQ = BQ * 8 / NT;          // 16-byte loads per thread and step
     static constexpr int BYTES = (BP + BQ) * 128;                     // of one LDS buffer
@@ -80,16 +80,18 @@ struct RowTile {
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
-// The tile of a product: the largest that still gives every CU a workgroup.  Large tiles need less of
-// the caches per product (256 x 256: a step's 64 KB for 2,048 cycles of products, 128 x 128: 32 KB for 512).
-typedef RowTile<8, 4, 2, 4> TileL;  // 256 x 256
-typedef RowTile<4, 4, 2, 2> TileM;  // 128 x 128
-typedef RowTile<2, 2, 2, 2> TileS;  // 64 x 64
-static inline int rowprod_size(int64_t p, int64_t q)
+// The tile of a product.  Large tiles need less of the caches per product (256 x 256: a step's 64 KB for 2,048
+// cycles of products, 128 x 128: 32 KB for 512), small ones give more workgroups.  Measured (us, 256 / 128 / 64):
+// 4096 x 8191 x 4096 251 / 339 / 600; 1024 x 4096 x 13120 270 / 126 / 239; 1024 x 2999 x 960 of fp32 130 / 55 / 77; 128 x
+// 10,000 x 1024 of fp32 125 / 55 / 46; 1024 x 512 x 1024 30 / 14 / 9.
+typedef RowTile<8, 4, 2, 4, 2> TileL;       // 256 x 256, 8 waves
+typedef RowTile<4, 2, 2, 4, 3> TileM;       // 128 x 128, 8 waves
+typedef RowTile<2, 2, 2, 2, 4> TileS;       // 64 x 64, 4 waves
+typedef RowTile<4, 4, 2, 2, 2> TileW;       // 128 x 128, 4 waves: 64 x 64 to a wave, for epilogues that want that
+static inline int64_t rowprod_tiles(int64_t p, int64_t q, int side) { return ((p + side - 1) / side) * ((q + side - 1) / side); }
+static inline int rowprod_size(int64_t p, int64_t q, int splits = 1)
 {
-    if (((p + 255) / 256) * ((q + 255) / 256) >= 200) return 2;
-    if (((p + 127) / 128) * ((q + 127) / 128) >= 200) return 1;
-    return 0;
+    return rowprod_tiles(p, q, 256) * splits >= 200 ? 2 : rowprod_tiles(p, q, 128) * splits >= 160 ? 1 : 0;
 }
 
 template <class T>
@@ -112,11 +114,12 @@ static __device__ __forceinline__ void rowprod_fetch(char *buf, const char *pb, 
                                          0);
 }
 
-// every load into LDS of this wave has landed, then every wave's
+// All but the last N loads into LDS of this wave have landed, then every wave's; and every wave has read what it
+// reads.  (The compiler's own barrier would wait for all of the loads.)
+template <int N>
 static __device__ __forceinline__ void rowprod_landed()
 {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 // One step's products.  The operand that more products follow each other with stays: the longer side's tiles
@@ -186,7 +189,7 @@ static __device__ __forceinline__ void rowprod_rows(int64_t r0, int64_t rows, in
 // q0, lane): lane l holds, for its tiles (i, j), rows q0 + 16 j + (l & 15) and columns p0 + 16 i +
 // 4 (l >> 4) + 0..3.
 template <class T, class Epi, bool ADAPT>
-__global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi epi)
+__global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
 {
     extern __shared__ __align__(16) char rowprod_lds[];
     int run, qt, split;
@@ -196,11 +199,13 @@ __global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi 
     const int t0 = run * a.prun, t1 = min(t0 + a.prun, a.ptiles);
     const int64_t q0 = (int64_t)qt * T::BQ, qw = q0 + wq * (16 * T::QT);
 
+    // what is fetched, a step at a time, ahead of what is multiplied: the run's tiles one after the other, then (the run is
+    // one tile) the adapters of the tile's rows
     uint32_t po[T::LP], qo[T::LQ];
     rowprod_rows<T>((int64_t)t0 * T::BP, a.P.rows, a.P.ld, tid, po);
     const char *pb = (const char *)(a.P.p + (int64_t)t0 * T::BP * a.P.ld), *qb = (const char *)a.Q.p;
+    const uint32_t chunk = ((tid & 7) ^ ((tid >> 3) & 7)) * 16;
     if (a.Q.perm) {
-        const uint32_t chunk = ((tid & 7) ^ ((tid >> 3) & 7)) * 16;
 #pragma unroll
         for (int i = 0; i < T::LQ; i++) {
             const int64_t r = q0 + i * (T::NT / 8) + (tid >> 3);
@@ -226,69 +231,100 @@ __global__ __launch_bounds__(T::NT, T::MINW) void rowprod_kernel(RowProd a, Epi 
     }
     const int steps = nseg * a.ksteps;
     const int s0 = (int)((int64_t)steps * split / a.splits), s1 = (int)((int64_t)steps * (split + 1) / a.splits);
-    char *b0 = rowprod_lds, *b1 = rowprod_lds + T::BYTES;
-    int seg = s0 / a.ksteps, k = s0 % a.ksteps;
-    auto fetch = [&](char *buf) {
-        const int64_t ps = (sp >> (4 * seg)) & 15, qs = (sq >> (4 * seg)) & 15;
-        rowprod_fetch<T>(buf, pb + (ps * a.P.piece + k * ROWPROD_K) * 2, po, qb + (qs * a.Q.piece + k * ROWPROD_K) * 2, qo, wave);
+    const int seg0 = s0 / a.ksteps, k0 = s0 % a.ksteps;
+
+    int f_tile = t0, f_step = s0, seg = seg0, k = k0;                 // the next step to fetch
+    // of the adapters: the one being fetched, its next values, where its rows end; -1: none left
+    int f_ad = -1, f_k = 0;
+    int64_t f_end = q0;
+    int32_t own[ADAPT ? T::LQ : 1];                                   // adapters of this thread's rows
+    const int64_t qend = q0 + T::BQ < a.Q.rows ? q0 + T::BQ : a.Q.rows;
+    if constexpr (ADAPT) {
+#pragma unroll
+        for (int i = 0; i < T::LQ; i++) {
+            const int64_t r = q0 + i * (T::NT / 8) + (tid >> 3);
+            own[i] = a.ad.of_row[r < a.Q.rows ? r : a.Q.rows - 1];
+        }
+        f_ad = a.ad.of_row[q0];                                       // (rows without an adapter are the last)
+        f_end = f_ad >= 0 ? a.ad.end[f_ad] : qend;
+    }
+    char *f_buf = rowprod_lds;
+    int fetched = 0, total = 0x7FFFFFFF;                              // steps so far; all there are, once that is known
+    // (when nothing is left the last step's addresses are read again: a wave always has as many loads on the way as the
+    // wait counts)
+    auto fetch = [&]() {
+        bool base = true;
+        if constexpr (ADAPT) base = f_tile < t1;
+        if (base) {
+            const int64_t ps = (sp >> (4 * seg)) & 15, qs = (sq >> (4 * seg)) & 15;
+            rowprod_fetch<T>(f_buf, pb + (ps * a.P.piece + k * ROWPROD_K) * 2, po, qb + (qs * a.Q.piece + k * ROWPROD_K) * 2, qo, wave);
+            if (f_tile < t1) {
+                fetched++;
+                if (++f_step < s1) {
+                    if (++k == a.ksteps) { k = 0; seg++; }
+                } else {
+                    f_tile++;
+                    if (f_tile < t1) {
+                        f_step = s0; seg = seg0; k = k0;
+                        pb += (int64_t)T::BP * a.P.ld * 2;
+                        if (f_tile + 1 == a.ptiles) rowprod_rows<T>((int64_t)f_tile * T::BP, a.P.rows, a.P.ld, tid, po);
+                    } else if (!ADAPT || f_ad < 0) {
+                        total = fetched;
+                    }
+                }
+            }
+        } else if constexpr (ADAPT) {
+            const int64_t p0 = (int64_t)t0 * T::BP;
+            const int ad = f_ad < 0 ? 0 : f_ad;
+            uint32_t ao[T::LP], uo[T::LQ];
+            rowprod_rows<T>(p0, a.P.rows, a.ad.kpad, tid, ao);
+            rowprod_rows<T>(q0, a.Q.rows, a.ad.kpad, tid, uo);
+            const char *bb = (const char *)(a.ad.b + ((int64_t)ad * a.P.rows + p0) * a.ad.kpad + f_k), *ub = (const char *)(a.ad.u + q0 * a.ad.kpad + f_k);
+#pragma unroll
+            for (int i = 0; i < T::LP; i++)
+                __builtin_amdgcn_global_load_lds((global_void *)(bb + ao[i]), (lds_void *)(f_buf + (i * T::NT + wave * 64) * 16), 16, 0, 0);
+#pragma unroll
+            for (int i = 0; i < T::LQ; i++) {
+                const char *src = own[i] == ad ? ub + uo[i] : (const char *)a.ad.zero;
+                __builtin_amdgcn_global_load_lds((global_void *)src, (lds_void *)(f_buf + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
+            }
+            if (f_ad >= 0) {
+                fetched++;
+                f_k += ROWPROD_K;
+                if (f_k == a.ad.kpad) {
+                    f_k = 0;
+                    f_ad = f_end < qend ? a.ad.of_row[f_end] : -1;
+                    if (f_ad >= 0) f_end = a.ad.end[f_ad];
+                    else total = fetched;
+                }
+            }
+        }
+        f_buf = f_buf == rowprod_lds + (T::ST - 1) * T::BYTES ? rowprod_lds : f_buf + T::BYTES;
     };
-    fetch(b0);
+    for (int i = 0; i < T::ST - 1; i++) fetch();
     typename Epi::template State<T> state;
     epi.begin(state, qw, lane);
-    rowprod_landed();
+    const char *buf = rowprod_lds;
+    int done = 0;
     for (int t = t0; t < t1; t++) {
         RowAcc<T> acc;
 #pragma unroll
         for (int i = 0; i < T::PT; i++)
 #pragma unroll
             for (int j = 0; j < T::QT; j++) acc.v[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = s0; s < s1; s++) {
-            bool more = true;                                         // uniform, as all of this
-            if (s + 1 < s1) {
-                if (++k == a.ksteps) { k = 0; seg++; }
-            } else {
-                seg = s0 / a.ksteps;
-                k = s0 % a.ksteps;
-                more = t + 1 < t1;
-                pb += (int64_t)T::BP * a.P.ld * 2;
-                if (more && t + 2 == a.ptiles) rowprod_rows<T>((int64_t)(t + 1) * T::BP, a.P.rows, a.P.ld, tid, po);
-            }
-            rowprod_step<T>(b0, wp, wq, lane, acc, [&]() {
-                if (more) fetch(b1);
-            });
-            if (s + 1 < s1) rowprod_landed();
-            char *x = b0; b0 = b1; b1 = x;
+        // (a run of several tiles: a tile's steps; else all that is fetched)
+        const int stop = done + (s1 - s0);
+        while (ADAPT ? done < total : done < stop) {
+            // (this also says that every wave is past the step before, whose buffer the next fetch writes)
+            rowprod_landed<(T::ST - 2) * (T::LP + T::LQ)>();
+            rowprod_step<T>(buf, wp, wq, lane, acc, fetch);
+            buf = buf == rowprod_lds + (T::ST - 1) * T::BYTES ? rowprod_lds : buf + T::BYTES;
+            done++;
         }
-        const int64_t p0 = (int64_t)t * T::BP;
-        if constexpr (ADAPT) {                                        // (a run is one tile)
-            const int64_t qend = q0 + T::BQ < a.Q.rows ? q0 + T::BQ : a.Q.rows;
-            for (int64_t pos = q0; pos < qend;) {
-                const int ad = a.ad.of_row[pos];
-                if (ad < 0) break;                                    // rows without an adapter are the last
-                pos = a.ad.end[ad];
-                rowprod_rows<T>(p0, a.P.rows, a.ad.kpad, tid, po);
-                rowprod_rows<T>(q0, a.Q.rows, a.ad.kpad, tid, qo);
-                const char *bb = (const char *)(a.ad.b + ((int64_t)ad * a.P.rows + p0) * a.ad.kpad), *ub = (const char *)(a.ad.u + q0 * a.ad.kpad);
-                for (int kk = 0; kk < a.ad.kpad; kk += ROWPROD_K) {
-                    rowprod_landed();                                 // (the buffer is free: every wave is past the last step)
-#pragma unroll
-                    for (int i = 0; i < T::LP; i++)
-                        __builtin_amdgcn_global_load_lds((global_void *)(bb + po[i] + kk * 2), (lds_void *)(b0 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < T::LQ; i++) {
-                        const int64_t r = q0 + i * (T::NT / 8) + (tid >> 3);
-                        const char *src = a.ad.of_row[r < a.Q.rows ? r : a.Q.rows - 1] == ad ? ub + qo[i] : (const char *)a.ad.zero;
-                        __builtin_amdgcn_global_load_lds((global_void *)(src + kk * 2), (lds_void *)(b0 + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
-                    }
-                    rowprod_landed();
-                    rowprod_step<T>(b0, wp, wq, lane, acc, []() {});
-                }
-            }
-        }
-        epi.tile(state, acc, p0 + wp * (16 * T::PT), qw, lane, split);
-        rowprod_landed();
+        epi.tile(state, acc, (int64_t)t * T::BP + wp * (16 * T::PT), qw, lane, split);
     }
     epi.end(state, run, wp, qw, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // (LDS is given away when the workgroup ends)
 }
 
 // p tiles that a workgroup takes one after the other, at most `most`: what the last round of workgroups leaves
@@ -315,8 +351,8 @@ static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 
     a.pruns = (a.ptiles + prun - 1) / prun;
     if (a.splits < 1) a.splits = 1;
     auto kern = rowprod_kernel<T, Epi, ADAPT>;
-    RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * T::BYTES));
-    hipLaunchKernelGGL(kern, dim3(rowprod_grid(a)), dim3(T::NT), 2 * T::BYTES, s, a, epi);
+    RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, T::ST * T::BYTES));
+    hipLaunchKernelGGL(kern, dim3(rowprod_grid(a)), dim3(T::NT), T::ST * T::BYTES, s, a, epi);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
@@ -325,7 +361,7 @@ static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 
 template <bool ADAPT = false, class Epi>
 static int rowprod_launch_any(RowProd &a, const Epi &epi, hipStream_t s)
 {
-    const int size = rowprod_size(a.P.rows, a.Q.rows * (a.splits > 1 ? a.splits : 1));
+    const int size = rowprod_size(a.P.rows, a.Q.rows, a.splits > 1 ? a.splits : 1);
     return size == 2 ? rowprod_launch<TileL, ADAPT>(a, epi, s) : size == 1 ? rowprod_launch<TileM, ADAPT>(a, epi, s) : rowprod_launch<TileS, ADAPT>(a, epi, s);
 }
 
