@@ -1,19 +1,20 @@
 // A shared projection with low-rank adapters of many tenants in one batch: y = W x + s_a B_a (A_a x).
 //
 // Rows are put in order of their adapter (a counting sort on the device; nothing is read back), so
-// that an adapter's rows lie together: u = s_a A_a x is then one small product per run of up to 16
+// that an adapter's rows lie together: u = s_a A_a x is then one small product per run of up to 32
 // rows, and in the large product a tile adds the terms of the few adapters that its rows have, as
-// further steps of the same sum in the same registers.  u enters that product as bf16 pieces (two or
-// three, 16 or 24 bits), so it is as exact as the result's type can show.
+// further steps of the same sum in the same registers.  u enters that product as three bf16 pieces.
 //
-// Up to 64 rows are bound by reading W once: no sort, the rows of W go straight into registers.
+// Products with fewer than 160 tiles of 128 x 128 go another way: the rows of W and x straight from memory
+// into the matrix instruction's registers, and an adapter's B times u on the vector units behind it.
+// (10,000 x 1024 to 128 in fp32, 250 adapters of rank 16: 165 us by tiles, 64 so.)
 #include "fewrows.h"
 #include "query_ops.h"
 
-#define FEW_ROWS 64
 #define SORT_ROWS 1024              // rows per workgroup of the sort
-#define UNIT_ROWS 16                // rows of one adapter that one workgroup multiplies by A
-#define CHUNK_ROWS 128              // rows of one adapter in one partial sum of its gradient
+#define UNIT_ROWS 32                // rows of one adapter that one workgroup multiplies by A
+#define CHUNK_ROWS 256              // rows of one adapter in one partial sum of its gradient
+#define FEW_ROWS 256                // up to here every row takes its own way through its adapter's A
 
 // ---- rows in order of their adapter ------------------------------------------------------------------
 
@@ -40,10 +41,24 @@ __global__ __launch_bounds__(WG) void clear_words_kernel(int32_t *p, int64_t n)
     if (i < n) p[i] = 0;
 }
 
+// lanes of the wave with the same key (below 2^bits); key < 0: none
+static __device__ __forceinline__ unsigned long long same_key(int key, int bits)
+{
+    unsigned long long m = __ballot(key >= 0);
+    for (int b = 0; b < bits; b++) {
+        const unsigned long long set = __ballot((key >> b) & 1);
+        m &= (key >> b) & 1 ? set : ~set;
+    }
+    return m;
+}
+
 __global__ __launch_bounds__(SORT_ROWS) void sort_count_kernel(SortView v)
 {
     const int64_t i = (int64_t)blockIdx.x * SORT_ROWS + threadIdx.x;
-    if (i < v.n) atomicAdd(&v.cnt[sort_key(v, i) * v.nb + blockIdx.x], 1);
+    const int key = i < v.n ? sort_key(v, i) : -1;
+    const unsigned long long m = same_key(key, 32 - __clz(v.na));
+    if (key >= 0 && (threadIdx.x & 63) == (unsigned)__ffsll((long long)m) - 1)     // one addition per key and wave
+        atomicAdd(&v.cnt[key * v.nb + blockIdx.x], (int)__popcll(m));
 }
 
 // exclusive prefix sum of n words by one workgroup of 1024; every thread takes a run of them
@@ -111,6 +126,77 @@ __global__ __launch_bounds__(SORT_ROWS) void sort_place_kernel(SortView v)
     }
 }
 
+// The whole sort by one workgroup, for a batch whose keys fit LDS: every wave counts a run of the rows, 64 at
+// a time, then places them behind the runs before it (in the batch's order, as above).
+#define SORT_ONE_ROWS 32768
+#define SORT_ONE_KEYS 1024
+__global__ __launch_bounds__(1024) void sort_one_kernel(SortView v)
+{
+    extern __shared__ int32_t sort_lds[];
+    __shared__ int32_t sums[1024];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keys = v.na + 1, bits = 32 - __clz(v.na);
+    int32_t *cnt = sort_lds;                                          // [16][keys]
+    uint16_t *key_of = (uint16_t *)(sort_lds + 16 * keys);            // [n]
+    const int n = (int)v.n, per = ((n + 15) / 16 + 63) / 64 * 64;     // rows per wave
+#pragma unroll 4
+    for (int i = tid; i < n; i += 1024) key_of[i] = (uint16_t)sort_key(v, i);
+    for (int i = tid; i < 16 * keys; i += 1024) cnt[i] = 0;
+    __syncthreads();
+    int32_t *mine = cnt + wave * keys;
+    for (int i0 = wave * per; i0 < min((wave + 1) * per, n); i0 += 64) {
+        const int key = i0 + lane < n ? key_of[i0 + lane] : -1;
+        const unsigned long long m = same_key(key, bits);
+        if (key >= 0 && lane == __ffsll((long long)m) - 1) mine[key] += __popcll(m);
+        wave_lds_sync();
+    }
+    __syncthreads();
+    // a thread per key: its rows, then exclusive sums over the keys of rows, units and chunks
+    int rows = 0;
+    if (tid < keys)
+        for (int w = 0; w < 16; w++) rows += cnt[w * keys + tid];
+    const auto scan = [&](int x) {
+        const int incl = (int)wave_incl_sum_u32((uint32_t)x);
+        __syncthreads();
+        if (lane == 63) sums[wave] = incl;
+        __syncthreads();
+        int before = 0;
+        for (int w = 0; w < wave; w++) before += sums[w];
+        return before + incl - x;
+    };
+    const int first = scan(rows), real = tid < v.na ? rows : 0;
+    const int unit0 = scan((real + UNIT_ROWS - 1) / UNIT_ROWS), chunk0 = scan((real + CHUNK_ROWS - 1) / CHUNK_ROWS);
+    if (tid < keys) {
+        v.first[tid] = first;
+        v.unit0[tid] = unit0;
+        v.chunk0[tid] = chunk0;
+        int at = first;
+        for (int w = 0; w < 16; w++) {
+            const int c = cnt[w * keys + tid];
+            cnt[w * keys + tid] = at;
+            at += c;
+        }
+        if (tid < v.na) {
+            for (int i = 0; i < rows; i += UNIT_ROWS) v.units[unit0 + i / UNIT_ROWS] = make_int4(tid, first + i, min(UNIT_ROWS, rows - i), 0);
+            for (int i = 0; i < rows; i += CHUNK_ROWS) v.chunks[chunk0 + i / CHUNK_ROWS] = make_int4(tid, first + i, min(CHUNK_ROWS, rows - i), 0);
+        }
+    }
+    if (tid == 0) v.first[v.na + 1] = n;
+    __syncthreads();
+    for (int i0 = wave * per; i0 < min((wave + 1) * per, n); i0 += 64) {
+        const int key = i0 + lane < n ? key_of[i0 + lane] : -1;
+        const unsigned long long m = same_key(key, bits);
+        const int base = key >= 0 ? mine[key] : 0;
+        wave_lds_sync();
+        if (key >= 0) {
+            const int pos = base + __popcll(m & ((1ull << lane) - 1ull));
+            v.perm[pos] = i0 + lane;
+            v.of_row[pos] = key < v.na ? key : -1;
+            if (lane == __ffsll((long long)m) - 1) mine[key] = base + __popcll(m);
+        }
+        wave_lds_sync();
+    }
+}
+
 static int64_t max_units(int64_t n, int na, int rows) { return n / rows + (na < n ? na : n) + 1; }
 
 static SortView sort_carve(Carve &w, const int32_t *adapter, int64_t n, int na)
@@ -133,6 +219,13 @@ static SortView sort_carve(Carve &w, const int32_t *adapter, int64_t n, int na)
 
 static int sort_launch(const SortView &v, hipStream_t s)
 {
+    if (v.n <= SORT_ONE_ROWS && v.na < SORT_ONE_KEYS) {
+        const size_t lds = (size_t)16 * (v.na + 1) * 4 + (size_t)(v.n + 1) / 2 * 4;
+        RAIRS_HIP(hipFuncSetAttribute((const void *)sort_one_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(1024), lds, s, v);
+        RAIRS_HIP(hipGetLastError());
+        return RAIRS_OK;
+    }
     const int64_t words = (v.na + 1) * v.nb;
     hipLaunchKernelGGL(clear_words_kernel, dim3((unsigned)((words + WG - 1) / WG)), dim3(WG), 0, s, v.cnt, words);
     hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)v.nb), dim3(SORT_ROWS), 0, s, v);
@@ -142,7 +235,7 @@ static int sort_launch(const SortView &v, hipStream_t s)
     return RAIRS_OK;
 }
 
-// ---- u = s_a A_a x for runs of up to 16 rows of one adapter -------------------------------------------
+// ---- u = s_a A_a x for runs of rows of one adapter ---------------------------------------------------
 
 // products of pieces of u and of B (or A) laid side by side: columns t r .. t r + r - 1 hold piece pu[t]
 // of u against piece pb[t]
@@ -182,7 +275,8 @@ struct ShrinkArgs {
     const int32_t *perm;
     const int4 *units;
     const int32_t *nunits;
-    float *u;                       // [n][r] in sorted order, or null
+    float *u;                       // [n][r] in sorted order, or (by_row) in the batch's, or null
+    int by_row;
     __bf16 *up;                     // [n][kpad] in sorted order, or null
     SideBySide side;
 };
@@ -191,37 +285,52 @@ struct ShrinkArgs {
 template <class S, int RT, bool VEC>
 __global__ __launch_bounds__(WG) void shrink_kernel(ShrinkArgs a)
 {
-    __shared__ float part[4][16][16 * RT + 1];           // [wave][row][rank]
+    __shared__ float part[3][UNIT_ROWS][16 * RT + 1];    // [wave][row][rank]
     if ((int)blockIdx.x >= *a.nunits) return;
     const int4 unit = a.units[blockIdx.x];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row = min(lane & 15, unit.z - 1);
-    const S *qrow[1] = {(const S *)a.x + (int64_t)a.perm[unit.y + row] * a.ldx};
+    const S *qrow[2];
     const S *prow[RT];
-    v4f acc[RT][1];
+    v4f acc[RT][2];
     float nrm[RT];
+#pragma unroll
+    for (int j = 0; j < 2; j++) qrow[j] = (const S *)a.x + (int64_t)a.perm[unit.y + min(16 * j + (lane & 15), unit.z - 1)] * a.ldx;
 #pragma unroll
     for (int i = 0; i < RT; i++) {
         const int j = min(16 * i + (lane & 15), a.r - 1);
         prow[i] = (const S *)a.a + ((int64_t)unit.x * a.r + j) * a.d;
-        acc[i][0] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+        acc[i][0] = acc[i][1] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
     }
     const int steps = (a.d + 4 * FewLoad<S>::CH - 1) / (4 * FewLoad<S>::CH);
-    few_dot<S, S, RT, 1, VEC, false>(prow, qrow, steps * wave / 4, steps * (wave + 1) / 4, a.d, lane, acc, nrm);
+    few_dot<S, S, RT, 2, VEC, false>(prow, qrow, steps * wave / 4, steps * (wave + 1) / 4, a.d, lane, acc, nrm);
+    if (wave)
 #pragma unroll
-    for (int i = 0; i < RT; i++)
+        for (int i = 0; i < RT; i++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) part[wave][lane & 15][16 * i + 4 * (lane >> 4) + e] = acc[i][0][e];
+            for (int j = 0; j < 2; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) part[wave - 1][16 * j + (lane & 15)][16 * i + 4 * (lane >> 4) + e] = acc[i][j][e];
     __syncthreads();
-    const float sc = a.scale ? a.scale[unit.x] : 1.0f;
-    for (int t = threadIdx.x; t < unit.z * a.r; t += WG) {
-        const int i = t / a.r, j = t - i * a.r;
-        const float x = ((part[0][i][j] + part[1][i][j]) + (part[2][i][j] + part[3][i][j])) * sc;
-        part[0][i][j] = x;
-        if (a.u) a.u[(int64_t)(unit.y + i) * a.r + j] = x;
+    if (wave == 0) {
+        const float sc = a.scale ? a.scale[unit.x] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < RT; i++)
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    float *p = &part[0][16 * j + (lane & 15)][16 * i + 4 * (lane >> 4) + e];
+                    constexpr int W = UNIT_ROWS * (16 * RT + 1);
+                    *p = ((acc[i][j][e] + p[0]) + (p[W] + p[2 * W])) * sc;
+                }
     }
-    if (!a.up) return;
     __syncthreads();
+    if (a.u)
+        for (int t = threadIdx.x; t < unit.z * a.r; t += WG) {
+            const int i = t / a.r, j = t - i * a.r;
+            a.u[(int64_t)(a.by_row ? a.perm[unit.y + i] : unit.y + i) * a.r + j] = part[0][i][j];
+        }
+    if (!a.up) return;
     for (int t = threadIdx.x; t < unit.z * a.side.kpad; t += WG) {
         const int i = t / a.side.kpad, k = t - i * a.side.kpad, b = k / a.r;
         __bf16 o = (__bf16)0.0f;
@@ -259,34 +368,34 @@ __global__ __launch_bounds__(WG) void pack_side_kernel(const S *__restrict__ src
 {
     if (blockIdx.x == 0)
         for (int k = threadIdx.x; k < side.kpad; k += WG) zero[k] = (__bf16)0.0f;
-    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x;
+    // a thread per eight values; the rows of a group of 64 first, so that a transposed source is read along its rows
+    const int eights = side.kpad / 8;
+    const int64_t id = (int64_t)blockIdx.x * WG + threadIdx.x, t = id / (64 * eights) * 64 + (id & 63);
     if (t >= total) return;
+    const int k0 = (int)(id / 64 % eights) * 8;
     const int64_t a = t / rows, o = t - a * rows;
     const S *p = src + a * batch + o * so;
-    __bf16 *d = dst + t * side.kpad;
-    for (int k0 = 0; k0 < side.kpad; k0 += 8) {
-        v8bf x;
+    v8bf x;
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const int k = k0 + e, b = k / side.r;
-            __bf16 v = (__bf16)0.0f;
-            if (b < side.np) {
-                __bf16 pc[3];
-                three_pieces((float)p[(k - b * side.r) * sj], pc);
-                const int w = side.pb[b];
-                v = w == 0 ? pc[0] : w == 1 ? pc[1] : pc[2];
-            }
-            x[e] = v;
+    for (int e = 0; e < 8; e++) {
+        const int k = k0 + e, b = k / side.r;
+        __bf16 v = (__bf16)0.0f;
+        if (b < side.np) {
+            __bf16 pc[3];
+            three_pieces((float)p[(k - b * side.r) * sj], pc);
+            const int w = side.pb[b];
+            v = w == 0 ? pc[0] : w == 1 ? pc[1] : pc[2];
         }
-        *(v8bf *)(d + k0) = x;
+        x[e] = v;
     }
+    *(v8bf *)(dst + t * side.kpad + k0) = x;
 }
 
 static int pack_side_launch(const void *src, int dtype, int64_t batch, int64_t so, int64_t sj, int64_t rows, int64_t adapters,
                             const SideBySide &side, __bf16 *dst, __bf16 *zero, hipStream_t s)
 {
     const int64_t total = rows * adapters;
-    const dim3 grid((unsigned)((total + WG - 1) / WG));
+    const dim3 grid((unsigned)((pad_to(total, 64) * (side.kpad / 8) + WG - 1) / WG));
     if (dtype == RAIRS_F32)
         hipLaunchKernelGGL(pack_side_kernel<float>, grid, dim3(WG), 0, s, (const float *)src, batch, so, sj, rows, total, side, dst, zero);
     else
@@ -330,87 +439,118 @@ __global__ __launch_bounds__(WG) void few_shrink_kernel(FewProjectArgs a, int ve
     if (lane == 0) a.u[row * a.r + j] = a.scale ? s * a.scale[ad] : s;
 }
 
-// 16 columns of y per workgroup: its waves share the sum over d_in, then each finishes one tile of 16 rows
-template <class S, int QT, bool VEC>
+// 16 PT columns of y for 64 rows per workgroup: its waves share the sum over d_in, then each finishes one tile of 16
+// rows.  The low-rank part is a row's own: its u against the columns' rows of its adapter's B, on the vector units.
+template <class S, int PT, int QT, bool VEC, bool BVEC>
 __global__ __launch_bounds__(WG) void few_project_kernel(FewProjectArgs a)
 {
-    __shared__ v4f part[4][QT][64];
+    __shared__ v4f part[4][PT][QT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int p0 = blockIdx.x * 16;
-    const S *prow[1] = {(const S *)a.w + (int64_t)min(p0 + (lane & 15), a.d_out - 1) * a.d_in};
+    const int p0 = blockIdx.x * 16 * PT;
+    const int64_t q0 = (int64_t)blockIdx.y * 16 * QT;
+    const S *prow[PT];
     const S *qrow[QT];
-    v4f acc[1][QT];
-    float nrm[1];
+    v4f acc[PT][QT];
+    float nrm[PT];
+#pragma unroll
+    for (int i = 0; i < PT; i++) prow[i] = (const S *)a.w + (int64_t)min(p0 + 16 * i + (lane & 15), a.d_out - 1) * a.d_in;
 #pragma unroll
     for (int j = 0; j < QT; j++) {
-        const int64_t q = min((int64_t)(16 * j + (lane & 15)), a.n - 1);
+        const int64_t q = min(q0 + 16 * j + (lane & 15), a.n - 1);
         qrow[j] = (const S *)a.x + q * a.ldx;
-        acc[0][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < PT; i++) acc[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
     }
     const int steps = (a.d_in + 4 * FewLoad<S>::CH - 1) / (4 * FewLoad<S>::CH);
-    few_dot<S, S, 1, QT, VEC, false>(prow, qrow, steps * wave / 4, steps * (wave + 1) / 4, a.d_in, lane, acc, nrm);
+    few_dot<S, S, PT, QT, VEC, false>(prow, qrow, steps * wave / 4, steps * (wave + 1) / 4, a.d_in, lane, acc, nrm);
 #pragma unroll
-    for (int j = 0; j < QT; j++) part[wave][j][lane] = acc[0][j];
+    for (int i = 0; i < PT; i++)
+#pragma unroll
+        for (int j = 0; j < QT; j++) part[wave][i][j][lane] = acc[i][j];
     __syncthreads();
     if (wave >= QT) return;
-    const int64_t q = 16 * wave + (lane & 15);
+    const int64_t q = q0 + 16 * wave + (lane & 15);
     if (q >= a.n) return;
-    v4f y = (part[0][wave][lane] + part[1][wave][lane]) + (part[2][wave][lane] + part[3][wave][lane]);
-    const int o0 = p0 + 4 * (lane >> 4);
     const int ad = a.adapter ? a.adapter[q] : -1;
-    if (ad >= 0 && ad < a.na) {
-        const float *u = a.u + q * a.r;
-        v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
-        const S *b = (const S *)a.b + (int64_t)ad * a.d_out * a.r;
-        for (int j = 0; j < a.r; j++) {
-            const float uj = u[j];
+    const bool own = ad >= 0 && ad < a.na;
+    constexpr int CH = FewLoad<S>::CH;
 #pragma unroll
-            for (int e = 0; e < 4; e++) z[e] = fmaf((float)b[(int64_t)min(o0 + e, a.d_out - 1) * a.r + j], uj, z[e]);
+    for (int i = 0; i < PT; i++) {
+        v4f y = (part[0][i][wave][lane] + part[1][i][wave][lane]) + (part[2][i][wave][lane] + part[3][i][wave][lane]);
+        const int o0 = p0 + 16 * i + 4 * (lane >> 4);
+        if (own) {
+            const float *u = a.u + q * a.r;
+            const S *b = (const S *)a.b + (int64_t)ad * a.d_out * a.r;
+            v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int j = 0; j < a.r; j += CH) {
+                FewFrag<S, CH> f[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) f[e] = few_load<S, CH, BVEC>(b + (int64_t)min(o0 + e, a.d_out - 1) * a.r, j, a.r);
+#pragma unroll
+                for (int w = 0; w < CH; w++) {
+                    const float uj = j + w < a.r ? u[j + w] : 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) z[e] = fmaf((float)f[e].e[w], uj, z[e]);
+                }
+            }
+            y += z;
         }
-        y += z;
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (o0 + e < a.d_out) {
+                if (a.bf16_out) ((__bf16 *)a.y)[q * a.ldy + o0 + e] = (__bf16)y[e];
+                else ((float *)a.y)[q * a.ldy + o0 + e] = y[e];
+            }
     }
-#pragma unroll
-    for (int e = 0; e < 4; e++)
-        if (o0 + e < a.d_out) {
-            if (a.bf16_out) ((__bf16 *)a.y)[q * a.ldy + o0 + e] = (__bf16)y[e];
-            else ((float *)a.y)[q * a.ldy + o0 + e] = y[e];
-        }
+}
+
+static bool row_vec(const void *p, int64_t ld, int dtype) { return (uintptr_t)p % 16 == 0 && ld * dtype_width(dtype) % 16 == 0; }
+
+template <class S, int PT, int QT>
+static void few_project_launch(const FewProjectArgs &a, bool vec, bool bvec, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.d_out + 16 * PT - 1) / (16 * PT)), (unsigned)((a.n + 16 * QT - 1) / (16 * QT)));
+    if (vec && bvec) hipLaunchKernelGGL((few_project_kernel<S, PT, QT, true, true>), grid, dim3(WG), 0, s, a);
+    else if (vec) hipLaunchKernelGGL((few_project_kernel<S, PT, QT, true, false>), grid, dim3(WG), 0, s, a);
+    else hipLaunchKernelGGL((few_project_kernel<S, PT, QT, false, false>), grid, dim3(WG), 0, s, a);
 }
 
 template <class S>
-static int few_project(const FewProjectArgs &a, hipStream_t s)
+static int few_project(const FewProjectArgs &a, int dtype, hipStream_t s)
 {
-    const bool vec = (uintptr_t)a.x % 16 == 0 && a.ldx * sizeof(S) % 16 == 0 && (uintptr_t)a.w % 16 == 0 && a.d_in * sizeof(S) % 16 == 0 &&
-                     (!a.adapter || (uintptr_t)a.a % 16 == 0);
-    if (a.adapter) {
-        hipLaunchKernelGGL(few_shrink_kernel<S>, dim3((unsigned)a.n, (unsigned)((a.r + 3) / 4)), dim3(WG), 0, s, a, (int)vec);
-        RAIRS_HIP(hipGetLastError());
-    }
-    const dim3 grid((unsigned)((a.d_out + 15) / 16));
-#define RAIRS_FEW(QT_)                                                                               \
-    if (vec) hipLaunchKernelGGL((few_project_kernel<S, QT_, true>), grid, dim3(WG), 0, s, a);        \
-    else hipLaunchKernelGGL((few_project_kernel<S, QT_, false>), grid, dim3(WG), 0, s, a)
-    if (a.n <= 16) { RAIRS_FEW(1); }
-    else if (a.n <= 32) { RAIRS_FEW(2); }
-    else { RAIRS_FEW(4); }
-#undef RAIRS_FEW
+    const bool vec = row_vec(a.x, a.ldx, dtype) && row_vec(a.w, a.d_in, dtype), bvec = a.adapter && row_vec(a.b, a.r, dtype);
+    // two tiles of columns where that leaves two workgroups for every CU
+    if (a.n <= 16) few_project_launch<S, 1, 1>(a, vec, bvec, s);
+    else if (a.n <= 32) few_project_launch<S, 1, 2>(a, vec, bvec, s);
+    else if ((int64_t)((a.d_out + 31) / 32) * ((a.n + 63) / 64) < 512) few_project_launch<S, 1, 4>(a, vec, bvec, s);
+    else few_project_launch<S, 2, 4>(a, vec, bvec, s);
+    RAIRS_HIP(hipGetLastError());
+    return RAIRS_OK;
+}
+
+template <class S>
+static int few_shrink(const FewProjectArgs &a, int dtype, hipStream_t s)
+{
+    const int vec = row_vec(a.x, a.ldx, dtype) && row_vec(a.a, a.d_in, dtype);
+    hipLaunchKernelGGL(few_shrink_kernel<S>, dim3((unsigned)a.n, (unsigned)((a.r + 3) / 4)), dim3(WG), 0, s, a, vec);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
 
 // ---- forward -------------------------------------------------------------------------------------------
 
-static bool row_vec(const void *p, int64_t ld, int dtype) { return (uintptr_t)p % 16 == 0 && ld * dtype_width(dtype) % 16 == 0; }
-
 int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t s)
 {
     const rairs_projection_t &p = g.p;
-    const bool adapters = p.n_adapters > 0;
+    const bool adapters = p.n_adapters > 0, bf = p.dtype == RAIRS_BF16;
+    const int64_t units = max_units(g.n, p.n_adapters, UNIT_ROWS);
     Carve w(ws);
     int rc = RAIRS_OK;
-    if (g.n <= FEW_ROWS) {
+    if (rowprod_size(p.d_out, g.n) == 0) {
         FewProjectArgs a = {};
+        SortView sv = {};
         a.u = adapters ? w.take<float>(g.n * p.rank) : nullptr;
+        if (adapters && g.n > FEW_ROWS) sv = sort_carve(w, g.adapter, g.n, p.n_adapters);
         if (bytes) *bytes = w.used;
         if (!ws) return RAIRS_OK;
         a.x = g.x; a.w = p.W; a.a = p.A; a.b = p.B;
@@ -418,7 +558,15 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         a.d_in = p.d_in; a.d_out = p.d_out; a.r = p.rank; a.na = p.n_adapters;
         a.adapter = adapters ? g.adapter : nullptr;
         a.scale = p.scale; a.y = g.y; a.bf16_out = g.ytype == RAIRS_BF16;
-        return p.dtype == RAIRS_BF16 ? few_project<__bf16>(a, s) : few_project<float>(a, s);
+        if (a.adapter && g.n <= FEW_ROWS) rc = bf ? few_shrink<__bf16>(a, p.dtype, s) : few_shrink<float>(a, p.dtype, s);
+        else if (a.adapter) {
+            if ((rc = sort_launch(sv, s))) return rc;
+            ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, a.u, 1, nullptr, {}};
+            const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
+            rc = bf ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s);
+        }
+        if (rc) return rc;
+        return bf ? few_project<__bf16>(a, p.dtype, s) : few_project<float>(a, p.dtype, s);
     }
     const int np = dtype_pieces(p.dtype);
     __bf16 *xroom = w.take<__bf16>(pack_room(p.dtype, g.n, p.d_in)), *wroom = w.take<__bf16>(pack_room(p.dtype, p.d_out, p.d_in));
@@ -443,9 +591,8 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     if ((rc = rairs_operand(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, wroom, rp.P, s))) return rc;
     if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, xroom, rp.Q, s))) return rc;
     if (use) {
-        ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side};
+        ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, 0, up, side};
         const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
-        const int64_t units = max_units(g.n, p.n_adapters, UNIT_ROWS);
         if ((rc = p.dtype == RAIRS_BF16 ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s))) return rc;
         if ((rc = pack_side_launch(p.B, p.dtype, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, p.n_adapters, side, bp, zero, s))) return rc;
         rp.ad = AdapterPart{up, bp, zero, sv.of_row, sv.first + 1, side.kpad};
@@ -470,64 +617,108 @@ __global__ __launch_bounds__(WG) void transpose_kernel(const S *__restrict__ src
         if (c0 + i < cols && r0 + x < rows) dst[batch + (int64_t)(c0 + i) * rows + r0 + x] = tile[x][i];
 }
 
-// Partial sums of an adapter's gradient over a chunk of its rows: part[chunk][j][i] = sum_rows u[row][j]
-// x[row][i].  A thread has one column and 16 ranks; u comes through scalar registers.
-#define GRAD_RANKS 16
-template <class S>
+// Partial sums of an adapter's gradient over a chunk of its rows: sum_rows x[row][i] u[row][j], by the fp32
+// matrix instruction (16 x 16 x 4), whose operands are rows as they lie: a lane takes 16 bytes of one of four
+// rows, its values go into as many products (product t has columns CH c + t), and one rank of u.  Rows are
+// rank-bound small change next to the projection; the fp32 rate is enough and nothing is rounded.  The
+// workgroup's waves take every fourth four of rows and are joined in LDS.
+// part[chunk][j][i], or turned [chunk][i][j].
+template <class S, int RT, bool VEC>
 __global__ __launch_bounds__(WG) void adapter_grad_kernel(const S *__restrict__ x, int64_t ldx, const int32_t *__restrict__ perm,
-                                                          const float *__restrict__ u, int r, int cols, const int4 *__restrict__ chunks,
-                                                          const int32_t *__restrict__ nchunks, float *__restrict__ part)
+                                                          const float *__restrict__ u, int r, int cols, int turned,
+                                                          const int4 *__restrict__ chunks, const int32_t *__restrict__ nchunks,
+                                                          float *__restrict__ part)
 {
+    constexpr int CH = FewLoad<S>::CH;
+    __shared__ v4f sums[3][CH * RT][64];
     if ((int)blockIdx.x >= *nchunks) return;
     const int4 ch = chunks[blockIdx.x];
-    const int i = blockIdx.y * WG + threadIdx.x, j0 = blockIdx.z * GRAD_RANKS;
-    const int ic = min(i, cols - 1), nj = min(GRAD_RANKS, r - j0);
-    float acc[GRAD_RANKS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, h = lane >> 4;
+    const int i0 = (blockIdx.y * 16 + c) * CH, j0 = blockIdx.z * 16 * RT;
+    v4f acc[CH][RT];
 #pragma unroll
-    for (int j = 0; j < GRAD_RANKS; j++) acc[j] = 0.0f;
-    const float *ub = u + (int64_t)ch.y * r + j0;
-#pragma unroll 4
-    for (int k = 0; k < ch.z; k++) {
-        const float xv = (float)x[(int64_t)perm[ch.y + k] * ldx + ic];
-        const float *uk = ub + (int64_t)k * r;
+    for (int t = 0; t < CH; t++)
 #pragma unroll
-        for (int j = 0; j < GRAD_RANKS; j++) acc[j] = fmaf(uk[min(j, nj - 1)], xv, acc[j]);
+        for (int j = 0; j < RT; j++) acc[t][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int AHEAD = 4;                                          // fours of rows on the way
+    for (int k0 = wave * 4; k0 < ch.z; k0 += 16 * AHEAD) {
+        FewFrag<S, CH> f[AHEAD];
+        float v[AHEAD][RT];
+        int64_t row[AHEAD];
+#pragma unroll
+        for (int w = 0; w < AHEAD; w++) row[w] = perm[ch.y + min(k0 + 16 * w + h, ch.z - 1)];
+#pragma unroll
+        for (int w = 0; w < AHEAD; w++) {
+            const int k = min(k0 + 16 * w + h, ch.z - 1);
+            f[w] = few_load<S, CH, VEC>(x + row[w] * ldx, i0, cols);
+#pragma unroll
+            for (int j = 0; j < RT; j++) v[w][j] = u[(int64_t)(ch.y + k) * r + min(j0 + 16 * j + c, r - 1)];
+        }
+#pragma unroll
+        for (int w = 0; w < AHEAD; w++) {
+            const bool in = k0 + 16 * w + h < ch.z;
+#pragma unroll
+            for (int t = 0; t < CH; t++)
+#pragma unroll
+                for (int j = 0; j < RT; j++)
+                    acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? (float)f[w].e[t] : 0.0f, in ? v[w][j] : 0.0f, acc[t][j], 0, 0, 0);
+        }
     }
-    if (i >= cols) return;
-    float *o = part + ((int64_t)blockIdx.x * r + j0) * cols + i;
+    if (wave)
 #pragma unroll
-    for (int j = 0; j < GRAD_RANKS; j++)
-        if (j < nj) o[(int64_t)j * cols] = acc[j];
+        for (int t = 0; t < CH; t++)
+#pragma unroll
+            for (int j = 0; j < RT; j++) sums[wave - 1][t * RT + j][lane] = acc[t][j];
+    __syncthreads();
+    if (wave) return;
+    float *o = part + (int64_t)blockIdx.x * r * cols;
+#pragma unroll
+    for (int t = 0; t < CH; t++)
+#pragma unroll
+        for (int j = 0; j < RT; j++) {
+            const v4f y = (acc[t][j] + sums[0][t * RT + j][lane]) + (sums[1][t * RT + j][lane] + sums[2][t * RT + j][lane]);
+            const int rank = j0 + 16 * j + c;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int i = (blockIdx.y * 16 + 4 * h + e) * CH + t;
+                if (rank < r && i < cols) o[turned ? (int64_t)i * r + rank : (int64_t)rank * cols + i] = y[e];
+            }
+        }
 }
 
-// out[a][j][i] (or, turned, out[a][i][j]) = the sum of the adapter's chunks in their order
+// an adapter's gradient: its chunks' sums in their order (both lie alike)
 template <class S>
-__global__ __launch_bounds__(WG) void adapter_join_kernel(const float *__restrict__ part, const int32_t *__restrict__ chunk0, int r, int cols,
-                                                          int turned, S *__restrict__ out)
+__global__ __launch_bounds__(WG) void adapter_join_kernel(const float *__restrict__ part, const int32_t *__restrict__ chunk0, int64_t size,
+                                                          S *__restrict__ out)
 {
     const int a = blockIdx.y;
     const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x;
-    if (t >= (int64_t)r * cols) return;
-    int j, i;
-    if (turned) { i = (int)(t / r); j = (int)(t - (int64_t)i * r); }
-    else { j = (int)(t / cols); i = (int)(t - (int64_t)j * cols); }
+    if (t >= size) return;
     float x = 0.0f;
-    for (int c = chunk0[a]; c < chunk0[a + 1]; c++) x += part[((int64_t)c * r + j) * cols + i];
-    out[(int64_t)a * r * cols + t] = (S)x;
+    for (int c = chunk0[a]; c < chunk0[a + 1]; c++) x += part[c * size + t];
+    out[a * size + t] = (S)x;
 }
 
 template <class S>
 static int adapter_grads(const ProjectArgs &g, const SortView &sv, const float *u, const float *v, float *part, hipStream_t s)
 {
     const rairs_projection_t &p = g.p;
-    const unsigned chunks = (unsigned)max_units(g.n, p.n_adapters, CHUNK_ROWS), rz = (unsigned)((p.rank + GRAD_RANKS - 1) / GRAD_RANKS);
+    const unsigned chunks = (unsigned)max_units(g.n, p.n_adapters, CHUNK_ROWS);
     const int32_t *nch = sv.chunk0 + p.n_adapters;
+    const int rt = p.rank <= 16 ? 1 : 2;
     for (int side = 0; side < 2; side++) {
         const int cols = side ? p.d_out : p.d_in;
-        hipLaunchKernelGGL(adapter_grad_kernel<S>, dim3(chunks, (unsigned)((cols + WG - 1) / WG), rz), dim3(WG), 0, s, (const S *)(side ? g.dy : g.x),
-                           side ? g.lddy : g.ldx, sv.perm, side ? u : v, p.rank, cols, sv.chunks, nch, part);
-        hipLaunchKernelGGL(adapter_join_kernel<S>, dim3((unsigned)(((int64_t)p.rank * cols + WG - 1) / WG), (unsigned)p.n_adapters), dim3(WG), 0, s,
-                           part, sv.chunk0, p.rank, cols, side, (S *)(side ? g.db : g.da));
+        const S *x = (const S *)(side ? g.dy : g.x);
+        const int64_t ld = side ? g.lddy : g.ldx, size = (int64_t)p.rank * cols;
+        const float *w = side ? u : v;
+        const dim3 grid(chunks, (unsigned)((cols + 16 * FewLoad<S>::CH - 1) / (16 * FewLoad<S>::CH)), (unsigned)((p.rank + 16 * rt - 1) / (16 * rt)));
+        const bool vec = row_vec(x, ld, p.dtype);
+        if (rt == 1 && vec) hipLaunchKernelGGL((adapter_grad_kernel<S, 1, true>), grid, dim3(WG), 0, s, x, ld, sv.perm, w, p.rank, cols, side, sv.chunks, nch, part);
+        else if (rt == 1) hipLaunchKernelGGL((adapter_grad_kernel<S, 1, false>), grid, dim3(WG), 0, s, x, ld, sv.perm, w, p.rank, cols, side, sv.chunks, nch, part);
+        else if (vec) hipLaunchKernelGGL((adapter_grad_kernel<S, 2, true>), grid, dim3(WG), 0, s, x, ld, sv.perm, w, p.rank, cols, side, sv.chunks, nch, part);
+        else hipLaunchKernelGGL((adapter_grad_kernel<S, 2, false>), grid, dim3(WG), 0, s, x, ld, sv.perm, w, p.rank, cols, side, sv.chunks, nch, part);
+        hipLaunchKernelGGL(adapter_join_kernel<S>, dim3((unsigned)((size + WG - 1) / WG), (unsigned)p.n_adapters), dim3(WG), 0, s, part, sv.chunk0, size,
+                           (S *)(side ? g.db : g.da));
         RAIRS_HIP(hipGetLastError());
     }
     return RAIRS_OK;
@@ -577,11 +768,11 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         const int64_t units = max_units(g.n, na, UNIT_ROWS);
         rc = bf ? transpose_launch<__bf16>(p.B, p.d_out, p.rank, na, bt, s) : transpose_launch<float>(p.B, p.d_out, p.rank, na, bt, s);
         if (rc) return rc;
-        ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, g.dx ? vp : nullptr, side};
+        ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, 0, g.dx ? vp : nullptr, side};
         const bool vec = row_vec(g.dy, g.lddy, p.dtype) && row_vec(bt, p.d_out, p.dtype);
         if ((rc = bf ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s))) return rc;
         if (g.da) {
-            ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, nullptr, side};
+            ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, 0, nullptr, side};
             const bool xvec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
             if ((rc = bf ? shrink_launch<__bf16>(su, units, xvec, s) : shrink_launch<float>(su, units, xvec, s))) return rc;
             if ((rc = bf ? adapter_grads<__bf16>(g, sv, u, v, part, s) : adapter_grads<float>(g, sv, u, v, part, s))) return rc;
