@@ -49,21 +49,26 @@ static __device__ __forceinline__ FewFrag<S, CH> few_load(const S *row, int k, i
     return f;
 }
 
-template <int CH>
-static __device__ __forceinline__ v4f few_mfma(const FewFrag<__bf16, CH> &a, const FewFrag<__bf16, CH> &b, v4f c)
-{
-    v8bf x, y;
-    __builtin_memcpy(&x, a.e, 16);
-    __builtin_memcpy(&y, b.e, 16);
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
-}
+// instruction e of a step's products (bf16: one; fp32: one for each value of a lane)
 template <class S, int CH>
-static __device__ __forceinline__ v4f few_mfma(const FewFrag<S, CH> &a, const FewFrag<float, CH> &b, v4f c)
-{
-#pragma unroll
-    for (int e = 0; e < CH; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32((float)a.e[e], b.e[e], c, 0, 0, 0);
-    return c;
-}
+struct FewMfma {
+    static constexpr int N = CH;
+    static __device__ __forceinline__ v4f go(const FewFrag<S, CH> &a, const FewFrag<float, CH> &b, int e, v4f c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x4f32((float)a.e[e], b.e[e], c, 0, 0, 0);
+    }
+};
+template <int CH>
+struct FewMfma<__bf16, CH> {
+    static constexpr int N = 1;
+    static __device__ __forceinline__ v4f go(const FewFrag<__bf16, CH> &a, const FewFrag<__bf16, CH> &b, int, v4f c)
+    {
+        v8bf x, y;
+        __builtin_memcpy(&x, a.e, 16);
+        __builtin_memcpy(&y, b.e, 16);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+    }
+};
 
 // KU steps: 4 KU CH values of every row, from value k on for this lane.  The loads of a row follow each other, so
 // that the pieces of a line are asked for at once (asked for a row tile later they cost a third of the
@@ -84,17 +89,23 @@ static __device__ __forceinline__ void few_steps(const S *const (&prow)[PT], con
 #pragma unroll
         for (int j = 0; j < QT; j++) b[s][j] = few_load<Q, CH, VEC, false>(qrow[j], k + s * STEP, d);
     __builtin_amdgcn_sched_barrier(0);                                // (all of them are under way first)
+    // (products onto the same sums as far apart as can be: each waits for the one before it)
 #pragma unroll
-    for (int i = 0; i < PT; i++)
+    for (int s = 0; s < KU; s++)
 #pragma unroll
-        for (int s = 0; s < KU; s++) {
+        for (int e = 0; e < FewMfma<S, CH>::N; e++)
 #pragma unroll
-            for (int j = 0; j < QT; j++) acc[i][j] = few_mfma(a[i][s], b[s][j], acc[i][j]);
-            if constexpr (NORM) {
+            for (int i = 0; i < PT; i++)
+#pragma unroll
+                for (int j = 0; j < QT; j++) acc[i][j] = FewMfma<S, CH>::go(a[i][s], b[s][j], e, acc[i][j]);
+    if constexpr (NORM) {
+#pragma unroll
+        for (int i = 0; i < PT; i++)
+#pragma unroll
+            for (int s = 0; s < KU; s++)
 #pragma unroll
                 for (int e = 0; e < CH; e++) nrm[i] = fmaf((float)a[i][s].e[e], (float)a[i][s].e[e], nrm[i]);
-            }
-        }
+    }
 }
 
 // acc += rows prow (many) times rows qrow (few) over the steps [s0, s1); prow/qrow: this lane's rows

@@ -446,8 +446,14 @@ __global__ __launch_bounds__(WG) void few_project_kernel(FewProjectArgs a)
 {
     __shared__ v4f part[4][PT][QT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int p0 = blockIdx.x * 16 * PT;
-    const int64_t q0 = (int64_t)blockIdx.y * 16 * QT;
+    // workgroups go round robin over the eight XCDs: the ones that read the same rows (of x, or of W if there are
+    // fewer rows of x) one after the other on one of them, whose L2 cache has them after the first
+    const int pt = (a.d_out + 16 * PT - 1) / (16 * PT), qt = (int)((a.n + 16 * QT - 1) / (16 * QT)), total = pt * qt, per = (total + 7) / 8;
+    const int id = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+    if ((int)(blockIdx.x / 8) >= per || id >= total) return;
+    const bool rows_first = a.n < a.d_out;
+    const int p0 = (rows_first ? id / qt : id % pt) * 16 * PT;
+    const int64_t q0 = (int64_t)(rows_first ? id % qt : id / pt) * 16 * QT;
     const S *prow[PT];
     const S *qrow[QT];
     v4f acc[PT][QT];
@@ -509,7 +515,8 @@ static bool row_vec(const void *p, int64_t ld, int dtype) { return (uintptr_t)p 
 template <class S, int PT, int QT>
 static void few_project_launch(const FewProjectArgs &a, bool vec, bool bvec, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.d_out + 16 * PT - 1) / (16 * PT)), (unsigned)((a.n + 16 * QT - 1) / (16 * QT)));
+    const int64_t total = (a.d_out + 16 * PT - 1) / (16 * PT) * ((a.n + 16 * QT - 1) / (16 * QT));
+    const dim3 grid((unsigned)(pad_to(total, 8)));
     if (vec && bvec) hipLaunchKernelGGL((few_project_kernel<S, PT, QT, true, true>), grid, dim3(WG), 0, s, a);
     else if (vec) hipLaunchKernelGGL((few_project_kernel<S, PT, QT, true, false>), grid, dim3(WG), 0, s, a);
     else hipLaunchKernelGGL((few_project_kernel<S, PT, QT, false, false>), grid, dim3(WG), 0, s, a);
