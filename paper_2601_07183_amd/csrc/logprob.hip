@@ -191,24 +191,48 @@ struct StatsState {
     }
 };
 
-template <bool ENT, int TOP>
+// NORM: the largest squared norm of the rows is wanted as well (a wave has all of the queries then)
+template <bool ENT, int TOP, bool NORM = false>
 struct StatsEpi {
     StatsArgs a;
+    const uint32_t *any_live;
+    float *xmax;                    // [parts]
     template <class T>
     struct State {
         StatsState<T::QT, ENT, TOP> s;
+        float most;
     };
     template <class T>
-    __device__ __forceinline__ void begin(State<T> &st, int64_t q0, int lane) const { st.s.begin(a, (int)q0, lane); }
+    __device__ __forceinline__ void begin(State<T> &st, int64_t q0, int lane) const
+    {
+        st.s.begin(a, (int)q0, lane);
+        st.most = 0.0f;
+    }
     template <class T>
     __device__ __forceinline__ void tile(State<T> &st, RowAcc<T> &acc, int64_t p0, int64_t q0, int lane, int) const
     {
         st.s.tile(a, acc.v, (int)p0, (int)q0, lane);
+        if constexpr (NORM) {
+#pragma unroll
+            for (int i = 0; i < T::PT; i++) {
+                float x = acc.nrm[i] + __shfl_xor(acc.nrm[i], 16);
+                x += __shfl_xor(x, 32);
+                const int p = (int)p0 + 16 * i + (lane & 15);
+                if (p < a.V && (!any_live || ((any_live[p >> 5] >> (p & 31)) & 1u))) st.most = fmaxf(st.most, x);
+            }
+        }
     }
     template <class T>
     __device__ __forceinline__ void end(State<T> &st, int run, int wp, int64_t q0, int lane) const
     {
         st.s.end(a, run * T::WP + wp, (int)q0, lane);
+        if constexpr (NORM) {
+            float x = fmaxf(st.most, lane_xor8(st.most));
+            x = fmaxf(x, lane_xor4(x));
+            x = fmaxf(x, lane_xor2(x));
+            x = fmaxf(x, lane_xor1(x));
+            if (lane == 0) xmax[run * T::WP + wp] = x;
+        }
     }
 };
 
@@ -963,7 +987,24 @@ static int finish_launch(FinishArgs &f, hipStream_t s)
 template <bool ENT, int TOP>
 static int stats_launch(RowProd &rp, const StatsArgs &st, bool large, int prun, hipStream_t s)
 {
-    return large ? rowprod_launch<TileL>(rp, StatsEpi<ENT, TOP>{st}, s, prun) : rowprod_launch<TileW>(rp, StatsEpi<ENT, TOP>{st}, s, prun);
+    return large ? rowprod_launch<TileL>(rp, StatsEpi<ENT, TOP>{st, nullptr, nullptr}, s, prun)
+                 : rowprod_launch<TileW>(rp, StatsEpi<ENT, TOP>{st, nullptr, nullptr}, s, prun);
+}
+
+// a few queries over rows that lie right
+template <class T, int FLAGS>
+static int few_tiles_launch(RowProd &rp, const StatsArgs &st, const uint32_t *any_live, float *xmax, int prun, hipStream_t s)
+{
+    return xmax ? rowprod_launch<T, FLAGS | ROW_NORM>(rp, StatsEpi<true, 2, true>{st, any_live, xmax}, s, prun)
+                : rowprod_launch<T, FLAGS>(rp, StatsEpi<true, 0>{st, nullptr, nullptr}, s, prun);
+}
+
+template <int FLAGS>
+static int few_tiles(RowProd &rp, const StatsArgs &st, const uint32_t *any_live, float *xmax, int prun, hipStream_t s)
+{
+    return st.n <= 16   ? few_tiles_launch<TileF1, FLAGS>(rp, st, any_live, xmax, prun, s)
+           : st.n <= 32 ? few_tiles_launch<TileF2, FLAGS>(rp, st, any_live, xmax, prun, s)
+                        : few_tiles_launch<TileF4, FLAGS>(rp, st, any_live, xmax, prun, s);
 }
 
 int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
@@ -974,13 +1015,15 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     const int64_t fills = (blocks + 16 * 4096 - 1) / (16 * 4096);
     const int rounds = few ? (int)((blocks + fills * 4096 - 1) / (fills * 4096)) : 1;
     const bool large = rowprod_size(a.V, a.n) == 2;
-    const int64_t ptiles = large ? (a.V + TileL::BP - 1) / TileL::BP : (a.V + TileW::BP - 1) / TileW::BP;
-    const int64_t qtiles = large ? (a.n + TileL::BQ - 1) / TileL::BQ : (a.n + TileW::BQ - 1) / TileW::BQ;
+    const int bp = few || large ? 256 : 128, bq = few ? 64 : bp;
+    const int64_t ptiles = (a.V + bp - 1) / bp, qtiles = (a.n + bq - 1) / bq;
     // (a start costs a few microseconds, a tile 27 at K = 1024 and 256 x 256; one workgroup of the large tile
     // fits a CU, two of the smaller)
     const double ksum = (double)kpad * (dtype_pieces(a.ttype) * dtype_pieces(a.qtype) == 9 ? 6 : dtype_pieces(a.qtype));
-    const int prun = few ? 1 : rowprod_run(ptiles, qtiles, large ? 256 : 512, 100.0 / (ksum + 200.0), 64);
-    const int nparts = (int)(few ? (blocks + rounds - 1) / rounds : (ptiles + prun - 1) / prun * 2);     // (both tiles: two waves along P)
+    const int prun = rowprod_run(ptiles, qtiles, few || large ? 256 : 512, few ? 0.3 : 100.0 / (ksum + 200.0), 64);
+    // (a few queries: by tiles, four waves along P, or rows straight from memory; there is room for either's parts)
+    const int runs = (int)((ptiles + prun - 1) / prun), few_parts = (int)((blocks + rounds - 1) / rounds);
+    const int most_parts = few ? std::max(4 * runs, few_parts) : 2 * runs;
     // Groups of 16 rows or of 64.  Per query, the smaller ones cost two more operations a row and 8 bytes for 16 rows
     // instead of 4 for 64, about 0.14 ps times V; the larger ones 64 rows of the table for each of the `top`, at about
     // 6 TB/s.  (A few queries: the vector units have nothing else to do.)
@@ -988,15 +1031,13 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     Carve w(ws);
     StatsArgs st = {};
     st.n = (int)a.n; st.V = (int)a.V; st.c = a.scale * LOG2E; st.live = a.live; st.ld_live = a.ld_live; st.targets = a.targets;
-    st.parts = w.take<float4>(a.n * nparts);
-    st.nparts = nparts;
+    st.parts = w.take<float4>(a.n * most_parts);
     st.wstride = (int)pad_to(blocks, 4);
     st.gmax = a.top ? w.take<float>(wide ? a.n * st.wstride : a.n * blocks * 8) : nullptr;
     st.nblocks = (int)blocks;
     st.wide = wide;
     st.zt = w.take<float>(a.n);
-    const int nx = few ? nparts : NORM_WGS;
-    float *xmax = w.take<float>(nx);
+    float *xmax = w.take<float>(few ? most_parts : NORM_WGS);
     uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
     // (packed whether they need it or not, so that the size does not depend on where the rows lie)
     __bf16 *qroom = few ? nullptr : w.take<__bf16>(pack_room(a.qtype, a.n, kpad));
@@ -1008,7 +1049,27 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     int rc = RAIRS_OK;
     const uint32_t *seen_by_any = any_live(a, seen, s, &rc);
     if (rc) return rc;
-    if (few) {
+    st.nparts = most_parts;
+    if (few && (f32_lies_right(a.table, a.ttype, a.ldt, a.d) && f32_lies_right(a.q, a.qtype, a.ldq, a.d))) {
+        st.nparts = 4 * runs;
+        RowProd rp = {};
+        rowprod_pieces(rp, 1, 1);
+        rp.ksteps = a.d / (ROWPROD_K / 2);
+        rp.P = f32_operand(a.table, a.ldt, a.V);
+        rp.Q = f32_operand(a.q, a.ldq, a.n);
+        rc = few_tiles<ROW_F32>(rp, st, seen_by_any, a.top ? xmax : nullptr, prun, s);
+        if (rc) return rc;
+    } else if (few && rows_lie_right(a.table, a.ttype, a.ldt, a.d) && rows_lie_right(a.q, a.qtype, a.ldq, a.d)) {
+        st.nparts = 4 * runs;
+        RowProd rp = {};
+        rowprod_pieces(rp, 1, 1);
+        rp.ksteps = a.d / ROWPROD_K;
+        rp.P = RowOperand{(const __bf16 *)a.table, a.ldt, 0, a.V, nullptr, nullptr};
+        rp.Q = RowOperand{(const __bf16 *)a.q, a.ldq, 0, a.n, nullptr, nullptr};
+        rc = few_tiles<0>(rp, st, seen_by_any, a.top ? xmax : nullptr, prun, s);
+        if (rc) return rc;
+    } else if (few) {
+        st.nparts = few_parts;
         FewStatsArgs fa = {st, a.table, a.q, a.ldt, a.ldq, a.d, rounds, seen_by_any, xmax};
         const bool vec = lies_vec(a.table, a.ttype, a.ldt) && lies_vec(a.q, a.qtype, a.ldq);
         rc = a.ttype == RAIRS_BF16 ? few_stats<__bf16, __bf16>(fa, vec, a.top != 0, s)
@@ -1048,7 +1109,7 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     f.scale = a.scale;
     f.slack = product_slack(a.d);
     f.xmax = xmax;
-    f.nxmax = nx;
+    f.nxmax = few ? st.nparts : NORM_WGS;
     f.logp = a.logp; f.lse = a.lse; f.entropy = a.entropy;
     f.top = a.top; f.top_ids = a.top_ids; f.top_logp = a.top_logp;
     return a.ttype == RAIRS_BF16 ? finish_launch<__bf16, __bf16>(f, s)

@@ -5,9 +5,11 @@
 // rows, and in the large product a tile adds the terms of the few adapters that its rows have, as
 // further steps of the same sum in the same registers.  u enters that product as three bf16 pieces.
 //
-// Products with fewer than 160 tiles of 128 x 128 go another way: the rows of W and x straight from memory
-// into the matrix instruction's registers, and an adapter's B times u on the vector units behind it.
-// (10,000 x 1024 to 128 in fp32, 250 adapters of rank 16: 165 us by tiles, 64 so.)
+// fp32 products of few tiles take the rows as they are and the fp32 instruction, u and B with them.  A few rows go
+// another way altogether: no sort, the rows of W and x straight from memory into the matrix instruction's
+// registers, and a row's own B times u on the vector units behind it.
+#include <algorithm>
+
 #include "fewrows.h"
 #include "query_ops.h"
 
@@ -128,7 +130,7 @@ __global__ __launch_bounds__(SORT_ROWS) void sort_place_kernel(SortView v)
 
 // The whole sort by one workgroup, for a batch whose keys fit LDS: every wave counts a run of the rows, 64 at
 // a time, then places them behind the runs before it (in the batch's order, as above).
-#define SORT_ONE_ROWS 32768
+#define SORT_ONE_ROWS 16384
 #define SORT_ONE_KEYS 1024
 __global__ __launch_bounds__(1024) void sort_one_kernel(SortView v)
 {
@@ -136,8 +138,9 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(SortView v)
     __shared__ int32_t sums[1024];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keys = v.na + 1, bits = 32 - __clz(v.na);
     int32_t *cnt = sort_lds;                                          // [16][keys]
-    uint16_t *key_of = (uint16_t *)(sort_lds + 16 * keys);            // [n]
-    const int n = (int)v.n, per = ((n + 15) / 16 + 63) / 64 * 64;     // rows per wave
+    const int n = (int)v.n;
+    uint16_t *key_of = (uint16_t *)(sort_lds + 16 * keys), *placed = key_of + (n + 1) / 2 * 2;     // [n] both
+    const int per = ((n + 15) / 16 + 63) / 64 * 64;     // rows per wave
 #pragma unroll 4
     for (int i = tid; i < n; i += 1024) key_of[i] = (uint16_t)sort_key(v, i);
     for (int i = tid; i < 16 * keys; i += 1024) cnt[i] = 0;
@@ -189,11 +192,16 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(SortView v)
         wave_lds_sync();
         if (key >= 0) {
             const int pos = base + __popcll(m & ((1ull << lane) - 1ull));
-            v.perm[pos] = i0 + lane;
-            v.of_row[pos] = key < v.na ? key : -1;
+            placed[pos] = (uint16_t)(i0 + lane);                      // (written out in runs: a line per lane would be as many accesses)
             if (lane == __ffsll((long long)m) - 1) mine[key] = base + __popcll(m);
         }
         wave_lds_sync();
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += 1024) {
+        const int r = placed[i], key = key_of[r];
+        v.perm[i] = r;
+        v.of_row[i] = key < v.na ? key : -1;
     }
 }
 
@@ -220,7 +228,7 @@ static SortView sort_carve(Carve &w, const int32_t *adapter, int64_t n, int na)
 static int sort_launch(const SortView &v, hipStream_t s)
 {
     if (v.n <= SORT_ONE_ROWS && v.na < SORT_ONE_KEYS) {
-        const size_t lds = (size_t)16 * (v.na + 1) * 4 + (size_t)(v.n + 1) / 2 * 4;
+        const size_t lds = (size_t)16 * (v.na + 1) * 4 + (size_t)((v.n + 1) / 2) * 8;
         RAIRS_HIP(hipFuncSetAttribute((const void *)sort_one_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
         hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(1024), lds, s, v);
         RAIRS_HIP(hipGetLastError());
@@ -240,7 +248,8 @@ static int sort_launch(const SortView &v, hipStream_t s)
 // products of pieces of u and of B (or A) laid side by side: columns t r .. t r + r - 1 hold piece pu[t]
 // of u against piece pb[t]
 struct SideBySide {
-    int np, r, kpad;
+    int np, r, kpad;                // kpad: units of two bytes
+    int f32;                        // u and B as they are (np = 1), for the fp32 instruction
     uint8_t pu[6], pb[6];
 };
 
@@ -256,6 +265,16 @@ static SideBySide side_by_side(int upieces, int bpieces, int r)
         x.pb[t] = (rp.sp >> (4 * t)) & 15;
         x.pu[t] = (rp.sq >> (4 * t)) & 15;
     }
+    return x;
+}
+
+static SideBySide side_f32(int r)
+{
+    SideBySide x = {};
+    x.np = 1;
+    x.r = r;
+    x.kpad = 2 * (int)pad_to(r, ROWPROD_K / 2);
+    x.f32 = 1;
     return x;
 }
 
@@ -275,17 +294,16 @@ struct ShrinkArgs {
     const int32_t *perm;
     const int4 *units;
     const int32_t *nunits;
-    float *u;                       // [n][r] in sorted order, or (by_row) in the batch's, or null
-    int by_row;
+    float *u;                       // [n][r] in sorted order, or null
     __bf16 *up;                     // [n][kpad] in sorted order, or null
     SideBySide side;
 };
 
-// a workgroup per unit; its waves share the sum, which is joined in LDS
-template <class S, int RT, bool VEC>
-__global__ __launch_bounds__(WG) void shrink_kernel(ShrinkArgs a)
+// a workgroup per unit; its NW waves share the sum, which is joined in LDS
+template <class S, int RT, int NW, bool VEC>
+__global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs a)
 {
-    __shared__ float part[3][UNIT_ROWS][16 * RT + 1];    // [wave][row][rank]
+    __shared__ float part[NW - 1][UNIT_ROWS][16 * RT + 1];    // [wave][row][rank]
     if ((int)blockIdx.x >= *a.nunits) return;
     const int4 unit = a.units[blockIdx.x];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -302,7 +320,7 @@ __global__ __launch_bounds__(WG) void shrink_kernel(ShrinkArgs a)
         acc[i][0] = acc[i][1] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
     }
     const int steps = (a.d + 4 * FewLoad<S>::CH - 1) / (4 * FewLoad<S>::CH);
-    few_dot<S, S, RT, 2, VEC, false>(prow, qrow, steps * wave / 4, steps * (wave + 1) / 4, a.d, lane, acc, nrm);
+    few_dot<S, S, RT, 2, VEC, false>(prow, qrow, steps * wave / NW, steps * (wave + 1) / NW, a.d, lane, acc, nrm);
     if (wave)
 #pragma unroll
         for (int i = 0; i < RT; i++)
@@ -321,17 +339,28 @@ __global__ __launch_bounds__(WG) void shrink_kernel(ShrinkArgs a)
                 for (int e = 0; e < 4; e++) {
                     float *p = &part[0][16 * j + (lane & 15)][16 * i + 4 * (lane >> 4) + e];
                     constexpr int W = UNIT_ROWS * (16 * RT + 1);
-                    *p = ((acc[i][j][e] + p[0]) + (p[W] + p[2 * W])) * sc;
+                    float x = acc[i][j][e];
+#pragma unroll
+                    for (int w = 0; w < NW - 1; w++) x += p[w * W];
+                    *p = x * sc;
                 }
     }
     __syncthreads();
     if (a.u)
-        for (int t = threadIdx.x; t < unit.z * a.r; t += WG) {
+        for (int t = threadIdx.x; t < unit.z * a.r; t += 64 * NW) {
             const int i = t / a.r, j = t - i * a.r;
-            a.u[(int64_t)(a.by_row ? a.perm[unit.y + i] : unit.y + i) * a.r + j] = part[0][i][j];
+            a.u[(int64_t)(unit.y + i) * a.r + j] = part[0][i][j];
         }
     if (!a.up) return;
-    for (int t = threadIdx.x; t < unit.z * a.side.kpad; t += WG) {
+    if (a.side.f32) {
+        const int k = a.side.kpad / 2;
+        for (int t = threadIdx.x; t < unit.z * k; t += 64 * NW) {
+            const int i = t / k, j = t - i * k;
+            ((float *)a.up)[(int64_t)(unit.y + i) * k + j] = j < a.r ? part[0][i][j] : 0.0f;
+        }
+        return;
+    }
+    for (int t = threadIdx.x; t < unit.z * a.side.kpad; t += 64 * NW) {
         const int i = t / a.side.kpad, k = t - i * a.side.kpad, b = k / a.r;
         __bf16 o = (__bf16)0.0f;
         if (b < a.side.np) {
@@ -348,13 +377,14 @@ template <class S>
 static int shrink_launch(const ShrinkArgs &a, int64_t units, bool vec, hipStream_t s)
 {
     const dim3 grid((unsigned)units);
-#define RAIRS_SHRINK(RT_)                                                                        \
-    if (vec) hipLaunchKernelGGL((shrink_kernel<S, RT_, true>), grid, dim3(WG), 0, s, a);         \
-    else hipLaunchKernelGGL((shrink_kernel<S, RT_, false>), grid, dim3(WG), 0, s, a)
-    if (a.r <= 16) { RAIRS_SHRINK(1); }
-    else if (a.r <= 32) { RAIRS_SHRINK(2); }
-    else if (a.r <= 64) { RAIRS_SHRINK(4); }
-    else { RAIRS_SHRINK(8); }
+    // (four waves where eight would not have the registers)
+#define RAIRS_SHRINK(RT_, NW_)                                                                            \
+    if (vec) hipLaunchKernelGGL((shrink_kernel<S, RT_, NW_, true>), grid, dim3(64 * NW_), 0, s, a);       \
+    else hipLaunchKernelGGL((shrink_kernel<S, RT_, NW_, false>), grid, dim3(64 * NW_), 0, s, a)
+    if (a.r <= 16) { RAIRS_SHRINK(1, 8); }
+    else if (a.r <= 32) { RAIRS_SHRINK(2, 8); }
+    else if (a.r <= 64) { RAIRS_SHRINK(4, 4); }
+    else { RAIRS_SHRINK(8, 4); }
 #undef RAIRS_SHRINK
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
@@ -375,6 +405,13 @@ __global__ __launch_bounds__(WG) void pack_side_kernel(const S *__restrict__ src
     const int k0 = (int)(id / 64 % eights) * 8;
     const int64_t a = t / rows, o = t - a * rows;
     const S *p = src + a * batch + o * so;
+    if (side.f32) {
+        v4f x;
+#pragma unroll
+        for (int e = 0; e < 4; e++) x[e] = k0 / 2 + e < side.r ? (float)p[(k0 / 2 + e) * sj] : 0.0f;
+        *(v4f *)(dst + t * side.kpad + k0) = x;
+        return;
+    }
     v8bf x;
 #pragma unroll
     for (int e = 0; e < 8; e++) {
@@ -490,11 +527,13 @@ __global__ __launch_bounds__(WG) void few_project_kernel(FewProjectArgs a)
             v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int j = 0; j < a.r; j += CH) {
                 FewFrag<S, CH> f[4];
+                FewFrag<float, CH> uv;                                // (BVEC: the rank is a multiple of CH)
+                if constexpr (BVEC) uv = few_load<float, CH, true>(u, j, a.r);
 #pragma unroll
                 for (int e = 0; e < 4; e++) f[e] = few_load<S, CH, BVEC>(b + (int64_t)min(o0 + e, a.d_out - 1) * a.r, j, a.r);
 #pragma unroll
                 for (int w = 0; w < CH; w++) {
-                    const float uj = j + w < a.r ? u[j + w] : 0.0f;
+                    const float uj = BVEC ? uv.e[w] : j + w < a.r ? u[j + w] : 0.0f;
 #pragma unroll
                     for (int e = 0; e < 4; e++) z[e] = fmaf((float)f[e].e[w], uj, z[e]);
                 }
@@ -546,6 +585,14 @@ static int few_shrink(const FewProjectArgs &a, int dtype, hipStream_t s)
 
 // ---- forward -------------------------------------------------------------------------------------------
 
+// Rows straight from memory: up to 256 of them, and what the workgroups read of W and x (a lane's 16 bytes are a
+// cache access each: about 10 TB/s) takes less than the launches of the other way (20 us).
+static bool few_rows(const rairs_projection_t &p, int64_t n)
+{
+    const double read = (double)((n + 63) / 64) * ((p.d_out + 31) / 32) * 96.0 * p.d_in * dtype_width(p.dtype);
+    return n <= 64 || (n <= FEW_ROWS && read < 200e6);
+}
+
 int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t s)
 {
     const rairs_projection_t &p = g.p;
@@ -553,11 +600,9 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     const int64_t units = max_units(g.n, p.n_adapters, UNIT_ROWS);
     Carve w(ws);
     int rc = RAIRS_OK;
-    if (rowprod_size(p.d_out, g.n) == 0) {
+    if (few_rows(p, g.n)) {
         FewProjectArgs a = {};
-        SortView sv = {};
         a.u = adapters ? w.take<float>(g.n * p.rank) : nullptr;
-        if (adapters && g.n > FEW_ROWS) sv = sort_carve(w, g.adapter, g.n, p.n_adapters);
         if (bytes) *bytes = w.used;
         if (!ws) return RAIRS_OK;
         a.x = g.x; a.w = p.W; a.a = p.A; a.b = p.B;
@@ -565,14 +610,7 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         a.d_in = p.d_in; a.d_out = p.d_out; a.r = p.rank; a.na = p.n_adapters;
         a.adapter = adapters ? g.adapter : nullptr;
         a.scale = p.scale; a.y = g.y; a.bf16_out = g.ytype == RAIRS_BF16;
-        if (a.adapter && g.n <= FEW_ROWS) rc = bf ? few_shrink<__bf16>(a, p.dtype, s) : few_shrink<float>(a, p.dtype, s);
-        else if (a.adapter) {
-            if ((rc = sort_launch(sv, s))) return rc;
-            ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, a.u, 1, nullptr, {}};
-            const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
-            rc = bf ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s);
-        }
-        if (rc) return rc;
+        if (a.adapter && (rc = bf ? few_shrink<__bf16>(a, p.dtype, s) : few_shrink<float>(a, p.dtype, s))) return rc;
         return bf ? few_project<__bf16>(a, p.dtype, s) : few_project<float>(a, p.dtype, s);
     }
     const int np = dtype_pieces(p.dtype);
@@ -580,32 +618,47 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     SortView sv = {};
     SideBySide side = {};
     __bf16 *up = nullptr, *bp = nullptr, *zero = nullptr;
+    // fp32 rows that lie right, and too few of them for large tiles: as they are
+    const bool f32 = rowprod_size(p.d_out, g.n) == 0 && f32_lies_right(p.W, p.dtype, p.d_in, p.d_in) &&
+                     f32_lies_right(g.x, p.dtype, g.ldx, p.d_in) && g.n * g.ldx < (1ll << 30);
     if (adapters) {
         sv = sort_carve(w, g.adapter, g.n, p.n_adapters);
         side = side_by_side(3, np, p.rank);
-        up = w.take<__bf16>(g.n * side.kpad);
-        bp = w.take<__bf16>((int64_t)p.n_adapters * p.d_out * side.kpad);
-        zero = w.take<__bf16>(side.kpad);
+        // (the size does not depend on where the rows lie)
+        const int room = std::max(side.kpad, side_f32(p.rank).kpad);
+        up = w.take<__bf16>(g.n * room);
+        bp = w.take<__bf16>((int64_t)p.n_adapters * p.d_out * room);
+        zero = w.take<__bf16>(room);
+        if (f32) side = side_f32(p.rank);
     }
     if (bytes) *bytes = w.used;
     if (!ws) return RAIRS_OK;
 
     const bool use = adapters && g.adapter;
     RowProd rp = {};
-    rowprod_pieces(rp, np, np);
-    rp.ksteps = (int)(pad_to(p.d_in, ROWPROD_K) / ROWPROD_K);
     if (use && (rc = sort_launch(sv, s))) return rc;
-    if ((rc = rairs_operand(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, wroom, rp.P, s))) return rc;
-    if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, xroom, rp.Q, s))) return rc;
+    if (f32) {
+        rowprod_pieces(rp, 1, 1);
+        rp.ksteps = p.d_in / (ROWPROD_K / 2);
+        rp.P = f32_operand(p.W, p.d_in, p.d_out);
+        rp.Q = f32_operand(g.x, g.ldx, g.n);
+        rp.Q.perm = use ? sv.perm : nullptr;
+    } else {
+        rowprod_pieces(rp, np, np);
+        rp.ksteps = (int)(pad_to(p.d_in, ROWPROD_K) / ROWPROD_K);
+        if ((rc = rairs_operand(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, wroom, rp.P, s))) return rc;
+        if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, xroom, rp.Q, s))) return rc;
+    }
     if (use) {
-        ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, 0, up, side};
+        ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side};
         const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
-        if ((rc = p.dtype == RAIRS_BF16 ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s))) return rc;
+        if ((rc = bf ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s))) return rc;
         if ((rc = pack_side_launch(p.B, p.dtype, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, p.n_adapters, side, bp, zero, s))) return rc;
         rp.ad = AdapterPart{up, bp, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.y, g.ldy, 0, p.d_out, g.n, use ? sv.perm : nullptr, g.ytype == RAIRS_BF16, 0};
-    return use ? rowprod_launch_any<true>(rp, e, s) : rowprod_launch_any(rp, e, s);
+    if (f32) return use ? rowprod_launch<TileS, ROW_F32 | ROW_ADAPT>(rp, e, s) : rowprod_launch<TileS, ROW_F32>(rp, e, s);
+    return use ? rowprod_launch_any<ROW_ADAPT>(rp, e, s) : rowprod_launch_any(rp, e, s);
 }
 
 // ---- backward ------------------------------------------------------------------------------------------
@@ -775,11 +828,11 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         const int64_t units = max_units(g.n, na, UNIT_ROWS);
         rc = bf ? transpose_launch<__bf16>(p.B, p.d_out, p.rank, na, bt, s) : transpose_launch<float>(p.B, p.d_out, p.rank, na, bt, s);
         if (rc) return rc;
-        ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, 0, g.dx ? vp : nullptr, side};
+        ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, g.dx ? vp : nullptr, side};
         const bool vec = row_vec(g.dy, g.lddy, p.dtype) && row_vec(bt, p.d_out, p.dtype);
         if ((rc = bf ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s))) return rc;
         if (g.da) {
-            ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, 0, nullptr, side};
+            ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, nullptr, side};
             const bool xvec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
             if ((rc = bf ? shrink_launch<__bf16>(su, units, xvec, s) : shrink_launch<float>(su, units, xvec, s))) return rc;
             if ((rc = bf ? adapter_grads<__bf16>(g, sv, u, v, part, s) : adapter_grads<float>(g, sv, u, v, part, s))) return rc;
@@ -800,5 +853,5 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         rp.ad = AdapterPart{vp, ap, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.dx, g.lddx, 0, p.d_in, g.n, use ? sv.perm : nullptr, bf, 0};
-    return use ? rowprod_launch_any<true>(rp, e, s) : rowprod_launch_any(rp, e, s);
+    return use ? rowprod_launch_any<ROW_ADAPT>(rp, e, s) : rowprod_launch_any(rp, e, s);
 }

@@ -38,6 +38,12 @@ static inline bool rows_lie_right(const void *p, int dtype, int64_t ld, int64_t 
 {
     return dtype == RAIRS_BF16 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld < (1 << 22) && cols % ROWPROD_K == 0;
 }
+// fp32 rows that lie right for the fp32 instruction: whole steps of 32 values
+static inline bool f32_lies_right(const void *p, int dtype, int64_t ld, int64_t cols)
+{
+    return dtype == RAIRS_F32 && (uintptr_t)p % 16 == 0 && ld % 4 == 0 && ld < (1 << 21) && cols % (ROWPROD_K / 2) == 0;
+}
+static inline RowOperand f32_operand(const void *p, int64_t ld, int64_t rows) { return RowOperand{(const __bf16 *)p, 2 * ld, 0, rows, nullptr, nullptr}; }
 static inline int64_t pack_room(int dtype, int64_t rows, int64_t cols) { return rows * pad_to(cols, ROWPROD_K) * dtype_pieces(dtype); }
 int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *room, RowOperand &out,
                   hipStream_t s, uint32_t *flags = nullptr, bool clear = false);

@@ -7,6 +7,10 @@
 // ones first (what is left out is below 2^-23 |P||Q|).  A piece list is only a longer sum, so bf16
 // rows, fp32 rows and byte rows share one kernel.
 //
+// Small products of fp32 rows take the rows as they are and the fp32 matrix instruction (a sixteenth of the
+// bf16 rate, against six products of pieces and the packing): lengths, strides and steps are then counted in
+// units of two bytes all the same, so that a step is 32 values.
+//
 // A workgroup stages 64 values of each of its rows in LDS, fetched straight into LDS by 16-byte loads into a ring
 // of two buffers (large tiles, whose products take longer than a load) or four (small ones).  Such a load writes lane l's bytes at base + 16 l, so the order in LDS is chosen by
 // the address that each lane reads: slot s of row r holds the row's 16-byte chunk s ^ (r & 7), which
@@ -19,11 +23,13 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 
 #define ROWPROD_K 64                // values of a row in LDS at a time
 
 // Rows of bf16 pieces: value k of piece i of row r at p[i * piece + r * ld + k]; ld a multiple of 8, below
-// 2^22, p 16-byte aligned, k up to a multiple of ROWPROD_K readable (zero beyond the row).
+// 2^22, p 16-byte aligned, k up to a multiple of ROWPROD_K readable (zero beyond the row).  Rows of fp32: units of
+// two bytes in place of values.
 struct RowOperand {
     const __bf16 *p;
     int64_t ld, piece;
@@ -73,7 +79,9 @@ template <int PT_, int QT_, int WP_, int WQ_, int ST_>
 struct RowTile {
     static constexpr int PT = PT_, QT = QT_, WP = WP_, WQ = WQ_, NT = 64 * WP * WQ, ST = ST_;
     static constexpr int BP = 16 * PT * WP, BQ = 16 * QT * WQ;
-    static constexpr int LP = BP * 8 / NT, LQ = BQ * 8 / NT;          // 16-byte loads per thread and step
+    static constexpr int LP = BP * 8 / NT, LQ = BQ * 8 / NT ? BQ * 8 / NT : 1;   // 16-byte loads per thread and step
+    static constexpr bool SOME_Q = BQ * 8 < NT;                       // (the first waves alone load Q)
+    static constexpr int LEAST = LP + (SOME_Q ? 0 : LQ);              // loads that every wave makes
     static constexpr int BYTES = (BP + BQ) * 128;                     // of one LDS buffer
 };
 
@@ -88,6 +96,10 @@ typedef RowTile<8, 4, 2, 4, 2> TileL;       // 256 x 256, 8 waves
 typedef RowTile<4, 2, 2, 4, 3> TileM;       // 128 x 128, 8 waves
 typedef RowTile<2, 2, 2, 2, 4> TileS;       // 64 x 64, 4 waves
 typedef RowTile<4, 4, 2, 2, 2> TileW;       // 128 x 128, 4 waves: 64 x 64 to a wave, for epilogues that want that
+// few queries, whose rows' loads are what counts: about 100 KB of them on the way
+typedef RowTile<4, 1, 4, 1, 4> TileF1;      // 256 x 16
+typedef RowTile<4, 2, 4, 1, 4> TileF2;      // 256 x 32
+typedef RowTile<4, 4, 4, 1, 3> TileF4;      // 256 x 64
 static inline int64_t rowprod_tiles(int64_t p, int64_t q, int side) { return ((p + side - 1) / side) * ((q + side - 1) / side); }
 static inline int rowprod_size(int64_t p, int64_t q, int splits = 1)
 {
@@ -97,7 +109,10 @@ static inline int rowprod_size(int64_t p, int64_t q, int splits = 1)
 template <class T>
 struct RowAcc {
     v4f v[T::PT][T::QT];
+    float nrm[T::PT];               // ROW_NORM: this lane's part of the squared norm of row 16 i + (lane & 15) of P
 };
+
+enum { ROW_ADAPT = 1, ROW_F32 = 2, ROW_NORM = 4 };        // with adapters; fp32 rows; norms wanted
 
 // one step's 16-byte chunks of both operands, straight into LDS: a row's place is a 32-bit offset from an
 // address that the workgroup shares
@@ -108,10 +123,11 @@ static __device__ __forceinline__ void rowprod_fetch(char *buf, const char *pb, 
 #pragma unroll
     for (int i = 0; i < T::LP; i++)
         __builtin_amdgcn_global_load_lds((global_void *)(pb + po[i]), (lds_void *)(buf + (i * T::NT + wave * 64) * 16), 16, 0, 0);
+    if (!T::SOME_Q || wave * 64 < T::BQ * 8)                          // uniform
 #pragma unroll
-    for (int i = 0; i < T::LQ; i++)
-        __builtin_amdgcn_global_load_lds((global_void *)(qb + qo[i]), (lds_void *)(buf + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16, 0,
-                                         0);
+        for (int i = 0; i < T::LQ; i++)
+            __builtin_amdgcn_global_load_lds((global_void *)(qb + qo[i]), (lds_void *)(buf + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16,
+                                             0, 0);
 }
 
 // All but the last N loads into LDS of this wave have landed, then every wave's; and every wave has read what it
@@ -127,27 +143,45 @@ static __device__ __forceinline__ void rowprod_landed()
 // where the operand reads of that half are out of its way.  128,000 x 4096 x 1024 at 256 x 256: 854 us so, 859
 // with the loads first, 922 with the loops the other way round; with both halves' operands read first, or
 // products and reads interleaved by hand, 960 to 1,025.
-template <class T, class F>
+template <class T, int FLAGS, class F>
 static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int wq, int lane, RowAcc<T> &acc, const F &fetch)
 {
 #pragma unroll
     for (int kk = 0; kk < 2; kk++) {
         const int slot = ((kk * 4 + (lane >> 4)) ^ (lane & 7)) * 16 + (lane & 15) * 128;
-        v8bf a[T::PT], b[T::QT];
+        v4u a[T::PT], b[T::QT];
 #pragma unroll
-        for (int i = 0; i < T::PT; i++) a[i] = *(const v8bf *)(buf + (wp * T::PT + i) * 2048 + slot);
+        for (int i = 0; i < T::PT; i++) a[i] = *(const v4u *)(buf + (wp * T::PT + i) * 2048 + slot);
 #pragma unroll
-        for (int j = 0; j < T::QT; j++) b[j] = *(const v8bf *)(buf + T::BP * 128 + (wq * T::QT + j) * 2048 + slot);
+        for (int j = 0; j < T::QT; j++) b[j] = *(const v4u *)(buf + T::BP * 128 + (wq * T::QT + j) * 2048 + slot);
 #pragma unroll
-        for (int x = 0; x < T::PT * T::QT; x++) {
-            if (kk == 0 && x == T::PT * T::QT / 2) {
-                __builtin_amdgcn_sched_barrier(0);
-                fetch();
-                __builtin_amdgcn_sched_barrier(0);
+        for (int e = 0; e < (FLAGS & ROW_F32 ? 4 : 1); e++)
+#pragma unroll
+            for (int x = 0; x < T::PT * T::QT; x++) {
+                if (kk == 0 && e == 0 && x == T::PT * T::QT / 2) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    fetch();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const int i = T::PT >= T::QT ? x % T::PT : x / T::QT, j = T::PT >= T::QT ? x / T::PT : x % T::QT;
+                if constexpr (FLAGS & ROW_F32)
+                    acc.v[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i][e]), __uint_as_float(b[j][e]), acc.v[i][j], 0, 0, 0);
+                else
+                    acc.v[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a[i]), __builtin_bit_cast(v8bf, b[j]),
+                                                                          acc.v[i][j], 0, 0, 0);
             }
-            const int i = T::PT >= T::QT ? x % T::PT : x / T::QT, j = T::PT >= T::QT ? x / T::PT : x % T::QT;
-            acc.v[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc.v[i][j], 0, 0, 0);
-        }
+        if constexpr (FLAGS & ROW_NORM)
+#pragma unroll
+            for (int i = 0; i < T::PT; i++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    if constexpr (FLAGS & ROW_F32) {
+                        acc.nrm[i] = fmaf(__uint_as_float(a[i][e]), __uint_as_float(a[i][e]), acc.nrm[i]);
+                    } else {
+                        const v2bf x = __builtin_bit_cast(v2bf, a[i][e]);
+                        acc.nrm[i] = __builtin_amdgcn_fdot2_f32_bf16(x, x, acc.nrm[i], false);
+                    }
+                }
     }
 }
 
@@ -188,9 +222,10 @@ static __device__ __forceinline__ void rowprod_rows(int64_t r0, int64_t rows, in
 // run: epi.begin(state, q0, lane), epi.tile(state, acc, p0, q0, lane, split) per tile, epi.end(state, run, wp,
 // q0, lane): lane l holds, for its tiles (i, j), rows q0 + 16 j + (l & 15) and columns p0 + 16 i +
 // 4 (l >> 4) + 0..3.
-template <class T, class Epi, bool ADAPT>
+template <class T, class Epi, int FLAGS>
 __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
 {
+    constexpr bool ADAPT = FLAGS & ROW_ADAPT;
     extern __shared__ __align__(16) char rowprod_lds[];
     int run, qt, split;
     if (!rowprod_tile(a, run, qt, split)) return;
@@ -312,12 +347,14 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
         for (int i = 0; i < T::PT; i++)
 #pragma unroll
             for (int j = 0; j < T::QT; j++) acc.v[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < T::PT; i++) acc.nrm[i] = 0.0f;
         // (a run of several tiles: a tile's steps; else all that is fetched)
         const int stop = done + (s1 - s0);
         while (ADAPT ? done < total : done < stop) {
             // (this also says that every wave is past the step before, whose buffer the next fetch writes)
-            rowprod_landed<(T::ST - 2) * (T::LP + T::LQ)>();
-            rowprod_step<T>(buf, wp, wq, lane, acc, fetch);
+            rowprod_landed<(T::ST - 2) * T::LEAST>();
+            rowprod_step<T, FLAGS>(buf, wp, wq, lane, acc, fetch);
             buf = buf == rowprod_lds + (T::ST - 1) * T::BYTES ? rowprod_lds : buf + T::BYTES;
             done++;
         }
@@ -342,7 +379,7 @@ static inline int rowprod_run(int64_t ptiles, int64_t qtiles, int slots, double 
 }
 
 // `prun`: p tiles that a workgroup takes one after the other
-template <class T, bool ADAPT = false, class Epi>
+template <class T, int FLAGS = 0, class Epi>
 static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 1)
 {
     a.ptiles = (int)((a.P.rows + T::BP - 1) / T::BP);
@@ -350,7 +387,7 @@ static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 
     a.prun = prun;
     a.pruns = (a.ptiles + prun - 1) / prun;
     if (a.splits < 1) a.splits = 1;
-    auto kern = rowprod_kernel<T, Epi, ADAPT>;
+    auto kern = rowprod_kernel<T, Epi, FLAGS>;
     RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, T::ST * T::BYTES));
     hipLaunchKernelGGL(kern, dim3(rowprod_grid(a)), dim3(T::NT), T::ST * T::BYTES, s, a, epi);
     RAIRS_HIP(hipGetLastError());
@@ -358,11 +395,11 @@ static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 
 }
 
 // the same with the tile chosen by rowprod_size
-template <bool ADAPT = false, class Epi>
+template <int FLAGS = 0, class Epi>
 static int rowprod_launch_any(RowProd &a, const Epi &epi, hipStream_t s)
 {
     const int size = rowprod_size(a.P.rows, a.Q.rows, a.splits > 1 ? a.splits : 1);
-    return size == 2 ? rowprod_launch<TileL, ADAPT>(a, epi, s) : size == 1 ? rowprod_launch<TileM, ADAPT>(a, epi, s) : rowprod_launch<TileS, ADAPT>(a, epi, s);
+    return size == 2 ? rowprod_launch<TileL, FLAGS>(a, epi, s) : size == 1 ? rowprod_launch<TileM, FLAGS>(a, epi, s) : rowprod_launch<TileS, FLAGS>(a, epi, s);
 }
 
 // ---- epilogues -------------------------------------------------------------------------------------
