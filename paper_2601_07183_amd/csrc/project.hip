@@ -12,6 +12,7 @@
 
 #include "fewrows.h"
 #include "query_ops.h"
+#include "rowpack.h"
 
 #define SORT_ROWS 1024              // rows per workgroup of the sort
 #define UNIT_ROWS 32                // rows of one adapter that one workgroup multiplies by A
@@ -132,16 +133,15 @@ __global__ __launch_bounds__(SORT_ROWS) void sort_place_kernel(SortView v)
 // a time, then places them behind the runs before it (in the batch's order, as above).
 #define SORT_ONE_ROWS 16384
 #define SORT_ONE_KEYS 1024
-__global__ __launch_bounds__(1024) void sort_one_kernel(SortView v)
+static __device__ void sort_one(const SortView &v, int32_t *sort_lds)
 {
-    extern __shared__ int32_t sort_lds[];
-    __shared__ int32_t sums[1024];
+    __shared__ int32_t sums[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keys = v.na + 1, bits = 32 - __clz(v.na);
     int32_t *cnt = sort_lds;                                          // [16][keys]
     const int n = (int)v.n;
-    uint16_t *key_of = (uint16_t *)(sort_lds + 16 * keys), *placed = key_of + (n + 1) / 2 * 2;     // [n] both
-    const int per = ((n + 15) / 16 + 63) / 64 * 64;     // rows per wave
-#pragma unroll 4
+    uint16_t *key_of = (uint16_t *)(sort_lds + 16 * keys), *rank_of = key_of + (n + 1) / 2 * 2;    // [n] both; a rank is the row's among its wave's
+    const int per = ((n + 15) / 16 + 63) / 64 * 64;                   // rows per wave
+#pragma unroll 8
     for (int i = tid; i < n; i += 1024) key_of[i] = (uint16_t)sort_key(v, i);
     for (int i = tid; i < 16 * keys; i += 1024) cnt[i] = 0;
     __syncthreads();
@@ -149,7 +149,12 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(SortView v)
     for (int i0 = wave * per; i0 < min((wave + 1) * per, n); i0 += 64) {
         const int key = i0 + lane < n ? key_of[i0 + lane] : -1;
         const unsigned long long m = same_key(key, bits);
-        if (key >= 0 && lane == __ffsll((long long)m) - 1) mine[key] += __popcll(m);
+        const int base = key >= 0 ? mine[key] : 0;
+        wave_lds_sync();
+        if (key >= 0) {
+            rank_of[i0 + lane] = (uint16_t)(base + __popcll(m & ((1ull << lane) - 1ull)));
+            if (lane == __ffsll((long long)m) - 1) mine[key] = base + __popcll(m);
+        }
         wave_lds_sync();
     }
     __syncthreads();
@@ -185,23 +190,10 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(SortView v)
     }
     if (tid == 0) v.first[v.na + 1] = n;
     __syncthreads();
-    for (int i0 = wave * per; i0 < min((wave + 1) * per, n); i0 += 64) {
-        const int key = i0 + lane < n ? key_of[i0 + lane] : -1;
-        const unsigned long long m = same_key(key, bits);
-        const int base = key >= 0 ? mine[key] : 0;
-        wave_lds_sync();
-        if (key >= 0) {
-            const int pos = base + __popcll(m & ((1ull << lane) - 1ull));
-            placed[pos] = (uint16_t)(i0 + lane);                      // (written out in runs: a line per lane would be as many accesses)
-            if (lane == __ffsll((long long)m) - 1) mine[key] = base + __popcll(m);
-        }
-        wave_lds_sync();
-    }
-    __syncthreads();
     for (int i = tid; i < n; i += 1024) {
-        const int r = placed[i], key = key_of[r];
-        v.perm[i] = r;
-        v.of_row[i] = key < v.na ? key : -1;
+        const int key = key_of[i], pos = cnt[i / per * keys + key] + rank_of[i];
+        v.perm[pos] = i;
+        v.of_row[pos] = key < v.na ? key : -1;
     }
 }
 
@@ -225,15 +217,11 @@ static SortView sort_carve(Carve &w, const int32_t *adapter, int64_t n, int na)
     return v;
 }
 
+static bool sorts_in_one(const SortView &v) { return v.n <= SORT_ONE_ROWS && v.na < SORT_ONE_KEYS; }
+static size_t sort_one_lds(const SortView &v) { return (size_t)16 * (v.na + 1) * 4 + (size_t)((v.n + 1) / 2) * 8; }
+
 static int sort_launch(const SortView &v, hipStream_t s)
 {
-    if (v.n <= SORT_ONE_ROWS && v.na < SORT_ONE_KEYS) {
-        const size_t lds = (size_t)16 * (v.na + 1) * 4 + (size_t)((v.n + 1) / 2) * 8;
-        RAIRS_HIP(hipFuncSetAttribute((const void *)sort_one_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(1024), lds, s, v);
-        RAIRS_HIP(hipGetLastError());
-        return RAIRS_OK;
-    }
     const int64_t words = (v.na + 1) * v.nb;
     hipLaunchKernelGGL(clear_words_kernel, dim3((unsigned)((words + WG - 1) / WG)), dim3(WG), 0, s, v.cnt, words);
     hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)v.nb), dim3(SORT_ROWS), 0, s, v);
@@ -301,8 +289,9 @@ struct ShrinkArgs {
 
 // a workgroup per unit; its NW waves share the sum, which is joined in LDS
 template <class S, int RT, int NW, bool VEC>
-__global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs a)
+__global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs one, ShrinkArgs two)
 {
+    const ShrinkArgs &a = blockIdx.y ? two : one;
     __shared__ float part[NW - 1][UNIT_ROWS][16 * RT + 1];    // [wave][row][rank]
     if ((int)blockIdx.x >= *a.nunits) return;
     const int4 unit = a.units[blockIdx.x];
@@ -374,13 +363,14 @@ __global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs a)
 }
 
 template <class S>
-static int shrink_launch(const ShrinkArgs &a, int64_t units, bool vec, hipStream_t s)
+static int shrink_launch(const ShrinkArgs &a, const ShrinkArgs *two, int64_t units, bool vec, hipStream_t s)
 {
-    const dim3 grid((unsigned)units);
+    const dim3 grid((unsigned)units, two ? 2 : 1);
+    const ShrinkArgs &b = two ? *two : a;
     // (four waves where eight would not have the registers)
 #define RAIRS_SHRINK(RT_, NW_)                                                                            \
-    if (vec) hipLaunchKernelGGL((shrink_kernel<S, RT_, NW_, true>), grid, dim3(64 * NW_), 0, s, a);       \
-    else hipLaunchKernelGGL((shrink_kernel<S, RT_, NW_, false>), grid, dim3(64 * NW_), 0, s, a)
+    if (vec) hipLaunchKernelGGL((shrink_kernel<S, RT_, NW_, true>), grid, dim3(64 * NW_), 0, s, a, b);       \
+    else hipLaunchKernelGGL((shrink_kernel<S, RT_, NW_, false>), grid, dim3(64 * NW_), 0, s, a, b)
     if (a.r <= 16) { RAIRS_SHRINK(1, 8); }
     else if (a.r <= 32) { RAIRS_SHRINK(2, 8); }
     else if (a.r <= 64) { RAIRS_SHRINK(4, 4); }
@@ -390,26 +380,35 @@ static int shrink_launch(const ShrinkArgs &a, int64_t units, bool vec, hipStream
     return RAIRS_OK;
 }
 
+// ---- what is laid out before the products ---------------------------------------------------------------
+
 // dst[a][o][t r + j] = piece pb[t] of src[a * batch + o * so + j * sj], zero up to kpad; and the row of
 // zeros behind them
+struct SideJob {
+    const void *src;
+    int64_t batch, so, sj, rows, total;
+    SideBySide side;
+    __bf16 *dst, *zero;
+};
+
 template <class S>
-__global__ __launch_bounds__(WG) void pack_side_kernel(const S *__restrict__ src, int64_t batch, int64_t so, int64_t sj, int64_t rows,
-                                                       int64_t total, SideBySide side, __bf16 *__restrict__ dst, __bf16 *__restrict__ zero)
+static __device__ __forceinline__ void pack_side(const SideJob &j, int64_t block)
 {
-    if (blockIdx.x == 0)
-        for (int k = threadIdx.x; k < side.kpad; k += WG) zero[k] = (__bf16)0.0f;
+    const SideBySide &side = j.side;
+    if (block == 0)
+        for (int k = threadIdx.x; k < side.kpad; k += 1024) j.zero[k] = (__bf16)0.0f;
     // a thread per eight values; the rows of a group of 64 first, so that a transposed source is read along its rows
     const int eights = side.kpad / 8;
-    const int64_t id = (int64_t)blockIdx.x * WG + threadIdx.x, t = id / (64 * eights) * 64 + (id & 63);
-    if (t >= total) return;
+    const int64_t id = block * 1024 + threadIdx.x, t = id / (64 * eights) * 64 + (id & 63);
+    if (t >= j.total) return;
     const int k0 = (int)(id / 64 % eights) * 8;
-    const int64_t a = t / rows, o = t - a * rows;
-    const S *p = src + a * batch + o * so;
+    const int64_t a = t / j.rows, o = t - a * j.rows;
+    const S *p = (const S *)j.src + a * j.batch + o * j.so;
     if (side.f32) {
         v4f x;
 #pragma unroll
-        for (int e = 0; e < 4; e++) x[e] = k0 / 2 + e < side.r ? (float)p[(k0 / 2 + e) * sj] : 0.0f;
-        *(v4f *)(dst + t * side.kpad + k0) = x;
+        for (int e = 0; e < 4; e++) x[e] = k0 / 2 + e < side.r ? (float)p[(k0 / 2 + e) * j.sj] : 0.0f;
+        *(v4f *)(j.dst + t * side.kpad + k0) = x;
         return;
     }
     v8bf x;
@@ -419,24 +418,97 @@ __global__ __launch_bounds__(WG) void pack_side_kernel(const S *__restrict__ src
         __bf16 v = (__bf16)0.0f;
         if (b < side.np) {
             __bf16 pc[3];
-            three_pieces((float)p[(k - b * side.r) * sj], pc);
+            three_pieces((float)p[(k - b * side.r) * j.sj], pc);
             const int w = side.pb[b];
             v = w == 0 ? pc[0] : w == 1 ? pc[1] : pc[2];
         }
         x[e] = v;
     }
-    *(v8bf *)(dst + t * side.kpad + k0) = x;
+    *(v8bf *)(j.dst + t * side.kpad + k0) = x;
 }
 
-static int pack_side_launch(const void *src, int dtype, int64_t batch, int64_t so, int64_t sj, int64_t rows, int64_t adapters,
-                            const SideBySide &side, __bf16 *dst, __bf16 *zero, hipStream_t s)
+// dst[b][c][r] = src[b][r][c], 32 x 32 values
+template <class S>
+static __device__ __forceinline__ void transpose_tile(S (&tile)[32][33], const S *__restrict__ src, int rows, int cols, S *__restrict__ dst,
+                                                      int64_t block)
 {
-    const int64_t total = rows * adapters;
-    const dim3 grid((unsigned)((pad_to(total, 64) * (side.kpad / 8) + WG - 1) / WG));
-    if (dtype == RAIRS_F32)
-        hipLaunchKernelGGL(pack_side_kernel<float>, grid, dim3(WG), 0, s, (const float *)src, batch, so, sj, rows, total, side, dst, zero);
-    else
-        hipLaunchKernelGGL(pack_side_kernel<__bf16>, grid, dim3(WG), 0, s, (const __bf16 *)src, batch, so, sj, rows, total, side, dst, zero);
+    const int rt = (rows + 31) / 32, ct = (cols + 31) / 32;
+    const int64_t batch = block / (rt * ct) * rows * cols;
+    const int in = (int)(block % (rt * ct)), r0 = in % rt * 32, c0 = in / rt * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    if (r0 + y < rows && c0 + x < cols) tile[y][x] = src[batch + (int64_t)(r0 + y) * cols + c0 + x];
+    __syncthreads();
+    if (c0 + y < cols && r0 + x < rows) dst[batch + (int64_t)(c0 + y) * rows + r0 + x] = tile[x][y];
+}
+
+// The sort, which is one workgroup's, and beside it what does not wait for it: the adapters' B (or A) as pieces, W
+// turned, B turned.  One launch after the other they took 20 us more (2,999 rows, 1024 x 960, 32 adapters).
+struct PrepArgs {
+    SortView sort;
+    int sorts;                      // workgroups: 0 or 1
+    unsigned side_blocks, cols_blocks, turn_blocks;
+    SideJob side;
+    const void *w, *b;              // [d_out][d_in], [na][d_out][r]
+    int d_in, d_out, r, vec;
+    __bf16 *wt;
+    int64_t opad;
+    void *bt;
+};
+
+template <class S, int NP>
+__global__ __launch_bounds__(1024) void prep_kernel(PrepArgs a)
+{
+    extern __shared__ __align__(16) char prep_lds[];
+    int64_t block = blockIdx.x;
+    if (block < a.sorts) {
+        sort_one(a.sort, (int32_t *)prep_lds);
+        return;
+    }
+    block -= a.sorts;
+    if (block < a.side_blocks) {
+        pack_side<S>(a.side, block);
+        return;
+    }
+    block -= a.side_blocks;
+    if (block < a.cols_blocks) {
+        const int half = threadIdx.x >> 9;
+        const int64_t rt = a.opad / 64, ct = (a.d_in + 63) / 64, t = block * 2 + half;
+        PackCols<S, NP> *sh = (PackCols<S, NP> *)prep_lds;
+        pack_cols_tile<S, NP, 512>(sh[half], threadIdx.x & 511, t < rt * ct, (const S *)a.w, a.d_in, a.d_out, a.d_in, nullptr, ORDER_SAME, a.vec, a.wt,
+                                   a.opad, a.d_in * a.opad, t % rt * 64, t / rt * 64);
+        return;
+    }
+    block -= a.cols_blocks;
+    transpose_tile<S>(*(S(*)[32][33])prep_lds, (const S *)a.b, a.d_out, a.r, (S *)a.bt, block);
+}
+
+static int prep_launch(PrepArgs &a, int dtype, hipStream_t s)
+{
+    int rc = RAIRS_OK;
+    size_t lds = 0;
+    if (a.sort.n) {
+        a.sorts = sorts_in_one(a.sort);
+        if (a.sorts) lds = sort_one_lds(a.sort);
+        else if ((rc = sort_launch(a.sort, s))) return rc;
+    }
+    if (a.side.dst) a.side_blocks = (unsigned)((pad_to(a.side.total, 64) * (a.side.side.kpad / 8) + 1023) / 1024);
+    if (a.wt) {
+        a.cols_blocks = (unsigned)((a.opad / 64 * ((a.d_in + 63) / 64) + 1) / 2);
+        lds = std::max(lds, dtype == RAIRS_F32 ? 2 * sizeof(PackCols<float, 3>) : 2 * sizeof(PackCols<__bf16, 1>));
+        a.vec = is_vec(a.w, a.d_in, dtype_width(dtype));
+    }
+    if (a.bt) {
+        a.turn_blocks = (unsigned)((a.d_out + 31) / 32 * ((a.r + 31) / 32)) * a.sort.na;
+        lds = std::max(lds, sizeof(float) * 32 * 33);
+    }
+    const unsigned blocks = a.sorts + a.side_blocks + a.cols_blocks + a.turn_blocks;
+    if (!blocks) return RAIRS_OK;
+    if (dtype == RAIRS_F32) {
+        RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<float, 3>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        hipLaunchKernelGGL((prep_kernel<float, 3>), dim3(blocks), dim3(1024), lds, s, a);
+    } else {
+        RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<__bf16, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        hipLaunchKernelGGL((prep_kernel<__bf16, 1>), dim3(blocks), dim3(1024), lds, s, a);
+    }
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
@@ -585,12 +657,14 @@ static int few_shrink(const FewProjectArgs &a, int dtype, hipStream_t s)
 
 // ---- forward -------------------------------------------------------------------------------------------
 
-// Rows straight from memory: up to 256 of them, and what the workgroups read of W and x (a lane's 16 bytes are a
-// cache access each: about 10 TB/s) takes less than the launches of the other way (20 us).
+// Rows straight from memory: up to 64 of them, or 256 where what the workgroups read of W and x (a lane's 16 bytes are a
+// cache access each: about 10 TB/s) takes less than the launches of the other way, 20 us, or with adapters
+// 40: a tile runs over all that its rows have.  This way / the other, us, rank 16: 64 x 4096 x 4096 bf16 23 / 23 and
+// with 32 adapters 30 / 86; 256 x 1024 x 1024 bf16 15 / 17 and 20 / 37; 128 x 2048 x 2048 fp32 27 / 46 and with 100 36 / 139.
 static bool few_rows(const rairs_projection_t &p, int64_t n)
 {
     const double read = (double)((n + 63) / 64) * ((p.d_out + 31) / 32) * 96.0 * p.d_in * dtype_width(p.dtype);
-    return n <= 64 || (n <= FEW_ROWS && read < 200e6);
+    return n <= 64 || (n <= FEW_ROWS && read < (p.n_adapters ? 400e6 : 200e6));
 }
 
 int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t s)
@@ -636,7 +710,12 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
 
     const bool use = adapters && g.adapter;
     RowProd rp = {};
-    if (use && (rc = sort_launch(sv, s))) return rc;
+    if (use) {
+        PrepArgs pa = {};
+        pa.sort = sv;
+        pa.side = SideJob{p.B, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, (int64_t)p.n_adapters * p.d_out, side, bp, zero};
+        if ((rc = prep_launch(pa, p.dtype, s))) return rc;
+    }
     if (f32) {
         rowprod_pieces(rp, 1, 1);
         rp.ksteps = p.d_in / (ROWPROD_K / 2);
@@ -652,8 +731,7 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     if (use) {
         ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side};
         const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
-        if ((rc = bf ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s))) return rc;
-        if ((rc = pack_side_launch(p.B, p.dtype, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, p.n_adapters, side, bp, zero, s))) return rc;
+        if ((rc = bf ? shrink_launch<__bf16>(sa, nullptr, units, vec, s) : shrink_launch<float>(sa, nullptr, units, vec, s))) return rc;
         rp.ad = AdapterPart{up, bp, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.y, g.ldy, 0, p.d_out, g.n, use ? sv.perm : nullptr, g.ytype == RAIRS_BF16, 0};
@@ -663,38 +741,39 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
 
 // ---- backward ------------------------------------------------------------------------------------------
 
-// dst[b][c][r] = src[b][r][c]
-template <class S>
-__global__ __launch_bounds__(WG) void transpose_kernel(const S *__restrict__ src, int rows, int cols, S *__restrict__ dst)
-{
-    __shared__ S tile[32][33];
-    const int64_t batch = (int64_t)blockIdx.z * rows * cols;
-    const int r0 = blockIdx.x * 32, c0 = blockIdx.y * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    for (int i = y; i < 32; i += 8)
-        if (r0 + i < rows && c0 + x < cols) tile[i][x] = src[batch + (int64_t)(r0 + i) * cols + c0 + x];
-    __syncthreads();
-    for (int i = y; i < 32; i += 8)
-        if (c0 + i < cols && r0 + x < rows) dst[batch + (int64_t)(c0 + i) * rows + r0 + x] = tile[x][i];
-}
-
 // Partial sums of an adapter's gradient over a chunk of its rows: sum_rows x[row][i] u[row][j], by the fp32
 // matrix instruction (16 x 16 x 4), whose operands are rows as they lie: a lane takes 16 bytes of one of four
 // rows, its values go into as many products (product t has columns CH c + t), and one rank of u.  Rows are
 // rank-bound small change next to the projection; the fp32 rate is enough and nothing is rounded.  The
 // workgroup's waves take every fourth four of rows and are joined in LDS.
 // part[chunk][j][i], or turned [chunk][i][j].
+struct AdapterGradArgs {            // of A: x and v; of B (turned): dy and u
+    const void *x[2];
+    int64_t ldx[2];
+    const float *u[2];
+    int cols[2];
+    float *part[2];
+    void *out[2];
+    const int32_t *perm, *chunk0;
+    const int4 *chunks;
+    int r, na;
+};
+
 template <class S, int RT, bool VEC>
-__global__ __launch_bounds__(WG) void adapter_grad_kernel(const S *__restrict__ x, int64_t ldx, const int32_t *__restrict__ perm,
-                                                          const float *__restrict__ u, int r, int cols, int turned,
-                                                          const int4 *__restrict__ chunks, const int32_t *__restrict__ nchunks,
-                                                          float *__restrict__ part)
+__global__ __launch_bounds__(WG) void adapter_grad_kernel(AdapterGradArgs a)
 {
+    const int r = a.r, rts = (r + 16 * RT - 1) / (16 * RT), turned = (int)blockIdx.z / rts, cols = a.cols[turned];
+    const S *__restrict__ x = (const S *)a.x[turned];
+    const float *__restrict__ u = a.u[turned];
+    const int64_t ldx = a.ldx[turned];
+    const int32_t *__restrict__ perm = a.perm;
+    if ((int)blockIdx.y * 16 * FewLoad<S>::CH >= cols) return;
     constexpr int CH = FewLoad<S>::CH;
     __shared__ v4f sums[3][CH * RT][64];
-    if ((int)blockIdx.x >= *nchunks) return;
-    const int4 ch = chunks[blockIdx.x];
+    if ((int)blockIdx.x >= a.chunk0[a.na]) return;
+    const int4 ch = a.chunks[blockIdx.x];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, h = lane >> 4;
-    const int i0 = (blockIdx.y * 16 + c) * CH, j0 = blockIdx.z * 16 * RT;
+    const int i0 = (blockIdx.y * 16 + c) * CH, j0 = ((int)blockIdx.z - turned * rts) * 16 * RT;
     v4f acc[CH][RT];
 #pragma unroll
     for (int t = 0; t < CH; t++)
@@ -731,7 +810,7 @@ __global__ __launch_bounds__(WG) void adapter_grad_kernel(const S *__restrict__ 
             for (int j = 0; j < RT; j++) sums[wave - 1][t * RT + j][lane] = acc[t][j];
     __syncthreads();
     if (wave) return;
-    float *o = part + (int64_t)blockIdx.x * r * cols;
+    float *o = a.part[turned] + (int64_t)blockIdx.x * r * cols;
 #pragma unroll
     for (int t = 0; t < CH; t++)
 #pragma unroll
@@ -748,47 +827,32 @@ __global__ __launch_bounds__(WG) void adapter_grad_kernel(const S *__restrict__ 
 
 // an adapter's gradient: its chunks' sums in their order (both lie alike)
 template <class S>
-__global__ __launch_bounds__(WG) void adapter_join_kernel(const float *__restrict__ part, const int32_t *__restrict__ chunk0, int64_t size,
-                                                          S *__restrict__ out)
+__global__ __launch_bounds__(WG) void adapter_join_kernel(AdapterGradArgs g)
 {
     const int a = blockIdx.y;
-    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x;
+    const int64_t size = (int64_t)g.r * g.cols[blockIdx.z], t = (int64_t)blockIdx.x * WG + threadIdx.x;
     if (t >= size) return;
+    const float *part = g.part[blockIdx.z];
     float x = 0.0f;
-    for (int c = chunk0[a]; c < chunk0[a + 1]; c++) x += part[c * size + t];
-    out[a * size + t] = (S)x;
+    for (int c = g.chunk0[a]; c < g.chunk0[a + 1]; c++) x += part[c * size + t];
+    ((S *)g.out[blockIdx.z])[a * size + t] = (S)x;
 }
 
 template <class S>
-static int adapter_grads(const ProjectArgs &g, const SortView &sv, const float *u, const float *v, float *part, hipStream_t s)
+static int adapter_grads(const ProjectArgs &g, const SortView &sv, const float *u, const float *v, float *apart, float *bpart, hipStream_t s)
 {
     const rairs_projection_t &p = g.p;
     const unsigned chunks = (unsigned)max_units(g.n, p.n_adapters, CHUNK_ROWS);
-    const int32_t *nch = sv.chunk0 + p.n_adapters;
-    const int rt = p.rank <= 16 ? 1 : 2;
-    for (int side = 0; side < 2; side++) {
-        const int cols = side ? p.d_out : p.d_in;
-        const S *x = (const S *)(side ? g.dy : g.x);
-        const int64_t ld = side ? g.lddy : g.ldx, size = (int64_t)p.rank * cols;
-        const float *w = side ? u : v;
-        const dim3 grid(chunks, (unsigned)((cols + 16 * FewLoad<S>::CH - 1) / (16 * FewLoad<S>::CH)), (unsigned)((p.rank + 16 * rt - 1) / (16 * rt)));
-        const bool vec = row_vec(x, ld, p.dtype);
-        if (rt == 1 && vec) hipLaunchKernelGGL((adapter_grad_kernel<S, 1, true>), grid, dim3(WG), 0, s, x, ld, sv.perm, w, p.rank, cols, side, sv.chunks, nch, part);
-        else if (rt == 1) hipLaunchKernelGGL((adapter_grad_kernel<S, 1, false>), grid, dim3(WG), 0, s, x, ld, sv.perm, w, p.rank, cols, side, sv.chunks, nch, part);
-        else if (vec) hipLaunchKernelGGL((adapter_grad_kernel<S, 2, true>), grid, dim3(WG), 0, s, x, ld, sv.perm, w, p.rank, cols, side, sv.chunks, nch, part);
-        else hipLaunchKernelGGL((adapter_grad_kernel<S, 2, false>), grid, dim3(WG), 0, s, x, ld, sv.perm, w, p.rank, cols, side, sv.chunks, nch, part);
-        hipLaunchKernelGGL(adapter_join_kernel<S>, dim3((unsigned)((size + WG - 1) / WG), (unsigned)p.n_adapters), dim3(WG), 0, s, part, sv.chunk0, size,
-                           (S *)(side ? g.db : g.da));
-        RAIRS_HIP(hipGetLastError());
-    }
-    return RAIRS_OK;
-}
-
-template <class S>
-static int transpose_launch(const void *src, int rows, int cols, int batches, void *dst, hipStream_t s)
-{
-    hipLaunchKernelGGL(transpose_kernel<S>, dim3((unsigned)((rows + 31) / 32), (unsigned)((cols + 31) / 32), (unsigned)batches), dim3(WG), 0, s,
-                       (const S *)src, rows, cols, (S *)dst);
+    const int rt = p.rank <= 16 ? 1 : 2, most = std::max(p.d_in, p.d_out);
+    const AdapterGradArgs a = {{g.x, g.dy}, {g.ldx, g.lddy}, {v, u}, {p.d_in, p.d_out}, {apart, bpart}, {g.da, g.db}, sv.perm, sv.chunk0, sv.chunks,
+                               p.rank, p.n_adapters};
+    const dim3 grid(chunks, (unsigned)((most + 16 * FewLoad<S>::CH - 1) / (16 * FewLoad<S>::CH)), 2 * (unsigned)((p.rank + 16 * rt - 1) / (16 * rt)));
+    const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(g.dy, g.lddy, p.dtype);
+    if (rt == 1 && vec) hipLaunchKernelGGL((adapter_grad_kernel<S, 1, true>), grid, dim3(WG), 0, s, a);
+    else if (rt == 1) hipLaunchKernelGGL((adapter_grad_kernel<S, 1, false>), grid, dim3(WG), 0, s, a);
+    else if (vec) hipLaunchKernelGGL((adapter_grad_kernel<S, 2, true>), grid, dim3(WG), 0, s, a);
+    else hipLaunchKernelGGL((adapter_grad_kernel<S, 2, false>), grid, dim3(WG), 0, s, a);
+    hipLaunchKernelGGL(adapter_join_kernel<S>, dim3((unsigned)(((int64_t)p.rank * most + WG - 1) / WG), (unsigned)p.n_adapters, 2), dim3(WG), 0, s, a);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
@@ -804,7 +868,7 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     SortView sv = {};
     SideBySide side = {};
     __bf16 *vp = nullptr, *ap = nullptr, *zero = nullptr;
-    float *u = nullptr, *v = nullptr, *part = nullptr;
+    float *u = nullptr, *v = nullptr, *apart = nullptr, *bpart = nullptr;
     char *bt = nullptr;
     if (adapters) {
         sv = sort_carve(w, g.adapter, g.n, na);
@@ -815,7 +879,8 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         u = w.take<float>(g.n * p.rank);
         v = w.take<float>(g.n * p.rank);
         bt = w.take<char>((int64_t)na * p.rank * p.d_out * dtype_width(p.dtype));
-        part = w.take<float>(max_units(g.n, na, CHUNK_ROWS) * p.rank * (p.d_in > p.d_out ? p.d_in : p.d_out));
+        apart = w.take<float>(max_units(g.n, na, CHUNK_ROWS) * p.rank * p.d_in);
+        bpart = w.take<float>(max_units(g.n, na, CHUNK_ROWS) * p.rank * p.d_out);
     }
     if (bytes) *bytes = w.used;
     if (!ws) return RAIRS_OK;
@@ -824,19 +889,23 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     const bool bf = p.dtype == RAIRS_BF16;
     int rc = RAIRS_OK;
     if (use) {
-        if ((rc = sort_launch(sv, s))) return rc;
-        const int64_t units = max_units(g.n, na, UNIT_ROWS);
-        rc = bf ? transpose_launch<__bf16>(p.B, p.d_out, p.rank, na, bt, s) : transpose_launch<float>(p.B, p.d_out, p.rank, na, bt, s);
-        if (rc) return rc;
-        ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, g.dx ? vp : nullptr, side};
-        const bool vec = row_vec(g.dy, g.lddy, p.dtype) && row_vec(bt, p.d_out, p.dtype);
-        if ((rc = bf ? shrink_launch<__bf16>(sa, units, vec, s) : shrink_launch<float>(sa, units, vec, s))) return rc;
-        if (g.da) {
-            ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, nullptr, side};
-            const bool xvec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
-            if ((rc = bf ? shrink_launch<__bf16>(su, units, xvec, s) : shrink_launch<float>(su, units, xvec, s))) return rc;
-            if ((rc = bf ? adapter_grads<__bf16>(g, sv, u, v, part, s) : adapter_grads<float>(g, sv, u, v, part, s))) return rc;
+        PrepArgs pa = {};
+        pa.sort = sv;
+        pa.b = p.B; pa.bt = bt;
+        pa.w = p.W; pa.d_in = p.d_in; pa.d_out = p.d_out; pa.r = p.rank; pa.opad = opad;
+        if (g.dx) {
+            pa.wt = wt;
+            pa.side = SideJob{p.A, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, (int64_t)na * p.d_in, side, ap, zero};
         }
+        if ((rc = prep_launch(pa, p.dtype, s))) return rc;
+        const int64_t units = max_units(g.n, na, UNIT_ROWS);
+        const ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, g.dx ? vp : nullptr, side};
+        const ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, nullptr, side};
+        const bool vec = row_vec(g.dy, g.lddy, p.dtype) && row_vec(bt, p.d_out, p.dtype) &&
+                         (!g.da || (row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype)));
+        if ((rc = bf ? shrink_launch<__bf16>(sa, g.da ? &su : nullptr, units, vec, s) : shrink_launch<float>(sa, g.da ? &su : nullptr, units, vec, s)))
+            return rc;
+        if (g.da && (rc = bf ? adapter_grads<__bf16>(g, sv, u, v, apart, bpart, s) : adapter_grads<float>(g, sv, u, v, apart, bpart, s))) return rc;
     } else if (g.da && adapters) {
         if ((rc = rairs_launch_clear_rows(g.da, na, (int64_t)p.rank * p.d_in, (int64_t)p.rank * p.d_in, p.dtype, s))) return rc;
         if ((rc = rairs_launch_clear_rows(g.db, na, (int64_t)p.rank * p.d_out, (int64_t)p.rank * p.d_out, p.dtype, s))) return rc;
@@ -845,11 +914,10 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     RowProd rp = {};
     rowprod_pieces(rp, np, np);
     rp.ksteps = (int)(opad / ROWPROD_K);
-    if ((rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, ORDER_SAME, wt, opad, s))) return rc;
+    if (!use && (rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, ORDER_SAME, wt, opad, s))) return rc;
     rp.P = RowOperand{wt, opad, p.d_in * opad, p.d_in, nullptr, nullptr};
     if ((rc = rairs_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, yroom, rp.Q, s))) return rc;
     if (use) {
-        if ((rc = pack_side_launch(p.A, p.dtype, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, na, side, ap, zero, s))) return rc;
         rp.ad = AdapterPart{vp, ap, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.dx, g.lddx, 0, p.d_in, g.n, use ? sv.perm : nullptr, bf, 0};

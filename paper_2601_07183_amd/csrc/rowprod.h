@@ -16,6 +16,8 @@
 // the address that each lane reads: slot s of row r holds the row's 16-byte chunk s ^ (r & 7), which
 // keeps a global access 128 bytes long and the operand reads (16 rows, one chunk) free of bank conflicts.
 #pragma once
+#include <algorithm>
+
 #include "device_util.h"
 
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -57,6 +59,7 @@ struct RowProd {
     int splits;                     // workgroups that share a tile's sum
     int ptiles, qtiles;             // tiles, and workgroups along P: each takes prun tiles
     int prun, pruns;
+    int band;                       // q tiles whose workgroups take the runs together
     AdapterPart ad;
 };
 
@@ -185,17 +188,19 @@ static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int
     }
 }
 
-// A workgroup's run of p tiles: neighbouring workgroups of one XCD (they are handed out round robin over
-// the eight) take the q tiles of the same run one after the other, so that its rows come from that
-// XCD's L2 cache after the first.
+// A workgroup's q tile and run of p tiles.  Workgroups are handed out round robin over the eight XCDs, each with
+// its own L2 cache: one XCD takes consecutive ids, and ids go over a band of q tiles, then to the next run, so that
+// what runs on an XCD at a time is about a square of tiles, whose rows its cache fetches once.
 static __device__ __forceinline__ bool rowprod_tile(const RowProd &a, int &run, int &qt, int &split)
 {
-    const uint32_t total = (uint32_t)(a.pruns * a.qtiles * a.splits), per = (total + 7) / 8;
+    const uint32_t all = (uint32_t)(a.pruns * a.qtiles), total = all * a.splits, per = (total + 7) / 8;
     const uint32_t id = (blockIdx.x % 8) * per + blockIdx.x / 8;
     if (blockIdx.x / 8 >= per || id >= total) return false;
-    qt = (int)(id % a.qtiles);
-    run = (int)(id / a.qtiles % a.pruns);
-    split = (int)(id / (a.qtiles * a.pruns));
+    split = (int)(id / all);
+    const uint32_t in = id % all, b = in / (uint32_t)(a.band * a.pruns), rest = in % (uint32_t)(a.band * a.pruns);
+    const uint32_t h = min((uint32_t)a.band, a.qtiles - b * a.band);
+    qt = (int)(b * a.band + rest % h);
+    run = (int)(rest / h);
     return true;
 }
 static inline unsigned rowprod_grid(const RowProd &a)
@@ -387,6 +392,14 @@ static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 
     a.prun = prun;
     a.pruns = (a.ptiles + prun - 1) / prun;
     if (a.splits < 1) a.splits = 1;
+    // the square: of the workgroups that an XCD has at a time, 32 or (small tiles: two a CU) 64
+    const int64_t total = (int64_t)a.pruns * a.qtiles, at_once = std::min<int64_t>((total * a.splits + 7) / 8, T::ST * T::BYTES > 80 * 1024 ? 32 : 64);
+    double least = 1e300;
+    for (int bands = 1; bands <= a.qtiles; bands++) {
+        const int h = (a.qtiles + bands - 1) / bands;
+        const double rows = (double)h * T::BQ + (double)at_once / h * T::BP;
+        if (rows < least) { least = rows; a.band = h; }
+    }
     auto kern = rowprod_kernel<T, Epi, FLAGS>;
     RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, T::ST * T::BYTES));
     hipLaunchKernelGGL(kern, dim3(rowprod_grid(a)), dim3(T::NT), T::ST * T::BYTES, s, a, epi);
