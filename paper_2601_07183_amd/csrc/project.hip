@@ -44,15 +44,20 @@ __global__ __launch_bounds__(WG) void clear_words_kernel(int32_t *p, int64_t n)
     if (i < n) p[i] = 0;
 }
 
-// lanes of the wave with the same key (below 2^bits); key < 0: none
+// lanes of the wave with the same key (below 2^bits, bits <= 13); key < 0: none
 static __device__ __forceinline__ unsigned long long same_key(int key, int bits)
 {
-    unsigned long long m = __ballot(key >= 0);
-    for (int b = 0; b < bits; b++) {
-        const unsigned long long set = __ballot((key >> b) & 1);
-        m &= (key >> b) & 1 ? set : ~set;
+    const unsigned long long any = __ballot(key >= 0);
+    uint32_t lo = (uint32_t)any, hi = (uint32_t)(any >> 32);
+#pragma unroll
+    for (int b = 0; b < 13; b++) {
+        if (b >= bits) break;                                         // uniform
+        const int mine = (int)((uint32_t)key << (31 - b)) >> 31;      // all bits or none
+        const unsigned long long set = __ballot(mine);
+        lo &= ~(mine ^ (uint32_t)set);
+        hi &= ~(mine ^ (uint32_t)(set >> 32));
     }
-    return m;
+    return (unsigned long long)hi << 32 | lo;
 }
 
 __global__ __launch_bounds__(SORT_ROWS) void sort_count_kernel(SortView v)
@@ -190,10 +195,23 @@ static __device__ void sort_one(const SortView &v, int32_t *sort_lds)
     }
     if (tid == 0) v.first[v.na + 1] = n;
     __syncthreads();
+    // (the order goes through LDS and out in runs: written from here, every lane's line would be an access)
+    constexpr int EACH = SORT_ONE_ROWS / 1024;
+    int pos[EACH];
+#pragma unroll
+    for (int u = 0; u < EACH; u++) {
+        const int i = tid + u * 1024;
+        pos[u] = i < n ? cnt[i / per * keys + key_of[i]] + rank_of[i] : 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < EACH; u++)
+        if (tid + u * 1024 < n) rank_of[pos[u]] = (uint16_t)(tid + u * 1024);
+    __syncthreads();
     for (int i = tid; i < n; i += 1024) {
-        const int key = key_of[i], pos = cnt[i / per * keys + key] + rank_of[i];
-        v.perm[pos] = i;
-        v.of_row[pos] = key < v.na ? key : -1;
+        const int r = rank_of[i], key = key_of[r];
+        v.perm[i] = r;
+        v.of_row[i] = key < v.na ? key : -1;
     }
 }
 
