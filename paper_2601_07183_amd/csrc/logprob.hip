@@ -762,7 +762,7 @@ struct GradArgs {
     const int64_t *targets;
     const float *lse, *entropy, *dlogp, *dentropy;
     __bf16 *g, *gt;                 // [n][vc], [vc][npad]; either null
-    int64_t gpiece, gtpiece;
+    PackLayout gto, gtto;
 };
 
 // G = scale (dlogp (1[v = t] - p) - dentropy p (log p + H)) in registers, rounded to bf16 once (bf16
@@ -865,7 +865,7 @@ struct GradEpi {
 #pragma unroll
                     for (int j = 0; j < 4; j++) {
                         const int q = q0 + 16 * j + c;
-                        __bf16 *to = a.g + u * a.gpiece + (int64_t)q * a.vc + p0 + 64 * b + 16 * h;
+                        __bf16 *to = a.g + (int64_t)q * a.gto.ld + (int64_t)((p0 + 64 * b) / 32 + h / 2) * a.gto.block + u * a.gto.piece + 16 * (h & 1);
                         if (q < a.n) {
                             *(v8bf *)to = __builtin_shufflevector(o[0][j], o[1][j], 0, 1, 2, 3, 4, 5, 6, 7);
                             *(v8bf *)(to + 8) = __builtin_shufflevector(o[2][j], o[3][j], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -876,7 +876,8 @@ struct GradEpi {
                     for (int i = 0; i < 4; i++)
 #pragma unroll
                         for (int r = 0; r < 4; r++) {
-                            __bf16 *to = a.gt + u * a.gtpiece + (int64_t)(p0 + 64 * b + 16 * i + 4 * h + r) * a.npad + q0 + 4 * c;
+                            __bf16 *to = a.gt + (int64_t)(p0 + 64 * b + 16 * i + 4 * h + r) * a.gtto.ld + (q0 / 32 + c / 8) * a.gtto.block + u * a.gtto.piece +
+                                         4 * (c & 7);
                             *(v4bf *)to = (v4bf){o[i][0][r], o[i][1][r], o[i][2][r], o[i][3][r]};
                         }
             }
@@ -985,8 +986,11 @@ static int finish_launch(FinishArgs &f, hipStream_t s)
 }
 
 template <bool ENT, int TOP>
-static int stats_launch(RowProd &rp, const StatsArgs &st, bool large, int prun, hipStream_t s)
+static int stats_launch(RowProd &rp, const StatsArgs &st, bool threes, bool large, int prun, hipStream_t s)
 {
+    if (threes)
+        return large ? rowprod_launch<TileT, ROW_THREES>(rp, StatsEpi<ENT, TOP>{st, nullptr, nullptr}, s, prun)
+                     : rowprod_launch<TileW, ROW_THREES>(rp, StatsEpi<ENT, TOP>{st, nullptr, nullptr}, s, prun);
     return large ? rowprod_launch<TileL>(rp, StatsEpi<ENT, TOP>{st, nullptr, nullptr}, s, prun)
                  : rowprod_launch<TileW>(rp, StatsEpi<ENT, TOP>{st, nullptr, nullptr}, s, prun);
 }
@@ -1014,16 +1018,16 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     // rounds of 64 rows per wave, up to 16, for 4,096 waves (four a SIMD) or a multiple
     const int64_t fills = (blocks + 16 * 4096 - 1) / (16 * 4096);
     const int rounds = few ? (int)((blocks + fills * 4096 - 1) / (fills * 4096)) : 1;
-    const bool large = rowprod_size(a.V, a.n) == 2;
-    const int bp = few || large ? 256 : 128, bq = few ? 64 : bp;
+    const bool large = rowprod_size(a.V, a.n) == 2, threes = !few && a.ttype == RAIRS_F32;
+    const int bp = few || large ? 256 : 128, bq = few ? 64 : threes ? 128 : bp;
     const int64_t ptiles = (a.V + bp - 1) / bp, qtiles = (a.n + bq - 1) / bq;
     // (a start costs a few microseconds, a tile 27 at K = 1024 and 256 x 256; one workgroup of the large tile
     // fits a CU, two of the smaller)
     const double ksum = (double)kpad * (dtype_pieces(a.ttype) * dtype_pieces(a.qtype) == 9 ? 6 : dtype_pieces(a.qtype));
-    const int prun = rowprod_run(ptiles, qtiles, few || large ? 256 : 512, few ? 0.3 : 100.0 / (ksum + 200.0), 64);
+    const int prun = rowprod_run(ptiles, qtiles, few || large || threes ? 256 : 512, few ? 0.3 : 100.0 / (ksum + 200.0), 64);
     // (a few queries: by tiles, four waves along P, or rows straight from memory; there is room for either's parts)
     const int runs = (int)((ptiles + prun - 1) / prun), few_parts = (int)((blocks + rounds - 1) / rounds);
-    const int most_parts = few ? std::max(4 * runs, few_parts) : 2 * runs;
+    const int most_parts = few ? std::max(4 * runs, few_parts) : (threes && large ? 4 : 2) * runs;
     // Groups of 16 rows or of 64.  Per query, the smaller ones cost two more operations a row and 8 bytes for 16 rows
     // instead of 4 for 64, about 0.14 ps times V; the larger ones 64 rows of the table for each of the `top`, at about
     // 6 TB/s.  (A few queries: the vector units have nothing else to do.)
@@ -1040,8 +1044,8 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     float *xmax = w.take<float>(few ? most_parts : NORM_WGS);
     uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
     // (packed whether they need it or not, so that the size does not depend on where the rows lie)
-    __bf16 *qroom = few ? nullptr : w.take<__bf16>(pack_room(a.qtype, a.n, kpad));
-    __bf16 *troom = few ? nullptr : w.take<__bf16>(pack_room(a.ttype, a.V, kpad));
+    __bf16 *qroom = few ? nullptr : w.take<__bf16>(pack_room(a.qtype, a.n, a.d));
+    __bf16 *troom = few ? nullptr : w.take<__bf16>(pack_room(a.ttype, a.V, a.d));
     uint32_t *piece_flags = w.take<uint32_t>(2);
     if (bytes) *bytes = w.used;
     if (!ws) return RAIRS_OK;
@@ -1088,18 +1092,17 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
             RAIRS_HIP(hipGetLastError());
         }
         RowProd rp = {};
-        rowprod_pieces(rp, dtype_pieces(a.ttype), dtype_pieces(a.qtype));
-        rp.ksteps = (int)(kpad / ROWPROD_K);
+        rowprod_sums(rp, dtype_pieces(a.ttype), dtype_pieces(a.qtype), threes ? pad_to(a.d, 32) : kpad);
         // (queries of byte vectors are whole numbers as a rule, whose lower pieces are zero: packing them says so, and
         // the products of those pieces are left out)
         const bool flags = a.ttype == RAIRS_U8;
-        if ((rc = rairs_operand(a.table, a.ttype, a.ldt, a.V, a.d, nullptr, troom, rp.P, s, flags ? piece_flags : nullptr, true))) return rc;
-        if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, qroom, rp.Q, s, flags ? piece_flags : nullptr, false))) return rc;
+        if ((rc = rairs_operand(a.table, a.ttype, a.ldt, a.V, a.d, nullptr, threes, troom, rp.P, s, flags ? piece_flags : nullptr, true))) return rc;
+        if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, threes, qroom, rp.Q, s, flags ? piece_flags : nullptr, false))) return rc;
         if (flags) rp.Q.pieces_there = piece_flags;
         const bool ent = a.entropy != nullptr;
-        if (a.top == 0) rc = ent ? stats_launch<true, 0>(rp, st, large, prun, s) : stats_launch<false, 0>(rp, st, large, prun, s);
-        else if (wide) rc = ent ? stats_launch<true, 1>(rp, st, large, prun, s) : stats_launch<false, 1>(rp, st, large, prun, s);
-        else rc = ent ? stats_launch<true, 2>(rp, st, large, prun, s) : stats_launch<false, 2>(rp, st, large, prun, s);
+        if (a.top == 0) rc = ent ? stats_launch<true, 0>(rp, st, threes, large, prun, s) : stats_launch<false, 0>(rp, st, threes, large, prun, s);
+        else if (wide) rc = ent ? stats_launch<true, 1>(rp, st, threes, large, prun, s) : stats_launch<false, 1>(rp, st, threes, large, prun, s);
+        else rc = ent ? stats_launch<true, 2>(rp, st, threes, large, prun, s) : stats_launch<false, 2>(rp, st, threes, large, prun, s);
         if (rc) return rc;
     }
     FinishArgs f = {};
@@ -1123,18 +1126,26 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
 #define GRAD_CHUNK_BYTES (1ll << 30)
 
 template <int NP, bool ENT>
-static int grad_launch(RowProd &rp, const GradArgs &ga, hipStream_t s)
+static int grad_launch(RowProd &rp, const GradArgs &ga, bool threes, hipStream_t s)
 {
+    if constexpr (NP == 3)
+        if (threes)
+            return rowprod_size(rp.P.rows, rp.Q.rows) == 2 ? rowprod_launch<TileT, ROW_THREES>(rp, GradEpi<NP, ENT>{ga}, s)
+                                                           : rowprod_launch<TileW, ROW_THREES>(rp, GradEpi<NP, ENT>{ga}, s);
+    // (three pieces of bytes' gradients: 128 x 128 alone, whose pieces fit the registers)
+    if constexpr (NP == 3) return rowprod_launch<TileW>(rp, GradEpi<NP, ENT>{ga}, s);
+    else
     return rowprod_size(rp.P.rows, rp.Q.rows) == 2 ? rowprod_launch<TileL>(rp, GradEpi<NP, ENT>{ga}, s) : rowprod_launch<TileW>(rp, GradEpi<NP, ENT>{ga}, s);
 }
 
 int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
 {
     const int np = dtype_pieces(a.qtype), tp = dtype_pieces(a.ttype);
-    const int64_t kpad = pad_to(a.d, ROWPROD_K), npad = pad_to(a.n, ROWPROD_K), dpad = pad_to(a.d, 4);
+    const bool threes = tp == 3;
+    const int64_t kpad = pad_to(a.d, threes ? 32 : ROWPROD_K), npad = pad_to(a.n, ROWPROD_K), dpad = pad_to(a.d, 4);
     const bool need_dt = a.dtable != nullptr, need_dq = a.dq != nullptr;
     int64_t vc = GRAD_CHUNK_BYTES / (2 * np * npad) / 1024 * 1024;
-    vc = vc < 1024 ? 1024 : vc;
+    vc = vc < 1024 ? 1024 : std::min<int64_t>(vc, 1 << 20);           // (rows of threes: below 2^22 values)
     const int64_t chunks = (a.V + vc - 1) / vc;
     vc = pad_to((a.V + chunks - 1) / chunks, ROWPROD_K);              // of about one size
     // the queries' product: its sum over the chunk is cut so that there are workgroups for every CU, of large tiles if
@@ -1145,8 +1156,8 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     if (splits * tm < 160) splits = std::min((512 + ts - 1) / ts, vc / 512);
     if (splits < 1) splits = 1;
     Carve w(ws);
-    __bf16 *qroom = w.take<__bf16>(pack_room(a.qtype, a.n, kpad));
-    __bf16 *troom = w.take<__bf16>(pack_room(a.ttype, vc, kpad));
+    __bf16 *qroom = w.take<__bf16>(pack_room(a.qtype, a.n, a.d));
+    __bf16 *troom = w.take<__bf16>(pack_room(a.ttype, vc, a.d));
     __bf16 *tcols = need_dq ? w.take<__bf16>((int64_t)a.d * vc * tp) : nullptr;
     __bf16 *qcols = need_dt ? w.take<__bf16>((int64_t)a.d * npad * np) : nullptr;
     __bf16 *g = need_dq ? w.take<__bf16>(a.n * vc * np) : nullptr;
@@ -1161,53 +1172,52 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     const uint32_t *seen_by_any = any_live(a, seen, s, &rc);
     if (rc) return rc;
     RowOperand Q = {};
-    if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, qroom, Q, s))) return rc;
+    const PackLayout qto = pack_layout(a.d, npad, threes);
+    if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, threes, qroom, Q, s))) return rc;
     if (need_dt) {
         hipLaunchKernelGGL(active_rows_kernel, dim3((unsigned)((a.n + WG - 1) / WG)), dim3(WG), 0, s, a.n, a.V, a.targets, a.live, a.ld_live,
                            a.dlogp, a.dentropy, active);
         RAIRS_HIP(hipGetLastError());
-        if ((rc = rairs_launch_pack_cols(a.q, a.qtype, a.ldq, a.n, a.d, active, ORDER_QUERIES, qcols, npad, s))) return rc;
+        if ((rc = rairs_launch_pack_cols(a.q, a.qtype, a.ldq, a.n, a.d, active, ORDER_QUERIES, qcols, npad, qto, s))) return rc;
     }
     for (int64_t v0 = 0; v0 < a.V; v0 += vc) {
         const int64_t rows = a.V - v0 < vc ? a.V - v0 : vc, cpad = pad_to(rows, ROWPROD_K);
         const char *t = (const char *)a.table + v0 * a.ldt * dtype_width(a.ttype);
         RowProd rp = {};
-        rowprod_pieces(rp, tp, np);
-        rp.ksteps = (int)(kpad / ROWPROD_K);
+        rowprod_sums(rp, tp, np, kpad);
         rp.Q = Q;
-        if ((rc = rairs_operand(t, a.ttype, a.ldt, rows, a.d, nullptr, troom, rp.P, s))) return rc;
+        if ((rc = rairs_operand(t, a.ttype, a.ldt, rows, a.d, nullptr, threes, troom, rp.P, s))) return rc;
         GradArgs ga = {};
         ga.n = (int)a.n; ga.V = (int)a.V; ga.v0 = (int)v0; ga.vc = (int)cpad; ga.npad = (int)npad;
         ga.scale = a.scale;
         ga.live = a.live; ga.ld_live = a.ld_live; ga.targets = a.targets;
         ga.lse = a.lse_in; ga.entropy = a.entropy_in; ga.dlogp = a.dlogp; ga.dentropy = a.dentropy;
         ga.g = g; ga.gt = gt;
-        ga.gpiece = a.n * cpad; ga.gtpiece = cpad * npad;
+        ga.gto = pack_layout(a.n, cpad, threes); ga.gtto = pack_layout(cpad, npad, threes);
         const bool ent = a.dentropy != nullptr;
-        if (np == 3) rc = ent ? grad_launch<3, true>(rp, ga, s) : grad_launch<3, false>(rp, ga, s);
-        else rc = ent ? grad_launch<1, true>(rp, ga, s) : grad_launch<1, false>(rp, ga, s);
+        if (np == 3) rc = ent ? grad_launch<3, true>(rp, ga, threes, s) : grad_launch<3, false>(rp, ga, threes, s);
+        else rc = ent ? grad_launch<1, true>(rp, ga, threes, s) : grad_launch<1, false>(rp, ga, threes, s);
         if (rc) return rc;
         if (need_dq) {
+            const PackLayout tto = pack_layout(a.d, cpad, threes);
             // (rows that nobody sees are zero here: their G is zero, and they may hold anything)
-            if ((rc = rairs_launch_pack_cols(t, a.ttype, a.ldt, rows, a.d, seen_by_any ? seen_by_any + v0 / 32 : nullptr, ORDER_TABLE, tcols, cpad, s)))
+            if ((rc = rairs_launch_pack_cols(t, a.ttype, a.ldt, rows, a.d, seen_by_any ? seen_by_any + v0 / 32 : nullptr, ORDER_TABLE, tcols, cpad, tto, s)))
                 return rc;
             RowProd dp = {};
-            rowprod_pieces(dp, tp, np);
-            dp.P = RowOperand{tcols, cpad, a.d * cpad, a.d, nullptr, nullptr};
-            dp.Q = RowOperand{g, cpad, a.n * cpad, a.n, nullptr, nullptr};
-            dp.ksteps = (int)(cpad / ROWPROD_K);
+            rowprod_sums(dp, tp, np, cpad);
+            dp.P = RowOperand{tcols, tto.ld, tto.piece, a.d, nullptr, nullptr};
+            dp.Q = RowOperand{g, ga.gto.ld, ga.gto.piece, a.n, nullptr, nullptr};
             dp.splits = (int)splits;
             StoreEpi e = {sums, dpad, a.n * dpad, a.d, a.n, nullptr, 0, v0 > 0};
-            if ((rc = rowprod_launch_any(dp, e, s))) return rc;
+            if ((rc = threes ? rowprod_launch_any<ROW_THREES>(dp, e, s) : rowprod_launch_any(dp, e, s))) return rc;
         }
         if (need_dt) {
             RowProd dp = {};
-            rowprod_pieces(dp, np, np);
-            dp.P = RowOperand{qcols, npad, a.d * npad, a.d, nullptr, nullptr};
-            dp.Q = RowOperand{gt, npad, cpad * npad, rows, nullptr, nullptr};
-            dp.ksteps = (int)(npad / ROWPROD_K);
+            rowprod_sums(dp, np, np, npad);
+            dp.P = RowOperand{qcols, qto.ld, qto.piece, a.d, nullptr, nullptr};
+            dp.Q = RowOperand{gt, ga.gtto.ld, ga.gtto.piece, rows, nullptr, nullptr};
             StoreEpi e = {(char *)a.dtable + v0 * a.lddt * dtype_width(a.ttype), a.lddt, 0, a.d, rows, nullptr, a.ttype == RAIRS_BF16, 0};
-            if ((rc = rowprod_launch_any(dp, e, s))) return rc;
+            if ((rc = threes ? rowprod_launch_any<ROW_THREES>(dp, e, s) : rowprod_launch_any(dp, e, s))) return rc;
         }
     }
     if (need_dq) {

@@ -251,45 +251,28 @@ static int sort_launch(const SortView &v, hipStream_t s)
 
 // ---- u = s_a A_a x for runs of rows of one adapter ---------------------------------------------------
 
-// products of pieces of u and of B (or A) laid side by side: columns t r .. t r + r - 1 hold piece pu[t]
-// of u against piece pb[t]
-struct SideBySide {
-    int np, r, kpad;                // kpad: units of two bytes
-    int f32;                        // u and B as they are (np = 1), for the fp32 instruction
-    uint8_t pu[6], pb[6];
+// u (rows) and B or A (columns) as operands of the large product.  bf16: u's three pieces side by side, the smallest
+// first, against three times B.  fp32: threes like the rows, or (F32) values for the fp32 instruction.
+enum { SIDE_BF16, SIDE_THREES, SIDE_F32 };
+struct Side {
+    int mode, r, kpad;              // kpad: units of two bytes
 };
 
-static SideBySide side_by_side(int upieces, int bpieces, int r)
+static Side side_of(int mode, int r)
 {
-    SideBySide x = {};
-    RowProd rp = {};
-    rowprod_pieces(rp, bpieces, upieces);
-    x.np = rp.nseg;
-    x.r = r;
-    x.kpad = (int)pad_to(x.np * r, ROWPROD_K);
-    for (int t = 0; t < rp.nseg; t++) {
-        x.pb[t] = (rp.sp >> (4 * t)) & 15;
-        x.pu[t] = (rp.sq >> (4 * t)) & 15;
-    }
-    return x;
+    return Side{mode, r, (int)(mode == SIDE_BF16 ? pad_to(3 * r, ROWPROD_K) : mode == SIDE_THREES ? 3 * pad_to(r, 32) : 2 * pad_to(r, 32))};
 }
 
-static SideBySide side_f32(int r)
+// place k of a row of u (ROWS) or of B, whose values are at(j)
+template <bool ROWS, class F>
+static __device__ __forceinline__ __bf16 side_piece(const Side &side, int k, const F &at)
 {
-    SideBySide x = {};
-    x.np = 1;
-    x.r = r;
-    x.kpad = 2 * (int)pad_to(r, ROWPROD_K / 2);
-    x.f32 = 1;
-    return x;
-}
-
-static __device__ __forceinline__ void three_pieces(float x, __bf16 (&o)[3])
-{
-    o[0] = (__bf16)x;
-    const float r = x - (float)o[0];
-    o[1] = (__bf16)r;
-    o[2] = (__bf16)(r - (float)o[1]);
+    const bool threes = side.mode == SIDE_THREES;
+    const int j = threes ? k / 96 * 32 + k % 32 : k % side.r, piece = threes ? k % 96 / 32 : ROWS ? 2 - k / side.r : 0;
+    if (threes ? j >= side.r : k >= 3 * side.r) return (__bf16)0.0f;
+    __bf16 pc[3];
+    split_pieces<3>(at(j), pc);
+    return piece == 0 ? pc[0] : piece == 1 ? pc[1] : pc[2];
 }
 
 struct ShrinkArgs {
@@ -302,7 +285,7 @@ struct ShrinkArgs {
     const int32_t *nunits;
     float *u;                       // [n][r] in sorted order, or null
     __bf16 *up;                     // [n][kpad] in sorted order, or null
-    SideBySide side;
+    Side side;
 };
 
 // a workgroup per unit; its NW waves share the sum, which is joined in LDS
@@ -359,7 +342,7 @@ __global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs one, ShrinkA
             a.u[(int64_t)(unit.y + i) * a.r + j] = part[0][i][j];
         }
     if (!a.up) return;
-    if (a.side.f32) {
+    if (a.side.mode == SIDE_F32) {
         const int k = a.side.kpad / 2;
         for (int t = threadIdx.x; t < unit.z * k; t += 64 * NW) {
             const int i = t / k, j = t - i * k;
@@ -368,15 +351,8 @@ __global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs one, ShrinkA
         return;
     }
     for (int t = threadIdx.x; t < unit.z * a.side.kpad; t += 64 * NW) {
-        const int i = t / a.side.kpad, k = t - i * a.side.kpad, b = k / a.r;
-        __bf16 o = (__bf16)0.0f;
-        if (b < a.side.np) {
-            __bf16 pc[3];
-            three_pieces(part[0][i][k - b * a.r], pc);
-            const int w = a.side.pu[b];
-            o = w == 0 ? pc[0] : w == 1 ? pc[1] : pc[2];
-        }
-        a.up[(int64_t)(unit.y + i) * a.side.kpad + k] = o;
+        const int i = t / a.side.kpad, k = t - i * a.side.kpad;
+        a.up[(int64_t)(unit.y + i) * a.side.kpad + k] = side_piece<true>(a.side, k, [&](int j) { return part[0][i][j]; });
     }
 }
 
@@ -400,19 +376,18 @@ static int shrink_launch(const ShrinkArgs &a, const ShrinkArgs *two, int64_t uni
 
 // ---- what is laid out before the products ---------------------------------------------------------------
 
-// dst[a][o][t r + j] = piece pb[t] of src[a * batch + o * so + j * sj], zero up to kpad; and the row of
-// zeros behind them
+// row a * rows + o of dst: src[a * batch + o * so + j * sj], j < r, as the side wants it; and the row of zeros
 struct SideJob {
     const void *src;
     int64_t batch, so, sj, rows, total;
-    SideBySide side;
+    Side side;
     __bf16 *dst, *zero;
 };
 
 template <class S>
 static __device__ __forceinline__ void pack_side(const SideJob &j, int64_t block)
 {
-    const SideBySide &side = j.side;
+    const Side &side = j.side;
     if (block == 0)
         for (int k = threadIdx.x; k < side.kpad; k += 1024) j.zero[k] = (__bf16)0.0f;
     // a thread per eight values; the rows of a group of 64 first, so that a transposed source is read along its rows
@@ -422,7 +397,7 @@ static __device__ __forceinline__ void pack_side(const SideJob &j, int64_t block
     const int k0 = (int)(id / 64 % eights) * 8;
     const int64_t a = t / j.rows, o = t - a * j.rows;
     const S *p = (const S *)j.src + a * j.batch + o * j.so;
-    if (side.f32) {
+    if (side.mode == SIDE_F32) {
         v4f x;
 #pragma unroll
         for (int e = 0; e < 4; e++) x[e] = k0 / 2 + e < side.r ? (float)p[(k0 / 2 + e) * j.sj] : 0.0f;
@@ -431,17 +406,7 @@ static __device__ __forceinline__ void pack_side(const SideJob &j, int64_t block
     }
     v8bf x;
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-        const int k = k0 + e, b = k / side.r;
-        __bf16 v = (__bf16)0.0f;
-        if (b < side.np) {
-            __bf16 pc[3];
-            three_pieces((float)p[(k - b * side.r) * j.sj], pc);
-            const int w = side.pb[b];
-            v = w == 0 ? pc[0] : w == 1 ? pc[1] : pc[2];
-        }
-        x[e] = v;
-    }
+    for (int e = 0; e < 8; e++) x[e] = side_piece<false>(side, k0 + e, [&](int w) { return (float)p[w * j.sj]; });
     *(v8bf *)(j.dst + t * side.kpad + k0) = x;
 }
 
@@ -469,6 +434,7 @@ struct PrepArgs {
     int d_in, d_out, r, vec;
     __bf16 *wt;
     int64_t opad;
+    PackLayout wto;
     void *bt;
 };
 
@@ -492,7 +458,7 @@ __global__ __launch_bounds__(1024) void prep_kernel(PrepArgs a)
         const int64_t rt = a.opad / 64, ct = (a.d_in + 63) / 64, t = block * 2 + half;
         PackCols<S, NP> *sh = (PackCols<S, NP> *)prep_lds;
         pack_cols_tile<S, NP, 512>(sh[half], threadIdx.x & 511, t < rt * ct, (const S *)a.w, a.d_in, a.d_out, a.d_in, nullptr, ORDER_SAME, a.vec, a.wt,
-                                   a.opad, a.d_in * a.opad, t % rt * 64, t / rt * 64);
+                                   a.opad, a.wto, t % rt * 64, t / rt * 64);
         return;
     }
     block -= a.cols_blocks;
@@ -675,6 +641,12 @@ static int few_shrink(const FewProjectArgs &a, int dtype, hipStream_t s)
 
 // ---- forward -------------------------------------------------------------------------------------------
 
+static int large_product(RowProd &rp, const StoreEpi &e, bool bf, bool adapters, hipStream_t s)
+{
+    if (bf) return adapters ? rowprod_launch_any<ROW_ADAPT>(rp, e, s) : rowprod_launch_any(rp, e, s);
+    return adapters ? rowprod_launch_any<ROW_THREES | ROW_ADAPT>(rp, e, s) : rowprod_launch_any<ROW_THREES>(rp, e, s);
+}
+
 // Rows straight from memory: up to 64 of them, or 256 where what the workgroups read of W and x (a lane's 16 bytes are a
 // cache access each: about 10 TB/s) takes less than the launches of the other way, 20 us, or with adapters
 // 40: a tile runs over all that its rows have.  This way / the other, us, rank 16: 64 x 4096 x 4096 bf16 23 / 23 and
@@ -708,20 +680,19 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     const int np = dtype_pieces(p.dtype);
     __bf16 *xroom = w.take<__bf16>(pack_room(p.dtype, g.n, p.d_in)), *wroom = w.take<__bf16>(pack_room(p.dtype, p.d_out, p.d_in));
     SortView sv = {};
-    SideBySide side = {};
+    Side side = {};
     __bf16 *up = nullptr, *bp = nullptr, *zero = nullptr;
     // fp32 rows that lie right, and too few of them for large tiles: as they are
     const bool f32 = rowprod_size(p.d_out, g.n) == 0 && f32_lies_right(p.W, p.dtype, p.d_in, p.d_in) &&
                      f32_lies_right(g.x, p.dtype, g.ldx, p.d_in) && g.n * g.ldx < (1ll << 30);
     if (adapters) {
         sv = sort_carve(w, g.adapter, g.n, p.n_adapters);
-        side = side_by_side(3, np, p.rank);
+        side = side_of(bf ? SIDE_BF16 : f32 ? SIDE_F32 : SIDE_THREES, p.rank);
         // (the size does not depend on where the rows lie)
-        const int room = std::max(side.kpad, side_f32(p.rank).kpad);
+        const int room = bf ? side.kpad : side_of(SIDE_THREES, p.rank).kpad;
         up = w.take<__bf16>(g.n * room);
         bp = w.take<__bf16>((int64_t)p.n_adapters * p.d_out * room);
         zero = w.take<__bf16>(room);
-        if (f32) side = side_f32(p.rank);
     }
     if (bytes) *bytes = w.used;
     if (!ws) return RAIRS_OK;
@@ -741,10 +712,9 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         rp.Q = f32_operand(g.x, g.ldx, g.n);
         rp.Q.perm = use ? sv.perm : nullptr;
     } else {
-        rowprod_pieces(rp, np, np);
-        rp.ksteps = (int)(pad_to(p.d_in, ROWPROD_K) / ROWPROD_K);
-        if ((rc = rairs_operand(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, wroom, rp.P, s))) return rc;
-        if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, xroom, rp.Q, s))) return rc;
+        rowprod_sums(rp, np, np, pad_to(p.d_in, bf ? ROWPROD_K : 32));
+        if ((rc = rairs_operand(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, !bf, wroom, rp.P, s))) return rc;
+        if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, !bf, xroom, rp.Q, s))) return rc;
     }
     if (use) {
         ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side};
@@ -754,7 +724,7 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     }
     StoreEpi e = {g.y, g.ldy, 0, p.d_out, g.n, use ? sv.perm : nullptr, g.ytype == RAIRS_BF16, 0};
     if (f32) return use ? rowprod_launch<TileS, ROW_F32 | ROW_ADAPT>(rp, e, s) : rowprod_launch<TileS, ROW_F32>(rp, e, s);
-    return use ? rowprod_launch_any<ROW_ADAPT>(rp, e, s) : rowprod_launch_any(rp, e, s);
+    return large_product(rp, e, bf, use, s);
 }
 
 // ---- backward ------------------------------------------------------------------------------------------
@@ -879,18 +849,18 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
 {
     const rairs_projection_t &p = g.p;
     const int np = dtype_pieces(p.dtype), na = p.n_adapters;
-    const bool adapters = na > 0;
+    const bool adapters = na > 0, bf = p.dtype == RAIRS_BF16;
     const int64_t opad = pad_to(p.d_out, ROWPROD_K);
     Carve w(ws);
     __bf16 *yroom = w.take<__bf16>(pack_room(p.dtype, g.n, p.d_out)), *wt = w.take<__bf16>((int64_t)p.d_in * opad * np);
     SortView sv = {};
-    SideBySide side = {};
+    Side side = {};
     __bf16 *vp = nullptr, *ap = nullptr, *zero = nullptr;
     float *u = nullptr, *v = nullptr, *apart = nullptr, *bpart = nullptr;
     char *bt = nullptr;
     if (adapters) {
         sv = sort_carve(w, g.adapter, g.n, na);
-        side = side_by_side(3, np, p.rank);
+        side = side_of(bf ? SIDE_BF16 : SIDE_THREES, p.rank);
         vp = w.take<__bf16>(g.n * side.kpad);
         ap = w.take<__bf16>((int64_t)na * p.d_in * side.kpad);
         zero = w.take<__bf16>(side.kpad);
@@ -904,13 +874,13 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     if (!ws) return RAIRS_OK;
 
     const bool use = adapters && g.adapter && g.n > 0;
-    const bool bf = p.dtype == RAIRS_BF16;
+    const PackLayout wto = pack_layout(p.d_in, opad, !bf);
     int rc = RAIRS_OK;
     if (use) {
         PrepArgs pa = {};
         pa.sort = sv;
         pa.b = p.B; pa.bt = bt;
-        pa.w = p.W; pa.d_in = p.d_in; pa.d_out = p.d_out; pa.r = p.rank; pa.opad = opad;
+        pa.w = p.W; pa.d_in = p.d_in; pa.d_out = p.d_out; pa.r = p.rank; pa.opad = opad; pa.wto = wto;
         if (g.dx) {
             pa.wt = wt;
             pa.side = SideJob{p.A, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, (int64_t)na * p.d_in, side, ap, zero};
@@ -930,14 +900,13 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     }
     if (!g.dx || g.n == 0) return RAIRS_OK;
     RowProd rp = {};
-    rowprod_pieces(rp, np, np);
-    rp.ksteps = (int)(opad / ROWPROD_K);
-    if (!use && (rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, ORDER_SAME, wt, opad, s))) return rc;
-    rp.P = RowOperand{wt, opad, p.d_in * opad, p.d_in, nullptr, nullptr};
-    if ((rc = rairs_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, yroom, rp.Q, s))) return rc;
+    rowprod_sums(rp, np, np, opad);
+    if (!use && (rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, ORDER_SAME, wt, opad, wto, s))) return rc;
+    rp.P = RowOperand{wt, wto.ld, 0, p.d_in, nullptr, nullptr};
+    if ((rc = rairs_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, !bf, yroom, rp.Q, s))) return rc;
     if (use) {
         rp.ad = AdapterPart{vp, ap, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.dx, g.lddx, 0, p.d_in, g.n, use ? sv.perm : nullptr, bf, 0};
-    return use ? rowprod_launch_any<ROW_ADAPT>(rp, e, s) : rowprod_launch_any(rp, e, s);
+    return large_product(rp, e, bf, use, s);
 }

@@ -20,16 +20,26 @@ struct Carve {
     }
 };
 
+// Where packed values go: value k of piece u of row r at r * ld + k / 32 * block + u * piece + k % 32
+struct PackLayout {
+    int64_t ld, piece;
+    int block;
+};
+// pieces one after the other, or (threes) together in every 32 values; kpad a multiple of 32
+static inline PackLayout pack_layout(int64_t rows, int64_t kpad, bool threes)
+{
+    return threes ? PackLayout{3 * kpad, 32, 96} : PackLayout{kpad, rows * kpad, 32};
+}
 // rows of a matrix as bf16 pieces with rows of kpad values, zero from `cols` on (and where live says so)
 // (perm: row r is src's row perm[r]; flags[i], if given: cleared if `clear`, else set if piece i + 1 of any value is
 // not zero)
 int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *dst,
-                           int64_t kpad, hipStream_t s, uint32_t *flags = nullptr, bool clear = false);
+                           int64_t kpad, PackLayout to, hipStream_t s, uint32_t *flags, bool clear);
 // the same, transposed: dst[c][place of r] = src[r][c], zero for r in [rows, rpad) and where live says so; rows keep
-// their places (order 0), or change them among their 64 as the gradient of the logits does (rowpack.hip)
+// their places (order 0), or change them among their 64 as the gradient of the logits does (rowpack.h)
 enum { ORDER_SAME = 0, ORDER_TABLE = 1, ORDER_QUERIES = 2 };
 int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, int order, __bf16 *dst,
-                           int64_t rpad, hipStream_t s);
+                           int64_t rpad, PackLayout to, hipStream_t s);
 
 // A matrix as an operand of rowprod: bf16 rows that lie right already are taken where they are, others
 // are packed into `room` (pack_room elements of it).  With a permutation (the product's row r is row
@@ -45,8 +55,16 @@ static inline bool f32_lies_right(const void *p, int dtype, int64_t ld, int64_t 
 }
 static inline RowOperand f32_operand(const void *p, int64_t ld, int64_t rows) { return RowOperand{(const __bf16 *)p, 2 * ld, 0, rows, nullptr, nullptr}; }
 static inline int64_t pack_room(int dtype, int64_t rows, int64_t cols) { return rows * pad_to(cols, ROWPROD_K) * dtype_pieces(dtype); }
-int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *room, RowOperand &out,
-                  hipStream_t s, uint32_t *flags = nullptr, bool clear = false);
+// (threes: both operands of the product are fp32)
+int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, bool threes, __bf16 *room,
+                  RowOperand &out, hipStream_t s, uint32_t *flags = nullptr, bool clear = false);
+// the products of an np-piece operand with an nq-piece one over kpad values
+static inline void rowprod_sums(RowProd &rp, int np, int nq, int64_t kpad)
+{
+    const bool threes = np == 3 && nq == 3;
+    rowprod_pieces(rp, threes ? 1 : np, threes ? 1 : nq);
+    rp.ksteps = (int)(kpad / (threes ? 32 : ROWPROD_K));
+}
 
 struct LogprobArgs {
     const void *q, *table;

@@ -58,7 +58,7 @@ struct PackCols {
 template <class S, int NP, int NT>
 static __device__ __forceinline__ void pack_cols_tile(PackCols<S, NP> &sh, int tid, bool inside, const S *__restrict__ src, int64_t ld, int64_t rows,
                                                       int64_t cols, const uint32_t *__restrict__ live, int order, int vec, __bf16 *__restrict__ dst,
-                                                      int64_t rpad, int64_t piece, int64_t r0, int64_t c0)
+                                                      int64_t rpad, const PackLayout &to, int64_t r0, int64_t c0)
 {
 #pragma unroll
     for (int h = 0; h < 512 / NT; h++) {
@@ -81,7 +81,7 @@ static __device__ __forceinline__ void pack_cols_tile(PackCols<S, NP> &sh, int t
         if (inside && c0 + c < cols && r0 + i0 < rpad)
 #pragma unroll
             for (int u = 0; u < NP; u++)
-                *(v8bf *)(dst + u * piece + (c0 + c) * rpad + r0 + i0) = *(const v8bf *)&sh.tile[u][c][i0];
+                *(v8bf *)(dst + (c0 + c) * to.ld + (r0 + i0) / 32 * to.block + u * to.piece + i0 % 32) = *(const v8bf *)&sh.tile[u][c][i0];
     }
 }
 

@@ -6,7 +6,7 @@
 template <class S, int NP>
 __global__ __launch_bounds__(WG) void pack_rows_kernel(const S *__restrict__ src, int64_t ld, int64_t rows, int64_t cols,
                                                        const int32_t *__restrict__ perm, int vec, __bf16 *__restrict__ dst,
-                                                       int64_t kpad, int64_t piece, uint32_t *__restrict__ flags, int clear)
+                                                       int64_t kpad, PackLayout to, uint32_t *__restrict__ flags, int clear)
 {
     if (flags && clear && blockIdx.x == 0 && threadIdx.x < 2) flags[threadIdx.x] = 0;
     uint32_t there = 0;
@@ -26,7 +26,7 @@ __global__ __launch_bounds__(WG) void pack_rows_kernel(const S *__restrict__ src
             for (int u = 1; u < NP; u++) there |= (float)pc[u] != 0.0f ? 1u << (u - 1) : 0u;
         }
 #pragma unroll
-        for (int u = 0; u < NP; u++) *(v8bf *)(dst + u * piece + r * kpad + i0) = o[u];
+        for (int u = 0; u < NP; u++) *(v8bf *)(dst + r * to.ld + i0 / 32 * to.block + u * to.piece + i0 % 32) = o[u];
     }
     if (NP > 1 && flags && !clear) {
         if (__any(there & 1u) && (threadIdx.x & 63) == 0) flags[0] = 1;      // (all that do write the same)
@@ -37,54 +37,52 @@ __global__ __launch_bounds__(WG) void pack_rows_kernel(const S *__restrict__ src
 template <class S, int NP>
 __global__ __launch_bounds__(WG) void pack_cols_kernel(const S *__restrict__ src, int64_t ld, int64_t rows, int64_t cols,
                                                        const uint32_t *__restrict__ live, int order, int vec,
-                                                       __bf16 *__restrict__ dst, int64_t rpad, int64_t piece)
+                                                       __bf16 *__restrict__ dst, int64_t rpad, PackLayout to)
 {
     __shared__ PackCols<S, NP> sh;
-    pack_cols_tile<S, NP, WG>(sh, threadIdx.x, true, src, ld, rows, cols, live, order, vec, dst, rpad, piece, (int64_t)blockIdx.x * 64,
+    pack_cols_tile<S, NP, WG>(sh, threadIdx.x, true, src, ld, rows, cols, live, order, vec, dst, rpad, to, (int64_t)blockIdx.x * 64,
                               (int64_t)blockIdx.y * 64);
 }
 
 int rairs_launch_pack_rows(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *dst,
-                           int64_t kpad, hipStream_t s, uint32_t *flags, bool clear)
+                           int64_t kpad, PackLayout to, hipStream_t s, uint32_t *flags, bool clear)
 {
     if (rows == 0) return RAIRS_OK;
-    const int64_t piece = rows * kpad, want = (rows * (kpad / 8) + WG - 1) / WG;
+    const int64_t want = (rows * (kpad / 8) + WG - 1) / WG;
     const dim3 grid((unsigned)(want < 8192 ? want : 8192));
     const int vec = is_vec(src, ld, dtype_width(dtype));
     if (dtype == RAIRS_F32)
-        hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, perm, vec, dst, kpad, piece, flags,
+        hipLaunchKernelGGL((pack_rows_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, perm, vec, dst, kpad, to, flags,
                            (int)clear);
     else if (dtype == RAIRS_BF16)
-        hipLaunchKernelGGL((pack_rows_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, perm, vec, dst, kpad, piece, flags,
+        hipLaunchKernelGGL((pack_rows_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, perm, vec, dst, kpad, to, flags,
                            (int)clear);
     else
-        hipLaunchKernelGGL((pack_rows_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, perm, vec, dst, kpad, piece, flags,
+        hipLaunchKernelGGL((pack_rows_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, perm, vec, dst, kpad, to, flags,
                            (int)clear);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
 
 int rairs_launch_pack_cols(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const uint32_t *live, int order, __bf16 *dst,
-                           int64_t rpad, hipStream_t s)
+                           int64_t rpad, PackLayout to, hipStream_t s)
 {
     if (cols == 0 || rpad == 0) return RAIRS_OK;
     const int vec = is_vec(src, ld, dtype_width(dtype));
-    const int64_t piece = cols * rpad;
     const dim3 grid((unsigned)((rpad + 63) / 64), (unsigned)((cols + 63) / 64));
     if (dtype == RAIRS_F32)
-        hipLaunchKernelGGL((pack_cols_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, live, order, vec, dst, rpad, piece);
+        hipLaunchKernelGGL((pack_cols_kernel<float, 3>), grid, dim3(WG), 0, s, (const float *)src, ld, rows, cols, live, order, vec, dst, rpad, to);
     else if (dtype == RAIRS_BF16)
-        hipLaunchKernelGGL((pack_cols_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, live, order, vec, dst, rpad, piece);
+        hipLaunchKernelGGL((pack_cols_kernel<__bf16, 1>), grid, dim3(WG), 0, s, (const __bf16 *)src, ld, rows, cols, live, order, vec, dst, rpad, to);
     else
-        hipLaunchKernelGGL((pack_cols_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, live, order, vec, dst, rpad, piece);
+        hipLaunchKernelGGL((pack_cols_kernel<uint8_t, 1>), grid, dim3(WG), 0, s, (const uint8_t *)src, ld, rows, cols, live, order, vec, dst, rpad, to);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
 
-int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, __bf16 *room, RowOperand &out,
-                  hipStream_t s, uint32_t *flags, bool clear)
+int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, bool threes, __bf16 *room,
+                  RowOperand &out, hipStream_t s, uint32_t *flags, bool clear)
 {
-    const int64_t kpad = pad_to(cols, ROWPROD_K);
     out.rows = rows;
     out.perm = nullptr;
     out.pieces_there = nullptr;
@@ -95,8 +93,10 @@ int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t 
         out.perm = perm;
         return RAIRS_OK;
     }
+    const int64_t kpad = pad_to(cols, threes ? 32 : ROWPROD_K);
+    const PackLayout to = pack_layout(rows, kpad, threes);
     out.p = room;
-    out.ld = kpad;
-    out.piece = rows * kpad;
-    return rairs_launch_pack_rows(src, dtype, ld, rows, cols, perm, room, kpad, s, flags, clear);
+    out.ld = to.ld;
+    out.piece = threes ? 0 : to.piece;
+    return rairs_launch_pack_rows(src, dtype, ld, rows, cols, perm, room, kpad, to, s, flags, clear);
 }

@@ -7,6 +7,11 @@
 // ones first (what is left out is below 2^-23 |P||Q|).  A piece list is only a longer sum, so bf16
 // rows, fp32 rows and byte rows share one kernel.
 //
+// fp32 with fp32 ("threes") goes by steps of 32 values with all three pieces of both in LDS, from rows in which each
+// 32 values' pieces follow each other: six products of what is read once, which halves the traffic (2,999 x 960 x 1024:
+// PENDING).  The products with smaller factors have sums of their own, added at the end, so that they
+// do not round the large one's.
+//
 // Small products of fp32 rows take the rows as they are and the fp32 matrix instruction (a sixteenth of the
 // bf16 rate, against six products of pieces and the packing): lengths, strides and steps are then counted in
 // units of two bytes all the same, so that a step is 32 values.
@@ -31,7 +36,7 @@ typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 
 // Rows of bf16 pieces: value k of piece i of row r at p[i * piece + r * ld + k]; ld a multiple of 8, below
 // 2^22, p 16-byte aligned, k up to a multiple of ROWPROD_K readable (zero beyond the row).  Rows of fp32: units of
-// two bytes in place of values.
+// two bytes in place of values.  Threes: 32 values of piece 0, of piece 1, of piece 2, then the next 32 values.
 struct RowOperand {
     const __bf16 *p;
     int64_t ld, piece;
@@ -48,14 +53,14 @@ struct AdapterPart {
     const __bf16 *zero;             // [kpad] zeros
     const int32_t *of_row;          // [q rows] adapter of each row in product order, -1: none
     const int32_t *end;             // [adapters] one past an adapter's last row
-    int kpad;                       // multiple of ROWPROD_K; 0: no adapters
+    int kpad;                       // multiple of ROWPROD_K (threes: of 96); 0: no adapters
 };
 
 struct RowProd {
     RowOperand P, Q;
     int nseg;                       // products of pieces
     uint32_t sp, sq;                // piece of P and of Q of each, four bits a product
-    int ksteps;                     // steps of ROWPROD_K per product
+    int ksteps;                     // steps of ROWPROD_K (threes and fp32: 32 values) per product
     int splits;                     // workgroups that share a tile's sum
     int ptiles, qtiles;             // tiles, and workgroups along P: each takes prun tiles
     int prun, pruns;
@@ -98,6 +103,8 @@ typedef __attribute__((address_space(1))) const void global_void;
 typedef RowTile<8, 4, 2, 4, 2> TileL;       // 256 x 256, 8 waves
 typedef RowTile<4, 2, 2, 4, 3> TileM;       // 128 x 128, 8 waves
 typedef RowTile<2, 2, 2, 2, 4> TileS;       // 64 x 64, 4 waves
+typedef RowTile<4, 4, 4, 2, 2> TileT;       // 256 x 128, 8 waves: what threes have for TileL
+typedef RowTile<2, 2, 2, 2, 3> TileU;       // 64 x 64: and for TileS (two workgroups a CU)
 typedef RowTile<4, 4, 2, 2, 2> TileW;       // 128 x 128, 4 waves: 64 x 64 to a wave, for epilogues that want that
 // few queries, whose rows' loads are what counts: about 100 KB of them on the way
 typedef RowTile<4, 1, 4, 1, 4> TileF1;      // 256 x 16
@@ -115,7 +122,31 @@ struct RowAcc {
     float nrm[T::PT];               // ROW_NORM: this lane's part of the squared norm of row 16 i + (lane & 15) of P
 };
 
-enum { ROW_ADAPT = 1, ROW_F32 = 2, ROW_NORM = 4 };        // with adapters; fp32 rows; norms wanted
+// with adapters; fp32 rows; norms wanted; three pieces together
+enum { ROW_ADAPT = 1, ROW_F32 = 2, ROW_NORM = 4, ROW_THREES = 8 };
+// bytes of one LDS buffer, loads that every wave makes for it
+template <class T, int FLAGS>
+struct RowStep {
+    static constexpr bool THREES = FLAGS & ROW_THREES;
+    static constexpr int BYTES = THREES ? T::BYTES * 3 / 2 : T::BYTES, LOADS = THREES ? T::LEAST * 3 / 2 : T::LEAST;
+    static constexpr int LP2 = THREES ? T::LP / 2 : 1, LQ2 = THREES ? T::LQ / 2 : 1;      // loads of third pieces
+    static constexpr int WAVES = T::NT == 256 && T::ST * BYTES > 80 * 1024 ? 1 : 2;       // per SIMD: four waves that have a CU to themselves
+    static_assert(!THREES || (!T::SOME_Q && T::LP % 2 == 0 && T::LQ % 2 == 0), "");
+};
+
+// Threes in LDS: pieces 0 and 1 of a row as any row's 128 bytes, then the third pieces, two rows to 128 bytes: slot s of
+// pair r holds chunk s ^ (r & 3) of the two.
+template <class T, int L>
+static __device__ __forceinline__ void rowprod_thirds(int64_t r0, int64_t rows, int64_t ld, int tid, uint32_t (&o)[L], int64_t (&row)[L])
+{
+    const uint32_t last = (uint32_t)(rows - 1 - r0 < 0x7FFFFFFF ? rows - 1 - r0 : 0x7FFFFFFF);
+#pragma unroll
+    for (int i = 0; i < L; i++) {
+        const uint32_t pair = i * (T::NT / 8) + (tid >> 3), x = (tid & 7) ^ (pair & 3), r = 2 * pair + (x >> 2);
+        row[i] = r0 + r;
+        o[i] = (r < last ? r : last) * (uint32_t)(ld * 2) + 128 + (x & 3) * 16;
+    }
+}
 
 // one step's 16-byte chunks of both operands, straight into LDS: a row's place is a 32-bit offset from an
 // address that the workgroup shares
@@ -131,6 +162,14 @@ static __device__ __forceinline__ void rowprod_fetch(char *buf, const char *pb, 
         for (int i = 0; i < T::LQ; i++)
             __builtin_amdgcn_global_load_lds((global_void *)(qb + qo[i]), (lds_void *)(buf + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16,
                                              0, 0);
+}
+
+template <class T, int L>
+static __device__ __forceinline__ void rowprod_fetch_thirds(char *buf, const char *base, const uint32_t (&o)[L], int wave)
+{
+#pragma unroll
+    for (int i = 0; i < L; i++)
+        __builtin_amdgcn_global_load_lds((global_void *)(base + o[i]), (lds_void *)(buf + (i * T::NT + wave * 64) * 16), 16, 0, 0);
 }
 
 // All but the last N loads into LDS of this wave have landed, then every wave's; and every wave has read what it
@@ -188,6 +227,46 @@ static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int
     }
 }
 
+// One step of threes: 32 values.  Fragments are read as they are needed, the largest products first.
+template <class T, class F>
+static __device__ __forceinline__ void rowprod_step_threes(const char *buf, int wp, int wq, int lane, RowAcc<T> &acc, v4f (&low)[T::PT][T::QT],
+                                                           const F &fetch)
+{
+    const int r = lane & 15, h = lane >> 4;
+    const int slot = (h ^ (r & 7)) * 16 + r * 128, slot1 = ((4 + h) ^ (r & 7)) * 16 + r * 128;
+    const int slot2 = ((4 * (r & 1) + h) ^ ((r >> 1) & 3)) * 16 + (r >> 1) * 128;
+    const char *pa = buf + wp * T::PT * 2048, *qa = buf + T::BP * 128 + wq * T::QT * 2048;
+    const char *pc = buf + T::BYTES + wp * T::PT * 1024, *qc = buf + T::BYTES + T::BP * 64 + wq * T::QT * 1024;
+    v8bf a0[T::PT], a1[T::PT], b0[T::QT], b1[T::QT];
+    const auto mul = [&](const v8bf (&a)[T::PT], const v8bf (&b)[T::QT], v4f (&c)[T::PT][T::QT]) {
+#pragma unroll
+        for (int i = 0; i < T::PT; i++)
+#pragma unroll
+            for (int j = 0; j < T::QT; j++) c[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c[i][j], 0, 0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < T::PT; i++) a0[i] = *(const v8bf *)(pa + i * 2048 + slot);
+#pragma unroll
+    for (int j = 0; j < T::QT; j++) b0[j] = *(const v8bf *)(qa + j * 2048 + slot);
+#pragma unroll
+    for (int j = 0; j < T::QT; j++) b1[j] = *(const v8bf *)(qa + j * 2048 + slot1);
+#pragma unroll
+    for (int i = 0; i < T::PT; i++) a1[i] = *(const v8bf *)(pa + i * 2048 + slot1);
+    mul(a0, b0, acc.v);
+    __builtin_amdgcn_sched_barrier(0);
+    fetch();
+    __builtin_amdgcn_sched_barrier(0);
+    mul(a0, b1, low);
+    mul(a1, b1, low);
+#pragma unroll
+    for (int j = 0; j < T::QT; j++) b1[j] = *(const v8bf *)(qc + j * 1024 + slot2);      // the third pieces
+    mul(a1, b0, low);
+#pragma unroll
+    for (int i = 0; i < T::PT; i++) a1[i] = *(const v8bf *)(pc + i * 1024 + slot2);
+    mul(a0, b1, low);
+    mul(a1, b0, low);
+}
+
 // A workgroup's q tile and run of p tiles.  Workgroups are handed out round robin over the eight XCDs, each with
 // its own L2 cache: one XCD takes consecutive ids, and ids go over a band of q tiles, then to the next run, so that
 // what runs on an XCD at a time is about a square of tiles, whose rows its cache fetches once.
@@ -228,9 +307,11 @@ static __device__ __forceinline__ void rowprod_rows(int64_t r0, int64_t rows, in
 // q0, lane): lane l holds, for its tiles (i, j), rows q0 + 16 j + (l & 15) and columns p0 + 16 i +
 // 4 (l >> 4) + 0..3.
 template <class T, class Epi, int FLAGS>
-__global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
+__global__ __launch_bounds__(T::NT, (RowStep<T, FLAGS>::WAVES)) void rowprod_kernel(RowProd a, Epi epi)
 {
-    constexpr bool ADAPT = FLAGS & ROW_ADAPT;
+    constexpr bool ADAPT = FLAGS & ROW_ADAPT, THREES = FLAGS & ROW_THREES;
+    constexpr int BYTES = RowStep<T, FLAGS>::BYTES, LP2 = RowStep<T, FLAGS>::LP2, LQ2 = RowStep<T, FLAGS>::LQ2;
+    constexpr int STEP = THREES ? 192 : ROWPROD_K * 2;                // bytes of a row per step
     extern __shared__ __align__(16) char rowprod_lds[];
     int run, qt, split;
     if (!rowprod_tile(a, run, qt, split)) return;
@@ -255,6 +336,12 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
         rowprod_rows<T>(q0, a.Q.rows, a.Q.ld, tid, qo);
         qb += q0 * a.Q.ld * 2;
     }
+    uint32_t po3[LP2], qo3[LQ2];                                      // of third pieces
+    int64_t prow3[LP2], qrow3[LQ2];
+    if constexpr (THREES) {                                           // (never through a permutation)
+        rowprod_thirds<T>((int64_t)t0 * T::BP, a.P.rows, a.P.ld, tid, po3, prow3);
+        rowprod_thirds<T>(q0, a.Q.rows, a.Q.ld, tid, qo3, qrow3);
+    }
     uint32_t sp = a.sp, sq = a.sq;
     int nseg = a.nseg;
     if (a.Q.pieces_there) {
@@ -277,7 +364,7 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
     // of the adapters: the one being fetched, its next values, where its rows end; -1: none left
     int f_ad = -1, f_k = 0;
     int64_t f_end = q0;
-    int32_t own[ADAPT ? T::LQ : 1];                                   // adapters of this thread's rows
+    int32_t own[ADAPT ? T::LQ : 1], own3[ADAPT ? LQ2 : 1];            // adapters of this thread's rows
     const int64_t qend = q0 + T::BQ < a.Q.rows ? q0 + T::BQ : a.Q.rows;
     if constexpr (ADAPT) {
 #pragma unroll
@@ -285,6 +372,9 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
             const int64_t r = q0 + i * (T::NT / 8) + (tid >> 3);
             own[i] = a.ad.of_row[r < a.Q.rows ? r : a.Q.rows - 1];
         }
+        if constexpr (THREES)
+#pragma unroll
+            for (int i = 0; i < LQ2; i++) own3[i] = a.ad.of_row[qrow3[i] < a.Q.rows ? qrow3[i] : a.Q.rows - 1];
         f_ad = a.ad.of_row[q0];                                       // (rows without an adapter are the last)
         f_end = f_ad >= 0 ? a.ad.end[f_ad] : qend;
     }
@@ -297,7 +387,12 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
         if constexpr (ADAPT) base = f_tile < t1;
         if (base) {
             const int64_t ps = (sp >> (4 * seg)) & 15, qs = (sq >> (4 * seg)) & 15;
-            rowprod_fetch<T>(f_buf, pb + (ps * a.P.piece + k * ROWPROD_K) * 2, po, qb + (qs * a.Q.piece + k * ROWPROD_K) * 2, qo, wave);
+            const char *pk = pb + ps * a.P.piece * 2 + (int64_t)k * STEP, *qk = qb + qs * a.Q.piece * 2 + (int64_t)k * STEP;
+            rowprod_fetch<T>(f_buf, pk, po, qk, qo, wave);
+            if constexpr (THREES) {
+                rowprod_fetch_thirds<T>(f_buf + T::BYTES, pk, po3, wave);
+                rowprod_fetch_thirds<T>(f_buf + T::BYTES + T::BP * 64, qk, qo3, wave);
+            }
             if (f_tile < t1) {
                 fetched++;
                 if (++f_step < s1) {
@@ -307,7 +402,10 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
                     if (f_tile < t1) {
                         f_step = s0; seg = seg0; k = k0;
                         pb += (int64_t)T::BP * a.P.ld * 2;
-                        if (f_tile + 1 == a.ptiles) rowprod_rows<T>((int64_t)f_tile * T::BP, a.P.rows, a.P.ld, tid, po);
+                        if (f_tile + 1 == a.ptiles) {
+                            rowprod_rows<T>((int64_t)f_tile * T::BP, a.P.rows, a.P.ld, tid, po);
+                            if constexpr (THREES) rowprod_thirds<T>((int64_t)f_tile * T::BP, a.P.rows, a.P.ld, tid, po3, prow3);
+                        }
                     } else if (!ADAPT || f_ad < 0) {
                         total = fetched;
                     }
@@ -328,9 +426,21 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
                 const char *src = own[i] == ad ? ub + uo[i] : (const char *)a.ad.zero;
                 __builtin_amdgcn_global_load_lds((global_void *)src, (lds_void *)(f_buf + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16, 0, 0);
             }
+            if constexpr (THREES) {
+                uint32_t ao3[LP2], uo3[LQ2];
+                rowprod_thirds<T>(p0, a.P.rows, a.ad.kpad, tid, ao3, prow3);
+                rowprod_thirds<T>(q0, a.Q.rows, a.ad.kpad, tid, uo3, qrow3);
+                rowprod_fetch_thirds<T>(f_buf + T::BYTES, bb, ao3, wave);
+#pragma unroll
+                for (int i = 0; i < LQ2; i++) {
+                    const char *src = own3[i] == ad ? ub + uo3[i] : (const char *)a.ad.zero;
+                    __builtin_amdgcn_global_load_lds((global_void *)src, (lds_void *)(f_buf + T::BYTES + T::BP * 64 + (i * T::NT + wave * 64) * 16), 16,
+                                                     0, 0);
+                }
+            }
             if (f_ad >= 0) {
                 fetched++;
-                f_k += ROWPROD_K;
+                f_k += STEP / 2;
                 if (f_k == a.ad.kpad) {
                     f_k = 0;
                     f_ad = f_end < qend ? a.ad.of_row[f_end] : -1;
@@ -339,7 +449,7 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
                 }
             }
         }
-        f_buf = f_buf == rowprod_lds + (T::ST - 1) * T::BYTES ? rowprod_lds : f_buf + T::BYTES;
+        f_buf = f_buf == rowprod_lds + (T::ST - 1) * BYTES ? rowprod_lds : f_buf + BYTES;
     };
     for (int i = 0; i < T::ST - 1; i++) fetch();
     typename Epi::template State<T> state;
@@ -354,15 +464,27 @@ __global__ __launch_bounds__(T::NT, 2) void rowprod_kernel(RowProd a, Epi epi)
             for (int j = 0; j < T::QT; j++) acc.v[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < T::PT; i++) acc.nrm[i] = 0.0f;
+        v4f low[T::PT][T::QT];
+        if constexpr (THREES)
+#pragma unroll
+            for (int i = 0; i < T::PT; i++)
+#pragma unroll
+                for (int j = 0; j < T::QT; j++) low[i][j] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
         // (a run of several tiles: a tile's steps; else all that is fetched)
         const int stop = done + (s1 - s0);
         while (ADAPT ? done < total : done < stop) {
             // (this also says that every wave is past the step before, whose buffer the next fetch writes)
-            rowprod_landed<(T::ST - 2) * T::LEAST>();
-            rowprod_step<T, FLAGS>(buf, wp, wq, lane, acc, fetch);
-            buf = buf == rowprod_lds + (T::ST - 1) * T::BYTES ? rowprod_lds : buf + T::BYTES;
+            rowprod_landed<(T::ST - 2) * RowStep<T, FLAGS>::LOADS>();
+            if constexpr (THREES) rowprod_step_threes<T>(buf, wp, wq, lane, acc, low, fetch);
+            else rowprod_step<T, FLAGS>(buf, wp, wq, lane, acc, fetch);
+            buf = buf == rowprod_lds + (T::ST - 1) * BYTES ? rowprod_lds : buf + BYTES;
             done++;
         }
+        if constexpr (THREES)
+#pragma unroll
+            for (int i = 0; i < T::PT; i++)
+#pragma unroll
+                for (int j = 0; j < T::QT; j++) acc.v[i][j] += low[i][j];
         epi.tile(state, acc, (int64_t)t * T::BP + wp * (16 * T::PT), qw, lane, split);
     }
     epi.end(state, run, wp, qw, lane);
@@ -392,8 +514,9 @@ static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 
     a.prun = prun;
     a.pruns = (a.ptiles + prun - 1) / prun;
     if (a.splits < 1) a.splits = 1;
+    constexpr int lds = T::ST * RowStep<T, FLAGS>::BYTES;
     // the square: of the workgroups that an XCD has at a time, 32 or (small tiles: two a CU) 64
-    const int64_t total = (int64_t)a.pruns * a.qtiles, at_once = std::min<int64_t>((total * a.splits + 7) / 8, T::ST * T::BYTES > 80 * 1024 ? 32 : 64);
+    const int64_t total = (int64_t)a.pruns * a.qtiles, at_once = std::min<int64_t>((total * a.splits + 7) / 8, lds > 80 * 1024 ? 32 : 64);
     double least = 1e300;
     for (int bands = 1; bands <= a.qtiles; bands++) {
         const int h = (a.qtiles + bands - 1) / bands;
@@ -401,8 +524,8 @@ static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 
         if (rows < least) { least = rows; a.band = h; }
     }
     auto kern = rowprod_kernel<T, Epi, FLAGS>;
-    RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, T::ST * T::BYTES));
-    hipLaunchKernelGGL(kern, dim3(rowprod_grid(a)), dim3(T::NT), T::ST * T::BYTES, s, a, epi);
+    RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    hipLaunchKernelGGL(kern, dim3(rowprod_grid(a)), dim3(T::NT), lds, s, a, epi);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
@@ -412,7 +535,10 @@ template <int FLAGS = 0, class Epi>
 static int rowprod_launch_any(RowProd &a, const Epi &epi, hipStream_t s)
 {
     const int size = rowprod_size(a.P.rows, a.Q.rows, a.splits > 1 ? a.splits : 1);
-    return size == 2 ? rowprod_launch<TileL, FLAGS>(a, epi, s) : size == 1 ? rowprod_launch<TileM, FLAGS>(a, epi, s) : rowprod_launch<TileS, FLAGS>(a, epi, s);
+    if constexpr (FLAGS & ROW_THREES)
+        return size == 2 ? rowprod_launch<TileT, FLAGS>(a, epi, s) : size == 1 ? rowprod_launch<TileM, FLAGS>(a, epi, s) : rowprod_launch<TileU, FLAGS>(a, epi, s);
+    else
+        return size == 2 ? rowprod_launch<TileL, FLAGS>(a, epi, s) : size == 1 ? rowprod_launch<TileM, FLAGS>(a, epi, s) : rowprod_launch<TileS, FLAGS>(a, epi, s);
 }
 
 // ---- epilogues -------------------------------------------------------------------------------------
