@@ -132,16 +132,31 @@ class _Table(C.Structure):
                 ("scale", C.c_float), ("d_live", C.c_void_p), ("ld_live", C.c_int64)]
 
 
-@contextlib.contextmanager
-def _on(device, stream):
+class _On:
     """The device of a call's tensors current, and `stream` the stream that its workspace and results are
-    allocated for (None: the device's current one)."""
-    with torch.cuda.device(device):
-        if stream is None:
-            yield torch.cuda.current_stream()
-        else:
-            with torch.cuda.stream(stream):
-                yield stream
+    allocated for (None: the device's current one); its address.  (A small projection takes less time than
+    switching to the device that is current already: that is left out.)"""
+    __slots__ = ("device", "stream", "ctx")
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.ctx = device, stream, None
+
+    def __enter__(self) -> C.c_void_p:
+        if self.stream is not None or torch.cuda.current_device() != self.device.index:
+            self.ctx = contextlib.ExitStack()
+            self.ctx.enter_context(torch.cuda.device(self.device))
+            if self.stream is not None:
+                self.ctx.enter_context(torch.cuda.stream(self.stream))
+                return C.c_void_p(self.stream.cuda_stream)
+        return C.c_void_p(_raw_stream(self.device.index))
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.close()
+        return False
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _rows(t: torch.Tensor, name: str, dtype, cols: int, device):
@@ -162,10 +177,10 @@ def _vec(t, name: str, dtype, n: int, device) -> C.c_void_p:
     return C.c_void_p(t.data_ptr() if n else 0)
 
 
-def _workspace(need: int):
+def _workspace(need: int, device):
     if need == 0:
         return None, C.c_void_p(0), C.c_size_t(0)
-    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
     return ws, C.c_void_p(ws.data_ptr()), C.c_size_t(need)
 
 
@@ -201,18 +216,20 @@ class Projection:
         lib, dev, n = load(), self.W.device, x.shape[0]
         px, ldx = _rows(x, "x", self.W.dtype, self.d_in, dev)
         pa = _vec(adapter, "adapter", torch.int32, n, dev)
-        with _on(dev, stream) as st:
-            if out is None:
+        with _On(dev, stream) as st:
+            given = out is not None
+            if not given:
                 out = torch.empty((n, self.d_out), dtype=out_dtype or torch.float32, device=dev)
             elif out.shape[0] != n or (out_dtype is not None and out.dtype != out_dtype):
                 raise ValueError("out does not fit")
             if out.dtype not in DTYPES:
                 raise TypeError(f"out: unsupported type {out.dtype}")
-            py, ldy = _rows(out, "out", out.dtype, self.d_out, dev)
+            py, ldy = _rows(out, "out", out.dtype, self.d_out, dev) if given else (
+                C.c_void_p(out.data_ptr() if n else 0), C.c_int64(self.d_out))
             need = lib.rairs_project_workspace_bytes(C.byref(self._s), C.c_int64(n))
-            ws, pw, nw = _workspace(need)
+            ws, pw, nw = _workspace(need, dev)
             _check(lib.rairs_project(C.byref(self._s), px, ldx, C.c_int64(n), pa, py, ldy, C.c_int(DTYPES[out.dtype]),
-                                     pw, nw, _stream_ptr(st)))
+                                     pw, nw, st))
         return out
 
     def backward(self, x: torch.Tensor, adapter: Optional[torch.Tensor], dy: torch.Tensor, x_grad: bool = True,
@@ -225,17 +242,17 @@ class Projection:
             raise ValueError("dy must have as many rows as x")
         pa = _vec(adapter, "adapter", torch.int32, n, dev)
         adapter_grad = adapter_grad and self.n_adapters > 0
-        with _on(dev, stream) as st:
+        with _On(dev, stream) as st:
             dx = torch.empty((n, self.d_in), dtype=t, device=dev) if x_grad else None
             da = torch.empty_like(self.A) if adapter_grad else None
             db = torch.empty_like(self.B) if adapter_grad else None
             need = lib.rairs_project_backward_workspace_bytes(C.byref(self._s), C.c_int64(n))
-            ws, pw, nw = _workspace(need)
+            ws, pw, nw = _workspace(need, dev)
             _check(lib.rairs_project_backward(
                 C.byref(self._s), px, ldx, C.c_int64(n), pa, pg, ldg,
                 C.c_void_p(dx.data_ptr() if x_grad and n else 0), C.c_int64(self.d_in),
                 C.c_void_p(da.data_ptr() if adapter_grad else 0), C.c_void_p(db.data_ptr() if adapter_grad else 0),
-                pw, nw, _stream_ptr(st)))
+                pw, nw, st))
         return dx, da, db
 
 
@@ -277,15 +294,15 @@ def _logprob(t, q, targets, top, entropy, stream) -> LogProb:
     qt = torch.float32 if t.dtype == DTYPES[torch.uint8] else {v: k for k, v in DTYPES.items()}[t.dtype]
     pq, ldq = _rows(q, "q", qt, t.d, dev)
     pt = _vec(targets, "targets", torch.int64, n, dev)
-    with _on(dev, stream) as st:
+    with _On(dev, stream) as st:
         need = lib.rairs_logprob_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(DTYPES[qt]), C.c_int(top))
-        ws, pw, nw = _workspace(need)
+        ws, pw, nw = _workspace(need, dev)
         r = LogProb(torch.empty(n, device=dev), torch.empty(n, device=dev), torch.empty(n, device=dev) if entropy else None,
                     torch.empty((n, top), dtype=torch.int64, device=dev) if top > 0 else None,
                     torch.empty((n, top), device=dev) if top > 0 else None)
         p = [C.c_void_p(x.data_ptr() if x is not None and n else 0) for x in r]
         _check(lib.rairs_logprob(C.byref(t), pq, ldq, C.c_int(DTYPES[qt]), C.c_int64(n), pt, p[0], p[1], p[2], C.c_int(top), p[3],
-                                 p[4], pw, nw, _stream_ptr(st)))
+                                 p[4], pw, nw, st))
     return r
 
 
@@ -309,15 +326,15 @@ def logprob_backward(q: torch.Tensor, table: torch.Tensor, targets: torch.Tensor
     f = [_vec(x, name, torch.float32, n, dev) for x, name in
          ((lse, "lse"), (entropy, "entropy"), (dlogp, "dlogp"), (dentropy, "dentropy"))]
     pt = _vec(targets, "targets", torch.int64, n, dev)
-    with _on(dev, stream) as st:
+    with _On(dev, stream) as st:
         need = lib.rairs_logprob_backward_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(DTYPES[qt]), C.c_int(int(table_grad)))
-        ws, pw, nw = _workspace(need)
+        ws, pw, nw = _workspace(need, dev)
         dq = torch.empty((n, t.d), dtype=qt, device=dev) if q_grad else None
         dt = torch.empty((t.V, t.d), dtype=table.dtype, device=dev) if table_grad else None
         _check(lib.rairs_logprob_backward(
             C.byref(t), pq, ldq, C.c_int(DTYPES[qt]), C.c_int64(n), pt, f[0], f[1], f[2], f[3],
             C.c_void_p(dq.data_ptr() if q_grad and n else 0), C.c_int64(t.d),
-            C.c_void_p(dt.data_ptr() if table_grad else 0), C.c_int64(t.d), pw, nw, _stream_ptr(st)))
+            C.c_void_p(dt.data_ptr() if table_grad else 0), C.c_int64(t.d), pw, nw, st))
     return dq, dt
 
 
@@ -463,17 +480,17 @@ class Index:
         n, dev = x.shape[0], projection.W.device
         px, ldx = _rows(x, "x", projection.W.dtype, projection.d_in, dev)
         pa = _vec(adapter, "adapter", torch.int32, n, dev)
-        with _on(dev, stream) as st:
+        with _On(dev, stream) as st:
             self._reserve(n, nprobe, refine_k)
             ids = torch.empty((n, k), dtype=torch.int64, device=dev)
             dists = torch.empty((n, k), dtype=torch.float32, device=dev)
             q = torch.empty((n, self.d), dtype=torch.float32, device=dev)
             need = self._lib.rairs_project_workspace_bytes(C.byref(projection._s), C.c_int64(n))
-            ws, pw, nw = _workspace(need)
+            ws, pw, nw = _workspace(need, dev)
             _check(self._lib.rairs_search_projected(
                 self._h, C.byref(projection._s), px, ldx, C.c_int64(n), pa, C.c_void_p(q.data_ptr() if n else 0), C.c_int(k),
                 C.c_int(nprobe), C.c_int(refine_k), C.c_void_p(ids.data_ptr() if n else 0),
-                C.c_void_p(dists.data_ptr() if n else 0), pw, nw, _stream_ptr(st)))
+                C.c_void_p(dists.data_ptr() if n else 0), pw, nw, st))
         return ids, dists, q
 
     def logprob(self, q: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, top: int = 0, live=None,

@@ -505,31 +505,40 @@ struct FewProjectArgs {
     int d_in, d_out, r, na;
     const int32_t *adapter;         // null: none
     const float *scale;
-    float *u;                       // [n][r]
+    float *u;                       // [n][r]; null: a workgroup makes its rows' own (up to 16 rows)
+    int avec;
     void *y;
     int bf16_out;
 };
 
-// u: a wave per row and rank
+// u[row][j] of adapter ad by a wave, in every lane
 template <class S>
-__global__ __launch_bounds__(WG) void few_shrink_kernel(FewProjectArgs a, int vec)
+static __device__ __forceinline__ float few_u(const FewProjectArgs &a, int64_t row, int ad, int j, int lane)
 {
-    const int lane = threadIdx.x & 63, j = blockIdx.y * (WG / 64) + (threadIdx.x >> 6);
-    const int64_t row = blockIdx.x;
-    const int ad = a.adapter[row];
-    if (j >= a.r || ad < 0 || ad >= a.na) return;
     constexpr int CH = FewLoad<S>::CH;
     const S *x = (const S *)a.x + row * a.ldx, *w = (const S *)a.a + ((int64_t)ad * a.r + j) * a.d_in;
     float s = 0.0f;
     for (int k = lane * CH; k < a.d_in; k += 64 * CH) {
-        const FewFrag<S, CH> f = vec ? few_load<S, CH, true>(x, k, a.d_in) : few_load<S, CH, false>(x, k, a.d_in);
-        const FewFrag<S, CH> g = vec ? few_load<S, CH, true>(w, k, a.d_in) : few_load<S, CH, false>(w, k, a.d_in);
+        const FewFrag<S, CH> f = a.avec ? few_load<S, CH, true>(x, k, a.d_in) : few_load<S, CH, false>(x, k, a.d_in);
+        const FewFrag<S, CH> g = a.avec ? few_load<S, CH, true>(w, k, a.d_in) : few_load<S, CH, false>(w, k, a.d_in);
 #pragma unroll
         for (int e = 0; e < CH; e++) s = fmaf((float)f.e[e], (float)g.e[e], s);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-    if (lane == 0) a.u[row * a.r + j] = a.scale ? s * a.scale[ad] : s;
+    return a.scale ? s * a.scale[ad] : s;
+}
+
+// u: a wave per row and rank
+template <class S>
+__global__ __launch_bounds__(WG) void few_shrink_kernel(FewProjectArgs a)
+{
+    const int lane = threadIdx.x & 63, j = blockIdx.y * (WG / 64) + (threadIdx.x >> 6);
+    const int64_t row = blockIdx.x;
+    const int ad = a.adapter[row];
+    if (j >= a.r || ad < 0 || ad >= a.na) return;
+    const float s = few_u<S>(a, row, ad, j, lane);
+    if (lane == 0) a.u[row * a.r + j] = s;
 }
 
 // 16 PT columns of y for 64 rows per workgroup: its waves share the sum over d_in, then each finishes one tile of 16
@@ -538,6 +547,7 @@ template <class S, int PT, int QT, bool VEC, bool BVEC>
 __global__ __launch_bounds__(WG) void few_project_kernel(FewProjectArgs a)
 {
     __shared__ v4f part[4][PT][QT][64];
+    __shared__ float own_u[QT == 1 ? 16 : 1][QT == 1 ? RAIRS_MAX_RANK : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // workgroups go round robin over the eight XCDs: the ones that read the same rows (of x, or of W if there are
     // fewer rows of x) one after the other on one of them, whose L2 cache has them after the first
@@ -566,6 +576,14 @@ __global__ __launch_bounds__(WG) void few_project_kernel(FewProjectArgs a)
     for (int i = 0; i < PT; i++)
 #pragma unroll
         for (int j = 0; j < QT; j++) part[wave][i][j][lane] = acc[i][j];
+    if constexpr (QT == 1)
+        if (a.adapter && !a.u)
+            for (int t = wave; t < (int)a.n * a.r; t += 4) {
+                const int row = t / a.r, j = t - row * a.r, ad = a.adapter[row];
+                if (ad < 0 || ad >= a.na) continue;
+                const float x = few_u<S>(a, row, ad, j, lane);
+                if (lane == 0) own_u[row][j] = x;
+            }
     __syncthreads();
     if (wave >= QT) return;
     const int64_t q = q0 + 16 * wave + (lane & 15);
@@ -578,7 +596,7 @@ __global__ __launch_bounds__(WG) void few_project_kernel(FewProjectArgs a)
         v4f y = (part[0][i][wave][lane] + part[1][i][wave][lane]) + (part[2][i][wave][lane] + part[3][i][wave][lane]);
         const int o0 = p0 + 16 * i + 4 * (lane >> 4);
         if (own) {
-            const float *u = a.u + q * a.r;
+            const float *u = QT == 1 && !a.u ? own_u[q & 15] : a.u + q * a.r;
             const S *b = (const S *)a.b + (int64_t)ad * a.d_out * a.r;
             v4f z = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int j = 0; j < a.r; j += CH) {
@@ -631,10 +649,9 @@ static int few_project(const FewProjectArgs &a, int dtype, hipStream_t s)
 }
 
 template <class S>
-static int few_shrink(const FewProjectArgs &a, int dtype, hipStream_t s)
+static int few_shrink(const FewProjectArgs &a, hipStream_t s)
 {
-    const int vec = row_vec(a.x, a.ldx, dtype) && row_vec(a.a, a.d_in, dtype);
-    hipLaunchKernelGGL(few_shrink_kernel<S>, dim3((unsigned)a.n, (unsigned)((a.r + 3) / 4)), dim3(WG), 0, s, a, vec);
+    hipLaunchKernelGGL(few_shrink_kernel<S>, dim3((unsigned)a.n, (unsigned)((a.r + 3) / 4)), dim3(WG), 0, s, a);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }
@@ -666,7 +683,9 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     int rc = RAIRS_OK;
     if (few_rows(p, g.n)) {
         FewProjectArgs a = {};
-        a.u = adapters ? w.take<float>(g.n * p.rank) : nullptr;
+        // (every workgroup for itself where that reads no more than 128 KB: less than a launch)
+        const bool own = g.n <= 16 && g.n * p.rank * p.d_in * dtype_width(p.dtype) <= 128 * 1024;
+        a.u = adapters && !own ? w.take<float>(g.n * p.rank) : nullptr;
         if (bytes) *bytes = w.used;
         if (!ws) return RAIRS_OK;
         a.x = g.x; a.w = p.W; a.a = p.A; a.b = p.B;
@@ -674,7 +693,8 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         a.d_in = p.d_in; a.d_out = p.d_out; a.r = p.rank; a.na = p.n_adapters;
         a.adapter = adapters ? g.adapter : nullptr;
         a.scale = p.scale; a.y = g.y; a.bf16_out = g.ytype == RAIRS_BF16;
-        if (a.adapter && (rc = bf ? few_shrink<__bf16>(a, p.dtype, s) : few_shrink<float>(a, p.dtype, s))) return rc;
+        a.avec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
+        if (a.adapter && !own && (rc = bf ? few_shrink<__bf16>(a, s) : few_shrink<float>(a, s))) return rc;
         return bf ? few_project<__bf16>(a, p.dtype, s) : few_project<float>(a, p.dtype, s);
     }
     const int np = dtype_pieces(p.dtype);

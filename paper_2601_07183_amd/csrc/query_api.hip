@@ -85,7 +85,6 @@ extern "C" int rairs_project(const rairs_projection_t *p, const void *d_x, int64
     g.p = *p;
     g.x = d_x; g.ldx = ld_x; g.n = n; g.adapter = d_adapter;
     g.y = d_y; g.ldy = ld_y; g.ytype = y_dtype;
-    if (!d_adapter) g.p.n_adapters = 0;
     return rairs_run_project(g, ws_or_any(d_ws), nullptr, (hipStream_t)hip_stream);
 }
 
