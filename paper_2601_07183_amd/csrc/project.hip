@@ -3,7 +3,9 @@
 // Rows are put in order of their adapter (a counting sort on the device; nothing is read back), so
 // that an adapter's rows lie together: u = s_a A_a x is then one small product per run of up to 32
 // rows, and in the large product a tile adds the terms of the few adapters that its rows have, as
-// further steps of the same sum in the same registers.  u enters that product as three bf16 pieces.
+// further steps of the same sum in the same registers, with u zero in the rows of the others.  (Zero times
+// an infinity is not zero: what is not finite in an adapter goes in as zero, and is added to the adapter's own
+// rows when they are written.)  u enters that product as three bf16 pieces.
 //
 // fp32 products of few tiles take the rows as they are and the fp32 instruction, u and B with them.  A few rows go
 // another way altogether: no sort, the rows of W and x straight from memory into the matrix instruction's
@@ -51,11 +53,12 @@ static __device__ __forceinline__ unsigned long long same_key(int key, int bits)
     uint32_t lo = (uint32_t)any, hi = (uint32_t)(any >> 32);
 #pragma unroll
     for (int b = 0; b < 13; b++) {
-        if (b >= bits) break;                                         // uniform
-        const int mine = (int)((uint32_t)key << (31 - b)) >> 31;      // all bits or none
-        const unsigned long long set = __ballot(mine);
-        lo &= ~(mine ^ (uint32_t)set);
-        hi &= ~(mine ^ (uint32_t)(set >> 32));
+        if (b < bits) {                                               // uniform
+            const int mine = (int)((uint32_t)key << (31 - b)) >> 31;  // all bits or none
+            const unsigned long long set = __ballot(mine);
+            lo &= ~(mine ^ (uint32_t)set);
+            hi &= ~(mine ^ (uint32_t)(set >> 32));
+        }
     }
     return (unsigned long long)hi << 32 | lo;
 }
@@ -275,6 +278,13 @@ static __device__ __forceinline__ __bf16 side_piece(const Side &side, int k, con
     return piece == 0 ? pc[0] : piece == 1 ? pc[1] : pc[2];
 }
 
+// what the packing of an adapter's columns found: word i says whether its workgroup i met a value that is not finite
+struct SideFlags {
+    uint32_t *found, *bad;          // [side_blocks]; [adapters] the same by adapter (of its own and its neighbours' values)
+    int64_t rows;                   // columns per adapter; 0: not wanted
+};
+static int64_t side_blocks(const Side &side, int64_t rows) { return (pad_to(rows, 64) * (side.kpad / 8) + 1023) / 1024; }
+
 struct ShrinkArgs {
     const void *x, *a;              // rows [n] of d; [adapters][r][d]
     int64_t ldx;
@@ -286,6 +296,7 @@ struct ShrinkArgs {
     float *u;                       // [n][r] in sorted order, or null
     __bf16 *up;                     // [n][kpad] in sorted order, or null
     Side side;
+    SideFlags flags;
 };
 
 // a workgroup per unit; its NW waves share the sum, which is joined in LDS
@@ -308,6 +319,11 @@ __global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs one, ShrinkA
         const int j = min(16 * i + (lane & 15), a.r - 1);
         prow[i] = (const S *)a.a + ((int64_t)unit.x * a.r + j) * a.d;
         acc[i][0] = acc[i][1] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    int bad = 0;
+    if (a.flags.rows) {
+        const int64_t per = 64 * (a.side.kpad / 8), lo = unit.x * a.flags.rows / 64 * per / 1024, hi = (((unit.x + 1) * a.flags.rows - 1) / 64 + 1) * per - 1;
+        for (int64_t b = lo + threadIdx.x; b <= hi / 1024; b += 64 * NW) bad |= a.flags.found[b];
     }
     const int steps = (a.d + 4 * FewLoad<S>::CH - 1) / (4 * FewLoad<S>::CH);
     few_dot<S, S, RT, 2, VEC, false>(prow, qrow, steps * wave / NW, steps * (wave + 1) / NW, a.d, lane, acc, nrm);
@@ -335,7 +351,8 @@ __global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs one, ShrinkA
                     *p = x * sc;
                 }
     }
-    __syncthreads();
+    bad = __syncthreads_or(bad);
+    if (a.flags.rows && threadIdx.x == 0) a.flags.bad[unit.x] = bad;  // (all of the adapter's units write the same)
     if (a.u)
         for (int t = threadIdx.x; t < unit.z * a.r; t += 64 * NW) {
             const int i = t / a.r, j = t - i * a.r;
@@ -382,6 +399,7 @@ struct SideJob {
     int64_t batch, so, sj, rows, total;
     Side side;
     __bf16 *dst, *zero;
+    uint32_t *found;
 };
 
 template <class S>
@@ -393,21 +411,31 @@ static __device__ __forceinline__ void pack_side(const SideJob &j, int64_t block
     // a thread per eight values; the rows of a group of 64 first, so that a transposed source is read along its rows
     const int eights = side.kpad / 8;
     const int64_t id = block * 1024 + threadIdx.x, t = id / (64 * eights) * 64 + (id & 63);
-    if (t >= j.total) return;
-    const int k0 = (int)(id / 64 % eights) * 8;
-    const int64_t a = t / j.rows, o = t - a * j.rows;
-    const S *p = (const S *)j.src + a * j.batch + o * j.so;
-    if (side.mode == SIDE_F32) {
-        v4f x;
+    int odd = 0;
+    if (t < j.total) {
+        const int k0 = (int)(id / 64 % eights) * 8;
+        const int64_t a = t / j.rows, o = t - a * j.rows;
+        const S *p = (const S *)j.src + a * j.batch + o * j.so;
+        const auto at = [&](int w) {
+            const float x = (float)p[w * j.sj];
+            const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+            odd |= !finite;
+            return finite ? x : 0.0f;
+        };
+        if (side.mode == SIDE_F32) {
+            v4f x;
 #pragma unroll
-        for (int e = 0; e < 4; e++) x[e] = k0 / 2 + e < side.r ? (float)p[(k0 / 2 + e) * j.sj] : 0.0f;
-        *(v4f *)(j.dst + t * side.kpad + k0) = x;
-        return;
+            for (int e = 0; e < 4; e++) x[e] = k0 / 2 + e < side.r ? at(k0 / 2 + e) : 0.0f;
+            *(v4f *)(j.dst + t * side.kpad + k0) = x;
+        } else {
+            v8bf x;
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[e] = side_piece<false>(side, k0 + e, at);
+            *(v8bf *)(j.dst + t * side.kpad + k0) = x;
+        }
     }
-    v8bf x;
-#pragma unroll
-    for (int e = 0; e < 8; e++) x[e] = side_piece<false>(side, k0 + e, [&](int w) { return (float)p[w * j.sj]; });
-    *(v8bf *)(j.dst + t * side.kpad + k0) = x;
+    odd = __syncthreads_or(odd);
+    if (threadIdx.x == 0) j.found[block] = odd;
 }
 
 // dst[b][c][r] = src[b][r][c], 32 x 32 values
@@ -474,7 +502,7 @@ static int prep_launch(PrepArgs &a, int dtype, hipStream_t s)
         if (a.sorts) lds = sort_one_lds(a.sort);
         else if ((rc = sort_launch(a.sort, s))) return rc;
     }
-    if (a.side.dst) a.side_blocks = (unsigned)((pad_to(a.side.total, 64) * (a.side.side.kpad / 8) + 1023) / 1024);
+    if (a.side.dst) a.side_blocks = (unsigned)side_blocks(a.side.side, a.side.total);
     if (a.wt) {
         a.cols_blocks = (unsigned)((a.opad / 64 * ((a.d_in + 63) / 64) + 1) / 2);
         lds = std::max(lds, dtype == RAIRS_F32 ? 2 * sizeof(PackCols<float, 3>) : 2 * sizeof(PackCols<__bf16, 1>));
@@ -658,10 +686,83 @@ static int few_shrink(const FewProjectArgs &a, hipStream_t s)
 
 // ---- forward -------------------------------------------------------------------------------------------
 
-static int large_product(RowProd &rp, const StoreEpi &e, bool bf, bool adapters, hipStream_t s)
+// Stores a tile and adds to its rows what their adapters' values that are not finite make of u (seldom).
+template <class S>
+struct AdapterEpi : StoreEpi {
+    const int32_t *of_row;
+    const uint32_t *bad;
+    const S *src;                   // as in SideJob
+    int64_t batch, so, sj;
+    const __bf16 *u;
+    Side side;
+    template <class T>
+    struct State : StoreEpi::State<T> {
+        uint32_t odd;               // of this lane's rows
+    };
+    template <class T>
+    __device__ __forceinline__ void begin(State<T> &st, int64_t q0, int lane) const
+    {
+        StoreEpi::begin<T>(st, q0, lane);
+        st.odd = 0;
+#pragma unroll
+        for (int j = 0; j < T::QT; j++) {
+            const int64_t q = q0 + 16 * j + (lane & 15);
+            const int ad = q < nq ? of_row[q] : -1;
+            if (ad >= 0 && bad[ad]) st.odd |= 1u << j;
+        }
+    }
+    __device__ __forceinline__ float u_at(int64_t q, int j) const
+    {
+        const __bf16 *p = u + q * side.kpad;
+        if (side.mode == SIDE_F32) return ((const float *)p)[j];
+        if (side.mode == SIDE_THREES) p += j / 32 * 96 + j % 32;
+        else p += j;
+        const int step = side.mode == SIDE_THREES ? 32 : side.r;
+        return ((float)p[0] + (float)p[step]) + (float)p[2 * step];
+    }
+    template <class T>
+    __device__ __forceinline__ void end(State<T> &st, int run, int wp, int64_t q0, int lane) const
+    {
+        if (!__any(st.odd)) return;
+#pragma unroll 1
+        for (int j = 0; j < T::QT; j++) {
+            if (!((st.odd >> j) & 1u)) continue;
+            const int64_t q = q0 + 16 * j + (lane & 15), row = perm ? perm[q] : q;
+            const S *b = src + of_row[q] * batch;
+#pragma unroll 1
+            for (int i = 0; i < 4 * T::PT; i++) {
+                // (a run is one tile; the lane that stored a value adds to it)
+                const int64_t p = (int64_t)run * T::BP + wp * (16 * T::PT) + 16 * (i / 4) + 4 * (lane >> 4) + i % 4;
+                if (p >= np) continue;
+                float x = 0.0f;
+                bool any = false;
+#pragma unroll 1
+                for (int k = 0; k < side.r; k++) {
+                    const float v = (float)b[p * so + k * sj];
+                    if ((__float_as_uint(v) & 0x7F800000u) != 0x7F800000u) continue;
+                    x = fmaf(v, u_at(q, k), x);
+                    any = true;
+                }
+                if (!any) continue;
+                if (bf16_out) ((__bf16 *)out)[row * ld + p] = (__bf16)((float)((__bf16 *)out)[row * ld + p] + x);
+                else ((float *)out)[row * ld + p] += x;
+            }
+        }
+    }
+};
+
+static int large_product(RowProd &rp, const StoreEpi &e, bool bf, bool f32, const SideJob *job, const __bf16 *u, const uint32_t *bad, hipStream_t s)
 {
-    if (bf) return adapters ? rowprod_launch_any<ROW_ADAPT>(rp, e, s) : rowprod_launch_any(rp, e, s);
-    return adapters ? rowprod_launch_any<ROW_THREES | ROW_ADAPT>(rp, e, s) : rowprod_launch_any<ROW_THREES>(rp, e, s);
+    if (!job) {
+        if (f32) return rowprod_launch<TileS, ROW_F32>(rp, e, s);
+        return bf ? rowprod_launch_any(rp, e, s) : rowprod_launch_any<ROW_THREES>(rp, e, s);
+    }
+    if (bf) {
+        const AdapterEpi<__bf16> ae = {e, rp.ad.of_row, bad, (const __bf16 *)job->src, job->batch, job->so, job->sj, u, job->side};
+        return rowprod_launch_any<ROW_ADAPT>(rp, ae, s);
+    }
+    const AdapterEpi<float> ae = {e, rp.ad.of_row, bad, (const float *)job->src, job->batch, job->so, job->sj, u, job->side};
+    return f32 ? rowprod_launch<TileS, ROW_F32 | ROW_ADAPT>(rp, ae, s) : rowprod_launch_any<ROW_THREES | ROW_ADAPT>(rp, ae, s);
 }
 
 // Rows straight from memory: up to 64 of them, or 256 where what the workgroups read of W and x (a lane's 16 bytes are a
@@ -701,6 +802,7 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     __bf16 *xroom = w.take<__bf16>(pack_room(p.dtype, g.n, p.d_in)), *wroom = w.take<__bf16>(pack_room(p.dtype, p.d_out, p.d_in));
     SortView sv = {};
     Side side = {};
+    SideFlags flags = {};
     __bf16 *up = nullptr, *bp = nullptr, *zero = nullptr;
     // fp32 rows that lie right, and too few of them for large tiles: as they are
     const bool f32 = rowprod_size(p.d_out, g.n) == 0 && f32_lies_right(p.W, p.dtype, p.d_in, p.d_in) &&
@@ -713,16 +815,20 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         up = w.take<__bf16>(g.n * room);
         bp = w.take<__bf16>((int64_t)p.n_adapters * p.d_out * room);
         zero = w.take<__bf16>(room);
+        flags.found = w.take<uint32_t>(side_blocks(Side{0, 0, room}, (int64_t)p.n_adapters * p.d_out));
+        flags.bad = w.take<uint32_t>(p.n_adapters);
+        flags.rows = p.d_out;
     }
     if (bytes) *bytes = w.used;
     if (!ws) return RAIRS_OK;
 
     const bool use = adapters && g.adapter;
     RowProd rp = {};
+    const SideJob job = {p.B, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, (int64_t)p.n_adapters * p.d_out, side, bp, zero, flags.found};
     if (use) {
         PrepArgs pa = {};
         pa.sort = sv;
-        pa.side = SideJob{p.B, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, (int64_t)p.n_adapters * p.d_out, side, bp, zero};
+        pa.side = job;
         if ((rc = prep_launch(pa, p.dtype, s))) return rc;
     }
     if (f32) {
@@ -737,14 +843,13 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, !bf, xroom, rp.Q, s))) return rc;
     }
     if (use) {
-        ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side};
+        ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side, flags};
         const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
         if ((rc = bf ? shrink_launch<__bf16>(sa, nullptr, units, vec, s) : shrink_launch<float>(sa, nullptr, units, vec, s))) return rc;
         rp.ad = AdapterPart{up, bp, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.y, g.ldy, 0, p.d_out, g.n, use ? sv.perm : nullptr, g.ytype == RAIRS_BF16, 0};
-    if (f32) return use ? rowprod_launch<TileS, ROW_F32 | ROW_ADAPT>(rp, e, s) : rowprod_launch<TileS, ROW_F32>(rp, e, s);
-    return large_product(rp, e, bf, use, s);
+    return large_product(rp, e, bf, f32, use ? &job : nullptr, up, flags.bad, s);
 }
 
 // ---- backward ------------------------------------------------------------------------------------------
@@ -875,6 +980,7 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     __bf16 *yroom = w.take<__bf16>(pack_room(p.dtype, g.n, p.d_out)), *wt = w.take<__bf16>((int64_t)p.d_in * opad * np);
     SortView sv = {};
     Side side = {};
+    SideFlags flags = {};
     __bf16 *vp = nullptr, *ap = nullptr, *zero = nullptr;
     float *u = nullptr, *v = nullptr, *apart = nullptr, *bpart = nullptr;
     char *bt = nullptr;
@@ -884,6 +990,9 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         vp = w.take<__bf16>(g.n * side.kpad);
         ap = w.take<__bf16>((int64_t)na * p.d_in * side.kpad);
         zero = w.take<__bf16>(side.kpad);
+        flags.found = w.take<uint32_t>(side_blocks(side, (int64_t)na * p.d_in));
+        flags.bad = w.take<uint32_t>(na);
+        flags.rows = g.dx ? p.d_in : 0;
         u = w.take<float>(g.n * p.rank);
         v = w.take<float>(g.n * p.rank);
         bt = w.take<char>((int64_t)na * p.rank * p.d_out * dtype_width(p.dtype));
@@ -896,6 +1005,7 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     const bool use = adapters && g.adapter && g.n > 0;
     const PackLayout wto = pack_layout(p.d_in, opad, !bf);
     int rc = RAIRS_OK;
+    const SideJob job = {p.A, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, (int64_t)na * p.d_in, side, ap, zero, flags.found};
     if (use) {
         PrepArgs pa = {};
         pa.sort = sv;
@@ -903,12 +1013,12 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         pa.w = p.W; pa.d_in = p.d_in; pa.d_out = p.d_out; pa.r = p.rank; pa.opad = opad; pa.wto = wto;
         if (g.dx) {
             pa.wt = wt;
-            pa.side = SideJob{p.A, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, (int64_t)na * p.d_in, side, ap, zero};
+            pa.side = job;
         }
         if ((rc = prep_launch(pa, p.dtype, s))) return rc;
         const int64_t units = max_units(g.n, na, UNIT_ROWS);
-        const ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, g.dx ? vp : nullptr, side};
-        const ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, nullptr, side};
+        const ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, g.dx ? vp : nullptr, side, flags};
+        const ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, nullptr, side, {}};
         const bool vec = row_vec(g.dy, g.lddy, p.dtype) && row_vec(bt, p.d_out, p.dtype) &&
                          (!g.da || (row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype)));
         if ((rc = bf ? shrink_launch<__bf16>(sa, g.da ? &su : nullptr, units, vec, s) : shrink_launch<float>(sa, g.da ? &su : nullptr, units, vec, s)))
@@ -928,5 +1038,5 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         rp.ad = AdapterPart{vp, ap, zero, sv.of_row, sv.first + 1, side.kpad};
     }
     StoreEpi e = {g.dx, g.lddx, 0, p.d_in, g.n, use ? sv.perm : nullptr, bf, 0};
-    return large_product(rp, e, bf, use, s);
+    return large_product(rp, e, bf, false, use ? &job : nullptr, vp, flags.bad, s);
 }

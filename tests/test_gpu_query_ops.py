@@ -87,6 +87,8 @@ PROJECTIONS = [
     (65, 257, 129, 17, 70, "many"), (130, 128, 127, 64, 2, "one"), (200, 96, 128, 8, 5, "none"),
     (300, 72, 130, 128, 7, "many"), (1025, 130, 66, 3, 11, "many"), (2100, 64, 64, 33, 200, "many"), (129, 200, 300, 1, 0, "none"),
     (500, 1000, 4, 16, 4096, "many"),
+    # each way of the product: fp32 rows as they are, packed rows in each size of tile; a sort by many workgroups
+    (400, 96, 72, 40, 9, "many"), (1100, 40, 2600, 6, 11, "many"), (3400, 40, 4000, 3, 9, "many"), (20_000, 32, 24, 4, 7, "many"),
 ]
 
 
@@ -135,6 +137,44 @@ def test_project_rows_do_not_touch_each_other(n, t):
     keep = torch.tensor([i not in (1, 3) and i % 3 != 2 for i in range(n)], device="cuda")
     assert torch.equal(y[keep], y2[keep])
     assert not y2[~keep].isfinite().any()
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n,d_in", [(7, 64), (300, 64), (300, 72), (2500, 72)])
+def test_adapters_that_are_not_finite_stay_alone(n, d_in, t):
+    # infinities and NaN in one tenant's B (forward) or A (gradient) reach the values that they are factors of, and no others
+    d_out = 700
+    x, w, a, b, s, ad = projection_data(n, d_in, d_out, 4, 3, t, 6)
+    ad[:] = torch.arange(n, dtype=torch.int32) % 4 - 1
+    x, w, a, s, ad = x.cuda(), w.cuda(), a.cuda(), s.cuda(), ad.cuda()
+    dy = torch.randn(n, d_out, generator=gen(8)).to(t).cuda()
+    for kind in (t, F32):
+        y = binding.Projection(w, a, b.cuda(), s).project(x, ad, out_dtype=kind)
+        b2 = b.clone()
+        b2[2, 5, 1], b2[1, 699, 3] = float("inf"), float("nan")
+        y2 = binding.Projection(w, a, b2.cuda(), s).project(x, ad, out_dtype=kind)
+        odd = torch.zeros(n, d_out, dtype=torch.bool, device="cuda")
+        odd[ad == 2, 5] = True
+        odd[ad == 1, 699] = True
+        assert torch.equal(y[~odd], y2[~odd]) and y[~odd].isfinite().all()
+        assert not y2[odd].isfinite().any()
+        assert y2[ad == 1, 699].isnan().all()
+    dx, da, db = binding.Projection(w, a, b.cuda(), s).backward(x, ad, dy)
+    a2 = a.clone()
+    a2[2, 3, 63] = float("nan")
+    dx2, da2, db2 = binding.Projection(w, a2, b.cuda(), s).backward(x, ad, dy)
+    odd = torch.zeros(n, d_in, dtype=torch.bool, device="cuda")
+    odd[ad == 2, 63] = True
+    assert torch.equal(dx[~odd], dx2[~odd]) and dx2[odd].isnan().all()
+    assert torch.equal(da, da2) and torch.equal(db[:2], db2[:2])
+
+
+@pytest.mark.parametrize("n,d_in,d_out", [(66, 4096, 4096), (300, 64, 96)])
+def test_a_batch_without_adapters_of_a_projection_that_has_them(n, d_in, d_out):
+    x, w, a, b, s, ad = projection_data(n, d_in, d_out, 2, 3, BF16, 2, "none")
+    want, mag = exact_project(x, w, a, b, s, ad)
+    y = binding.Projection(w.cuda(), a.cuda(), b.cuda(), s.cuda()).project(x.cuda())
+    close(y, want, sum_err(d_in) * mag + half(F32) * want.abs(), "y")
 
 
 @pytest.mark.parametrize("t", [F32, BF16])
@@ -409,7 +449,7 @@ BACKWARDS = [
     # n, v, d, live, table gradient
     (1, 1, 1, None, True), (1, 500, 64, None, True), (7, 65, 33, "shared", True), (64, 1000, 96, "rows", True),
     (65, 63, 130, None, True), (130, 700, 64, "shared", True), (100, 3000, 72, "rows", False), (300, 129, 1000, None, True),
-    (20, 200, 24, "none", True), (128, 40_000, 16, "shared", False),
+    (20, 200, 24, "none", True), (128, 40_000, 16, "shared", False), (520, 26_000, 40, "shared", True),
 ]
 
 
