@@ -763,6 +763,7 @@ struct GradArgs {
     const float *lse, *entropy, *dlogp, *dentropy;
     __bf16 *g, *gt;                 // [n][vc], [vc][npad]; either null
     PackLayout gto, gtto;
+    const float2 *rows;             // fp32 (NP 3): row_stats_kernel's
 };
 
 // G = scale (dlogp (1[v = t] - p) - dentropy p (log p + H)) in registers, rounded to bf16 once (bf16
@@ -775,7 +776,7 @@ struct GradEpi {
     GradArgs a;
     template <class T>
     struct State {
-        float da[T::QT], db[T::QT], H[T::QT], lse[T::QT];
+        float da[T::QT], db[T::QT], H[T::QT], lse[T::QT], m[NP == 3 ? T::QT : 1];
         int32_t target[T::QT];      // from the chunk's first row on, or far below it
     };
     template <class T>
@@ -791,7 +792,13 @@ struct GradEpi {
             st.da[j] = in && seen ? a.dlogp[row] * a.scale : 0.0f;
             st.db[j] = ENT && in ? a.dentropy[row] * a.scale : 0.0f;
             st.H[j] = ENT && st.db[j] != 0.0f ? a.entropy[row] : 0.0f;
-            st.lse[j] = a.lse[row];
+            if constexpr (NP == 3) {
+                const float2 r = a.rows[row];
+                st.m[j] = r.x;
+                st.lse[j] = r.y;
+            } else {
+                st.lse[j] = a.lse[row];
+            }
             st.target[j] = in && seen ? (int32_t)(t - a.v0) : -0x7FFFFFFF;
         }
     }
@@ -821,7 +828,7 @@ struct GradEpi {
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
                         // (log p in natural units: scale times the product is exact inside the sum, which log2(e) is not)
-                        const float lp = fmaf(z[r], a.scale, -lse), pr = exp2_fast(lp * LOG2E);
+                        const float lp = fmaf(NP == 3 ? z[r] - st.m[NP == 3 ? j : 0] : z[r], a.scale, -lse), pr = exp2_fast(lp * LOG2E);
                         float g = -da * pr;
                         if constexpr (ENT) g -= db * pr * (fmaxf(lp, -1e4f) + st.H[j]);
                         x[r] = g;
@@ -832,7 +839,7 @@ struct GradEpi {
 #pragma unroll
                         for (int r = 0; r < 4; r++)
                             if (at == (uint32_t)r) {
-                                const float lp = fmaf(z[r], a.scale, -lse), pr = exp2_fast(lp * LOG2E);
+                                const float lp = fmaf(NP == 3 ? z[r] - st.m[NP == 3 ? j : 0] : z[r], a.scale, -lse), pr = exp2_fast(lp * LOG2E);
                                 float g = da * (1.0f - pr);
                                 if constexpr (ENT) g -= db * pr * (fmaxf(lp, -1e4f) + st.H[j]);
                                 x[r] = g;
@@ -885,21 +892,36 @@ struct GradEpi {
     }
 };
 
-// bit i: row i passes a gradient
-__global__ __launch_bounds__(WG) void active_rows_kernel(int64_t n, int64_t V, const int64_t *__restrict__ targets,
-                                                         const uint32_t *__restrict__ live, int64_t ld_live, const float *__restrict__ dlogp,
-                                                         const float *__restrict__ dentropy, uint32_t *__restrict__ out)
+// For log p of fp32 rows: {largest product m, ln s} where m and s say the same as the lse that is given, to eight
+// half steps of it, else {0, lse} (the softmax may be over more than this table: its parts on several devices).  lse is
+// rounded at its own size, 2^-24 |lse|, which log p of a likely row inherits and 1 - p then magnifies; scale (z - m) - ln s
+// is rounded at the size of log p.  A wave per query.
+__global__ __launch_bounds__(WG) void row_stats_kernel(StatsArgs a, float scale, const float *__restrict__ lse, float2 *__restrict__ out)
 {
-    const int64_t i = (int64_t)blockIdx.x * WG + threadIdx.x;
-    bool on = false;
-    if (i < n) {
-        const int64_t t = targets[i];
-        const bool seen = t >= 0 && t < V && (!live || ((live[i * ld_live + (t >> 5)] >> (t & 31)) & 1u));
-        on = (seen && dlogp[i] != 0.0f) || (dentropy && dentropy[i] != 0.0f);
-    }
-    const unsigned long long b = __ballot(on);
     const int lane = threadIdx.x & 63;
-    if ((lane & 31) == 0 && i < n) out[i >> 5] = (uint32_t)(b >> lane);
+    const int64_t row = (int64_t)blockIdx.x * (WG / 64) + (threadIdx.x >> 6);
+    if (row >= a.n) return;
+    const float4 *parts = a.parts + row * a.nparts;
+    float m = HIDDEN, s = 0.0f, e = 0.0f;
+    const auto add = [&](float pm, float ps) {
+        float pe = 0.0f;
+        const float m1 = max_of(m, pm);
+        rebase(s, e, m, m1, a.c);
+        rebase(ps, pe, pm, m1, a.c);
+        s += ps;
+        m = m1;
+    };
+    for (int i = lane; i < a.nparts; i += 64) add(parts[i].x, parts[i].y);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const float pm = __shfl_xor(m, o), ps = __shfl_xor(s, o);
+        add(pm, ps);
+    }
+    if (lane) return;
+    const float given = lse[row];
+    const double logs = log((double)s), own = (double)m * scale + logs;
+    const bool same = m > HIDDEN && fabs(own - given) <= 0x1p-21 * (fabs((double)given) + 1.0);
+    out[row] = same ? make_float2(m, (float)logs) : make_float2(0.0f, given);
 }
 
 // sums of the splits, in their order; rows of dpad values, a multiple of four
@@ -1141,7 +1163,7 @@ static int grad_launch(RowProd &rp, const GradArgs &ga, bool threes, hipStream_t
 int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
 {
     const int np = dtype_pieces(a.qtype), tp = dtype_pieces(a.ttype);
-    const bool threes = tp == 3;
+    const bool threes = tp == 3, again = np == 3;
     const int64_t kpad = pad_to(a.d, threes ? 32 : ROWPROD_K), npad = pad_to(a.n, ROWPROD_K), dpad = pad_to(a.d, 4);
     const bool need_dt = a.dtable != nullptr, need_dq = a.dq != nullptr;
     int64_t vc = GRAD_CHUNK_BYTES / (2 * np * npad) / 1024 * 1024;
@@ -1164,7 +1186,19 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     __bf16 *gt = need_dt ? w.take<__bf16>(vc * npad * np) : nullptr;
     float *sums = need_dq ? w.take<float>(splits * a.n * dpad) : nullptr;
     uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
-    uint32_t *active = need_dt ? w.take<uint32_t>((a.n + 31) / 32) : nullptr;
+    // fp32: the statistics once more, by tiles as in the forward pass
+    StatsArgs st = {};
+    const auto large_of = [&](int64_t rows) { return rowprod_size(rows, a.n) == 2; };
+    const auto parts_of = [&](int64_t rows) {
+        const bool l = large_of(rows);
+        return (threes && l ? 4 : 2) * ((rows + (l ? 255 : 127)) / (l ? 256 : 128));
+    };
+    if (again) {
+        for (int64_t v0 = 0; v0 < a.V; v0 += vc) st.nparts += (int)parts_of(std::min(vc, a.V - v0));
+        st.parts = w.take<float4>(a.n * st.nparts);
+        st.zt = w.take<float>(a.n);
+    }
+    float2 *rows_stats = again ? w.take<float2>(a.n) : nullptr;
     if (bytes) *bytes = w.used;
     if (!ws) return RAIRS_OK;
 
@@ -1173,24 +1207,66 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     if (rc) return rc;
     RowOperand Q = {};
     const PackLayout qto = pack_layout(a.d, npad, threes);
-    if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, threes, qroom, Q, s))) return rc;
+    const auto chunk = [&](int64_t v0) { return (const char *)a.table + v0 * a.ldt * dtype_width(a.ttype); };
+    // what is laid out first: the queries and the table's first rows, both ways round
+    PackJobs jobs = {};
+    RowOperand P0 = {};
+    const auto turn_table = [&](int64_t v0, int64_t rows, int64_t cpad) {
+        PackJob &j = jobs.job[jobs.n++];
+        j = PackJob{};
+        j.src = chunk(v0); j.dst = tcols; j.dtype = a.ttype; j.turned = 1; j.ld = a.ldt; j.rows = rows; j.cols = a.d; j.pad = cpad;
+        j.to = pack_layout(a.d, cpad, threes); j.order = ORDER_TABLE;
+        // (rows that nobody sees are zero here: their G is zero, and they may hold anything)
+        j.live = seen_by_any ? seen_by_any + v0 / 32 : nullptr;
+    };
+    rairs_operand_job(a.q, a.qtype, a.ldq, a.n, a.d, threes, qroom, Q, jobs);
     if (need_dt) {
-        hipLaunchKernelGGL(active_rows_kernel, dim3((unsigned)((a.n + WG - 1) / WG)), dim3(WG), 0, s, a.n, a.V, a.targets, a.live, a.ld_live,
-                           a.dlogp, a.dentropy, active);
+        PackJob &j = jobs.job[jobs.n++];
+        j = PackJob{};
+        j.src = a.q; j.dst = qcols; j.dtype = a.qtype; j.turned = 1; j.ld = a.ldq; j.rows = a.n; j.cols = a.d; j.pad = npad;
+        j.to = qto; j.order = ORDER_QUERIES;
+        j.live = a.live; j.ld_live = a.ld_live; j.targets = a.targets; j.V = a.V; j.dlogp = a.dlogp; j.dentropy = a.dentropy;
+    }
+    if (again) {
+        st.n = (int)a.n; st.c = a.scale * LOG2E; st.ld_live = a.ld_live; st.targets = a.targets;
+        float4 *parts = st.parts;
+        for (int64_t v0 = 0; v0 < a.V; v0 += vc) {
+            const int64_t rows = std::min(vc, a.V - v0);
+            RowProd rp = {};
+            rairs_operand_job(chunk(v0), a.ttype, a.ldt, rows, a.d, threes, troom, rp.P, jobs);
+            if (need_dq && vc >= a.V) turn_table(0, rows, pad_to(rows, ROWPROD_K));
+            if ((rc = rairs_launch_pack(jobs, s))) return rc;
+            jobs.n = 0;
+            P0 = rp.P;
+            rowprod_sums(rp, tp, np, kpad);
+            rp.Q = Q;
+            st.V = (int)rows;
+            st.live = a.live ? a.live + v0 / 32 : nullptr;
+            if ((rc = stats_launch<false, 0>(rp, st, threes, large_of(rows), 1, s))) return rc;
+            st.parts += parts_of(rows);
+        }
+        st.parts = parts;
+        hipLaunchKernelGGL(row_stats_kernel, dim3((unsigned)((a.n + WG / 64 - 1) / (WG / 64))), dim3(WG), 0, s, st, a.scale, a.lse_in, rows_stats);
         RAIRS_HIP(hipGetLastError());
-        if ((rc = rairs_launch_pack_cols(a.q, a.qtype, a.ldq, a.n, a.d, active, ORDER_QUERIES, qcols, npad, qto, s))) return rc;
     }
     for (int64_t v0 = 0; v0 < a.V; v0 += vc) {
         const int64_t rows = a.V - v0 < vc ? a.V - v0 : vc, cpad = pad_to(rows, ROWPROD_K);
-        const char *t = (const char *)a.table + v0 * a.ldt * dtype_width(a.ttype);
         RowProd rp = {};
+        if (again && vc >= a.V) {
+            rp.P = P0;                                                // (laid out above)
+        } else {
+            rairs_operand_job(chunk(v0), a.ttype, a.ldt, rows, a.d, threes, troom, rp.P, jobs);
+            if (need_dq) turn_table(v0, rows, cpad);
+            if ((rc = rairs_launch_pack(jobs, s))) return rc;
+            jobs.n = 0;
+        }
         rowprod_sums(rp, tp, np, kpad);
         rp.Q = Q;
-        if ((rc = rairs_operand(t, a.ttype, a.ldt, rows, a.d, nullptr, threes, troom, rp.P, s))) return rc;
         GradArgs ga = {};
         ga.n = (int)a.n; ga.V = (int)a.V; ga.v0 = (int)v0; ga.vc = (int)cpad; ga.npad = (int)npad;
         ga.scale = a.scale;
         ga.live = a.live; ga.ld_live = a.ld_live; ga.targets = a.targets;
+        ga.rows = rows_stats;
         ga.lse = a.lse_in; ga.entropy = a.entropy_in; ga.dlogp = a.dlogp; ga.dentropy = a.dentropy;
         ga.g = g; ga.gt = gt;
         ga.gto = pack_layout(a.n, cpad, threes); ga.gtto = pack_layout(cpad, npad, threes);
@@ -1200,9 +1276,6 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         if (rc) return rc;
         if (need_dq) {
             const PackLayout tto = pack_layout(a.d, cpad, threes);
-            // (rows that nobody sees are zero here: their G is zero, and they may hold anything)
-            if ((rc = rairs_launch_pack_cols(t, a.ttype, a.ldt, rows, a.d, seen_by_any ? seen_by_any + v0 / 32 : nullptr, ORDER_TABLE, tcols, cpad, tto, s)))
-                return rc;
             RowProd dp = {};
             rowprod_sums(dp, tp, np, cpad);
             dp.P = RowOperand{tcols, tto.ld, tto.piece, a.d, nullptr, nullptr};

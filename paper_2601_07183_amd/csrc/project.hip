@@ -485,8 +485,8 @@ __global__ __launch_bounds__(1024) void prep_kernel(PrepArgs a)
         const int half = threadIdx.x >> 9;
         const int64_t rt = a.opad / 64, ct = (a.d_in + 63) / 64, t = block * 2 + half;
         PackCols<S, NP> *sh = (PackCols<S, NP> *)prep_lds;
-        pack_cols_tile<S, NP, 512>(sh[half], threadIdx.x & 511, t < rt * ct, (const S *)a.w, a.d_in, a.d_out, a.d_in, nullptr, ORDER_SAME, a.vec, a.wt,
-                                   a.opad, a.wto, t % rt * 64, t / rt * 64);
+        pack_cols_tile<S, NP, 512>(sh[half], threadIdx.x & 511, t < rt * ct, (const S *)a.w, a.d_in, a.d_out, a.d_in, ORDER_SAME, a.vec, a.wt, a.opad,
+                                   a.wto, t % rt * 64, t / rt * 64, [](int64_t) { return true; });
         return;
     }
     block -= a.cols_blocks;

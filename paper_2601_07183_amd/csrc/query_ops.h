@@ -58,6 +58,31 @@ static inline int64_t pack_room(int dtype, int64_t rows, int64_t cols) { return 
 // (threes: both operands of the product are fp32)
 int rairs_operand(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, const int32_t *perm, bool threes, __bf16 *room,
                   RowOperand &out, hipStream_t s, uint32_t *flags = nullptr, bool clear = false);
+// Several matrices laid out by one launch.
+struct PackJob {
+    const void *src;
+    __bf16 *dst;
+    int dtype, turned;              // turned: as rairs_launch_pack_cols does, else as rairs_launch_pack_rows
+    int64_t ld, rows, cols, pad;    // pad: values of a row of dst
+    PackLayout to;
+    int order;
+    const uint32_t *live;
+    // turned, if targets are given: rows that pass no gradient (their target outside the mask `live`, [ld_live] words a row,
+    // or dlogp 0, and dentropy 0) are zero instead
+    const int64_t *targets;
+    int64_t ld_live, V;
+    const float *dlogp, *dentropy;
+    int vec;                        // (set by the launch, as is what follows)
+    unsigned blocks;
+};
+#define PACK_JOBS 4
+struct PackJobs {
+    PackJob job[PACK_JOBS];
+    int n;
+};
+int rairs_launch_pack(PackJobs &jobs, hipStream_t s);
+// an operand as rairs_operand makes it, its packing (if it needs any) left to `jobs`
+void rairs_operand_job(const void *src, int dtype, int64_t ld, int64_t rows, int64_t cols, bool threes, __bf16 *room, RowOperand &out, PackJobs &jobs);
 // the products of an np-piece operand with an nq-piece one over kpad values
 static inline void rowprod_sums(RowProd &rp, int np, int nq, int64_t kpad)
 {

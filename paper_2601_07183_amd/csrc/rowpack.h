@@ -50,21 +50,21 @@ static __device__ __forceinline__ int place_of(int r, int order)
     return order == 0 ? r : order == 1 ? 16 * ((r >> 2) & 3) + 4 * (r >> 4) + (r & 3) : 4 * (r & 15) + (r >> 4);
 }
 
-// one tile, by NT threads (barriers are the workgroup's: all of it is in here); `inside`: there is such a tile
+// one tile, by NT threads, rows that are not live zero (barriers are the workgroup's: all of it is in here); `inside`: there is such a tile
 template <class S, int NP>
 struct PackCols {
     __bf16 tile[NP][64][72];        // [piece][column][row], rows of 144 bytes
 };
-template <class S, int NP, int NT>
+template <class S, int NP, int NT, class Live>
 static __device__ __forceinline__ void pack_cols_tile(PackCols<S, NP> &sh, int tid, bool inside, const S *__restrict__ src, int64_t ld, int64_t rows,
-                                                      int64_t cols, const uint32_t *__restrict__ live, int order, int vec, __bf16 *__restrict__ dst,
-                                                      int64_t rpad, const PackLayout &to, int64_t r0, int64_t c0)
+                                                      int64_t cols, int order, int vec, __bf16 *__restrict__ dst, int64_t rpad,
+                                                      const PackLayout &to, int64_t r0, int64_t c0, const Live &live)
 {
 #pragma unroll
     for (int h = 0; h < 512 / NT; h++) {
         const int t = tid + h * NT, r = t >> 3, i0 = (t & 7) * 8;
         float x[8];
-        const bool in = inside && r0 + r < rows && row_live(live, r0 + r);
+        const bool in = inside && r0 + r < rows && live(r0 + r);
         if (in) load8(src + (r0 + r) * ld, c0 + i0, cols, vec, x);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
