@@ -380,7 +380,7 @@ struct FinishShared {
     float lval[LIST];
     uint32_t lid[LIST];
     float kth_in[256];
-    float red[16];
+    float red[16], red5[NT > 64 ? 16 : 1][5];
     float kth_out;
     int count, nbest, wcnt[16];
 };
@@ -406,6 +406,36 @@ static __device__ __forceinline__ float team_fold(FinishShared<NT> &sh, float x,
         for (int w = 1; w < NT / 64; w++) x = f(x, sh.red[w]);
     }
     return x;
+}
+
+// sums of s, e and q2, the largest x2, the least zero
+template <int NT>
+static __device__ __forceinline__ void team_fold5(FinishShared<NT> &sh, float &s, float &e, float &q2, float &x2, float &zero)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        s += __shfl_xor(s, o);
+        e += __shfl_xor(e, o);
+        q2 += __shfl_xor(q2, o);
+        x2 = fmaxf(x2, __shfl_xor(x2, o));
+        zero = fminf(zero, __shfl_xor(zero, o));
+    }
+    if constexpr (NT > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            float *to = sh.red5[threadIdx.x >> 6];
+            to[0] = s; to[1] = e; to[2] = q2; to[3] = x2; to[4] = zero;
+        }
+        __syncthreads();
+        s = sh.red5[0][0]; e = sh.red5[0][1]; q2 = sh.red5[0][2]; x2 = sh.red5[0][3]; zero = sh.red5[0][4];
+        for (int w = 1; w < NT / 64; w++) {
+            s += sh.red5[w][0];
+            e += sh.red5[w][1];
+            q2 += sh.red5[w][2];
+            x2 = fmaxf(x2, sh.red5[w][3]);
+            zero = fminf(zero, sh.red5[w][4]);
+        }
+    }
 }
 
 // rows of an entry of the lists: the row itself, a group of 16 or one of 64
@@ -576,8 +606,6 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
     const int tid = threadIdx.x % NT;
     const int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / NT;
     if (row >= a.st.n) return;                                        // (teams of a workgroup do not wait for each other)
-    const auto largest = [](float x, float y) { return fmaxf(x, y); };
-    const auto sum = [](float x, float y) { return x + y; };
     const float4 *parts = a.st.parts + row * a.st.nparts;
     const float c = a.st.c;
     float m = HIDDEN, s = 0.0f, e = 0.0f;
@@ -590,10 +618,21 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
         e += p.z;
         m = m1;
     }
+    // |q|^2 and the table's largest squared norm, for the margin
+    float q2 = 0.0f, x2 = 0.0f, zero = 1.0f;
+    const Q *q = (const Q *)a.q + row * a.ldq;
+    if (a.top) {
+        for (int k = tid; k < a.d; k += NT) {
+            const float x = (float)q[k];
+            q2 = fmaf(x, x, q2);
+            zero = x == 0.0f ? zero : 0.0f;
+        }
+#pragma unroll 8
+        for (int i = tid; i < a.nxmax; i += NT) x2 = fmaxf(x2, a.xmax[i]);
+    }
     const float top = team_fold(sh, m, [](float x, float y) { return max_of(x, y); });
     rebase(s, e, m, top, c);
-    s = team_fold(sh, s, sum);
-    e = team_fold(sh, e, sum);
+    team_fold5<NT>(sh, s, e, q2, x2, zero);
     const bool empty = top == HIDDEN && s == 0.0f;
     const float mc = top * c, logs = log2f(s);
     if (tid == 0) {
@@ -611,19 +650,6 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
     }
     if (a.top == 0) return;
 
-    // |q|^2 and the table's largest squared norm, for the margin; and the groups' maxima
-    float q2 = 0.0f, x2 = 0.0f, zero = 1.0f;
-    const Q *q = (const Q *)a.q + row * a.ldq;
-    for (int k = tid; k < a.d; k += NT) {
-        const float x = (float)q[k];
-        q2 = fmaf(x, x, q2);
-        zero = x == 0.0f ? zero : 0.0f;
-    }
-#pragma unroll 8
-    for (int i = tid; i < a.nxmax; i += NT) x2 = fmaxf(x2, a.xmax[i]);
-    q2 = team_fold(sh, q2, sum);
-    x2 = team_fold(sh, x2, largest);
-    zero = team_fold(sh, zero, [](float x, float y) { return x * y; });
     // what a product may be off by (components whose squares underflow, and a group's row in the last bits of a
     // denormal, have terms of their own); not finite: nothing can be told apart
     const float under = sqrtf((float)a.d) * 1.1e-19f;
@@ -1157,7 +1183,9 @@ static int grad_launch(RowProd &rp, const GradArgs &ga, bool threes, hipStream_t
     // (three pieces of bytes' gradients: 128 x 128 alone, whose pieces fit the registers)
     if constexpr (NP == 3) return rowprod_launch<TileW>(rp, GradEpi<NP, ENT>{ga}, s);
     else
-    return rowprod_size(rp.P.rows, rp.Q.rows) == 2 ? rowprod_launch<TileL>(rp, GradEpi<NP, ENT>{ga}, s) : rowprod_launch<TileW>(rp, GradEpi<NP, ENT>{ga}, s);
+    return rowprod_size(rp.P.rows, rp.Q.rows) == 2
+               ? rowprod_launch<TileL>(rp, GradEpi<NP, ENT>{ga}, s, rowprod_run((rp.P.rows + 255) / 256, (rp.Q.rows + 255) / 256, 256, 0.2, 64))
+               : rowprod_launch<TileW>(rp, GradEpi<NP, ENT>{ga}, s);
 }
 
 int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
@@ -1175,7 +1203,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     const int64_t tl = rowprod_tiles(a.d, a.n, 256), tm = rowprod_tiles(a.d, a.n, 128), ts = rowprod_tiles(a.d, a.n, 64);
     int64_t splits = (256 + tl - 1) / tl;
     if (splits > vc / 2048) splits = std::min((256 + tm - 1) / tm, vc / 1024);
-    if (splits * tm < 160) splits = std::min((512 + ts - 1) / ts, vc / 512);
+    if (splits * tm < 160) splits = std::min((512 + ts - 1) / ts, vc / (threes ? 128 : 512));
     if (splits < 1) splits = 1;
     Carve w(ws);
     __bf16 *qroom = w.take<__bf16>(pack_room(a.qtype, a.n, a.d));
