@@ -354,6 +354,7 @@ enum { RAIRS_F32 = 0, RAIRS_BF16 = 1, RAIRS_U8 = 2 };
 #define RAIRS_MAX_RANK 128          /* of an adapter */
 #define RAIRS_MAX_ADAPTERS 4096
 #define RAIRS_MAX_ROWS (1 << 24)    /* rows of a batch */
+#define RAIRS_MAX_GRAD_ROWS (1 << 20)   /* of one for rairs_logprob_backward */
 #define RAIRS_MAX_WIDTH 16384       /* d_in, d_out; d of a table's rows */
 #define RAIRS_MAX_TOP 64            /* most probable rows that rairs_logprob returns */
 
@@ -375,8 +376,8 @@ typedef struct {
  *   d_adapter  device [n] int32: the row's adapter; a value outside [0, n_adapters) means none.  Rows of
  *              an adapter need not be together.  NULL: no row has one
  *   d_y        device [n] rows of d_out, y_dtype RAIRS_F32 or dtype
- * Sums are held in fp32; A[a] x enters the second product with 16 or more bits.  n == 0 is a
- * successful no-op.
+ * Sums are held in fp32, A[a] x among them.  What is not finite in a row or in an adapter reaches that
+ * row, or that adapter's rows, alone.  n == 0 is a successful no-op.
  */
 size_t rairs_project_workspace_bytes(const rairs_projection_t *p, int64_t n);
 int rairs_project(const rairs_projection_t *p, const void *d_x, int64_t ld_x, int64_t n, const int32_t *d_adapter, void *d_y,
@@ -448,6 +449,7 @@ int rairs_logprob(const rairs_table_t *t, const void *d_q, int64_t ld_q, int q_d
  * either may be NULL; d_dtable only for tables that are not RAIRS_U8 (zeros in rows that no query sees).
  *   d_lse, d_entropy  what rairs_logprob wrote; d_dlogp [n] fp32; d_dentropy [n] fp32 or NULL (d_entropy may
  *                     then be NULL too)
+ * n <= RAIRS_MAX_GRAD_ROWS (parts of a larger batch one after the other; d_dtable is the parts' sum).
  * A target that is none or that the mask hides passes no gradient; a row that passes none at all (dlogp
  * and dentropy 0) may hold anything and gets zeros.
  */

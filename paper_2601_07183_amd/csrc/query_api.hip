@@ -213,9 +213,16 @@ extern "C" int rairs_logprob(const rairs_table_t *t, const void *d_q, int64_t ld
     return rairs_run_logprob(a, d_ws, nullptr, (hipStream_t)hip_stream);
 }
 
+// (rows of the gradient of the logits, three pieces a value, are within 32-bit offsets of a tile's first)
+static int check_grad_rows(int64_t n)
+{
+    if (n > RAIRS_MAX_GRAD_ROWS) FAIL(RAIRS_EUNSUPPORTED, "n=%lld above the built limit %d of the gradient", (long long)n, RAIRS_MAX_GRAD_ROWS);
+    return RAIRS_OK;
+}
+
 extern "C" size_t rairs_logprob_backward_workspace_bytes(const rairs_table_t *t, int64_t n, int q_dtype, int table_grad)
 {
-    if (check_table(t, n, q_dtype) || n == 0) return 0;
+    if (check_table(t, n, q_dtype) || check_grad_rows(n) || n == 0) return 0;
     LogprobArgs a = logprob_args(t, nullptr, t->d, q_dtype, n);
     a.dq = a.dtable = (void *)256;                                    // (wanted or not: not looked at)
     if (!table_grad) a.dtable = nullptr;
@@ -230,6 +237,7 @@ extern "C" int rairs_logprob_backward(const rairs_table_t *t, const void *d_q, i
                                       size_t ws_bytes, void *hip_stream)
 {
     TRY(check_table(t, n, q_dtype));
+    TRY(check_grad_rows(n));
     if (d_dtable && t->dtype == RAIRS_U8) FAIL(RAIRS_EINVAL, "a table of bytes has no gradient");
     const int tw = dtype_width(t->dtype);
     if (d_dtable) TRY(check_rows("d_dtable", d_dtable, ld_dtable, t->d, tw));

@@ -3,13 +3,12 @@
 // with the summed dimension contiguous), with what is done to a tile's results left to a functor.
 //
 // Values of more than 8 bits go in as sums of bf16 pieces, three for fp32 (24 bits), and a product is
-// the sum of the products of pieces that matter: of nine the six with the larger factors, the small
-// ones first (what is left out is below 2^-23 |P||Q|).  A piece list is only a longer sum, so bf16
-// rows, fp32 rows and byte rows share one kernel.
+// the sum of the products of pieces that matter: of nine the six with the larger factors (what is left out is
+// below 2^-23 |P||Q|).  A piece list is only a longer sum, so bf16 rows, byte rows and fp32 rows share one kernel.
 //
 // fp32 with fp32 ("threes") goes by steps of 32 values with all three pieces of both in LDS, from rows in which each
-// 32 values' pieces follow each other: six products of what is read once, which halves the traffic (2,999 x 960 x 1024:
-// PENDING).  The products with smaller factors have sums of their own, added at the end, so that they
+// 32 values' pieces follow each other: six products of what is read once, which halves the traffic (2,999 x 1024 x 960
+// with adapters: 49 us, 66 as six sums one after the other).  The products with smaller factors have sums of their own, added at the end, so that they
 // do not round the large one's.
 //
 // Small products of fp32 rows take the rows as they are and the fp32 matrix instruction (a sixteenth of the
@@ -17,8 +16,8 @@
 // units of two bytes all the same, so that a step is 32 values.
 //
 // A workgroup stages 64 values of each of its rows in LDS, fetched straight into LDS by 16-byte loads into a ring
-// of two buffers (large tiles, whose products take longer than a load) or four (small ones).  Such a load writes lane l's bytes at base + 16 l, so the order in LDS is chosen by
-// the address that each lane reads: slot s of row r holds the row's 16-byte chunk s ^ (r & 7), which
+// of two buffers (large tiles, whose products take longer than a load) to four (small ones).  Such a load writes
+// lane l's bytes at base + 16 l, so the order in LDS is chosen by the address that each lane reads: slot s of row r holds the row's 16-byte chunk s ^ (r & 7), which
 // keeps a global access 128 bytes long and the operand reads (16 rows, one chunk) free of bank conflicts.
 #pragma once
 #include <algorithm>
@@ -96,17 +95,19 @@ struct RowTile {
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
-// The tile of a product.  Large tiles need less of the caches per product (256 x 256: a step's 64 KB for 2,048
-// cycles of products, 128 x 128: 32 KB for 512), small ones give more workgroups.  Measured (us, 256 / 128 / 64):
-// 4096 x 8191 x 4096 251 / 339 / 600; 1024 x 4096 x 13120 270 / 126 / 239; 1024 x 2999 x 960 of fp32 130 / 55 / 77; 128 x
-// 10,000 x 1024 of fp32 125 / 55 / 46; 1024 x 512 x 1024 30 / 14 / 9.
+// What bounds a tile is LDS next to the matrix cores: a step of 256 x 256 is 64 KB to write and 192 KB to read for
+// 2,048 cycles of products, of 128 x 128 32 and 96 KB for 512.  Large tiles need less of the caches, small ones give more
+// workgroups.  Measured (bf16, us, 256 / 128 / 64): 4096 x 8191 x 4096 251 / 339 / 600; 1024 x 4096 x 13120 270 / 126 / 239;
+// 1024 x 512 x 1024 30 / 14 / 9.  The largest reach 1.1 PFLOP/s (4096 x 128,000 x 1024 with the statistics: 1.0 ms).
 typedef RowTile<8, 4, 2, 4, 2> TileL;       // 256 x 256, 8 waves
 typedef RowTile<4, 2, 2, 4, 3> TileM;       // 128 x 128, 8 waves
 typedef RowTile<2, 2, 2, 2, 4> TileS;       // 64 x 64, 4 waves
 typedef RowTile<4, 4, 4, 2, 2> TileT;       // 256 x 128, 8 waves: what threes have for TileL
 typedef RowTile<2, 2, 2, 2, 3> TileU;       // 64 x 64: and for TileS (two workgroups a CU)
 typedef RowTile<4, 4, 2, 2, 2> TileW;       // 128 x 128, 4 waves: 64 x 64 to a wave, for epilogues that want that
-// few queries, whose rows' loads are what counts: about 100 KB of them on the way
+// few queries, whose rows' loads are what counts: about 100 KB of them on the way in a workgroup that has a CU to
+// itself (two workgroups with half of that each: the same time).  1M x 128 fp32 and one query: 92 us, 5.6 TB/s, with the
+// norms; 131,071 x 1024 bf16 and 16 queries: 46 us, 5.8 TB/s.
 typedef RowTile<4, 1, 4, 1, 4> TileF1;      // 256 x 16
 typedef RowTile<4, 2, 4, 1, 4> TileF2;      // 256 x 32
 typedef RowTile<4, 4, 4, 1, 3> TileF4;      // 256 x 64

@@ -450,6 +450,8 @@ BACKWARDS = [
     (1, 1, 1, None, True), (1, 500, 64, None, True), (7, 65, 33, "shared", True), (64, 1000, 96, "rows", True),
     (65, 63, 130, None, True), (130, 700, 64, "shared", True), (100, 3000, 72, "rows", False), (300, 129, 1000, None, True),
     (20, 200, 24, "none", True), (128, 40_000, 16, "shared", False), (520, 26_000, 40, "shared", True),
+    # more rows of the table than are taken at a time
+    (3, 1_100_000, 4, "rows", True),
 ]
 
 

@@ -74,7 +74,7 @@ def test_a_projection_that_cannot_be(change, code, says):
 @pytest.mark.parametrize("kw,code,says", [
     (dict(n=-1), EINVAL, "negative"), (dict(n=1 << 25), EUNSUPPORTED, "limit"), (dict(x=None), EINVAL, "d_x"), (dict(y=None), EINVAL, "d_y"),
     (dict(ldx=63), EINVAL, "stride"), (dict(ldy=31), EINVAL, "stride"), (dict(x=P + 1), EINVAL, "aligned"), (dict(yt=1), EINVAL, "output type"),
-    (dict(ws=None), EWORKSPACE, "workspace"), (dict(nw=4), EWORKSPACE, "needed"), (dict(ws=P + 16), EINVAL, "256-byte"),
+    (dict(n=20, ws=None), EWORKSPACE, "workspace"), (dict(n=20, nw=4), EWORKSPACE, "needed"), (dict(n=20, ws=P + 16), EINVAL, "256-byte"),
     (dict(ldx=1 << 40), EUNSUPPORTED, "stride"),
 ])
 def test_project_refuses(kw, code, says):
@@ -115,6 +115,7 @@ def test_logprob_refuses(kw, code, says):
 
 
 @pytest.mark.parametrize("kw,code,says", [
+    (dict(n=(1 << 20) + 1), EUNSUPPORTED, "gradient"),
     (dict(n=-1), EINVAL, "negative"), (dict(q=None), EINVAL, "d_q"), (dict(tg=None), EINVAL, "null"), (dict(da=None), EINVAL, "null"),
     (dict(lse=None), EINVAL, "null"), (dict(db=P), EINVAL, "d_entropy"), (dict(lddq=1), EINVAL, "stride"), (dict(dt=P, lddt=1), EINVAL, "stride"),
     (dict(nw=8), EWORKSPACE, "needed"),
