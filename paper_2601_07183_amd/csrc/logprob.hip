@@ -31,10 +31,10 @@ struct StatsArgs {
     const int64_t *targets;
     float4 *parts;                  // [n][nparts] {m, s, e, 0}; m: the largest product itself, not times c
     int nparts;
-    // Groups of block b (rows 64 b .. 64 b + 63): [b][n][4] {largest, second} of rows 64 b + 16 i + 4 h + r for h = 0..3
-    // (a wave's store is one run of memory), or, wide, [n][b] the largest of all (a sixteenth of that; a query's are
-    // read in one run)
-    float *gmax;
+    // Groups of block b (rows 64 b .. 64 b + 63): [b][n][4] the largest of rows 64 b + 16 i + 4 h + r for h = 0..3 (a wave's
+    // store is one run of memory) and, apart, the second largest; or, wide, [n][b] the largest of all (a sixteenth of that;
+    // a query's are read in one run)
+    float *gmax, *gsecond;
     int nblocks;
     int wide, wstride;              // (a query's run is filled up to a multiple of four values)
     float *zt;                      // [n] the target's product
@@ -141,8 +141,11 @@ struct StatsState {
                             g = max_of(g, x);
                         }
                     if (blk < a.nblocks) {
-                        float2 *to = (float2 *)a.gmax + ((int64_t)blk * a.n + q0 + 16 * j) * 4;
-                        if (in) to[4 * (lane & 15) + h] = make_float2(g, g2);
+                        const int64_t at = ((int64_t)blk * a.n + q0 + 16 * j) * 4;    // uniform
+                        if (in) {
+                            (a.gmax + at)[4 * (lane & 15) + h] = g;
+                            (a.gsecond + at)[4 * (lane & 15) + h] = g2;
+                        }
                     }
                 } else {
 #pragma unroll
@@ -660,10 +663,8 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
 
     // entry i of the query's groups: block i >> shift, its part i & 3 if it has four
     const int shift = a.st.wide ? 0 : 2, ngroups = a.st.nblocks << shift;
-    const float *wmax = a.st.gmax + row * a.st.wstride;
-    const auto group_at = [&](int i) {
-        return a.st.wide ? wmax + i : a.st.gmax + ((((int64_t)(i >> 2) * a.st.n + row) << 2) + (i & 3)) * 2;
-    };
+    const auto group_at = [&](int i) { return a.st.wide ? (int64_t)i : (((int64_t)(i >> 2) * a.st.n + row) << 2) + (i & 3); };
+    const float *gmax = a.st.wide ? a.st.gmax + row * a.st.wstride : a.st.gmax;
     // A thread's groups are four sets; of each it keeps the largest value, where that is, and the second largest.
     // (loads first, then straight-line code: a load whose use is behind a branch is moved there, and loads then wait
     // for one another)
@@ -674,30 +675,17 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
         where[set] = x > most[set] ? i : where[set];
         most[set] = fmaxf(most[set], x);
     };
-    // place k of set u of this thread
-    const auto group_of = [&](int u, int k) { return a.st.wide ? 4 * (tid + k * NT) + u : tid + (u + 4 * k) * NT; };
-    if (a.st.wide) {
-        const int fours = (ngroups + 3) / 4;
-        for (int k = 0; tid + k * NT < fours; k += 8) {
-            v4f x[8];
+    // place k of set u of this thread: four sets are 16 bytes
+    const auto group_of = [&](int u, int k) { return 4 * (tid + k * NT) + u; };
+    const int fours = (ngroups + 3) / 4;
+    for (int k = 0; tid + k * NT < fours; k += 8) {
+        v4f x[8];
 #pragma unroll
-            for (int u = 0; u < 8; u++) x[u] = *(const v4f *)(wmax + 4 * min(tid + (k + u) * NT, fours - 1));
+        for (int u = 0; u < 8; u++) x[u] = *(const v4f *)(gmax + group_at(4 * min(tid + (k + u) * NT, fours - 1)));
 #pragma unroll
-            for (int u = 0; u < 8; u++)
+        for (int u = 0; u < 8; u++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) keep(e, group_of(e, k + u) < ngroups ? x[u][e] : HIDDEN, group_of(e, k + u));
-        }
-    } else {
-        for (int k = 0; tid + 4 * k * NT < ngroups; k += 4) {
-            float x[16];
-#pragma unroll
-            for (int u = 0; u < 16; u++) x[u] = *group_at(min(group_of(u & 3, k + (u >> 2)), ngroups - 1));
-#pragma unroll
-            for (int u = 0; u < 16; u++) {
-                const int i = group_of(u & 3, k + (u >> 2));
-                keep(u & 3, i < ngroups ? x[u] : HIDDEN, i);
-            }
-        }
+            for (int e = 0; e < 4; e++) keep(e, group_of(e, k + u) < ngroups ? x[u][e] : HIDDEN, group_of(e, k + u));
     }
     if (!empty && eps < 1e38f) {                                      // (the same in every thread)
         const float thr = kth_set_max<NT>(sh, most, a.top, tid) - 2.0f * eps;
@@ -716,7 +704,7 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
             for (int k = 0; group_of(u, k) < ngroups; k += 8) {
                 float x[8];
 #pragma unroll
-                for (int w = 0; w < 8; w++) x[w] = *group_at(min(group_of(u, k + w), ngroups - 1));
+                for (int w = 0; w < 8; w++) x[w] = gmax[group_at(min(group_of(u, k + w), ngroups - 1))];
                 uint32_t hits = 0;
 #pragma unroll
                 for (int w = 0; w < 8; w++) {
@@ -734,10 +722,10 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
         if (groups <= FinishShared<NT>::ITEMS)
             for (int u0 = tid; u0 < groups; u0 += NT) {
                 const int i = (int)sh.id[u0];
-                const float *g = group_at(i);
-                const float x = g[0];
+                const int64_t g = group_at(i);
+                const float x = gmax[g];
                 // the group's best row alone, or all of its rows if another may reach the bound too; wide: the group
-                const int rows = !a.st.wide && g[1] >= thr ? 16 : 1, at = atomicAdd(&sh.count, rows);
+                const int rows = !a.st.wide && a.st.gsecond[g] >= thr ? 16 : 1, at = atomicAdd(&sh.count, rows);
                 for (int u = 0; u < rows && at + u < FinishShared<NT>::LIST; u++) {
                     sh.lval[at + u] = x;
                     sh.lid[at + u] = a.st.wide ? (uint32_t)i
@@ -761,7 +749,7 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
             // rows, so that a block whose rows can only equal the K-th best comes too late to displace it
             for (int i0 = 0; i0 < ngroups; i0 += NT) {
                 const int i = i0 + tid;
-                const float x = i < ngroups ? *group_at(i) : HIDDEN;
+                const float x = i < ngroups ? gmax[group_at(i)] : HIDDEN;
                 finish_entries<S, Q, NT>(a, sh, row, tid, x >= thr && x > HIDDEN, (uint32_t)i, a.st.wide ? ENTRY_WIDE : ENTRY_GROUP, floor, [&]() {
                     if (sh.nbest < a.top) return false;
                     const double k = sh.best[a.top - 1], up = zeros ? 0.0 : (double)x + (double)eps;
@@ -983,8 +971,9 @@ __global__ __launch_bounds__(WG) void clear_rows_kernel(void *out, int64_t n, in
 
 // ---- launches ----------------------------------------------------------------------------------------
 
-// Up to here a tile has all of the queries, so that the table is read once (FEWSIDES), and a query is finished by a
-// whole workgroup.
+// Up to here a tile has all of the queries, so that the table is read once and as it is, and a query is finished by a
+// whole workgroup.  So / by the larger tiles, us: 64 queries, 131,071 x 1024 bf16 74 / 133, 1M x 128 fp32 275 / 609; one
+// query 66 / 131 and 134 / 594.
 #define FEW_ROWS 64
 
 static int lies_vec(const void *p, int dtype, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * dtype_width(dtype) % 16 == 0; }
@@ -1091,7 +1080,8 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     st.n = (int)a.n; st.V = (int)a.V; st.c = a.scale * LOG2E; st.live = a.live; st.ld_live = a.ld_live; st.targets = a.targets;
     st.parts = w.take<float4>(a.n * most_parts);
     st.wstride = (int)pad_to(blocks, 4);
-    st.gmax = a.top ? w.take<float>(wide ? a.n * st.wstride : a.n * blocks * 8) : nullptr;
+    st.gmax = a.top ? w.take<float>(wide ? a.n * st.wstride : a.n * blocks * 4) : nullptr;
+    st.gsecond = a.top && !wide ? w.take<float>(a.n * blocks * 4) : nullptr;
     st.nblocks = (int)blocks;
     st.wide = wide;
     st.zt = w.take<float>(a.n);
