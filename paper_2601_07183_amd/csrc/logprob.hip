@@ -491,7 +491,7 @@ struct DotLoad {                    // values per lane and step (eight bytes: si
     static constexpr int CH = sizeof(S) == 1 ? 8 : 16 / sizeof(S);
 };
 
-// <q, t> in float64 for U rows at once by `lanes` lanes (1 to 16), whose own place is `sub`; the order of a
+// <q, t> in float64 for U rows at once by `lanes` lanes (1 to 64), whose own place is `sub`; the order of a
 // sum depends on d alone, so equal rows get equal values
 template <class S, class Q, bool VEC, int U>
 static __device__ __forceinline__ void dot_exact(const S *const (&t)[U], const Q *q, int d, int sub, int lanes, double (&x)[U])
@@ -1021,7 +1021,7 @@ template <class S, class Q>
 static int finish_launch(FinishArgs &f, hipStream_t s)
 {
     f.dot_lanes = 1;
-    while (f.dot_lanes < 16 && f.dot_lanes * DotLoad<S>::CH < f.d) f.dot_lanes *= 2;
+    while (f.dot_lanes < 64 && f.dot_lanes * DotLoad<S>::CH < f.d) f.dot_lanes *= 2;
     if (f.st.n <= FEW_ROWS) hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 1024, 1>), dim3((unsigned)f.st.n), dim3(1024), 0, s, f);
     else hipLaunchKernelGGL((logprob_finish_kernel<S, Q, 64, 4>), dim3((unsigned)((f.st.n + 3) / 4)), dim3(256), 0, s, f);
     RAIRS_HIP(hipGetLastError());
