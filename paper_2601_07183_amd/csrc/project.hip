@@ -462,6 +462,7 @@ struct PrepArgs {
     SortView sort;
     int sorts;                      // workgroups: 0 or 1
     unsigned side_blocks, cols_blocks, turn_blocks;
+    PackJobs rows;                  // W (forward) and the batch, in the batch's order
     SideJob side;
     const void *w, *b;              // [d_out][d_in], [na][d_out][r]
     int d_in, d_out, r, vec;
@@ -495,7 +496,26 @@ __global__ __launch_bounds__(1024) void prep_kernel(PrepArgs a)
         return;
     }
     block -= a.cols_blocks;
+    for (int i = 0; i < a.rows.n; i++) {
+        if (block < a.rows.job[i].blocks) {
+            pack_rows_job<S, NP, 1024>(a.rows.job[i], block);
+            return;
+        }
+        block -= a.rows.job[i].blocks;
+    }
     transpose_tile<S>(*(S(*)[32][33])prep_lds, (const S *)a.b, a.d_out, a.r, (S *)a.bt, block);
+}
+
+// The batch as an operand, to be taken through a permutation that is not known yet: laid out beside the sort, where 32-bit
+// offsets reach all of its rows then; false: it is laid out after it.
+static bool batch_operand(const void *x, int dtype, int64_t ld, int64_t n, int64_t cols, const int32_t *perm, __bf16 *room, RowOperand &out, PackJobs &jobs)
+{
+    PackJobs mine = {};
+    rairs_operand_job(x, dtype, ld, n, cols, dtype == RAIRS_F32, room, out, mine);
+    if (n * out.ld >= (1ll << 31)) return false;
+    if (mine.n) jobs.job[jobs.n++] = mine.job[0];
+    out.perm = perm;
+    return true;
 }
 
 static int prep_launch(PrepArgs &a, int dtype, hipStream_t s)
@@ -517,7 +537,13 @@ static int prep_launch(PrepArgs &a, int dtype, hipStream_t s)
         a.turn_blocks = (unsigned)((a.d_out + 31) / 32 * ((a.r + 31) / 32)) * a.sort.na;
         lds = std::max(lds, sizeof(float) * 32 * 33);
     }
-    const unsigned blocks = a.sorts + a.side_blocks + a.cols_blocks + a.turn_blocks;
+    unsigned blocks = a.sorts + a.side_blocks + a.cols_blocks + a.turn_blocks;
+    for (int i = 0; i < a.rows.n; i++) {
+        PackJob &j = a.rows.job[i];
+        j.blocks = (unsigned)std::min<int64_t>((j.rows * (j.pad / 8) + 1023) / 1024, 2048);
+        j.vec = is_vec(j.src, j.ld, dtype_width(dtype));
+        blocks += j.blocks;
+    }
     if (!blocks) return RAIRS_OK;
     if (dtype == RAIRS_F32) {
         RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<float, 3>, hipFuncAttributeMaxDynamicSharedMemorySize, SORT_ONE_LDS));   // (the same for every call)
@@ -832,10 +858,17 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     const bool use = adapters && g.adapter;
     RowProd rp = {};
     const SideJob job = {p.B, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, (int64_t)p.n_adapters * p.d_out, side, bp, zero, flags.found};
+    PackJobs jobs = {};
+    bool late = false;
+    if (!f32) {
+        rairs_operand_job(p.W, p.dtype, p.d_in, p.d_out, p.d_in, !bf, wroom, rp.P, jobs);
+        late = !batch_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, xroom, rp.Q, jobs);
+    }
     if (use) {
         PrepArgs pa = {};
         pa.sort = sv;
         pa.side = job;
+        pa.rows = jobs;
         if ((rc = prep_launch(pa, p.dtype, s))) return rc;
     }
     if (f32) {
@@ -846,8 +879,8 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         rp.Q.perm = use ? sv.perm : nullptr;
     } else {
         rowprod_sums(rp, np, np, pad_to(p.d_in, bf ? ROWPROD_K : 32));
-        if ((rc = rairs_operand(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, !bf, wroom, rp.P, s))) return rc;
-        if ((rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, !bf, xroom, rp.Q, s))) return rc;
+        if (!use && (rc = rairs_launch_pack(jobs, s))) return rc;
+        if (late && (rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, !bf, xroom, rp.Q, s))) return rc;
     }
     if (use) {
         ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side, flags};
@@ -1014,9 +1047,14 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     const PackLayout wto = pack_layout(p.d_in, opad, !bf);
     int rc = RAIRS_OK;
     const SideJob job = {p.A, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, (int64_t)na * p.d_in, side, ap, zero, flags.found};
+    RowProd rp = {};
+    PackJobs jobs = {};
+    bool late = false;
+    if (g.dx && g.n > 0) late = !batch_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, yroom, rp.Q, jobs);
     if (use) {
         PrepArgs pa = {};
         pa.sort = sv;
+        pa.rows = jobs;
         pa.b = p.B; pa.bt = bt;
         pa.w = p.W; pa.d_in = p.d_in; pa.d_out = p.d_out; pa.r = p.rank; pa.opad = opad; pa.wto = wto;
         if (g.dx) {
@@ -1037,11 +1075,11 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         if ((rc = rairs_launch_clear_rows(g.db, na, (int64_t)p.rank * p.d_out, (int64_t)p.rank * p.d_out, p.dtype, s))) return rc;
     }
     if (!g.dx || g.n == 0) return RAIRS_OK;
-    RowProd rp = {};
     rowprod_sums(rp, np, np, opad);
+    if (!use && (rc = rairs_launch_pack(jobs, s))) return rc;
     if (!use && (rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, ORDER_SAME, wt, opad, wto, s))) return rc;
     rp.P = RowOperand{wt, wto.ld, 0, p.d_in, nullptr, nullptr};
-    if ((rc = rairs_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, !bf, yroom, rp.Q, s))) return rc;
+    if (late && (rc = rairs_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, !bf, yroom, rp.Q, s))) return rc;
     if (use) {
         rp.ad = AdapterPart{vp, ap, zero, sv.of_row, sv.first + 1, side.kpad};
     }

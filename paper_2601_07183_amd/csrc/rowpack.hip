@@ -37,31 +37,10 @@ __global__ __launch_bounds__(WG) void pack_rows_kernel(const S *__restrict__ src
 }
 
 template <class S, int NP>
-static __device__ __forceinline__ void pack_rows_job(const PackJob &a, int64_t block)
-{
-    const int64_t per = a.pad / 8, total = a.rows * per;
-    for (int64_t t = block * WG + threadIdx.x; t < total; t += (int64_t)a.blocks * WG) {
-        const int64_t r = t / per, i0 = (t - r * per) * 8;
-        float x[8];
-        load8((const S *)a.src + r * a.ld, i0, a.cols, a.vec, x);
-        v8bf o[NP];
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            __bf16 pc[NP];
-            split_pieces<NP>(x[e], pc);
-#pragma unroll
-            for (int u = 0; u < NP; u++) o[u][e] = pc[u];
-        }
-#pragma unroll
-        for (int u = 0; u < NP; u++) *(v8bf *)(a.dst + r * a.to.ld + i0 / 32 * a.to.block + u * a.to.piece + i0 % 32) = o[u];
-    }
-}
-
-template <class S, int NP>
 static __device__ __forceinline__ void pack_job(const PackJob &a, int64_t block, char *lds)
 {
     if (!a.turned) {
-        pack_rows_job<S, NP>(a, block);
+        pack_rows_job<S, NP, WG>(a, block);
         return;
     }
     const int64_t rt = (a.pad + 63) / 64;

@@ -339,9 +339,15 @@ __global__ __launch_bounds__(T::NT, (RowStep<T, FLAGS>::WAVES)) void rowprod_ker
     }
     uint32_t po3[LP2], qo3[LQ2];                                      // of third pieces
     int64_t prow3[LP2], qrow3[LQ2];
-    if constexpr (THREES) {                                           // (never through a permutation)
+    if constexpr (THREES) {
         rowprod_thirds<T>((int64_t)t0 * T::BP, a.P.rows, a.P.ld, tid, po3, prow3);
         rowprod_thirds<T>(q0, a.Q.rows, a.Q.ld, tid, qo3, qrow3);
+        if (a.Q.perm)
+#pragma unroll
+            for (int i = 0; i < LQ2; i++) {
+                const uint32_t place = (tid & 7) ^ ((tid >> 3) & 3);  // (the pair's, as in rowprod_thirds)
+                qo3[i] = (uint32_t)a.Q.perm[qrow3[i] < a.Q.rows ? qrow3[i] : a.Q.rows - 1] * (uint32_t)(a.Q.ld * 2) + 128 + (place & 3) * 16;
+            }
     }
     uint32_t sp = a.sp, sq = a.sq;
     int nseg = a.nseg;
