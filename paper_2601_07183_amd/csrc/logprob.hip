@@ -370,9 +370,9 @@ struct FinishArgs {
 };
 
 // A query is finished by a team of threads: a wave of its own in a large batch, a workgroup of 16 waves if
-// there are few queries and one has to be done soon.  Lists in LDS are per team.  (One query, 1M rows, top 10: 27 us, a
-// chain of some ten steps that wait for one another; 4,096 queries, 128,000 x 1024 bf16, top 20: 184 us, of them 40 the
-// groups' 262 MB and about as much the rows scored again.)
+// there are few queries and one has to be done soon.  Lists in LDS are per team.  (One query, 1M rows, top 10: 21 us, a
+// chain of some ten steps that wait for one another; 4,096 queries, 128,000 x 1024 bf16, top 20: 160 us, of them 20 the
+// groups' 131 MB and about as much the rows scored again.)
 template <int NT>
 struct FinishShared {
     static constexpr int LIST = NT == 64 ? 384 : 1024;    // rows (wide: groups) that reach the bound
@@ -1298,24 +1298,29 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         if (np == 3) rc = ent ? grad_launch<3, true>(rp, ga, threes, s) : grad_launch<3, false>(rp, ga, threes, s);
         else rc = ent ? grad_launch<1, true>(rp, ga, threes, s) : grad_launch<1, false>(rp, ga, threes, s);
         if (rc) return rc;
+        RowProd pq = {}, pt = {};
+        StoreEpi eq = {}, et = {};
         if (need_dq) {
             const PackLayout tto = pack_layout(a.d, cpad, threes);
-            RowProd dp = {};
-            rowprod_sums(dp, tp, np, cpad);
-            dp.P = RowOperand{tcols, tto.ld, tto.piece, a.d, nullptr, nullptr};
-            dp.Q = RowOperand{g, ga.gto.ld, ga.gto.piece, a.n, nullptr, nullptr};
-            dp.splits = (int)splits;
-            StoreEpi e = {sums, dpad, a.n * dpad, a.d, a.n, nullptr, 0, v0 > 0};
-            if ((rc = threes ? rowprod_launch_any<ROW_THREES>(dp, e, s) : rowprod_launch_any(dp, e, s))) return rc;
+            rowprod_sums(pq, tp, np, cpad);
+            pq.P = RowOperand{tcols, tto.ld, tto.piece, a.d, nullptr, nullptr};
+            pq.Q = RowOperand{g, ga.gto.ld, ga.gto.piece, a.n, nullptr, nullptr};
+            pq.splits = (int)splits;
+            eq = StoreEpi{sums, dpad, a.n * dpad, a.d, a.n, nullptr, 0, v0 > 0};
         }
         if (need_dt) {
-            RowProd dp = {};
-            rowprod_sums(dp, np, np, npad);
-            dp.P = RowOperand{qcols, qto.ld, qto.piece, a.d, nullptr, nullptr};
-            dp.Q = RowOperand{gt, ga.gtto.ld, ga.gtto.piece, rows, nullptr, nullptr};
-            StoreEpi e = {(char *)a.dtable + v0 * a.lddt * dtype_width(a.ttype), a.lddt, 0, a.d, rows, nullptr, a.ttype == RAIRS_BF16, 0};
-            if ((rc = threes ? rowprod_launch_any<ROW_THREES>(dp, e, s) : rowprod_launch_any(dp, e, s))) return rc;
+            rowprod_sums(pt, np, np, npad);
+            pt.P = RowOperand{qcols, qto.ld, qto.piece, a.d, nullptr, nullptr};
+            pt.Q = RowOperand{gt, ga.gtto.ld, ga.gtto.piece, rows, nullptr, nullptr};
+            et = StoreEpi{(char *)a.dtable + v0 * a.lddt * dtype_width(a.ttype), a.lddt, 0, a.d, rows, nullptr, a.ttype == RAIRS_BF16, 0};
         }
+        // (both of small tiles: side by side; fp32 1,000 x 1,024 x 96 22.5 us, one after the other 26.6)
+        if (need_dq && need_dt && rowprod_size(a.d, a.n, (int)splits) == 0 && rowprod_size(a.d, rows) == 0) {
+            if ((rc = threes ? rowprod_launch_pair<TileU, ROW_THREES>(pq, eq, pt, et, s) : rowprod_launch_pair<TileS>(pq, eq, pt, et, s))) return rc;
+            continue;
+        }
+        if (need_dq && (rc = threes ? rowprod_launch_any<ROW_THREES>(pq, eq, s) : rowprod_launch_any(pq, eq, s))) return rc;
+        if (need_dt && (rc = threes ? rowprod_launch_any<ROW_THREES>(pt, et, s) : rowprod_launch_any(pt, et, s))) return rc;
     }
     if (need_dq) {
         hipLaunchKernelGGL(join_splits_kernel, dim3((unsigned)((a.n * dpad / 4 + WG - 1) / WG)), dim3(WG), 0, s, sums, (int)splits, a.n, a.d,

@@ -271,11 +271,11 @@ static __device__ __forceinline__ void rowprod_step_threes(const char *buf, int 
 // A workgroup's q tile and run of p tiles.  Workgroups are handed out round robin over the eight XCDs, each with
 // its own L2 cache: one XCD takes consecutive ids, and ids go over a band of q tiles, then to the next run, so that
 // what runs on an XCD at a time is about a square of tiles, whose rows its cache fetches once.
-static __device__ __forceinline__ bool rowprod_tile(const RowProd &a, int &run, int &qt, int &split)
+static __device__ __forceinline__ bool rowprod_tile(const RowProd &a, uint32_t block, int &run, int &qt, int &split)
 {
     const uint32_t all = (uint32_t)(a.pruns * a.qtiles), total = all * a.splits, per = (total + 7) / 8;
-    const uint32_t id = (blockIdx.x % 8) * per + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= per || id >= total) return false;
+    const uint32_t id = (block % 8) * per + block / 8;
+    if (block / 8 >= per || id >= total) return false;
     split = (int)(id / all);
     const uint32_t in = id % all, b = in / (uint32_t)(a.band * a.pruns), rest = in % (uint32_t)(a.band * a.pruns);
     const uint32_t h = min((uint32_t)a.band, a.qtiles - b * a.band);
@@ -308,14 +308,14 @@ static __device__ __forceinline__ void rowprod_rows(int64_t r0, int64_t rows, in
 // q0, lane): lane l holds, for its tiles (i, j), rows q0 + 16 j + (l & 15) and columns p0 + 16 i +
 // 4 (l >> 4) + 0..3.
 template <class T, class Epi, int FLAGS>
-__global__ __launch_bounds__(T::NT, (RowStep<T, FLAGS>::WAVES)) void rowprod_kernel(RowProd a, Epi epi)
+static __device__ __forceinline__ void rowprod_run_tiles(const RowProd &a, const Epi &epi, uint32_t block)
 {
     constexpr bool ADAPT = FLAGS & ROW_ADAPT, THREES = FLAGS & ROW_THREES;
     constexpr int BYTES = RowStep<T, FLAGS>::BYTES, LP2 = RowStep<T, FLAGS>::LP2, LQ2 = RowStep<T, FLAGS>::LQ2;
     constexpr int STEP = THREES ? 192 : ROWPROD_K * 2;                // bytes of a row per step
     extern __shared__ __align__(16) char rowprod_lds[];
     int run, qt, split;
-    if (!rowprod_tile(a, run, qt, split)) return;
+    if (!rowprod_tile(a, block, run, qt, split)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wp = wave % T::WP, wq = wave / T::WP;
     const int t0 = run * a.prun, t1 = min(t0 + a.prun, a.ptiles);
@@ -498,6 +498,26 @@ __global__ __launch_bounds__(T::NT, (RowStep<T, FLAGS>::WAVES)) void rowprod_ker
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // (LDS is given away when the workgroup ends)
 }
 
+template <class T, class Epi, int FLAGS>
+__global__ __launch_bounds__(T::NT, (RowStep<T, FLAGS>::WAVES)) void rowprod_kernel(RowProd a, Epi epi)
+{
+    rowprod_run_tiles<T, Epi, FLAGS>(a, epi, blockIdx.x);
+}
+
+// two products that do not wait for each other, of few workgroups each; `first`: the first one's
+template <class Epi>
+struct RowProdPair {
+    RowProd a[2];
+    Epi epi[2];
+    uint32_t first;
+};
+template <class T, class Epi, int FLAGS>
+__global__ __launch_bounds__(T::NT, (RowStep<T, FLAGS>::WAVES)) void rowprod_pair_kernel(RowProdPair<Epi> p)
+{
+    const int which = blockIdx.x >= p.first;
+    rowprod_run_tiles<T, Epi, FLAGS>(p.a[which], p.epi[which], which ? blockIdx.x - p.first : blockIdx.x);
+}
+
 // p tiles that a workgroup takes one after the other, at most `most`: what the last round of workgroups leaves
 // idle against the start of each (about `start` tiles' time), with room for `slots` workgroups at once
 static inline int rowprod_run(int64_t ptiles, int64_t qtiles, int slots, double start, int most)
@@ -512,27 +532,49 @@ static inline int rowprod_run(int64_t ptiles, int64_t qtiles, int slots, double 
     return best;
 }
 
-// `prun`: p tiles that a workgroup takes one after the other
-template <class T, int FLAGS = 0, class Epi>
-static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 1)
+// the launch's part of a product; `prun`: p tiles that a workgroup takes one after the other
+template <class T, int FLAGS>
+static void rowprod_plan(RowProd &a, int prun)
 {
     a.ptiles = (int)((a.P.rows + T::BP - 1) / T::BP);
     a.qtiles = (int)((a.Q.rows + T::BQ - 1) / T::BQ);
     a.prun = prun;
     a.pruns = (a.ptiles + prun - 1) / prun;
     if (a.splits < 1) a.splits = 1;
-    constexpr int lds = T::ST * RowStep<T, FLAGS>::BYTES;
     // the square: of the workgroups that an XCD has at a time, 32 or (small tiles: two a CU) 64
-    const int64_t total = (int64_t)a.pruns * a.qtiles, at_once = std::min<int64_t>((total * a.splits + 7) / 8, lds > 80 * 1024 ? 32 : 64);
+    const int64_t total = (int64_t)a.pruns * a.qtiles;
+    const int64_t at_once = std::min<int64_t>((total * a.splits + 7) / 8, T::ST * RowStep<T, FLAGS>::BYTES > 80 * 1024 ? 32 : 64);
     double least = 1e300;
     for (int bands = 1; bands <= a.qtiles; bands++) {
         const int h = (a.qtiles + bands - 1) / bands;
         const double rows = (double)h * T::BQ + (double)at_once / h * T::BP;
         if (rows < least) { least = rows; a.band = h; }
     }
+}
+
+template <class T, int FLAGS = 0, class Epi>
+static int rowprod_launch(RowProd &a, const Epi &epi, hipStream_t s, int prun = 1)
+{
+    rowprod_plan<T, FLAGS>(a, prun);
+    constexpr int lds = T::ST * RowStep<T, FLAGS>::BYTES;
     auto kern = rowprod_kernel<T, Epi, FLAGS>;
     RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     hipLaunchKernelGGL(kern, dim3(rowprod_grid(a)), dim3(T::NT), lds, s, a, epi);
+    RAIRS_HIP(hipGetLastError());
+    return RAIRS_OK;
+}
+
+template <class T, int FLAGS = 0, class Epi>
+static int rowprod_launch_pair(const RowProd &a, const Epi &ea, const RowProd &b, const Epi &eb, hipStream_t s)
+{
+    RowProdPair<Epi> p = {{a, b}, {ea, eb}, 0};
+    rowprod_plan<T, FLAGS>(p.a[0], 1);
+    rowprod_plan<T, FLAGS>(p.a[1], 1);
+    p.first = rowprod_grid(p.a[0]);
+    constexpr int lds = T::ST * RowStep<T, FLAGS>::BYTES;
+    auto kern = rowprod_pair_kernel<T, Epi, FLAGS>;
+    RAIRS_HIP(hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    hipLaunchKernelGGL(kern, dim3(p.first + rowprod_grid(p.a[1])), dim3(T::NT), lds, s, p);
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }

@@ -569,6 +569,35 @@ def test_backward_of_an_empty_batch_clears_the_table_gradient():
     assert r.top_ids.shape == (0, 3)
 
 
+def far_rows(t, ld):
+    """The same matrix on the GPU with rows `ld` elements apart (what lies between is never written)."""
+    v = torch.empty(len(t) * ld, dtype=t.dtype, device="cuda").view(len(t), ld)[:, :t.shape[1]]
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_rows_further_apart_than_32_bits_reach(t):
+    n, d_in, d_out, ld = 600, 64, 40, 4_000_000
+    x, w, a, b, s, ad = projection_data(n, d_in, d_out, 4, 3, t, 21)
+    p = binding.Projection(w.cuda(), a.cuda(), b.cuda(), s.cuda())
+    # (rows that lie otherwise may go another way, which rounds otherwise: both are within the bounds)
+    want, mag = exact_project(x, w, a, b, s, ad)
+    y = p.project(far_rows(x, ld), ad.cuda(), out=far_rows(torch.zeros(n, d_out), ld))
+    close(y, want, (sum_err(d_in) + sum_err(4)) * mag + half(F32) * want.abs(), "y")
+    dy = torch.randn(n, d_out, generator=gen(1)).to(t)
+    grads = p.backward(x.cuda(), ad.cuda(), dy.cuda())
+    # the sums of absolute products: the same gradients of absolute values
+    mags = binding.Projection(w.abs().cuda(), a.abs().cuda(), b.abs().cuda(), s.cuda()).backward(x.abs().cuda(), ad.cuda(), dy.abs().cuda())
+    err = 2 * (sum_err(n) + sum_err(d_in) + sum_err(d_out) + half(t))
+    for u, v, m in zip(grads, p.backward(far_rows(x, ld), ad.cuda(), far_rows(dy, ld)), mags):
+        close(v, u.double().cpu(), err * 1.01 * m.double().cpu(), "gradient")
+    for m, top in ((5, 3), (200, 3)):
+        q, table, targets, scale, _ = logprob_data(m, 1200, 64, t, 3)
+        check_logprob(binding.logprob(q.cuda(), far_rows(table, ld), targets.cuda(), scale=scale, top=top),
+                      exact_logprob(q, table, targets, scale, None, top), 1200, top)
+
+
 # ---- streams, graphs, and the run of them together ----------------------------------------------------
 
 
