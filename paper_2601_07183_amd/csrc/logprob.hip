@@ -782,8 +782,9 @@ struct GradArgs {
     const float2 *rows;             // fp32 (NP 3): row_stats_kernel's
 };
 
-// G = scale (dlogp (1[v = t] - p) - dentropy p (log p + H)) in registers, rounded to bf16 once (bf16
-// rows: at most 2^-8 of a value, as the result is when it is stored) or kept in three pieces (fp32), written for the
+// G = scale (dlogp (1[v = t] - p) - dentropy p (log p + H)) in registers, in NP bf16 pieces: two for bf16 rows (16 bits: at
+// most 2^-16 of a value, so that a gradient is off by its own rounding and little else; one piece would be half the work of
+// both products, 1.8 ms instead of 3.0 for 4,095 x 65,537 x 1024, and 2.3e-3 off instead of 1.7e-3) or three (fp32), written for the
 // products with the table (rows of queries) and with the queries (rows of the table).  Both sum over what
 // they have in common with the operand beside them, so their columns lie in the order that a wave holds
 // them in (ORDER_TABLE, ORDER_QUERIES): a lane's values are 32 or 8 bytes in a row, the lanes of a row 128.
@@ -873,40 +874,76 @@ struct GradEpi {
                     for (int r = 0; r < 4; r++) x[r] = (bits >> r) & 1u ? x[r] : 0.0f;
                 }
             }
-            // pieces, one after the other: rounded off what is left
-#pragma unroll
-            for (int u = 0; u < NP; u++) {
-                v4bf o[4][4];
+            if constexpr (NP == 2) {
+                // both pieces of a value in one register, where the value was (beside them they would not fit a wave's with the
+                // largest tile), and written by one copy of the code
 #pragma unroll
                 for (int i = 0; i < 4; i++)
 #pragma unroll
                     for (int j = 0; j < 4; j++)
 #pragma unroll
                         for (int r = 0; r < 4; r++) {
-                            o[i][j][r] = (__bf16)acc.v[4 * b + i][j][r];
-                            if (u + 1 < NP) acc.v[4 * b + i][j][r] -= (float)o[i][j][r];
+                            const float x = acc.v[4 * b + i][j][r], hi = (float)(__bf16)x;
+                            acc.v[4 * b + i][j][r] = __builtin_bit_cast(float, (v2bf){(__bf16)(x - hi), (__bf16)hi});
                         }
-                if (a.g)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const int q = q0 + 16 * j + c;
-                        __bf16 *to = a.g + (int64_t)q * a.gto.ld + (int64_t)((p0 + 64 * b) / 32 + h / 2) * a.gto.block + u * a.gto.piece + 16 * (h & 1);
-                        if (q < a.n) {
-                            *(v8bf *)to = __builtin_shufflevector(o[0][j], o[1][j], 0, 1, 2, 3, 4, 5, 6, 7);
-                            *(v8bf *)(to + 8) = __builtin_shufflevector(o[2][j], o[3][j], 0, 1, 2, 3, 4, 5, 6, 7);
-                        }
-                    }
-                if (a.gt)
+#pragma unroll 1
+                for (int u = 0; u < 2; u++) {
+                    const uint32_t half = u ? 0x05040100u : 0x07060302u;      // of two registers: the upper halves are first pieces
+                    const auto pair = [&](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), half); };
+                    write<T>(
+                        u, p0 + 64 * b, q0, lane,
+                        [&](int i, int j) {
+                            const v4f x = acc.v[4 * b + i][j];
+                            return (v2u){pair(x[0], x[1]), pair(x[2], x[3])};
+                        },
+                        [&](int i, int r) {
+                            return (v2u){pair(acc.v[4 * b + i][0][r], acc.v[4 * b + i][1][r]), pair(acc.v[4 * b + i][2][r], acc.v[4 * b + i][3][r])};
+                        });
+                }
+            } else {
+                // pieces, one after the other: rounded off what is left
+#pragma unroll 1
+                for (int u = 0; u < NP; u++) {
+                    v4bf o[4][4];
 #pragma unroll
                     for (int i = 0; i < 4; i++)
 #pragma unroll
-                        for (int r = 0; r < 4; r++) {
-                            __bf16 *to = a.gt + (int64_t)(p0 + 64 * b + 16 * i + 4 * h + r) * a.gtto.ld + (q0 / 32 + c / 8) * a.gtto.block + u * a.gtto.piece +
-                                         4 * (c & 7);
-                            *(v4bf *)to = (v4bf){o[i][0][r], o[i][1][r], o[i][2][r], o[i][3][r]};
-                        }
+                        for (int j = 0; j < 4; j++)
+#pragma unroll
+                            for (int r = 0; r < 4; r++) {
+                                o[i][j][r] = (__bf16)acc.v[4 * b + i][j][r];
+                                acc.v[4 * b + i][j][r] -= (float)o[i][j][r];
+                            }
+                    write<T>(
+                        u, p0 + 64 * b, q0, lane, [&](int i, int j) { return __builtin_bit_cast(v2u, o[i][j]); },
+                        [&](int i, int r) { return __builtin_bit_cast(v2u, (v4bf){o[i][0][r], o[i][1][r], o[i][2][r], o[i][3][r]}); });
+                }
             }
         }
+    }
+    // piece u of 64 x 64 values: by_row(i, j) a query's four, by_col(i, r) a row's
+    template <class T, class R, class C>
+    __device__ __forceinline__ void write(int u, int p, int q0, int lane, const R &by_row, const C &by_col) const
+    {
+        const int h = lane >> 4, c = lane & 15;
+        if (a.g)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int q = q0 + 16 * j + c;
+                __bf16 *to = a.g + (int64_t)q * a.gto.ld + (int64_t)(p / 32 + h / 2) * a.gto.block + u * a.gto.piece + 16 * (h & 1);
+                if (q < a.n) {
+                    *(v4u *)to = __builtin_shufflevector(by_row(0, j), by_row(1, j), 0, 1, 2, 3);
+                    *(v4u *)(to + 8) = __builtin_shufflevector(by_row(2, j), by_row(3, j), 0, 1, 2, 3);
+                }
+            }
+        if (a.gt)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    __bf16 *to = a.gt + (int64_t)(p + 16 * i + 4 * h + r) * a.gtto.ld + (q0 / 32 + c / 8) * a.gtto.block + u * a.gtto.piece + 4 * (c & 7);
+                    *(v2u *)to = by_col(i, r);
+                }
     }
 };
 
@@ -1164,10 +1201,10 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
                                   : finish_launch<uint8_t, float>(f, s);
 }
 
-// G is made for as many of the table's rows at a time as 1 GB of it hold.  (In pieces of 128 MB, which the last-level
+// G is made for as many of the table's rows at a time as 2 GB of it hold.  (In pieces of 128 MB, which the last-level
 // cache would keep, 4,095 x 65,537 x 1024 took 2.5 ms instead of 1.9: five launches of each product that fill the card
 // less well, and partial sums read again each time.)
-#define GRAD_CHUNK_BYTES (1ll << 30)
+#define GRAD_CHUNK_BYTES (2ll << 30)
 
 template <int NP, bool ENT>
 static int grad_launch(RowProd &rp, const GradArgs &ga, bool threes, hipStream_t s)
@@ -1187,10 +1224,11 @@ static int grad_launch(RowProd &rp, const GradArgs &ga, bool threes, hipStream_t
 int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
 {
     const int np = dtype_pieces(a.qtype), tp = dtype_pieces(a.ttype);
+    const int gp = np == 3 ? 3 : 2;                                   // pieces of the logits' gradient
     const bool threes = tp == 3, again = np == 3;
     const int64_t kpad = pad_to(a.d, threes ? 32 : ROWPROD_K), npad = pad_to(a.n, ROWPROD_K), dpad = pad_to(a.d, 4);
     const bool need_dt = a.dtable != nullptr, need_dq = a.dq != nullptr;
-    int64_t vc = GRAD_CHUNK_BYTES / (2 * np * npad) / 1024 * 1024;
+    int64_t vc = GRAD_CHUNK_BYTES / (2 * gp * npad) / 1024 * 1024;
     vc = vc < 1024 ? 1024 : std::min<int64_t>(vc, 1 << 20);           // (rows of threes: below 2^22 values)
     const int64_t chunks = (a.V + vc - 1) / vc;
     vc = pad_to((a.V + chunks - 1) / chunks, ROWPROD_K);              // of about one size
@@ -1206,8 +1244,8 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     __bf16 *troom = w.take<__bf16>(pack_room(a.ttype, vc, a.d));
     __bf16 *tcols = need_dq ? w.take<__bf16>((int64_t)a.d * vc * tp) : nullptr;
     __bf16 *qcols = need_dt ? w.take<__bf16>((int64_t)a.d * npad * np) : nullptr;
-    __bf16 *g = need_dq ? w.take<__bf16>(a.n * vc * np) : nullptr;
-    __bf16 *gt = need_dt ? w.take<__bf16>(vc * npad * np) : nullptr;
+    __bf16 *g = need_dq ? w.take<__bf16>(a.n * vc * gp) : nullptr;
+    __bf16 *gt = need_dt ? w.take<__bf16>(vc * npad * gp) : nullptr;
     float *sums = need_dq ? w.take<float>(splits * a.n * dpad) : nullptr;
     uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
     // fp32: the statistics once more, by tiles as in the forward pass
@@ -1296,20 +1334,20 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         ga.gto = pack_layout(a.n, cpad, threes); ga.gtto = pack_layout(cpad, npad, threes);
         const bool ent = a.dentropy != nullptr;
         if (np == 3) rc = ent ? grad_launch<3, true>(rp, ga, threes, s) : grad_launch<3, false>(rp, ga, threes, s);
-        else rc = ent ? grad_launch<1, true>(rp, ga, threes, s) : grad_launch<1, false>(rp, ga, threes, s);
+        else rc = ent ? grad_launch<2, true>(rp, ga, threes, s) : grad_launch<2, false>(rp, ga, threes, s);
         if (rc) return rc;
         RowProd pq = {}, pt = {};
         StoreEpi eq = {}, et = {};
         if (need_dq) {
             const PackLayout tto = pack_layout(a.d, cpad, threes);
-            rowprod_sums(pq, tp, np, cpad);
+            rowprod_sums(pq, tp, gp, cpad);
             pq.P = RowOperand{tcols, tto.ld, tto.piece, a.d, nullptr, nullptr};
             pq.Q = RowOperand{g, ga.gto.ld, ga.gto.piece, a.n, nullptr, nullptr};
             pq.splits = (int)splits;
             eq = StoreEpi{sums, dpad, a.n * dpad, a.d, a.n, nullptr, 0, v0 > 0};
         }
         if (need_dt) {
-            rowprod_sums(pt, np, np, npad);
+            rowprod_sums(pt, np, gp, npad);
             pt.P = RowOperand{qcols, qto.ld, qto.piece, a.d, nullptr, nullptr};
             pt.Q = RowOperand{gt, ga.gtto.ld, ga.gtto.piece, rows, nullptr, nullptr};
             et = StoreEpi{(char *)a.dtable + v0 * a.lddt * dtype_width(a.ttype), a.lddt, 0, a.d, rows, nullptr, a.ttype == RAIRS_BF16, 0};

@@ -696,3 +696,46 @@ def test_projected_search_and_logprob_of_an_index(small_index_int, small_index):
         same = binding.logprob(q, raw.to(kind).cuda(), targets.cuda(), scale=scale, top=7)
         assert all(torch.equal(u, v) for u, v in zip(r, same))
         ix.free()
+
+
+@pytest.mark.parametrize("entropy", [False, True])
+@pytest.mark.parametrize("n,v", [(20, 24), (130, 700), (520, 26_000)])
+def test_logprob_backward_of_bf16_rows_keeps_sixteen_bits_of_the_logits_gradient(n, v, entropy):
+    # Small whole numbers: every product is exact.  16 queries pass a gradient and 24 rows are live, the first and the
+    # last of both among them, so that the sums have few terms (zeros add exactly).
+    d, scale, g = 24, 0.25, gen(n + v)
+    q = torch.randint(-2, 3, (n, d), generator=g).to(BF16)
+    table = torch.randint(-2, 3, (v, d), generator=g).to(BF16)
+    live = torch.cat([torch.tensor([0, v - 1]), 1 + torch.randperm(v - 2, generator=g)[:22]])
+    mask = torch.zeros(v, dtype=torch.bool)
+    mask[live] = True
+    on = torch.cat([torch.tensor([0, n - 1]), 1 + torch.randperm(n - 2, generator=g)[:14]])
+    targets = torch.full((n,), -1)
+    targets[on] = live[torch.randint(0, 24, (16,), generator=g)]
+    da, db = torch.randn(n, generator=g), torch.zeros(n)
+    if entropy:
+        db[on] = torch.randn(16, generator=g)
+    else:
+        db = None
+    words = pack(mask)
+    r = binding.logprob(q.cuda(), table.cuda(), targets.cuda(), scale=scale, live=words)
+    dq, dt = binding.logprob_backward(q.cuda(), table.cuda(), targets.cuda(), r.lse, da.cuda(), scale=scale, live=words,
+                                      entropy=r.entropy if entropy else None, dentropy=db.cuda() if entropy else None, table_grad=True)
+    w = exact_logprob(q, table, targets, scale, mask, 1)
+    wq, wt, _, T = exact_backward(q, table, targets, scale, mask, da, db, w)
+    p, Q = w["p"], q.double()
+    logp = torch.where(p > 0, p.log(), 0.0)
+    a = torch.where(targets >= 0, da.double(), 0.0)[:, None]
+    hit = torch.nn.functional.one_hot(targets.clamp(min=0), v) * (targets >= 0)[:, None]
+    mag = scale * a.abs() * (hit * (1 - p) + (1 - hit) * p)
+    soft = scale * a.abs() * p
+    if entropy:
+        b = scale * db.double().abs()[:, None] * p
+        mag = mag + b * (logp.abs() + w["h"][:, None])
+        soft = soft + b * (logp.abs() + w["h"][:, None] + 1)
+    # p by its logarithm: lse is rounded (at most 24 + log 24), log p in two steps, its multiple of log2(e) and the power of
+    # two in one each: under 16 of fp32's half steps of |lse| + |log p| + 4, entropy as much; then two pieces of G
+    e = 16 * U * (w["lse"].abs() + torch.where(p > 0, logp.abs(), 0.0).max(1).values + 4)
+    eg = soft * 1.01 * e[:, None] + mag * half(BF16) ** 2
+    close(dq, wq, eg @ T.abs() + sum_err(24) * (mag @ T.abs()) + half(BF16) * wq.abs() * 1.01, "dq")
+    close(dt, wt, eg.t() @ Q.abs() + sum_err(16) * (mag.t() @ Q.abs()) + half(BF16) * wt.abs() * 1.01, "dtable")
