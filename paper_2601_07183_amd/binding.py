@@ -299,9 +299,9 @@ def _logprob(t, q, targets, top, entropy, stream) -> LogProb:
     with _On(dev, stream) as st:
         need = lib.rairs_logprob_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(DTYPES[qt]), C.c_int(top))
         ws, pw, nw = _workspace(need, dev)
-        r = LogProb(torch.empty(n, device=dev), torch.empty(n, device=dev), torch.empty(n, device=dev) if entropy else None,
-                    torch.empty((n, top), dtype=torch.int64, device=dev) if top > 0 else None,
-                    torch.empty((n, top), device=dev) if top > 0 else None)
+        values = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)     # (whatever torch's default type is)
+        r = LogProb(values(n), values(n), values(n) if entropy else None,
+                    torch.empty((n, top), dtype=torch.int64, device=dev) if top > 0 else None, values(n, top) if top > 0 else None)
         p = [C.c_void_p(x.data_ptr() if x is not None and n else 0) for x in r]
         _check(lib.rairs_logprob(C.byref(t), pq, ldq, C.c_int(DTYPES[qt]), C.c_int64(n), pt, p[0], p[1], p[2], C.c_int(top), p[3],
                                  p[4], pw, nw, st))

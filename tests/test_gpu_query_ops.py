@@ -739,3 +739,27 @@ def test_logprob_backward_of_bf16_rows_keeps_sixteen_bits_of_the_logits_gradient
     eg = soft * 1.01 * e[:, None] + mag * half(BF16) ** 2
     close(dq, wq, eg @ T.abs() + sum_err(24) * (mag @ T.abs()) + half(BF16) * wq.abs() * 1.01, "dq")
     close(dt, wt, eg.t() @ Q.abs() + sum_err(16) * (mag.t() @ Q.abs()) + half(BF16) * wt.abs() * 1.01, "dtable")
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float64])
+def test_calls_under_another_default_type(default):
+    # what is returned does not depend on torch's default type
+    x, w, a, b, s, ad = projection_data(70, 24, 16, 3, 2, F32, 3)
+    table, targets = torch.randn(90, 16, generator=gen(1)).cuda(), torch.randint(0, 90, (70,), generator=gen(2)).cuda()
+    p = binding.Projection(w.cuda(), a.cuda(), b.cuda(), s.cuda())
+    x, ad, da = x.cuda(), ad.cuda(), torch.ones(70, device="cuda")
+
+    def chain():
+        y = p.project(x, ad)
+        r = binding.logprob(y, table, targets, scale=0.3, top=5)
+        dy, dt = binding.logprob_backward(y, table, targets, r.lse, da, scale=0.3, table_grad=True)
+        return (y, *r, dy, dt, *p.backward(x, ad, dy))
+
+    want = chain()
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        got = chain()
+    finally:
+        torch.set_default_dtype(before)
+    assert all(u.dtype == v.dtype and torch.equal(u, v) for u, v in zip(want, got))

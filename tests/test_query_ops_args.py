@@ -161,3 +161,38 @@ def test_the_binding_checks_its_tensors():
         binding.logprob(torch.zeros(2, 8), torch.zeros(5, 8), torch.zeros(2, dtype=torch.int64))
     with pytest.raises(TypeError):
         binding.logprob(torch.zeros(2, 8), torch.zeros(5, 8, dtype=torch.float16), torch.zeros(2, dtype=torch.int64))
+
+
+class NoDevice:
+    """Stands in for a call's device and stream where only the allocation of its results is looked at."""
+
+    def __init__(self, *_):
+        pass
+
+    def __enter__(self):
+        return C.c_void_p(0)
+
+    def __exit__(self, *_):
+        return False
+
+
+class NoLibrary:
+    def __getattr__(self, name):
+        return lambda *_: 0
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float16, torch.float64, torch.float32])
+def test_results_of_logprob_are_fp32_whatever_the_default_type_is(default, monkeypatch):
+    # the kernels write four bytes a value
+    monkeypatch.setattr(binding, "load", NoLibrary)
+    monkeypatch.setattr(binding, "_On", NoDevice)
+    monkeypatch.setattr(binding, "_rows", lambda *_: (C.c_void_p(0), C.c_int64(8)))
+    monkeypatch.setattr(binding, "_vec", lambda *_: C.c_void_p(0))
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        r = binding.logprob(torch.zeros(3, 8, dtype=torch.float32), torch.zeros(5, 8, dtype=torch.float32), torch.zeros(3, dtype=torch.int64), top=2)
+    finally:
+        torch.set_default_dtype(before)
+    assert [x.dtype for x in r] == [torch.float32] * 3 + [torch.int64, torch.float32]
+    assert [tuple(x.shape) for x in r] == [(3,), (3,), (3,), (3, 2), (3, 2)]
