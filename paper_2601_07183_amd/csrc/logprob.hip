@@ -1,9 +1,11 @@
 // Log probabilities of a table's rows under a softmax over inner products, and their gradients.
 //
 // One pass over the logits l = scale <q, t_v>, which are never written: a wave that has a tile's products
-// in registers folds them into a running maximum m, s = sum 2^(z - m) and e = sum 2^(z - m) (z - m) with
-// z = l log2(e), and leaves one {m, s, e} per query and run of table rows ("part").  From them
-//     lse = ln 2 (m + log2 s),     entropy = ln 2 (log2 s - e / s).
+// in registers folds them into a running maximum m, s = sum 2^t and e = sum 2^t t with t = (<q, t_v> - m) scale log2(e),
+// and leaves one {m, s, e} per query and run of table rows ("part").  From them
+//     lse = scale m + ln 2 log2 s,     entropy = ln 2 (log2 s - e / s).
+// m is the largest product itself: rounded to a multiple of log2(e) first, which would save an operation a value, it would
+// not be given back by lse, and logits past 2^31 would overflow against it.
 // For the most probable rows it also leaves the largest products of every 16 (or 64) rows ("group"): a row
 // among the K best lies in a group whose maximum is at least the K-th best maximum less what the sums can
 // be off by.  Groups of 16 also say which row the maximum is, in the value's last four bits, and what the
@@ -66,7 +68,7 @@ static __device__ __forceinline__ void rebase(float &s, float &e, float m0, floa
 {
     if (m0 == m1) return;
     if (m0 == HIDDEN) { s = 0.0f; e = 0.0f; return; }
-    const float d = m0 * c - m1 * c, f = exp2_fast(d);
+    const float d = (m0 - m1) * c, f = exp2_fast(d);
     e = f * fmaf(s, fmaxf(d, -1e4f), e);
     s *= f;
 }
@@ -158,18 +160,24 @@ struct StatsState {
                 }
                 top = max_of(top, g);
             }
-            if (__any(!(top <= m[j]))) {                              // (ever more seldom)
+            // (the row in a maximum's last bits makes it up to 2^-19 of itself smaller or larger)
+            if (__any(!((TOP == 2 ? fmaf(fabsf(top), 0x1p-19f, top) : top) <= m[j]))) {      // (ever more seldom)
+                if constexpr (TOP == 2) {
+                    top = HIDDEN;
+#pragma unroll
+                    for (int i = 0; i < PT; i++) top = max_of(max_of(max_of(top, acc[i][j][0]), acc[i][j][1]), max_of(acc[i][j][2], acc[i][j][3]));
+                }
                 const float m1 = max_of(m[j], top);
                 rebase(s[j], e[j], m[j], m1, a.c);
                 m[j] = m1;
             }
-            const float mc = m[j] == HIDDEN ? 0.0f : m[j] * a.c;
+            const float from = m[j] == HIDDEN ? 0.0f : m[j];
             float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
             for (int i = 0; i < PT; i++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const float t = fmaf(acc[i][j][r], a.c, -mc), x = exp2_fast(t);
+                    const float t = (acc[i][j][r] - from) * a.c, x = exp2_fast(t);
                     if (r & 1) s1 += x;
                     else s0 += x;
                     if constexpr (ENT) e[j] = fmaf(x, fmaxf(t, -1e4f), e[j]);
@@ -379,6 +387,7 @@ struct FinishShared {
     static constexpr int ITEMS = NT == 64 ? 256 : 1024;   // rows to score at a time
     double val[ITEMS + RAIRS_MAX_TOP];
     double best[RAIRS_MAX_TOP];
+    double lse;
     uint32_t id[ITEMS + RAIRS_MAX_TOP];
     uint32_t best_id[RAIRS_MAX_TOP];
     uint32_t take[ITEMS];
@@ -639,15 +648,17 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
     rebase(s, e, m, top, c);
     team_fold5<NT>(sh, s, e, q2, x2, zero);
     const bool empty = top == HIDDEN && s == 0.0f;
-    const float mc = top * c, logs = log2f(s);
+    const float logs = log2f(s);
     if (tid == 0) {
-        a.lse[row] = empty ? NEG_INF : (mc + logs) * LN2;
+        const double ln_sum = (double)logs * 0.6931471805599453;
+        sh.lse = (double)top * (double)a.scale + ln_sum;
+        a.lse[row] = empty ? NEG_INF : (float)sh.lse;
         if (a.entropy) a.entropy[row] = empty ? 0.0f : fmaxf((logs - e / s) * LN2, 0.0f);
         const int64_t t = a.st.targets[row];
         float lp = 0.0f;
         if (t >= 0 && t < a.st.V) {
             const bool seen = !a.st.live || ((a.st.live[row * a.st.ld_live + (t >> 5)] >> (t & 31)) & 1u);
-            lp = seen ? (fmaf(a.st.zt[row], c, -mc) - logs) * LN2 : NEG_INF;
+            lp = seen ? (float)(((double)a.st.zt[row] - (double)top) * (double)a.scale - ln_sum) : NEG_INF;
         }
         a.logp[row] = lp;
         sh.nbest = 0;
@@ -763,7 +774,7 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
         const bool have = tid < sh.nbest;
         a.top_ids[row * a.top + tid] = have ? (int64_t)sh.best_id[tid] : -1;
         a.top_logp[row * a.top + tid] =
-            have ? (float)(sh.best[tid] * (double)a.scale - ((double)mc + (double)logs) * 0.6931471805599453) : NEG_INF;
+            have ? (float)(sh.best[tid] * (double)a.scale - sh.lse) : NEG_INF;
     }
 }
 
@@ -837,7 +848,7 @@ struct GradEpi {
             for (int j = 0; j < 4; j++) {
                 const int q = q0 + 16 * j + c;
                 const bool in = q < a.n;
-                const float da = st.da[j], db = st.db[j], lse = st.lse[j];
+                const float da = st.da[j], db = st.db[j];
                 const bool dead = da == 0.0f && db == 0.0f;
                 const uint32_t dp = (uint32_t)(st.target[j] - p0 - 64 * b);
 #pragma unroll
@@ -846,8 +857,7 @@ struct GradEpi {
                     const v4f z = x;
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        // (log p in natural units: scale times the product is exact inside the sum, which log2(e) is not)
-                        const float lp = fmaf(NP == 3 ? z[r] - st.m[NP == 3 ? j : 0] : z[r], a.scale, -lse), pr = exp2_fast(lp * LOG2E);
+                        const float lp = log_p(st, z[r], j), pr = exp2_fast(lp * LOG2E);
                         float g = -da * pr;
                         if constexpr (ENT) g -= db * pr * (fmaxf(lp, -1e4f) + st.H[j]);
                         x[r] = g;
@@ -858,7 +868,7 @@ struct GradEpi {
 #pragma unroll
                         for (int r = 0; r < 4; r++)
                             if (at == (uint32_t)r) {
-                                const float lp = fmaf(NP == 3 ? z[r] - st.m[NP == 3 ? j : 0] : z[r], a.scale, -lse), pr = exp2_fast(lp * LOG2E);
+                                const float lp = log_p(st, z[r], j), pr = exp2_fast(lp * LOG2E);
                                 float g = da * (1.0f - pr);
                                 if constexpr (ENT) g -= db * pr * (fmaxf(lp, -1e4f) + st.H[j]);
                                 x[r] = g;
@@ -920,6 +930,14 @@ struct GradEpi {
                 }
             }
         }
+    }
+    // log p of a product, in natural units.  fp32: scale times a difference is exact inside the sum, which log2(e) is not.
+    // bf16: the logit is rounded as lse is, so that a row that has all of the probability has 1 - p = 0 however large both are
+    template <class S>
+    __device__ __forceinline__ float log_p(const S &st, float z, int j) const
+    {
+        if constexpr (NP == 3) return fmaf(z - st.m[j], a.scale, -st.lse[j]);
+        else return z * a.scale - st.lse[j];
     }
     // piece u of 64 x 64 values: by_row(i, j) a query's four, by_col(i, r) a row's
     template <class T, class R, class C>

@@ -763,3 +763,79 @@ def test_calls_under_another_default_type(default):
     finally:
         torch.set_default_dtype(before)
     assert all(u.dtype == v.dtype and torch.equal(u, v) for u, v in zip(want, got))
+
+
+@pytest.mark.parametrize("scale", [0.3, 0.7, 123.4, 1e5 / 3])
+@pytest.mark.parametrize("tt", [F32, BF16, U8])
+@pytest.mark.parametrize("n,v,d", [(1, 1, 1), (3, 200, 64), (100, 90, 1), (70, 700, 64)])
+def test_the_only_live_row_has_all_of_the_probability(n, v, d, tt, scale):
+    # One live row, whole numbers: the logit is scale times an exact product, lse is that rounded, the row's log p is 0 and the
+    # gradients are zero, whatever scale times log2(e) rounds to.  Of two equal rows each has log p = -ln 2.
+    # Bounds: the sum of powers of two is relative to a rounded maximum, so it is 2^t of one |t| <= 1 (the logits are below
+    # 2^24), within a step of fp32 (2 U, or 2.9 U of its logarithm to base 2), and the logarithm is off by a step of at most 2^-24
+    # (U): 3.9 U ln 2, under 4 U absolute.  Entropy also takes t times the sum over the sum, three roundings of at most U each:
+    # 6.9 U ln 2, under 8 U.  Two rows: two powers, a sum, a logarithm of the size of 1: under 8 U, entropy 12 U.
+    # A gradient of bf16 rows takes lse as it is: zero where 4 U do not change what lse is rounded to.
+    scale = float(np.float32(scale))
+    g = gen(v + d)
+    q = torch.randint(0, 4, (n, d), generator=g).to(F32 if tt == U8 else tt)
+    table = torch.randint(0, 4, (v, d), generator=g).to(tt)
+    q[:, 0], table[:, 0] = 3, 5
+    at = v // 2
+    targets = torch.full((n,), at)
+    mask = torch.zeros(v, dtype=torch.bool)
+    mask[at] = True
+    words = pack(mask)
+    r = binding.logprob(q.cuda(), table.cuda(), targets.cuda(), scale=scale, top=2, live=words)
+    logit = (q.double() @ table.double().t())[:, at] * scale
+    close(r.lse, logit, half(F32) * logit + 4 * U, "lse")
+    for x in (r.logp, r.top_logp[:, 0]):
+        close(x, torch.zeros(n, dtype=torch.float64), 4 * U, "log p")
+    close(r.entropy, torch.zeros(n, dtype=torch.float64), 8 * U, "entropy")
+    assert torch.equal(r.top_ids.cpu(), torch.tensor([at, -1]).expand(n, 2))
+    da = torch.randn(n, generator=g).cuda()
+    dq, dt = binding.logprob_backward(q.cuda(), table.cuda(), targets.cuda(), r.lse, da, scale=scale, live=words, table_grad=tt != U8)
+    G = scale * da.double().cpu().abs() * 4 * U
+    if tt == BF16:
+        clear = (logit - 4 * U).float() == (logit + 4 * U).float()
+        G = torch.where(clear, 0.0, scale * da.double().cpu().abs() * (4 * U + 2 * half(F32) * logit))
+    close(dq, torch.zeros(n, d, dtype=torch.float64), 1.01 * G[:, None] * table[at].double(), "dq")
+    if dt is not None:
+        close(dt[at], torch.zeros(d, dtype=torch.float64), 1.01 * G @ q.double(), "dtable")
+        assert not dt[mask.logical_not().cuda()].any()
+    if v > 2:
+        table[at + 1] = table[at]
+        mask[at + 1] = True
+        r = binding.logprob(q.cuda(), table.cuda(), targets.cuda(), scale=scale, top=2, live=pack(mask))
+        close(r.lse, logit + math.log(2), half(F32) * (logit + 1) + 8 * U, "lse")
+        for x in (r.logp, r.top_logp[:, 0], r.top_logp[:, 1]):
+            close(x, torch.full((n,), -math.log(2), dtype=torch.float64), 8 * U, "log p")
+        close(r.entropy, torch.full((n,), math.log(2), dtype=torch.float64), 12 * U, "entropy")
+        assert torch.equal(r.top_ids.cpu(), torch.tensor([at, at + 1]).expand(n, 2))
+
+
+@pytest.mark.parametrize("tt", [F32, BF16, U8])
+@pytest.mark.parametrize("n", [2, 100])
+@pytest.mark.parametrize("top", [0, 3])
+@pytest.mark.parametrize("size", [1e8, 1e10, 1e20])
+def test_logprob_of_logits_past_every_power_of_two(n, size, top, tt):
+    # whole numbers, every product of a query another one: the best row has all of the probability and lse is its logit,
+    # also where a step of fp32 in a logit is thousands
+    d, v = 24, 130
+    g = gen(n + v)
+    q = torch.randint(0, 4, (n, d), generator=g).to(F32 if tt == U8 else tt)
+    table = torch.randint(0, 4, (v, d), generator=g).to(tt)
+    q[:, 0] = 4
+    table[:, 0] = torch.arange(v).remainder(100).to(tt)
+    ip = q.double() @ table.double().t()
+    ip2, order = ip.sort(dim=1, descending=True, stable=True)
+    one = ip2[:, 0] > ip2[:, 1]
+    scale = float(np.float32(size / 400.0))
+    r = binding.logprob(q.cuda(), table.cuda(), order[:, 0].cuda(), scale=scale, top=top)
+    ties = (ip == ip2[:, :1]).sum(1).double()
+    close(r.lse, ip2[:, 0] * scale, half(F32) * ip2[:, 0] * scale + 10.0, "lse")
+    assert one.any()
+    # (as many equal rows: the logarithm of their number)
+    close(r.logp, -ties.log(), 8 * U, "log p of the best row")
+    if top:
+        assert torch.equal(r.top_ids[:, 0].cpu(), order[:, 0])
