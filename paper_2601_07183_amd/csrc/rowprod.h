@@ -221,7 +221,8 @@ static __device__ __forceinline__ void rowprod_step(const char *buf, int wp, int
                     if constexpr (FLAGS & ROW_F32) {
                         acc.nrm[i] = fmaf(__uint_as_float(a[i][e]), __uint_as_float(a[i][e]), acc.nrm[i]);
                     } else {
-                        const v2bf x = __builtin_bit_cast(v2bf, a[i][e]);
+                        const uint32_t word = a[i][e];                // (a cast of a vector's element as it stands takes the vector's first)
+                        const v2bf x = __builtin_bit_cast(v2bf, word);
                         acc.nrm[i] = __builtin_amdgcn_fdot2_f32_bf16(x, x, acc.nrm[i], false);
                     }
                 }

@@ -839,3 +839,24 @@ def test_logprob_of_logits_past_every_power_of_two(n, size, top, tt):
     close(r.logp, -ties.log(), 8 * U, "log p of the best row")
     if top:
         assert torch.equal(r.top_ids[:, 0].cpu(), order[:, 0])
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n", [1, 20, 40, 100])
+@pytest.mark.parametrize("at", range(8))
+def test_top_rows_whose_products_lose_bits_in_fp32(n, t, at):
+    # Rows of 2^20, a small s, -2^20 in values that are added one after the other: fp32 loses s = 13/256, which is more than the 8/256
+    # and 7/256 that other rows have exactly.  The margin has to know of the large values, wherever they stand in a row.
+    d, v = 128, 3000
+    q = torch.zeros(n, d)
+    q[:, [at, 32 + at, 64 + at]] = 1.0
+    table = torch.zeros(v, d)
+    table[:, 32 + at] = -1.0
+    table[[100, 2000], 32 + at] = torch.tensor([8 / 256, 7 / 256])
+    table[[700, 2999], at], table[[700, 2999], 64 + at] = 2.0 ** 20, -(2.0 ** 20)
+    table[[700, 2999], 32 + at] = torch.tensor([13 / 256, 12 / 256])
+    q, table = q.to(t), table.to(t)
+    r = binding.logprob(q.cuda(), table.cuda(), torch.zeros(n, dtype=torch.int64).cuda(), top=4)
+    assert torch.equal(r.top_ids.cpu(), torch.tensor([700, 2999, 100, 2000]).expand(n, 4))
+    r = binding.logprob(q.cuda(), table.cuda(), torch.zeros(n, dtype=torch.int64).cuda(), top=1)
+    assert torch.equal(r.top_ids.cpu(), torch.tensor([700]).expand(n, 1))
