@@ -435,7 +435,8 @@ int rairs_index_table(const rairs_index_t *h, rairs_table_t *out);
  *              first, of equal ones the smaller id; missing entries are id -1, -inf.  A query whose
  *              products are not all finite, or whose or whose table's squared norms are not in fp32, may get
  *              missing entries instead.
- * Products of fp32 rows are as exact as fp32 sums are.  n == 0 is a successful no-op.
+ * Products of fp32 rows are as exact as fp32 sums are.  A live row's product and its logit have to be in fp32, the
+ * product above -3.4e38 (a lower one counts as hidden by the mask).  n == 0 is a successful no-op.
  */
 size_t rairs_logprob_workspace_bytes(const rairs_table_t *t, int64_t n, int q_dtype, int top);
 int rairs_logprob(const rairs_table_t *t, const void *d_q, int64_t ld_q, int q_dtype, int64_t n, const int64_t *d_targets,

@@ -19,9 +19,9 @@
 #define LOG2E 1.4426950408889634f
 #define LN2 0.6931471805599453f
 #define NEG_INF (-__builtin_huge_valf())
-// the product of a row that the mask hides: finite, and none of its last bits set, so that bits written
-// into it make it smaller
-#define HIDDEN (-0x1.2cecp+126f)
+// The product of a row that the mask hides: the lowest value whose last four bits are zero, so that a row written into them
+// makes it smaller.  Live products are above -3.4e38 (the caller's), 2.8e34 away: times a scale of 1e-30 still a logit that is out of reach.
+#define HIDDEN (-0x1.ffffep+127f)
 
 // ---- statistics of a tile ----------------------------------------------------------------------------
 
@@ -647,7 +647,7 @@ __global__ __launch_bounds__(NT * TEAMS, NT == 64 ? 3 : 4) void logprob_finish_k
     const float top = team_fold(sh, m, [](float x, float y) { return max_of(x, y); });
     rebase(s, e, m, top, c);
     team_fold5<NT>(sh, s, e, q2, x2, zero);
-    const bool empty = top == HIDDEN && s == 0.0f;
+    const bool empty = top == HIDDEN;
     const float logs = log2f(s);
     if (tid == 0) {
         const double ln_sum = (double)logs * 0.6931471805599453;

@@ -860,3 +860,38 @@ def test_top_rows_whose_products_lose_bits_in_fp32(n, t, at):
     assert torch.equal(r.top_ids.cpu(), torch.tensor([700, 2999, 100, 2000]).expand(n, 4))
     r = binding.logprob(q.cuda(), table.cuda(), torch.zeros(n, dtype=torch.int64).cuda(), top=1)
     assert torch.equal(r.top_ids.cpu(), torch.tensor([700]).expand(n, 1))
+
+
+@pytest.mark.parametrize("scale", [1.0, 1e-30])
+@pytest.mark.parametrize("tt", [F32, BF16])
+@pytest.mark.parametrize("n,v,d,live", [(1, 1, 1, [0]), (3, 200, 64, [7]), (100, 90, 1, [89]), (70, 700, 64, [3, 699]), (300, 60_000, 24, [40_001])])
+def test_products_near_the_lowest_value_of_fp32_are_live_rows(n, v, d, live, tt, scale):
+    # live rows' products are about -1.5e38 and -3.3e38 (hidden ones' as much above zero): the rows count, and alone have log p = 0
+    scale = float(np.float32(scale))
+    q, table = torch.zeros(n, d).to(tt), torch.zeros(v, d).to(tt)
+    q[:, 0] = torch.where(torch.arange(n) % 2 == 0, -1.5e19, -1.8e19).to(tt)
+    table[:, 0] = -1e19
+    mask = torch.zeros(v, dtype=torch.bool)
+    for i in live:
+        table[i, 0] = 1e19 if i % 2 else 1.8e19
+        mask[i] = True
+    targets = torch.full((n,), live[-1])
+    r = binding.logprob(q.cuda(), table.cuda(), targets.cuda(), scale=scale, top=3, live=pack(mask))
+    ip = (q.double() @ table.double().t())[:, live]
+    order = ip.sort(dim=1, descending=True, stable=True).indices
+    best = ip.max(1).values
+    close(r.lse, best * scale, 4 * U * best.abs() * scale, "lse")
+    ids = torch.full((n, 3), -1)
+    ids[:, : len(live)] = torch.tensor(live)[order]
+    assert torch.equal(r.top_ids.cpu(), ids)
+    assert not r.entropy.any() if len(live) == 1 else r.entropy.isfinite().all()
+    if len(live) == 1:
+        # (the best rows' products are taken in float64, lse comes from one that is rounded as fp32 sums are)
+        assert not r.logp.any()
+        close(r.top_logp[:, 0], torch.zeros(n, dtype=torch.float64), sum_err(d) * best.abs() * scale, "top_logp")
+        da = torch.ones(n, device="cuda")
+        dq, dt = binding.logprob_backward(q.cuda(), table.cuda(), targets.cuda(), r.lse, da, scale=scale, live=pack(mask), table_grad=True)
+        assert not dq.any() and not dt.any()
+    # nothing live stays nothing
+    r = binding.logprob(q.cuda(), table.cuda(), targets.cuda(), scale=scale, top=3, live=pack(torch.zeros(v, dtype=torch.bool)))
+    assert (r.lse == -math.inf).all() and (r.logp == -math.inf).all() and not r.entropy.any() and (r.top_ids == -1).all()
