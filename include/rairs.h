@@ -357,6 +357,7 @@ enum { RAIRS_F32 = 0, RAIRS_BF16 = 1, RAIRS_U8 = 2 };
 #define RAIRS_MAX_GRAD_ROWS (1 << 20)   /* of one for rairs_logprob_backward */
 #define RAIRS_MAX_WIDTH 16384       /* d_in, d_out; d of a table's rows */
 #define RAIRS_MAX_TOP 64            /* most probable rows that rairs_logprob returns */
+#define RAIRS_MAX_TABLE_ROWS 0x7FFFFF00ll   /* 2^31 - 256: the last tile's end is an int */
 
 /*
  * y = W x + scale[a] B[a] (A[a] x): the shared projection and n_adapters low-rank adapters, all of one
@@ -409,7 +410,7 @@ int rairs_search_projected(rairs_index_t *h, const rairs_projection_t *p, const 
  * A table of vectors and how it is scored: l_v = scale <q, t_v>, scale within [1e-30, 1e30].
  * d_live: device words, bit v & 31 of word v >> 5 set where a query may see row v; ld_live words from one
  * query's mask to the next, 0 for a mask that all queries share; NULL: all rows are live.  Rows of the
- * table that no query sees may hold anything.  V < 2^31 - 64.
+ * table that no query sees may hold anything.  V <= RAIRS_MAX_TABLE_ROWS.
  */
 typedef struct {
     const void *vectors;     /* device [V] rows of d */

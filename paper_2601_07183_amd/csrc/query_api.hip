@@ -157,7 +157,7 @@ static int check_table(const rairs_table_t *t, int64_t n, int q_dtype)
     if (t->d < 1) FAIL(RAIRS_EINVAL, "d=%d: need d >= 1", t->d);
     if (t->d > RAIRS_MAX_WIDTH) FAIL(RAIRS_EUNSUPPORTED, "d=%d above the built limit %d", t->d, RAIRS_MAX_WIDTH);
     if (t->V < 1) FAIL(RAIRS_EINVAL, "a table needs at least one row");
-    if (t->V >= (1ll << 31) - 64) FAIL(RAIRS_EUNSUPPORTED, "V=%lld: need V < 2^31 - 64", (long long)t->V);
+    if (t->V > RAIRS_MAX_TABLE_ROWS) FAIL(RAIRS_EUNSUPPORTED, "V=%lld above the built limit %lld", (long long)t->V, (long long)RAIRS_MAX_TABLE_ROWS);
     if (!(t->scale >= 1e-30f && t->scale <= 1e30f)) FAIL(RAIRS_EINVAL, "scale must be within [1e-30, 1e30]");
     if (t->ld_live < 0 || (t->ld_live > 0 && t->ld_live < (t->V + 31) / 32))
         FAIL(RAIRS_EINVAL, "ld_live=%lld: need 0 or at least %lld words", (long long)t->ld_live, (long long)((t->V + 31) / 32));

@@ -196,3 +196,12 @@ def test_results_of_logprob_are_fp32_whatever_the_default_type_is(default, monke
         torch.set_default_dtype(before)
     assert [x.dtype for x in r] == [torch.float32] * 3 + [torch.int64, torch.float32]
     assert [tuple(x.shape) for x in r] == [(3,), (3,), (3,), (3, 2), (3, 2)]
+
+
+def test_a_table_whose_last_tile_does_not_end_within_an_int_is_refused():
+    # tiles have up to 256 rows, and a tile's end is compared with V
+    lib = binding.load()
+    for v, code in ((2 ** 31 - 256, EWORKSPACE), (2 ** 31 - 255, EUNSUPPORTED), (2 ** 31 - 65, EUNSUPPORTED)):
+        for call in (logprob, logprob_backward):
+            assert call(table(V=v), ws=None) == code, v
+        assert (lib.rairs_logprob_workspace_bytes(C.byref(table(V=v)), C.c_int64(4), C.c_int(0), C.c_int(0)) > 0) == (code == EWORKSPACE)
