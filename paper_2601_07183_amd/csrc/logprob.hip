@@ -1001,28 +1001,32 @@ __global__ __launch_bounds__(WG) void row_stats_kernel(StatsArgs a, float scale,
 __global__ __launch_bounds__(WG) void join_splits_kernel(const float *__restrict__ part, int splits, int64_t n, int cols, int dpad,
                                                          void *__restrict__ out, int64_t ld, int bf16_out)
 {
-    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x, total = n * dpad;
-    if (t * 4 >= total) return;
-    v4f x = *(const v4f *)(part + t * 4);
-    for (int s = 1; s < splits; s++) x += *(const v4f *)(part + s * total + t * 4);
-    const int64_t r = t * 4 / dpad, o = r * ld;
-    const int c = (int)(t * 4 - r * dpad);
+    const int64_t total = n * dpad;
+    for (int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x; t * 4 < total; t += (int64_t)gridDim.x * WG) {
+        v4f x = *(const v4f *)(part + t * 4);
+        for (int s = 1; s < splits; s++) x += *(const v4f *)(part + s * total + t * 4);
+        const int64_t r = t * 4 / dpad, o = r * ld;
+        const int c = (int)(t * 4 - r * dpad);
 #pragma unroll
-    for (int e = 0; e < 4; e++)
-        if (c + e < cols) {
-            if (bf16_out) ((__bf16 *)out)[o + c + e] = (__bf16)x[e];
-            else ((float *)out)[o + c + e] = x[e];
-        }
+        for (int e = 0; e < 4; e++)
+            if (c + e < cols) {
+                if (bf16_out) ((__bf16 *)out)[o + c + e] = (__bf16)x[e];
+                else ((float *)out)[o + c + e] = x[e];
+            }
+    }
 }
 
 __global__ __launch_bounds__(WG) void clear_rows_kernel(void *out, int64_t n, int64_t cols, int64_t ld, int width)
 {
-    const int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x;
-    if (t >= n * cols) return;
-    const int64_t r = t / cols, o = r * ld + (t - r * cols);
-    if (width == 4) ((float *)out)[o] = 0.0f;
-    else ((uint16_t *)out)[o] = 0;
+    for (int64_t t = (int64_t)blockIdx.x * WG + threadIdx.x; t < n * cols; t += (int64_t)gridDim.x * WG) {
+        const int64_t r = t / cols, o = r * ld + (t - r * cols);
+        if (width == 4) ((float *)out)[o] = 0.0f;
+        else ((uint16_t *)out)[o] = 0;
+    }
 }
+
+// workgroups for `threads` threads whose kernel goes on from there (a grid of 2^32 threads is none)
+static unsigned capped(int64_t threads) { return (unsigned)std::min<int64_t>((threads + WG - 1) / WG, 1 << 20); }
 
 // ---- launches ----------------------------------------------------------------------------------------
 
@@ -1379,7 +1383,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         if (need_dt && (rc = threes ? rowprod_launch_any<ROW_THREES>(pt, et, s) : rowprod_launch_any(pt, et, s))) return rc;
     }
     if (need_dq) {
-        hipLaunchKernelGGL(join_splits_kernel, dim3((unsigned)((a.n * dpad / 4 + WG - 1) / WG)), dim3(WG), 0, s, sums, (int)splits, a.n, a.d,
+        hipLaunchKernelGGL(join_splits_kernel, dim3(capped(a.n * dpad / 4)), dim3(WG), 0, s, sums, (int)splits, a.n, a.d,
                            (int)dpad, a.dq, a.lddq, (int)(a.qtype == RAIRS_BF16));
         RAIRS_HIP(hipGetLastError());
     }
@@ -1389,7 +1393,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
 int rairs_launch_clear_rows(void *out, int64_t n, int64_t cols, int64_t ld, int dtype, hipStream_t s)
 {
     if (n == 0 || cols == 0) return RAIRS_OK;
-    hipLaunchKernelGGL(clear_rows_kernel, dim3((unsigned)((n * cols + WG - 1) / WG)), dim3(WG), 0, s, out, n, cols, ld, dtype_width(dtype));
+    hipLaunchKernelGGL(clear_rows_kernel, dim3(capped(n * cols)), dim3(WG), 0, s, out, n, cols, ld, dtype_width(dtype));
     RAIRS_HIP(hipGetLastError());
     return RAIRS_OK;
 }

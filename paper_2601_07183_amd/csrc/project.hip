@@ -458,10 +458,12 @@ static __device__ __forceinline__ void transpose_tile(S (&tile)[32][33], const S
 
 // The sort, which is one workgroup's, and beside it what does not wait for it: the adapters' B (or A) as pieces, W
 // turned, B turned.  One launch after the other they took 20 us more (2,999 rows, 1024 x 960, 32 adapters).
+#define PREP_MOST (1 << 20)
 struct PrepArgs {
     SortView sort;
     int sorts;                      // workgroups: 0 or 1
     unsigned side_blocks, cols_blocks, turn_blocks;
+    int64_t side_from, turn_from;   // where this launch goes on: of either at most PREP_MOST at a time, as a grid has less than 2^32 threads
     PackJobs rows;                  // W (forward) and the batch, in the batch's order
     SideJob side;
     const void *w, *b;              // [d_out][d_in], [na][d_out][r]
@@ -483,7 +485,7 @@ __global__ __launch_bounds__(1024) void prep_kernel(PrepArgs a)
     }
     block -= a.sorts;
     if (block < a.side_blocks) {
-        pack_side<S>(a.side, block);
+        pack_side<S>(a.side, block + a.side_from);
         return;
     }
     block -= a.side_blocks;
@@ -503,7 +505,7 @@ __global__ __launch_bounds__(1024) void prep_kernel(PrepArgs a)
         }
         block -= a.rows.job[i].blocks;
     }
-    transpose_tile<S>(*(S(*)[32][33])prep_lds, (const S *)a.b, a.d_out, a.r, (S *)a.bt, block);
+    transpose_tile<S>(*(S(*)[32][33])prep_lds, (const S *)a.b, a.d_out, a.r, (S *)a.bt, block + a.turn_from);
 }
 
 // The batch as an operand, to be taken through a permutation that is not known yet: laid out beside the sort, where 32-bit
@@ -527,33 +529,40 @@ static int prep_launch(PrepArgs &a, int dtype, hipStream_t s)
         if (a.sorts) lds = sort_one_lds(a.sort);
         else if ((rc = sort_launch(a.sort, s))) return rc;
     }
-    if (a.side.dst) a.side_blocks = (unsigned)side_blocks(a.side.side, a.side.total);
+    int64_t side_work = 0, turn_work = 0;
+    if (a.side.dst) side_work = side_blocks(a.side.side, a.side.total);
     if (a.wt) {
         a.cols_blocks = (unsigned)((a.opad / 64 * ((a.d_in + 63) / 64) + 1) / 2);
         lds = std::max(lds, dtype == RAIRS_F32 ? 2 * sizeof(PackCols<float, 3>) : 2 * sizeof(PackCols<__bf16, 1>));
         a.vec = is_vec(a.w, a.d_in, dtype_width(dtype));
     }
     if (a.bt) {
-        a.turn_blocks = (unsigned)((a.d_out + 31) / 32 * ((a.r + 31) / 32)) * a.sort.na;
+        turn_work = (int64_t)((a.d_out + 31) / 32 * ((a.r + 31) / 32)) * a.sort.na;
         lds = std::max(lds, sizeof(float) * 32 * 33);
     }
-    unsigned blocks = a.sorts + a.side_blocks + a.cols_blocks + a.turn_blocks;
     for (int i = 0; i < a.rows.n; i++) {
         PackJob &j = a.rows.job[i];
         j.blocks = (unsigned)std::min<int64_t>((j.rows * (j.pad / 8) + 1023) / 1024, 2048);
         j.vec = is_vec(j.src, j.ld, dtype_width(dtype));
-        blocks += j.blocks;
     }
-    if (!blocks) return RAIRS_OK;
-    if (dtype == RAIRS_F32) {
-        RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<float, 3>, hipFuncAttributeMaxDynamicSharedMemorySize, SORT_ONE_LDS));   // (the same for every call)
-        hipLaunchKernelGGL((prep_kernel<float, 3>), dim3(blocks), dim3(1024), lds, s, a);
-    } else {
-        RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<__bf16, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, SORT_ONE_LDS));   // (the same for every call)
-        hipLaunchKernelGGL((prep_kernel<__bf16, 1>), dim3(blocks), dim3(1024), lds, s, a);
+    if (dtype == RAIRS_F32) RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<float, 3>, hipFuncAttributeMaxDynamicSharedMemorySize, SORT_ONE_LDS));   // (the same for every call)
+    else RAIRS_HIP(hipFuncSetAttribute((const void *)prep_kernel<__bf16, 1>, hipFuncAttributeMaxDynamicSharedMemorySize, SORT_ONE_LDS));
+    for (;;) {
+        a.side_blocks = (unsigned)std::min<int64_t>(side_work - a.side_from, PREP_MOST);
+        a.turn_blocks = (unsigned)std::min<int64_t>(turn_work - a.turn_from, PREP_MOST);
+        unsigned blocks = a.sorts + a.side_blocks + a.cols_blocks + a.turn_blocks;
+        for (int i = 0; i < a.rows.n; i++) blocks += a.rows.job[i].blocks;
+        if (!blocks) return RAIRS_OK;
+        if (dtype == RAIRS_F32) hipLaunchKernelGGL((prep_kernel<float, 3>), dim3(blocks), dim3(1024), lds, s, a);
+        else hipLaunchKernelGGL((prep_kernel<__bf16, 1>), dim3(blocks), dim3(1024), lds, s, a);
+        RAIRS_HIP(hipGetLastError());
+        // (what is left of the most adapters' values)
+        a.sorts = 0;
+        a.cols_blocks = 0;
+        a.rows.n = 0;
+        a.side_from += a.side_blocks;
+        a.turn_from += a.turn_blocks;
     }
-    RAIRS_HIP(hipGetLastError());
-    return RAIRS_OK;
 }
 
 // ---- a few rows ----------------------------------------------------------------------------------------

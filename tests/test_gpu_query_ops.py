@@ -8,6 +8,7 @@ parts.  A result rounded to type t adds half a step, finfo(t).eps / 2 of the val
 intermediate rounded to it.  2^x of a rounded argument: an error e of the logarithm is a relative
 error of about e of the probability.
 """
+import ctypes as C
 import math
 
 import numpy as np
@@ -895,3 +896,41 @@ def test_products_near_the_lowest_value_of_fp32_are_live_rows(n, v, d, live, tt,
     # nothing live stays nothing
     r = binding.logprob(q.cuda(), table.cuda(), targets.cuda(), scale=scale, top=3, live=pack(torch.zeros(v, dtype=torch.bool)))
     assert (r.lse == -math.inf).all() and (r.logp == -math.inf).all() and not r.entropy.any() and (r.top_ids == -1).all()
+
+
+def test_an_empty_batch_clears_a_table_gradient_of_more_values_than_a_grid_has_threads():
+    v, d, ld = 2 ** 22 + 1, 1024, 1032
+    out = torch.ones(v, ld, dtype=BF16, device="cuda")
+    t = binding._Table(vectors=out.data_ptr(), ld=ld, V=v, d=d, dtype=1, scale=1.0, d_live=None, ld_live=0)
+    none = C.c_void_p(0)
+    binding._check(binding.load().rairs_logprob_backward(
+        C.byref(t), none, C.c_int64(d), C.c_int(1), C.c_int64(0), none, none, none, none, none, none, C.c_int64(d),
+        C.c_void_p(out.data_ptr()), C.c_int64(ld), none, C.c_size_t(0), none))
+    torch.cuda.synchronize()
+    assert float(out[:, :d].abs().max()) == 0.0 and float(out[:, d:].min()) == 1.0
+
+
+def test_project_backward_of_the_most_adapters_of_the_largest_rank():
+    # B alone has 2^33 values: more tiles to turn than a grid has threads for
+    d_in, d_out, rank, na, n = 8, 16384, 128, 4096, 3
+    g = gen(4)
+    a, b = torch.zeros(na, rank, d_in, dtype=BF16, device="cuda"), torch.zeros(na, d_out, rank, dtype=BF16, device="cuda")
+    ad = torch.tensor([na - 1, 0, na - 1], dtype=torch.int32)
+    for k in (0, na - 1):
+        a[k], b[k] = torch.randn(rank, d_in, generator=g).to(BF16), torch.randn(d_out, rank, generator=g).to(BF16)
+    w = torch.randn(d_out, d_in, generator=g).to(BF16)
+    x, dy = torch.randn(n, d_in, generator=g).to(BF16), torch.randn(n, d_out, generator=g).to(BF16)
+    dx, da, db = binding.Projection(w.cuda(), a, b).backward(x.cuda(), ad.cuda(), dy.cuda())
+    X, D, W = x.double(), dy.double(), w.double()
+    wx, mx = D @ W, D.abs() @ W.abs()
+    for k, rows in ((0, [1]), (na - 1, [0, 2])):
+        A, B = a[k].double().cpu(), b[k].double().cpu()
+        v, mv = D[rows] @ B, D[rows].abs() @ B.abs()
+        u, mu = X[rows] @ A.t(), X[rows].abs() @ A.t().abs()
+        wx[rows] += v @ A
+        mx[rows] += mv @ A.abs()
+        wa, wb = v.t() @ X[rows], D[rows].t() @ u
+        close(da[k], wa, (sum_err(d_out) + sum_err(2)) * (mv.t() @ X[rows].abs()) * 1.01 + half(BF16) * wa.abs(), "dA")
+        close(db[k], wb, (sum_err(d_in) + sum_err(2)) * (D[rows].abs().t() @ mu) * 1.01 + half(BF16) * wb.abs(), "dB")
+    close(dx, wx, (sum_err(d_out) + sum_err(rank)) * mx * 1.01 + half(BF16) * wx.abs(), "dx")
+    assert float(da[1:na - 1].abs().max()) == 0.0 and float(db[1:na - 1].abs().max()) == 0.0
