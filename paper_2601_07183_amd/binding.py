@@ -393,6 +393,7 @@ class Index:
         _check(self._lib.rairs_index_upload(C.byref(s), _stream_ptr(stream), C.byref(self._h)))
         del keep
         self.d, self.M, self.nlist, self.ntotal = hx.d, hx.M, hx.nlist, hx.ntotal
+        self.device = torch.device("cuda", torch.cuda.current_device())
         self._ws = None                 # torch tensor that serves as the handle's workspace
 
     # --- workspace: device memory comes from PyTorch ------------------------------------------
@@ -479,7 +480,7 @@ class Index:
                          stream=None):
         """rairs_search_projected: rows [n][d_in] through the projection and into the search; returns ids,
         distances and the queries that were searched with [n][d]."""
-        n, dev = x.shape[0], projection.W.device
+        n, dev = x.shape[0], self._on_device(projection.W, "the projection")
         px, ldx = _rows(x, "x", projection.W.dtype, projection.d_in, dev)
         pa = _vec(adapter, "adapter", torch.int32, n, dev)
         with _On(dev, stream) as st:
@@ -498,10 +499,19 @@ class Index:
     def logprob(self, q: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, top: int = 0, live=None,
                 entropy: bool = True, stream=None) -> LogProb:
         """logprob over the index's own vectors (rairs_index_table): float32 queries, targets are vector ids."""
+        dev = self._on_device(q, "q")
+        return _logprob(self._table(scale, live, q.shape[0], dev), q, targets, top, entropy, stream)
+
+    def _on_device(self, t: torch.Tensor, name: str):
+        if t.device != self.device:
+            raise TypeError(f"{name}: expected on the index's device {self.device}, got {t.device}")
+        return self.device
+
+    def _table(self, scale: float, live, n: int, dev):
         t = _Table()
         _check(self._lib.rairs_index_table(self._h, C.byref(t)))
         t.scale = scale
-        return _logprob(_with_mask(t, live, q.shape[0], q.device), q, targets, top, entropy, stream)
+        return _with_mask(t, live, n, dev)
 
     # --- stages ---------------------------------------------------------------------------
     def coarse(self, queries: torch.Tensor, nprobe: int, stream=None):

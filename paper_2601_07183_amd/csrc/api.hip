@@ -1121,6 +1121,17 @@ static int search_few(rairs_index *h, char *ws, int ws_source, const float *d_qu
     return RAIRS_OK;
 }
 
+int rairs_search_ready(rairs_index *h, int64_t nq, int k, int nprobe, int refine_k)
+{
+    int rc = check_common(h, nq);
+    if (rc) return rc;
+    if ((rc = check_nprobe(h, nprobe))) return rc;
+    if ((rc = check_k(k, refine_k))) return rc;
+    if (nq == 0) return RAIRS_OK;
+    char *ws = nullptr;
+    return acquire_ws(h, WS_HANDLE, rairs_workspace_bytes(h, nq, nprobe, refine_k), &ws);
+}
+
 static int search_impl(rairs_index *h, int ws_source, const float *d_queries, int64_t nq, int k, int nprobe,
                        int refine_k, int64_t *d_out_ids, float *d_out_dists, void *hip_stream)
 {

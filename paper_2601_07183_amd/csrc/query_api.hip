@@ -130,8 +130,7 @@ extern "C" int rairs_search_projected(rairs_index_t *h, const rairs_projection_t
     TRY(check_projection(p, n));
     if (p->d_out != h->v.d) FAIL(RAIRS_EINVAL, "the projection's d_out=%d is not the index's d=%d", p->d_out, h->v.d);
     // (what the search would refuse is refused before anything is enqueued)
-    if (n > 0 && rairs_workspace_bytes(h, n, nprobe, refine_k) == 0) return RAIRS_EINVAL;
-    if (k < 1 || k > refine_k) FAIL(RAIRS_EINVAL, "k=%d: need 1 <= k <= refine_k", k);
+    TRY(rairs_search_ready(h, n, k, nprobe, refine_k));
     if (n > 0 && (!d_out_ids || !d_out_dists)) FAIL(RAIRS_EINVAL, "null device pointer");
     TRY(rairs_project(p, d_x, ld_x, n, d_adapter, d_queries, p->d_out, RAIRS_F32, d_ws, ws_bytes, hip_stream));
     return rairs_search(h, d_queries, n, k, nprobe, refine_k, d_out_ids, d_out_dists, hip_stream);

@@ -130,6 +130,8 @@ struct rairs_index {
 };
 
 void rairs_set_error(const char *fmt, ...);
+// what rairs_search would refuse for these arguments (RAIRS_OK: nothing), its workspace found or grown
+int rairs_search_ready(rairs_index *h, int64_t nq, int k, int nprobe, int refine_k);
 
 #define RAIRS_HIP(call)                                                              \
     do {                                                                             \

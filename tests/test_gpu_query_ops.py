@@ -934,3 +934,40 @@ def test_project_backward_of_the_most_adapters_of_the_largest_rank():
         close(db[k], wb, (sum_err(d_in) + sum_err(2)) * (D[rows].abs().t() @ mu) * 1.01 + half(BF16) * wb.abs(), "dB")
     close(dx, wx, (sum_err(d_out) + sum_err(rank)) * mx * 1.01 + half(BF16) * wx.abs(), "dx")
     assert float(da[1:na - 1].abs().max()) == 0.0 and float(db[1:na - 1].abs().max()) == 0.0
+
+
+def test_projected_search_refuses_before_anything_is_enqueued(small_index):
+    # a caller's workspace that the search finds too small: the queries are not written either
+    base, hx = small_index
+    ix = binding.Index(hx)
+    x, w, a, b, s, ad = projection_data(90, 24, hx.d, 4, 3, F32, 8)
+    p = binding.Projection(w.cuda(), a.cuda(), b.cuda(), s.cuda())
+    x, ad = x.cuda(), ad.cuda()
+    q = torch.full((90, hx.d), 123.0, device="cuda")
+    ids, dists = torch.full((90, 5), 7, device="cuda"), torch.full((90, 5), 7.0, device="cuda")
+    lib = binding.load()
+    pw = torch.empty(1 << 24, dtype=U8, device="cuda")
+
+    def call(k=5, nprobe=4, refine_k=40):
+        ptr = [C.c_void_p(t.data_ptr()) for t in (x, ad, q, ids, dists, pw)]
+        rc = lib.rairs_search_projected(ix._h, C.byref(p._s), ptr[0], C.c_int64(24), C.c_int64(90), ptr[1], ptr[2], C.c_int(k), C.c_int(nprobe),
+                                        C.c_int(refine_k), ptr[3], ptr[4], ptr[5], C.c_size_t(pw.numel()), binding._stream_ptr(None))
+        torch.cuda.synchronize()
+        return rc
+
+    ix.set_workspace(torch.empty(256, dtype=U8, device="cuda"))
+    assert call() == -5 and "workspace" in lib.rairs_last_error().decode()
+    for kw, code in ((dict(k=0), -1), (dict(k=41), -1), (dict(nprobe=0), -1), (dict(refine_k=5000), -4)):
+        assert call(**kw) == code, kw
+    assert (q == 123.0).all() and (ids == 7).all() and (dists == 7.0).all()
+    ix.set_workspace(torch.empty(ix.workspace_bytes(90, 4, 40), dtype=U8, device="cuda"))
+    assert call() == 0
+    want = ix.search_projected(p, x, ad, 5, 4, 40)
+    assert torch.equal(q, want[2]) and torch.equal(ids, want[0]) and torch.equal(dists, want[1])
+    # tensors of another device than the index's
+    ix.device = torch.device("cuda", 1)
+    with pytest.raises(TypeError, match="index's device"):
+        ix.search_projected(p, x, ad, 5, 4, 40)
+    with pytest.raises(TypeError, match="index's device"):
+        ix.logprob(q, torch.zeros(90, dtype=torch.int64, device="cuda"))
+    ix.free()
