@@ -293,7 +293,7 @@ def _with_mask(t, live, n: int, dev):
 
 def _logprob(t, q, targets, top, entropy, stream) -> LogProb:
     lib, dev, n = load(), q.device, q.shape[0]
-    qt = torch.float32 if t.dtype == DTYPES[torch.uint8] else {v: k for k, v in DTYPES.items()}[t.dtype]
+    qt = _query_type(t)
     pq, ldq = _rows(q, "q", qt, t.d, dev)
     pt = _vec(targets, "targets", torch.int64, n, dev)
     with _On(dev, stream) as st:
@@ -316,28 +316,36 @@ def logprob(q: torch.Tensor, table: torch.Tensor, targets: torch.Tensor, scale: 
     return _logprob(_table(table, scale, live, q.shape[0]), q, targets, top, entropy, stream)
 
 
-def logprob_backward(q: torch.Tensor, table: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor,
-                     scale: float = 1.0, live: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
-                     dentropy: Optional[torch.Tensor] = None, q_grad: bool = True, table_grad: bool = False, stream=None):
-    """rairs_logprob_backward: (dq, dtable) for the gradients dlogp, dentropy [n] of logprob's results; None for
-    what is not wanted.  lse and entropy are logprob's."""
-    lib, dev, n = load(), q.device, q.shape[0]
-    t = _table(table, scale, live, n)
-    qt = torch.float32 if table.dtype == torch.uint8 else table.dtype
+def _query_type(t):
+    return torch.float32 if t.dtype == DTYPES[torch.uint8] else {v: k for k, v in DTYPES.items()}[t.dtype]
+
+
+def _logprob_backward(t, q, targets, lse, dlogp, entropy, dentropy, q_grad, table_dtype, stream):
+    """table_dtype: the type of the table's gradient, None: not wanted."""
+    lib, dev, n, qt = load(), q.device, q.shape[0], _query_type(t)
     pq, ldq = _rows(q, "q", qt, t.d, dev)
     f = [_vec(x, name, torch.float32, n, dev) for x, name in
          ((lse, "lse"), (entropy, "entropy"), (dlogp, "dlogp"), (dentropy, "dentropy"))]
     pt = _vec(targets, "targets", torch.int64, n, dev)
     with _On(dev, stream) as st:
-        need = lib.rairs_logprob_backward_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(DTYPES[qt]), C.c_int(int(table_grad)))
+        need = lib.rairs_logprob_backward_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(DTYPES[qt]), C.c_int(int(table_dtype is not None)))
         ws, pw, nw = _workspace(need, dev)
         dq = torch.empty((n, t.d), dtype=qt, device=dev) if q_grad else None
-        dt = torch.empty((t.V, t.d), dtype=table.dtype, device=dev) if table_grad else None
+        dt = torch.empty((t.V, t.d), dtype=table_dtype, device=dev) if table_dtype is not None else None
         _check(lib.rairs_logprob_backward(
             C.byref(t), pq, ldq, C.c_int(DTYPES[qt]), C.c_int64(n), pt, f[0], f[1], f[2], f[3],
             C.c_void_p(dq.data_ptr() if q_grad and n else 0), C.c_int64(t.d),
-            C.c_void_p(dt.data_ptr() if table_grad else 0), C.c_int64(t.d), pw, nw, st))
+            C.c_void_p(dt.data_ptr() if dt is not None else 0), C.c_int64(t.d), pw, nw, st))
     return dq, dt
+
+
+def logprob_backward(q: torch.Tensor, table: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor,
+                     scale: float = 1.0, live: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                     dentropy: Optional[torch.Tensor] = None, q_grad: bool = True, table_grad: bool = False, stream=None):
+    """rairs_logprob_backward: (dq, dtable) for the gradients dlogp, dentropy [n] of logprob's results; None for
+    what is not wanted.  lse and entropy are logprob's."""
+    return _logprob_backward(_table(table, scale, live, q.shape[0]), q, targets, lse, dlogp, entropy, dentropy, q_grad,
+                             table.dtype if table_grad else None, stream)
 
 
 def host_struct(hx):
@@ -501,6 +509,13 @@ class Index:
         """logprob over the index's own vectors (rairs_index_table): float32 queries, targets are vector ids."""
         dev = self._on_device(q, "q")
         return _logprob(self._table(scale, live, q.shape[0], dev), q, targets, top, entropy, stream)
+
+    def logprob_backward(self, q: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor, scale: float = 1.0,
+                         live=None, entropy=None, dentropy=None, stream=None) -> torch.Tensor:
+        """dq [n][d] float32 for the gradients dlogp, dentropy [n] of logprob's results (the index's vectors stay);
+        lse and entropy are logprob's."""
+        dev = self._on_device(q, "q")
+        return _logprob_backward(self._table(scale, live, q.shape[0], dev), q, targets, lse, dlogp, entropy, dentropy, True, None, stream)[0]
 
     def _on_device(self, t: torch.Tensor, name: str):
         if t.device != self.device:

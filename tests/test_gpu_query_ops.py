@@ -971,3 +971,45 @@ def test_projected_search_refuses_before_anything_is_enqueued(small_index):
     with pytest.raises(TypeError, match="index's device"):
         ix.logprob(q, torch.zeros(90, dtype=torch.int64, device="cuda"))
     ix.free()
+
+
+def test_adapters_learn_over_the_vectors_of_an_index(small_index_int, small_index):
+    # projection, log probabilities of the index's own vectors, and the gradients back to the adapters, against 64-bit autograd
+    for (base, hx), kind in ((small_index, F32), (small_index_int, U8)):
+        ix = binding.Index(hx)
+        n, d_in, rank, na = 96, 40, 4, 3
+        x, w, a, b, s, ad = projection_data(n, d_in, hx.d, rank, na, F32, 14)
+        g = gen(3)
+        raw = torch.from_numpy(np.ascontiguousarray(hx.raw)).float()
+        scale = float(np.float32(0.2 / float(raw.norm(dim=1).mean())))
+        targets = torch.randint(0, hx.ntotal, (n,), generator=g)
+        mask = torch.rand(hx.ntotal, generator=g) < 0.8
+        mask[targets] = True
+        words, tg = pack(mask), targets.cuda()
+        p = binding.Projection(w.cuda(), a.cuda(), b.cuda(), s.cuda())
+        y = p.project(x.cuda(), ad.cuda())
+        r = ix.logprob(y, tg, scale=scale, live=words)
+        dlogp, dent = torch.full((n,), -1.0 / n, device="cuda"), torch.full((n,), 0.1 / n, device="cuda")
+        dy = ix.logprob_backward(y, tg, r.lse, dlogp, scale=scale, live=words, entropy=r.entropy, dentropy=dent)
+        table = raw.to(kind).cuda()
+        same, none = binding.logprob_backward(y, table, tg, r.lse, dlogp, scale=scale, live=words, entropy=r.entropy, dentropy=dent)
+        assert torch.equal(dy, same) and none is None
+        dx, da, db = p.backward(x.cuda(), ad.cuda(), dy)
+        X, A, B = (v.double().requires_grad_() for v in (x, a, b))
+        rows = []
+        for i in range(n):
+            k = int(ad[i])
+            yi = w.double() @ X[i]
+            if 0 <= k < na:
+                yi = yi + float(s[k]) * (B[k] @ (A[k] @ X[i]))
+            rows.append(yi)
+        z = (scale * (torch.stack(rows) @ raw.double().t())).masked_fill(~mask, -math.inf)
+        logp = torch.log_softmax(z, 1)
+        prob = logp.exp()
+        entropy = -torch.where(prob > 0, prob * logp.clamp(min=-1e30), 0.0).sum(1)
+        loss = -logp[torch.arange(n), targets].mean() + 0.1 * entropy.mean()
+        loss.backward()
+        # relative to the largest gradient, as for the chain over a table above, and sums over 3,000 vectors instead of 500
+        for got, want in ((dx, X.grad), (da, A.grad), (db, B.grad)):
+            close(got, want, 6 * 4000 * U * float(want.abs().max()), "gradient")
+        ix.free()
