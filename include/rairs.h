@@ -449,7 +449,10 @@ int rairs_logprob(const rairs_table_t *t, const void *d_q, int64_t ld_q, int q_d
  *   G[i][v] = scale (dlogp[i] (1[v = target] - p[v]) - dentropy[i] p[v] (log p[v] + entropy[i]))
  *   d_dq [n] rows of d, the queries' type: G T;   d_dtable [V] rows of d, the table's type: G^T q,
  * either may be NULL; d_dtable only for tables that are not RAIRS_U8 (zeros in rows that no query sees).
- *   d_lse, d_entropy  what rairs_logprob wrote; d_dlogp [n] fp32; d_dentropy [n] fp32 or NULL (d_entropy may
+ *   d_lse, d_entropy  what rairs_logprob wrote, or the same of a larger table of which this is a part (p is relative to it
+ *                     then; a query whose target is elsewhere passes the gradient of its entropy alone); of fp32 queries an lse
+ *                     within 2^-21 (|lse| + 1) of what this table's products give is taken from those, which are more exact
+ *                     than it is; d_dlogp [n] fp32; d_dentropy [n] fp32 or NULL (d_entropy may
  *                     then be NULL too)
  * n <= RAIRS_MAX_GRAD_ROWS (parts of a larger batch one after the other; d_dtable is the parts' sum).
  * A target that is none or that the mask hides passes no gradient; a row that passes none at all (dlogp

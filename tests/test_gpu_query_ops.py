@@ -1013,3 +1013,30 @@ def test_adapters_learn_over_the_vectors_of_an_index(small_index_int, small_inde
         for got, want in ((dx, X.grad), (da, A.grad), (db, B.grad)):
             close(got, want, 6 * 4000 * U * float(want.abs().max()), "gradient")
         ix.free()
+
+
+@pytest.mark.parametrize("entropy", [False, True])
+@pytest.mark.parametrize("tt", [F32, BF16, U8])
+@pytest.mark.parametrize("n,v,d", [(6, 90, 24), (130, 700, 64), (300, 20_000, 40)])
+def test_logprob_backward_with_the_lse_of_a_larger_table(n, v, d, tt, entropy):
+    # the table is a part of a larger one, and p is relative to the whole; every third query's lse is the part's own
+    q, table, _, scale, _ = logprob_data(n, 2 * v, d, tt, n + v)
+    g = gen(n)
+    targets = torch.randint(-1, v, (n,), generator=g)
+    da, db = torch.randn(n, generator=g), torch.randn(n, generator=g) if entropy else None
+    own = torch.arange(n) % 3 == 0
+    mask = torch.ones(n, 2 * v, dtype=torch.bool)
+    mask[own, v:] = False
+    r = binding.logprob(q.cuda(), table.cuda(), targets.cuda(), scale=scale, live=pack(mask))
+    part = table[:v].contiguous().cuda()
+    dq, dt = binding.logprob_backward(q.cuda(), part, targets.cuda(), r.lse, da.cuda(), scale=scale, entropy=r.entropy if entropy else None,
+                                      dentropy=db.cuda() if entropy else None, table_grad=tt != U8)
+    w = exact_logprob(q, table, targets, scale, mask, 1)
+    w["seen"] = torch.ones(n, v, dtype=torch.bool)
+    w["p"] = w["p"][:, :v]
+    wq, wt, mag, T = exact_backward(q, table[:v], targets, scale, None, da, db, w)
+    rel = 4 * w["tol"] * (w["h"] + 2 + math.log(2 * v + 1)) + (half(BF16) ** 2 if tt == BF16 else 2 ** -22)
+    eg = mag * rel[:, None] + 1e-30
+    close(dq, wq, eg @ T.abs() + sum_err(v) * (mag @ T.abs()) + half(q.dtype) * wq.abs() * 1.01, "dq")
+    if tt != U8:
+        close(dt, wt, eg.t() @ q.double().abs() + sum_err(n) * (mag.t() @ q.double().abs()) + half(tt) * wt.abs() * 1.01, "dtable")
