@@ -1113,6 +1113,10 @@ static int few_tiles(RowProd &rp, const StatsArgs &st, const uint32_t *any_live,
                         : few_tiles_launch<TileF4, FLAGS>(rp, st, any_live, xmax, prun, s);
 }
 
+// The forward pass holds the parts and groups of as many queries at a time as this (10,000 queries over 1M rows in groups of
+// 16: 5 GB); the table is laid out once.
+#define STATS_BYTES (8ll << 30)
+
 int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t s)
 {
     const bool few = a.n <= FEW_ROWS;
@@ -1120,30 +1124,44 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     // rounds of 64 rows per wave, up to 16, for 4,096 waves (four a SIMD) or a multiple
     const int64_t fills = (blocks + 16 * 4096 - 1) / (16 * 4096);
     const int rounds = few ? (int)((blocks + fills * 4096 - 1) / (fills * 4096)) : 1;
-    const bool large = rowprod_size(a.V, a.n) == 2, threes = !few && a.ttype == RAIRS_F32;
-    const int bp = few || large ? 256 : 128, bq = few ? 64 : threes ? 128 : bp;
-    const int64_t ptiles = (a.V + bp - 1) / bp, qtiles = (a.n + bq - 1) / bq;
-    // (a start costs a few microseconds, a tile 27 at K = 1024 and 256 x 256; one workgroup of the large tile
-    // fits a CU, two of the smaller)
+    const bool threes = !few && a.ttype == RAIRS_F32;
     const double ksum = (double)kpad * (dtype_pieces(a.ttype) * dtype_pieces(a.qtype) == 9 ? 6 : dtype_pieces(a.qtype));
-    const int prun = rowprod_run(ptiles, qtiles, few || large || threes ? 256 : 512, few ? 0.3 : 100.0 / (ksum + 200.0), 64);
-    // (a few queries: by tiles, four waves along P, or rows straight from memory; there is room for either's parts)
-    const int runs = (int)((ptiles + prun - 1) / prun), few_parts = (int)((blocks + rounds - 1) / rounds);
-    const int most_parts = few ? std::max(4 * runs, few_parts) : (threes && large ? 4 : 2) * runs;
+    const int few_parts = (int)((blocks + rounds - 1) / rounds);
+    bool large;
+    int prun, runs, most_parts;
+    const auto plan = [&](int64_t n) {
+        large = rowprod_size(a.V, n) == 2;
+        const int bp = few || large ? 256 : 128, bq = few ? 64 : threes ? 128 : bp;
+        const int64_t ptiles = (a.V + bp - 1) / bp, qtiles = (n + bq - 1) / bq;
+        // (a start costs a few microseconds, a tile 27 at K = 1024 and 256 x 256; one workgroup of the large tile
+        // fits a CU, two of the smaller)
+        prun = rowprod_run(ptiles, qtiles, few || large || threes ? 256 : 512, few ? 0.3 : 100.0 / (ksum + 200.0), 64);
+        // (a few queries: by tiles, four waves along P, or rows straight from memory; there is room for either's parts)
+        runs = (int)((ptiles + prun - 1) / prun);
+        most_parts = few ? std::max(4 * runs, few_parts) : (threes && large ? 4 : 2) * runs;
+    };
     // Groups of 16 rows or of 64.  Per query, the smaller ones cost two more operations a row and 8 bytes for 16 rows
     // instead of 4 for 64, about 0.14 ps times V; the larger ones 64 rows of the table for each of the `top`, at about
     // 6 TB/s.  (A few queries: the vector units have nothing else to do.)
     const int wide = !few && a.V > 76ll * a.top * a.d * dtype_width(a.ttype);
+    plan(a.n);
+    int64_t nc = a.n;                                                 // queries at a time: whole tiles, about as many each time
+    const int64_t each = 16ll * most_parts + (!a.top ? 0 : wide ? pad_to(blocks, 4) * 4 : blocks * 32);
+    if (!few && a.n * each > STATS_BYTES) {
+        const int64_t fit = std::max<int64_t>(STATS_BYTES / each / 256 * 256, 256), times = (a.n + fit - 1) / fit;
+        nc = pad_to((a.n + times - 1) / times, 256);
+        plan(nc);
+    }
     Carve w(ws);
     StatsArgs st = {};
-    st.n = (int)a.n; st.V = (int)a.V; st.c = a.scale * LOG2E; st.live = a.live; st.ld_live = a.ld_live; st.targets = a.targets;
-    st.parts = w.take<float4>(a.n * most_parts);
+    st.V = (int)a.V; st.c = a.scale * LOG2E; st.ld_live = a.ld_live;
+    st.parts = w.take<float4>(nc * most_parts);
     st.wstride = (int)pad_to(blocks, 4);
-    st.gmax = a.top ? w.take<float>(wide ? a.n * st.wstride : a.n * blocks * 4) : nullptr;
-    st.gsecond = a.top && !wide ? w.take<float>(a.n * blocks * 4) : nullptr;
+    st.gmax = a.top ? w.take<float>(wide ? nc * st.wstride : nc * blocks * 4) : nullptr;
+    st.gsecond = a.top && !wide ? w.take<float>(nc * blocks * 4) : nullptr;
     st.nblocks = (int)blocks;
     st.wide = wide;
-    st.zt = w.take<float>(a.n);
+    st.zt = w.take<float>(nc);
     float *xmax = w.take<float>(few ? most_parts : NORM_WGS);
     uint32_t *seen = w.take<uint32_t>(a.ld_live ? (a.V + 31) / 32 : 0);
     // (packed whether they need it or not, so that the size does not depend on where the rows lie)
@@ -1157,6 +1175,31 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
     const uint32_t *seen_by_any = any_live(a, seen, s, &rc);
     if (rc) return rc;
     st.nparts = most_parts;
+    FinishArgs f = {};
+    f.table = a.table; f.ldt = a.ldt; f.ldq = a.ldq; f.d = a.d;
+    f.vec = lies_vec(a.q, a.qtype, a.ldq) && lies_vec(a.table, a.ttype, a.ldt);
+    f.scale = a.scale;
+    f.slack = product_slack(a.d);
+    f.xmax = xmax;
+    f.top = a.top;
+    // the queries from q0 on: of their statistics, and of what they are finished with
+    const auto queries = [&](int64_t q0, int64_t n) {
+        st.n = (int)n;
+        st.targets = a.targets + q0;
+        st.live = a.live ? a.live + q0 * a.ld_live : nullptr;
+        f.q = (const char *)a.q + q0 * a.ldq * dtype_width(a.qtype);
+        f.logp = a.logp + q0; f.lse = a.lse + q0; f.entropy = a.entropy ? a.entropy + q0 : nullptr;
+        f.top_ids = a.top ? a.top_ids + q0 * a.top : nullptr;
+        f.top_logp = a.top ? a.top_logp + q0 * a.top : nullptr;
+    };
+    const auto finish = [&]() {
+        f.st = st;
+        f.nxmax = few ? st.nparts : NORM_WGS;
+        return a.ttype == RAIRS_BF16 ? finish_launch<__bf16, __bf16>(f, s)
+               : a.ttype == RAIRS_F32 ? finish_launch<float, float>(f, s)
+                                      : finish_launch<uint8_t, float>(f, s);
+    };
+    queries(0, nc < a.n ? nc : a.n);
     if (few && (f32_lies_right(a.table, a.ttype, a.ldt, a.d) && f32_lies_right(a.q, a.qtype, a.ldq, a.d))) {
         st.nparts = 4 * runs;
         RowProd rp = {};
@@ -1203,30 +1246,25 @@ int rairs_run_logprob(const LogprobArgs &a, void *ws, size_t *bytes, hipStream_t
         if ((rc = rairs_operand(a.q, a.qtype, a.ldq, a.n, a.d, nullptr, threes, qroom, rp.Q, s, flags ? piece_flags : nullptr, false))) return rc;
         if (flags) rp.Q.pieces_there = piece_flags;
         const bool ent = a.entropy != nullptr;
-        if (a.top == 0) rc = ent ? stats_launch<true, 0>(rp, st, threes, large, prun, s) : stats_launch<false, 0>(rp, st, threes, large, prun, s);
-        else if (wide) rc = ent ? stats_launch<true, 1>(rp, st, threes, large, prun, s) : stats_launch<false, 1>(rp, st, threes, large, prun, s);
-        else rc = ent ? stats_launch<true, 2>(rp, st, threes, large, prun, s) : stats_launch<false, 2>(rp, st, threes, large, prun, s);
-        if (rc) return rc;
+        const __bf16 *q = rp.Q.p;
+        for (int64_t q0 = 0; q0 < a.n; q0 += nc) {
+            queries(q0, std::min(nc, a.n - q0));
+            rp.Q.p = q + q0 * rp.Q.ld;
+            rp.Q.rows = st.n;
+            if (a.top == 0) rc = ent ? stats_launch<true, 0>(rp, st, threes, large, prun, s) : stats_launch<false, 0>(rp, st, threes, large, prun, s);
+            else if (wide) rc = ent ? stats_launch<true, 1>(rp, st, threes, large, prun, s) : stats_launch<false, 1>(rp, st, threes, large, prun, s);
+            else rc = ent ? stats_launch<true, 2>(rp, st, threes, large, prun, s) : stats_launch<false, 2>(rp, st, threes, large, prun, s);
+            if (rc || (rc = finish())) return rc;
+        }
+        return RAIRS_OK;
     }
-    FinishArgs f = {};
-    f.st = st;
-    f.table = a.table; f.q = a.q; f.ldt = a.ldt; f.ldq = a.ldq; f.d = a.d;
-    f.vec = lies_vec(a.q, a.qtype, a.ldq) && lies_vec(a.table, a.ttype, a.ldt);
-    f.scale = a.scale;
-    f.slack = product_slack(a.d);
-    f.xmax = xmax;
-    f.nxmax = few ? st.nparts : NORM_WGS;
-    f.logp = a.logp; f.lse = a.lse; f.entropy = a.entropy;
-    f.top = a.top; f.top_ids = a.top_ids; f.top_logp = a.top_logp;
-    return a.ttype == RAIRS_BF16 ? finish_launch<__bf16, __bf16>(f, s)
-           : a.ttype == RAIRS_F32 ? finish_launch<float, float>(f, s)
-                                  : finish_launch<uint8_t, float>(f, s);
+    return finish();
 }
 
-// G is made for as many of the table's rows at a time as 2 GB of it hold.  (In pieces of 128 MB, which the last-level
-// cache would keep, 4,095 x 65,537 x 1024 took 2.5 ms instead of 1.9: five launches of each product that fill the card
-// less well, and partial sums read again each time.)
-#define GRAD_CHUNK_BYTES (2ll << 30)
+// G is made for as many of the table's rows at a time as this holds, with what is laid out of the rows themselves beside it.
+// (In pieces of 128 MB, which the last-level cache would keep, 4,095 x 65,537 x 1024 took 2.5 ms instead of 1.9, with G in one
+// piece: five launches of each product that fill the card less well, and partial sums read again each time.)
+#define GRAD_CHUNK_BYTES (8ll << 30)
 
 template <int NP, bool ENT>
 static int grad_launch(RowProd &rp, const GradArgs &ga, bool threes, hipStream_t s)
@@ -1250,10 +1288,14 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     const bool threes = tp == 3, again = np == 3;
     const int64_t kpad = pad_to(a.d, threes ? 32 : ROWPROD_K), npad = pad_to(a.n, ROWPROD_K), dpad = pad_to(a.d, 4);
     const bool need_dt = a.dtable != nullptr, need_dq = a.dq != nullptr;
-    int64_t vc = GRAD_CHUNK_BYTES / (2 * gp * npad) / 1024 * 1024;
+    // bytes of a row of the table: G both ways, the row as it lies and turned
+    const int64_t row = 2 * tp * pad_to(a.d, ROWPROD_K), each = 2 * gp * npad * (int64_t)(need_dq + need_dt) + row + (need_dq ? 2 * tp * a.d : 0);
+    int64_t vc = GRAD_CHUNK_BYTES / each / 1024 * 1024;
     vc = vc < 1024 ? 1024 : std::min<int64_t>(vc, 1 << 20);           // (rows of threes: below 2^22 values)
     const int64_t chunks = (a.V + vc - 1) / vc;
     vc = pad_to((a.V + chunks - 1) / chunks, ROWPROD_K);              // of about one size
+    // (fp32: the statistics need no G, and rows that are all laid out for them stay for the gradient)
+    const int64_t vs = !again ? vc : std::max(vc, std::min(a.V, std::max<int64_t>(GRAD_CHUNK_BYTES / row / 1024 * 1024, 1024)));
     // the queries' product: its sum over the chunk is cut so that there are workgroups for every CU, of large tiles if
     // pieces of 2,048 rows (of the small tiles' 512) are enough for that
     const int64_t tl = rowprod_tiles(a.d, a.n, 256), tm = rowprod_tiles(a.d, a.n, 128), ts = rowprod_tiles(a.d, a.n, 64);
@@ -1263,7 +1305,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     if (splits < 1) splits = 1;
     Carve w(ws);
     __bf16 *qroom = w.take<__bf16>(pack_room(a.qtype, a.n, a.d));
-    __bf16 *troom = w.take<__bf16>(pack_room(a.ttype, vc, a.d));
+    __bf16 *troom = w.take<__bf16>(pack_room(a.ttype, vs, a.d));
     __bf16 *tcols = need_dq ? w.take<__bf16>((int64_t)a.d * vc * tp) : nullptr;
     __bf16 *qcols = need_dt ? w.take<__bf16>((int64_t)a.d * npad * np) : nullptr;
     __bf16 *g = need_dq ? w.take<__bf16>(a.n * vc * gp) : nullptr;
@@ -1273,12 +1315,18 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     // fp32: the statistics once more, by tiles as in the forward pass
     StatsArgs st = {};
     const auto large_of = [&](int64_t rows) { return rowprod_size(rows, a.n) == 2; };
+    const auto run_of = [&](int64_t rows) {
+        const bool l = large_of(rows);
+        const int64_t side = l ? 256 : 128, ptiles = (rows + side - 1) / side, qtiles = (a.n + (threes ? 127 : side - 1)) / (threes ? 128 : side);
+        return rowprod_run(ptiles, qtiles, l || threes ? 256 : 512, 100.0 / ((double)kpad * (threes ? 6 : 3) + 200.0), 64);
+    };
     const auto parts_of = [&](int64_t rows) {
         const bool l = large_of(rows);
-        return (threes && l ? 4 : 2) * ((rows + (l ? 255 : 127)) / (l ? 256 : 128));
+        const int64_t ptiles = (rows + (l ? 255 : 127)) / (l ? 256 : 128);
+        return (threes && l ? 4 : 2) * ((ptiles + run_of(rows) - 1) / run_of(rows));
     };
     if (again) {
-        for (int64_t v0 = 0; v0 < a.V; v0 += vc) st.nparts += (int)parts_of(std::min(vc, a.V - v0));
+        for (int64_t v0 = 0; v0 < a.V; v0 += vs) st.nparts += (int)parts_of(std::min(vs, a.V - v0));
         st.parts = w.take<float4>(a.n * st.nparts);
         st.zt = w.take<float>(a.n);
     }
@@ -1314,8 +1362,8 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     if (again) {
         st.n = (int)a.n; st.c = a.scale * LOG2E; st.ld_live = a.ld_live; st.targets = a.targets;
         float4 *parts = st.parts;
-        for (int64_t v0 = 0; v0 < a.V; v0 += vc) {
-            const int64_t rows = std::min(vc, a.V - v0);
+        for (int64_t v0 = 0; v0 < a.V; v0 += vs) {
+            const int64_t rows = std::min(vs, a.V - v0);
             RowProd rp = {};
             rairs_operand_job(chunk(v0), a.ttype, a.ldt, rows, a.d, threes, troom, rp.P, jobs);
             if (need_dq && vc >= a.V) turn_table(0, rows, pad_to(rows, ROWPROD_K));
@@ -1326,7 +1374,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
             rp.Q = Q;
             st.V = (int)rows;
             st.live = a.live ? a.live + v0 / 32 : nullptr;
-            if ((rc = stats_launch<false, 0>(rp, st, threes, large_of(rows), 1, s))) return rc;
+            if ((rc = stats_launch<false, 0>(rp, st, threes, large_of(rows), run_of(rows), s))) return rc;
             st.parts += parts_of(rows);
         }
         st.parts = parts;
@@ -1336,14 +1384,16 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
     for (int64_t v0 = 0; v0 < a.V; v0 += vc) {
         const int64_t rows = a.V - v0 < vc ? a.V - v0 : vc, cpad = pad_to(rows, ROWPROD_K);
         RowProd rp = {};
-        if (again && vc >= a.V) {
+        if (again && vs >= a.V) {
             rp.P = P0;                                                // (laid out above)
+            rp.P.p += v0 * P0.ld;
+            rp.P.rows = rows;
         } else {
             rairs_operand_job(chunk(v0), a.ttype, a.ldt, rows, a.d, threes, troom, rp.P, jobs);
-            if (need_dq) turn_table(v0, rows, cpad);
-            if ((rc = rairs_launch_pack(jobs, s))) return rc;
-            jobs.n = 0;
         }
+        if (need_dq && !(again && vc >= a.V)) turn_table(v0, rows, cpad);
+        if ((rc = rairs_launch_pack(jobs, s))) return rc;
+        jobs.n = 0;
         rowprod_sums(rp, tp, np, kpad);
         rp.Q = Q;
         GradArgs ga = {};

@@ -1040,3 +1040,64 @@ def test_logprob_backward_with_the_lse_of_a_larger_table(n, v, d, tt, entropy):
     close(dq, wq, eg @ T.abs() + sum_err(v) * (mag @ T.abs()) + half(q.dtype) * wq.abs() * 1.01, "dq")
     if tt != U8:
         close(dt, wt, eg.t() @ q.double().abs() + sum_err(n) * (mag.t() @ q.double().abs()) + half(tt) * wt.abs() * 1.01, "dtable")
+
+
+def sampled_exact(q, table, targets, scale, rows):
+    """Log probabilities of some queries in 64 bits on the GPU: lse, log p of the target, the products."""
+    ip = q[rows].double() @ table.double().t()
+    z = ip * scale
+    lse = z.logsumexp(1)
+    return ip, lse, z.gather(1, targets[rows][:, None])[:, 0] - lse
+
+
+def test_logprob_of_a_batch_that_is_taken_in_parts():
+    # groups of 16 rows for 40,000 queries over 500,000 rows: 10 GB, so two parts; queries at the parts' ends among the checked
+    n, v, d, top = 40_000, 500_000, 128, 50
+    g = torch.Generator(device="cuda").manual_seed(5)
+    table = torch.randn(v, d, generator=g, device="cuda").to(BF16)
+    q = torch.randn(n, d, generator=g, device="cuda").to(BF16)
+    targets = torch.randint(0, v, (n,), generator=g, device="cuda")
+    scale = 0.25
+    r = binding.logprob(q, table, targets, scale=scale, top=top)
+    rows = torch.tensor([0, 1, 19_999, 20_000, 20_223, 20_224, 20_225, 33_333, 39_999], device="cuda")
+    ip, lse, logp = sampled_exact(q, table, targets, scale, rows)
+    # a logit is off by fp32 sums of up to 8 |q||t|, about 1,100, and the rounding of lse
+    tol = scale * sum_err(d) * 1200 + 8 * U * 80
+    assert float((r.lse[rows].double() - lse).abs().max()) <= tol
+    assert float((r.logp[rows].double() - logp).abs().max()) <= 2 * tol
+    assert torch.equal(r.top_ids[rows], ip.sort(dim=1, descending=True, stable=True).indices[:, :top])
+
+
+@pytest.mark.parametrize("tt", [F32, U8])
+def test_logprob_backward_of_a_table_that_is_taken_in_parts(tt):
+    # few queries, wide rows: 8 GB do not hold the rows' pieces both ways; whole numbers, so that products are exact
+    n, v, d = 5, 400_000, 4096
+    if tt == U8:
+        v = 800_000
+    g = torch.Generator(device="cuda").manual_seed(6)
+    table = torch.randint(0, 3, (v, d), generator=g, device="cuda", dtype=U8)
+    if tt == F32:
+        table = table.float()
+    q = torch.randint(0, 2, (n, d), generator=g, device="cuda").float()
+    targets = torch.tensor([0, v - 1, v // 2, 7, -1], device="cuda")
+    scale = 2.0 ** -6
+    r = binding.logprob(q, table, targets, scale=scale)
+    da = torch.ones(n, device="cuda")
+    dq, dt = binding.logprob_backward(q, table, targets, r.lse, da, scale=scale, table_grad=tt == F32)
+    parts = [table[i:i + 100_000].double() for i in range(0, v, 100_000)] if tt == F32 else None
+    step = 100_000
+    z = torch.cat([q.double() @ (parts[i // step] if parts else table[i:i + step].double()).t() for i in range(0, v, step)], 1) * scale
+    logp = z - z.logsumexp(1)[:, None]
+    p = logp.exp()
+    G = -p * (targets >= 0)[:, None]
+    G[torch.arange(4, device="cuda"), targets[:4]] += 1.0
+    G *= scale
+    want = sum(G[:, i:i + step] @ (parts[i // step] if parts else table[i:i + step].double()) for i in range(0, v, step))
+    # p is off by its logarithm: lse (about 80) is rounded, log p too; sums of up to v terms of at most 2 |G|
+    e = 16 * U * 160
+    tol = (1.01 * e + sum_err(v) + 2 ** -22) * 2 * scale * 2
+    assert float((dq.double() - want).abs().max()) <= tol
+    if dt is not None:
+        wt = G.t() @ q.double()
+        err = (dt.double() - wt).abs()
+        assert float((err - (1.01 * e + sum_err(n) + 2 ** -22) * (G.abs().t() @ q.double() + p.t() @ q.double() * scale * e)).max()) <= 1e-12

@@ -205,3 +205,26 @@ def test_a_table_whose_last_tile_does_not_end_within_an_int_is_refused():
         for call in (logprob, logprob_backward):
             assert call(table(V=v), ws=None) == code, v
         assert (lib.rairs_logprob_workspace_bytes(C.byref(table(V=v)), C.c_int64(4), C.c_int(0), C.c_int(0)) > 0) == (code == EWORKSPACE)
+
+
+def test_workspaces_do_not_grow_with_the_product_of_batch_and_table():
+    # what is held for every pair of a query and a row (or 16 of them) is bounded by parts; what is left are the pieces of
+    # the table (6 bytes a value of fp32, 2 of others; backward up to 8 GB at a time), of the queries and of a few gradients
+    lib = binding.load()
+    GB = 1 << 30
+    for dtype, piece in ((0, 6), (1, 2), (2, 2)):
+        for v, d in ((1_000_000, 64), (1_000_000, 1024), (100_000, 4096), (20_000_000, 64)):
+            t = table(V=v, d=d, ld=d, dtype=dtype)
+            qt = 0 if dtype == 2 else dtype
+            for n in (1, 16, 65, 10_000, 1 << 20):
+                fwd = lib.rairs_logprob_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(qt), C.c_int(50))
+                rows = 6 * n * d if qt == 0 else 2 * n * d
+                assert 0 < fwd <= 9 * GB + (piece * v * d if n > 64 else 0) + 2 * rows, (dtype, v, d, n, fwd / GB)
+                for grad in (0, 1):
+                    if grad and dtype == 2:
+                        continue
+                    back = lib.rairs_logprob_backward_workspace_bytes(C.byref(t), C.c_int64(n), C.c_int(qt), C.c_int(grad))
+                    # sums of dq in at most 8 parts of a large batch, or of a small one for a few thousand workgroups
+                    sums = max(8 * 4 * n * d, GB)
+                    parts = 16 * n * (v // 256 // 16 + 64) if qt == 0 else 0
+                    assert 0 < back <= 17 * GB + 3 * rows + sums + parts, (dtype, v, d, n, grad, back / GB)
