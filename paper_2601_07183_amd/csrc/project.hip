@@ -48,6 +48,64 @@ __global__ __launch_bounds__(WG) void clear_words_kernel(int32_t *p, int64_t n)
     if (i < n) p[i] = 0;
 }
 
+// Adapters that have rows, numbered in their order, where a batch may have far fewer than there are: what is laid out of
+// adapters is laid out of these alone.
+struct UsedView {
+    const int32_t *adapter;         // [n]
+    int64_t n;
+    int na, most;                   // adapters; how many may have rows
+    int32_t *number;                // [n] of the row's adapter, -1: none
+    int32_t *orig, *of;             // [most] adapter of a number (the first one's for numbers that none has), [na] number of an adapter or -1
+};
+__global__ __launch_bounds__(1024) void used_kernel(UsedView v)
+{
+    __shared__ uint32_t bits[RAIRS_MAX_ADAPTERS / 32];
+    __shared__ int32_t before[RAIRS_MAX_ADAPTERS / 32 + 1];
+    const int tid = threadIdx.x, words = (v.na + 31) / 32;
+    for (int w = tid; w < words; w += 1024) bits[w] = 0;
+    __syncthreads();
+    for (int64_t i = tid; i < v.n; i += 1024) {
+        const int a = v.adapter[i];
+        if (a >= 0 && a < v.na) atomicOr(&bits[a >> 5], 1u << (a & 31));
+    }
+    __syncthreads();
+    if (tid == 0) {
+        int s = 0;
+        for (int w = 0; w < words; w++) {
+            before[w] = s;
+            s += __popc(bits[w]);
+        }
+        before[words] = s;
+    }
+    __syncthreads();
+    const auto number = [&](int a) { return (bits[a >> 5] >> (a & 31)) & 1u ? before[a >> 5] + __popc(bits[a >> 5] & ((1u << (a & 31)) - 1u)) : -1; };
+    for (int a = tid; a < v.na; a += 1024) {
+        const int k = number(a);
+        v.of[a] = k;
+        if (k >= 0) v.orig[k] = a;
+    }
+    for (int k = before[words] + tid; k < v.most; k += 1024) v.orig[k] = 0;
+    for (int64_t i = tid; i < v.n; i += 1024) {
+        const int a = v.adapter[i];
+        v.number[i] = a >= 0 && a < v.na ? number(a) : -1;
+    }
+}
+
+// A launch more (6 us) against what is not laid out: 32 MB of it take as long.
+static bool numbers_used(const rairs_projection_t &p, int64_t n, int64_t bytes_each) { return p.n_adapters > n && (p.n_adapters - n) * bytes_each > 32ll << 20; }
+static UsedView used_carve(Carve &w, const rairs_projection_t &p, const int32_t *adapter, int64_t n)
+{
+    return UsedView{adapter, n, p.n_adapters, (int)n, w.take<int32_t>(n), w.take<int32_t>(n), w.take<int32_t>(p.n_adapters)};
+}
+static int used_launch(const UsedView &v, hipStream_t s)
+{
+    hipLaunchKernelGGL(used_kernel, dim3(1), dim3(1024), 0, s, v);
+    RAIRS_HIP(hipGetLastError());
+    return RAIRS_OK;
+}
+// (orig: null where adapters are their own numbers)
+static __device__ __forceinline__ int64_t orig_of(const int32_t *orig, int64_t a) { return orig ? orig[a] : a; }
+
 // lanes of the wave with the same key (below 2^bits, bits <= 13); key < 0: none
 static __device__ __forceinline__ unsigned long long same_key(int key, int bits)
 {
@@ -300,6 +358,7 @@ struct ShrinkArgs {
     __bf16 *up;                     // [n][kpad] in sorted order, or null
     Side side;
     SideFlags flags;
+    const int32_t *orig, *aorig;    // of the scale, of a
 };
 
 // A workgroup per unit; its NW waves share the sum, which is joined in LDS.  Bound by the loads: a lane's 16 bytes lie in a
@@ -317,12 +376,13 @@ __global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs one, ShrinkA
     const S *prow[RT];
     v4f acc[RT][2];
     float nrm[RT];
+    const int64_t ad = orig_of(a.aorig, unit.x);
 #pragma unroll
     for (int j = 0; j < 2; j++) qrow[j] = (const S *)a.x + (int64_t)a.perm[unit.y + min(16 * j + (lane & 15), unit.z - 1)] * a.ldx;
 #pragma unroll
     for (int i = 0; i < RT; i++) {
         const int j = min(16 * i + (lane & 15), a.r - 1);
-        prow[i] = (const S *)a.a + ((int64_t)unit.x * a.r + j) * a.d;
+        prow[i] = (const S *)a.a + (ad * a.r + j) * a.d;
         acc[i][0] = acc[i][1] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
     }
     int bad = 0;
@@ -341,7 +401,7 @@ __global__ __launch_bounds__(64 * NW) void shrink_kernel(ShrinkArgs one, ShrinkA
                 for (int e = 0; e < 4; e++) part[wave - 1][16 * j + (lane & 15)][16 * i + 4 * (lane >> 4) + e] = acc[i][j][e];
     __syncthreads();
     if (wave == 0) {
-        const float sc = a.scale ? a.scale[unit.x] : 1.0f;
+        const float sc = a.scale ? a.scale[orig_of(a.orig, unit.x)] : 1.0f;
 #pragma unroll
         for (int i = 0; i < RT; i++)
 #pragma unroll
@@ -405,6 +465,7 @@ struct SideJob {
     Side side;
     __bf16 *dst, *zero;
     uint32_t *found;
+    const int32_t *orig;            // of row block a; null: a
 };
 
 template <class S>
@@ -420,7 +481,7 @@ static __device__ __forceinline__ void pack_side(const SideJob &j, int64_t block
     if (t < j.total) {
         const int k0 = (int)(id / 64 % eights) * 8;
         const int64_t a = t / j.rows, o = t - a * j.rows;
-        const S *p = (const S *)j.src + a * j.batch + o * j.so;
+        const S *p = (const S *)j.src + orig_of(j.orig, a) * j.batch + o * j.so;
         const auto at = [&](int w) {
             const float x = (float)p[w * j.sj];
             const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
@@ -443,15 +504,15 @@ static __device__ __forceinline__ void pack_side(const SideJob &j, int64_t block
     if (threadIdx.x == 0) j.found[block] = odd;
 }
 
-// dst[b][c][r] = src[b][r][c], 32 x 32 values
+// dst[b][c][r] = src[orig b][r][c], 32 x 32 values
 template <class S>
 static __device__ __forceinline__ void transpose_tile(S (&tile)[32][33], const S *__restrict__ src, int rows, int cols, S *__restrict__ dst,
-                                                      int64_t block)
+                                                      int64_t block, const int32_t *__restrict__ orig)
 {
     const int rt = (rows + 31) / 32, ct = (cols + 31) / 32;
-    const int64_t batch = block / (rt * ct) * rows * cols;
+    const int64_t b = block / (rt * ct), batch = b * rows * cols, from = orig_of(orig, b) * rows * cols;
     const int in = (int)(block % (rt * ct)), r0 = in % rt * 32, c0 = in / rt * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    if (r0 + y < rows && c0 + x < cols) tile[y][x] = src[batch + (int64_t)(r0 + y) * cols + c0 + x];
+    if (r0 + y < rows && c0 + x < cols) tile[y][x] = src[from + (int64_t)(r0 + y) * cols + c0 + x];
     __syncthreads();
     if (c0 + y < cols && r0 + x < rows) dst[batch + (int64_t)(c0 + y) * rows + r0 + x] = tile[x][y];
 }
@@ -467,6 +528,7 @@ struct PrepArgs {
     PackJobs rows;                  // W (forward) and the batch, in the batch's order
     SideJob side;
     const void *w, *b;              // [d_out][d_in], [na][d_out][r]
+    const int32_t *orig;            // of b's, null: as they are
     int d_in, d_out, r, vec;
     __bf16 *wt;
     int64_t opad;
@@ -505,7 +567,7 @@ __global__ __launch_bounds__(1024) void prep_kernel(PrepArgs a)
         }
         block -= a.rows.job[i].blocks;
     }
-    transpose_tile<S>(*(S(*)[32][33])prep_lds, (const S *)a.b, a.d_out, a.r, (S *)a.bt, block + a.turn_from);
+    transpose_tile<S>(*(S(*)[32][33])prep_lds, (const S *)a.b, a.d_out, a.r, (S *)a.bt, block + a.turn_from, a.orig);
 }
 
 // The batch as an operand, to be taken through a permutation that is not known yet: laid out beside the sort, where 32-bit
@@ -737,6 +799,7 @@ struct AdapterEpi : StoreEpi {
     int64_t batch, so, sj;
     const __bf16 *u;
     Side side;
+    const int32_t *orig;
     template <class T>
     struct State : StoreEpi::State<T> {
         uint32_t odd;               // of this lane's rows
@@ -770,7 +833,7 @@ struct AdapterEpi : StoreEpi {
         for (int j = 0; j < T::QT; j++) {
             if (!((st.odd >> j) & 1u)) continue;
             const int64_t q = q0 + 16 * j + (lane & 15), row = perm ? perm[q] : q;
-            const S *b = src + of_row[q] * batch;
+            const S *b = src + orig_of(orig, of_row[q]) * batch;
 #pragma unroll 1
             for (int i = 0; i < 4 * T::PT; i++) {
                 // (a run is one tile; the lane that stored a value adds to it)
@@ -800,10 +863,10 @@ static int large_product(RowProd &rp, const StoreEpi &e, bool bf, bool f32, cons
         return bf ? rowprod_launch_any(rp, e, s) : rowprod_launch_any<ROW_THREES>(rp, e, s);
     }
     if (bf) {
-        const AdapterEpi<__bf16> ae = {e, rp.ad.of_row, bad, (const __bf16 *)job->src, job->batch, job->so, job->sj, u, job->side};
+        const AdapterEpi<__bf16> ae = {e, rp.ad.of_row, bad, (const __bf16 *)job->src, job->batch, job->so, job->sj, u, job->side, job->orig};
         return rowprod_launch_any<ROW_ADAPT>(rp, ae, s);
     }
-    const AdapterEpi<float> ae = {e, rp.ad.of_row, bad, (const float *)job->src, job->batch, job->so, job->sj, u, job->side};
+    const AdapterEpi<float> ae = {e, rp.ad.of_row, bad, (const float *)job->src, job->batch, job->so, job->sj, u, job->side, job->orig};
     return f32 ? rowprod_launch<TileS, ROW_F32 | ROW_ADAPT>(rp, ae, s) : rowprod_launch_any<ROW_THREES | ROW_ADAPT>(rp, ae, s);
 }
 
@@ -821,7 +884,6 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
 {
     const rairs_projection_t &p = g.p;
     const bool adapters = p.n_adapters > 0, bf = p.dtype == RAIRS_BF16;
-    const int64_t units = max_units(g.n, p.n_adapters, UNIT_ROWS);
     Carve w(ws);
     int rc = RAIRS_OK;
     if (few_rows(p, g.n)) {
@@ -843,6 +905,8 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     const int np = dtype_pieces(p.dtype);
     __bf16 *xroom = w.take<__bf16>(pack_room(p.dtype, g.n, p.d_in)), *wroom = w.take<__bf16>(pack_room(p.dtype, p.d_out, p.d_in));
     SortView sv = {};
+    UsedView used = {};
+    int na = p.n_adapters;          // or how many of them are laid out
     Side side = {};
     SideFlags flags = {};
     __bf16 *up = nullptr, *bp = nullptr, *zero = nullptr;
@@ -850,15 +914,19 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
     const bool f32 = rowprod_size(p.d_out, g.n) == 0 && f32_lies_right(p.W, p.dtype, p.d_in, p.d_in) &&
                      f32_lies_right(g.x, p.dtype, g.ldx, p.d_in) && g.n * g.ldx < (1ll << 30);
     if (adapters) {
-        sv = sort_carve(w, g.adapter, g.n, p.n_adapters);
         side = side_of(bf ? SIDE_BF16 : f32 ? SIDE_F32 : SIDE_THREES, p.rank);
         // (the size does not depend on where the rows lie)
         const int room = bf ? side.kpad : side_of(SIDE_THREES, p.rank).kpad;
+        if (numbers_used(p, g.n, 2ll * p.d_out * room)) {
+            used = used_carve(w, p, g.adapter, g.n);
+            na = used.most;
+        }
+        sv = sort_carve(w, used.na ? used.number : g.adapter, g.n, na);
         up = w.take<__bf16>(g.n * room);
-        bp = w.take<__bf16>((int64_t)p.n_adapters * p.d_out * room);
+        bp = w.take<__bf16>((int64_t)na * p.d_out * room);
         zero = w.take<__bf16>(room);
-        flags.found = w.take<uint32_t>(side_blocks(Side{0, 0, room}, (int64_t)p.n_adapters * p.d_out));
-        flags.bad = w.take<uint32_t>(p.n_adapters);
+        flags.found = w.take<uint32_t>(side_blocks(Side{0, 0, room}, (int64_t)na * p.d_out));
+        flags.bad = w.take<uint32_t>(na);
         flags.rows = p.d_out;
     }
     if (bytes) *bytes = w.used;
@@ -866,7 +934,7 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
 
     const bool use = adapters && g.adapter;
     RowProd rp = {};
-    const SideJob job = {p.B, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, (int64_t)p.n_adapters * p.d_out, side, bp, zero, flags.found};
+    const SideJob job = {p.B, (int64_t)p.d_out * p.rank, p.rank, 1, p.d_out, (int64_t)na * p.d_out, side, bp, zero, flags.found, used.orig};
     PackJobs jobs = {};
     bool late = false;
     if (!f32) {
@@ -874,6 +942,7 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         late = !batch_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, xroom, rp.Q, jobs);
     }
     if (use) {
+        if (used.na && (rc = used_launch(used, s))) return rc;
         PrepArgs pa = {};
         pa.sort = sv;
         pa.side = job;
@@ -892,7 +961,8 @@ int rairs_run_project(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t
         if (late && (rc = rairs_operand(g.x, p.dtype, g.ldx, g.n, p.d_in, use ? sv.perm : nullptr, !bf, xroom, rp.Q, s))) return rc;
     }
     if (use) {
-        ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + p.n_adapters, nullptr, up, side, flags};
+        ShrinkArgs sa = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, nullptr, up, side, flags, used.orig, used.orig};
+        const int64_t units = max_units(g.n, na, UNIT_ROWS);
         const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype);
         if ((rc = bf ? shrink_launch<__bf16>(sa, nullptr, units, vec, s) : shrink_launch<float>(sa, nullptr, units, vec, s))) return rc;
         rp.ad = AdapterPart{up, bp, zero, sv.of_row, sv.first + 1, side.kpad};
@@ -920,6 +990,7 @@ struct AdapterGradArgs {            // of A: x and v; of B (turned): dy and u
     const int32_t *perm, *chunk0;
     const int4 *chunks;
     int r, na;
+    const int32_t *of;              // number of an adapter, -1: it has no rows; null: its own
 };
 
 template <class S, int RT, bool VEC>
@@ -997,18 +1068,20 @@ __global__ __launch_bounds__(WG) void adapter_join_kernel(AdapterGradArgs g)
     if (t >= size) return;
     const float *part = g.part[blockIdx.z];
     float x = 0.0f;
-    for (int c = g.chunk0[a]; c < g.chunk0[a + 1]; c++) x += part[c * size + t];
+    const int k = g.of ? g.of[a] : a;
+    if (k >= 0)
+        for (int c = g.chunk0[k]; c < g.chunk0[k + 1]; c++) x += part[c * size + t];
     ((S *)g.out[blockIdx.z])[a * size + t] = (S)x;
 }
 
 template <class S>
-static int adapter_grads(const ProjectArgs &g, const SortView &sv, const float *u, const float *v, float *apart, float *bpart, hipStream_t s)
+static int adapter_grads(const ProjectArgs &g, const SortView &sv, const int32_t *of, const float *u, const float *v, float *apart, float *bpart, hipStream_t s)
 {
     const rairs_projection_t &p = g.p;
-    const unsigned chunks = (unsigned)max_units(g.n, p.n_adapters, CHUNK_ROWS);
+    const unsigned chunks = (unsigned)max_units(g.n, sv.na, CHUNK_ROWS);
     const int rt = p.rank <= 16 ? 1 : 2, most = std::max(p.d_in, p.d_out);
     const AdapterGradArgs a = {{g.x, g.dy}, {g.ldx, g.lddy}, {v, u}, {p.d_in, p.d_out}, {apart, bpart}, {g.da, g.db}, sv.perm, sv.chunk0, sv.chunks,
-                               p.rank, p.n_adapters};
+                               p.rank, sv.na, of};
     const dim3 grid(chunks, (unsigned)((most + 16 * FewLoad<S>::CH - 1) / (16 * FewLoad<S>::CH)), 2 * (unsigned)((p.rank + 16 * rt - 1) / (16 * rt)));
     const bool vec = row_vec(g.x, g.ldx, p.dtype) && row_vec(g.dy, g.lddy, p.dtype);
     if (rt == 1 && vec) hipLaunchKernelGGL((adapter_grad_kernel<S, 1, true>), grid, dim3(WG), 0, s, a);
@@ -1023,8 +1096,10 @@ static int adapter_grads(const ProjectArgs &g, const SortView &sv, const float *
 int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hipStream_t s)
 {
     const rairs_projection_t &p = g.p;
-    const int np = dtype_pieces(p.dtype), na = p.n_adapters;
-    const bool adapters = na > 0, bf = p.dtype == RAIRS_BF16;
+    const int np = dtype_pieces(p.dtype);
+    const bool adapters = p.n_adapters > 0, bf = p.dtype == RAIRS_BF16;
+    UsedView used = {};
+    int na = p.n_adapters;          // or how many of them are laid out
     const int64_t opad = pad_to(p.d_out, ROWPROD_K);
     Carve w(ws);
     __bf16 *yroom = w.take<__bf16>(pack_room(p.dtype, g.n, p.d_out)), *wt = w.take<__bf16>((int64_t)p.d_in * opad * np);
@@ -1035,8 +1110,13 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     float *u = nullptr, *v = nullptr, *apart = nullptr, *bpart = nullptr;
     char *bt = nullptr;
     if (adapters) {
-        sv = sort_carve(w, g.adapter, g.n, na);
         side = side_of(bf ? SIDE_BF16 : SIDE_THREES, p.rank);
+        // (A as pieces, B turned)
+        if (g.n > 0 && numbers_used(p, g.n, 2ll * p.d_in * side.kpad + (int64_t)p.d_out * p.rank * dtype_width(p.dtype))) {
+            used = used_carve(w, p, g.adapter, g.n);
+            na = used.most;
+        }
+        sv = sort_carve(w, used.na ? used.number : g.adapter, g.n, na);
         vp = w.take<__bf16>(g.n * side.kpad);
         ap = w.take<__bf16>((int64_t)na * p.d_in * side.kpad);
         zero = w.take<__bf16>(side.kpad);
@@ -1055,16 +1135,17 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
     const bool use = adapters && g.adapter && g.n > 0;
     const PackLayout wto = pack_layout(p.d_in, opad, !bf);
     int rc = RAIRS_OK;
-    const SideJob job = {p.A, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, (int64_t)na * p.d_in, side, ap, zero, flags.found};
+    const SideJob job = {p.A, (int64_t)p.rank * p.d_in, 1, p.d_in, p.d_in, (int64_t)na * p.d_in, side, ap, zero, flags.found, used.orig};
     RowProd rp = {};
     PackJobs jobs = {};
     bool late = false;
     if (g.dx && g.n > 0) late = !batch_operand(g.dy, p.dtype, g.lddy, g.n, p.d_out, use ? sv.perm : nullptr, yroom, rp.Q, jobs);
     if (use) {
+        if (used.na && (rc = used_launch(used, s))) return rc;
         PrepArgs pa = {};
         pa.sort = sv;
         pa.rows = jobs;
-        pa.b = p.B; pa.bt = bt;
+        pa.b = p.B; pa.bt = bt; pa.orig = used.orig;
         pa.w = p.W; pa.d_in = p.d_in; pa.d_out = p.d_out; pa.r = p.rank; pa.opad = opad; pa.wto = wto;
         if (g.dx) {
             pa.wt = wt;
@@ -1072,16 +1153,16 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         }
         if ((rc = prep_launch(pa, p.dtype, s))) return rc;
         const int64_t units = max_units(g.n, na, UNIT_ROWS);
-        const ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, g.dx ? vp : nullptr, side, flags};
-        const ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, nullptr, side, {}};
+        const ShrinkArgs sa = {g.dy, bt, g.lddy, p.d_out, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, v, g.dx ? vp : nullptr, side, flags, used.orig, nullptr};
+        const ShrinkArgs su = {g.x, p.A, g.ldx, p.d_in, p.rank, p.scale, sv.perm, sv.units, sv.unit0 + na, u, nullptr, side, {}, used.orig, used.orig};
         const bool vec = row_vec(g.dy, g.lddy, p.dtype) && row_vec(bt, p.d_out, p.dtype) &&
                          (!g.da || (row_vec(g.x, g.ldx, p.dtype) && row_vec(p.A, p.d_in, p.dtype)));
         if ((rc = bf ? shrink_launch<__bf16>(sa, g.da ? &su : nullptr, units, vec, s) : shrink_launch<float>(sa, g.da ? &su : nullptr, units, vec, s)))
             return rc;
-        if (g.da && (rc = bf ? adapter_grads<__bf16>(g, sv, u, v, apart, bpart, s) : adapter_grads<float>(g, sv, u, v, apart, bpart, s))) return rc;
+        if (g.da && (rc = bf ? adapter_grads<__bf16>(g, sv, used.of, u, v, apart, bpart, s) : adapter_grads<float>(g, sv, used.of, u, v, apart, bpart, s))) return rc;
     } else if (g.da && adapters) {
-        if ((rc = rairs_launch_clear_rows(g.da, na, (int64_t)p.rank * p.d_in, (int64_t)p.rank * p.d_in, p.dtype, s))) return rc;
-        if ((rc = rairs_launch_clear_rows(g.db, na, (int64_t)p.rank * p.d_out, (int64_t)p.rank * p.d_out, p.dtype, s))) return rc;
+        if ((rc = rairs_launch_clear_rows(g.da, p.n_adapters, (int64_t)p.rank * p.d_in, (int64_t)p.rank * p.d_in, p.dtype, s))) return rc;
+        if ((rc = rairs_launch_clear_rows(g.db, p.n_adapters, (int64_t)p.rank * p.d_out, (int64_t)p.rank * p.d_out, p.dtype, s))) return rc;
     }
     if (!g.dx || g.n == 0) return RAIRS_OK;
     rowprod_sums(rp, np, np, opad);

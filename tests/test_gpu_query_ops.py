@@ -910,12 +910,14 @@ def test_an_empty_batch_clears_a_table_gradient_of_more_values_than_a_grid_has_t
     assert float(out[:, :d].abs().max()) == 0.0 and float(out[:, d:].min()) == 1.0
 
 
-def test_project_backward_of_the_most_adapters_of_the_largest_rank():
-    # B alone has 2^33 values: more tiles to turn than a grid has threads for
-    d_in, d_out, rank, na, n = 8, 16384, 128, 4096, 3
+@pytest.mark.parametrize("n", [3, 4096])
+def test_project_backward_of_the_most_adapters_of_the_largest_rank(n):
+    # B alone has 2^33 values: more tiles to turn than a grid has threads for, where all of it is turned
+    d_in, d_out, rank, na = 8, 16384, 128, 4096
     g = gen(4)
     a, b = torch.zeros(na, rank, d_in, dtype=BF16, device="cuda"), torch.zeros(na, d_out, rank, dtype=BF16, device="cuda")
-    ad = torch.tensor([na - 1, 0, na - 1], dtype=torch.int32)
+    ad = torch.full((n,), -1, dtype=torch.int32)
+    ad[:3] = torch.tensor([na - 1, 0, na - 1])
     for k in (0, na - 1):
         a[k], b[k] = torch.randn(rank, d_in, generator=g).to(BF16), torch.randn(d_out, rank, generator=g).to(BF16)
     w = torch.randn(d_out, d_in, generator=g).to(BF16)
@@ -1101,3 +1103,45 @@ def test_logprob_backward_of_a_table_that_is_taken_in_parts(tt):
         wt = G.t() @ q.double()
         err = (dt.double() - wt).abs()
         assert float((err - (1.01 * e + sum_err(n) + 2 ** -22) * (G.abs().t() @ q.double() + p.t() @ q.double() * scale * e)).max()) <= 1e-12
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n,d_in,d_out,rank,na,mix", [(300, 128, 256, 16, 2000, "many"), (70, 4096, 4096, 8, 300, "many"),
+                                                      (257, 100, 384, 33, 4096, "many"), (1100, 128, 256, 16, 4000, "one")])
+def test_far_more_adapters_than_rows(n, d_in, d_out, rank, na, mix, t):
+    # only the adapters that have rows are laid out; the others' gradients are zeros, and what they hold reaches nobody
+    g = gen(n + na)
+    x = torch.randn(n, d_in, generator=g).to(t)
+    w = (torch.randn(d_out, d_in, generator=g) / math.sqrt(d_in)).to(t)
+    dy = torch.randn(n, d_out, generator=g).to(t)
+    ad = torch.randint(-1, na + 1, (n,), generator=g, dtype=torch.int32)
+    ad[:3] = torch.tensor([0, na - 1, na - 1])
+    if mix == "one":
+        ad[3:] = na // 2
+    ids = sorted({int(k) for k in ad if 0 <= k < na})
+    few_a = (torch.randn(len(ids), rank, d_in, generator=g) / math.sqrt(d_in)).to(t)
+    few_b = torch.randn(len(ids), d_out, rank, generator=g).to(t)
+    few_s = torch.rand(len(ids), generator=g) + 0.5
+    a = torch.full((na, rank, d_in), float("nan"), dtype=t, device="cuda")
+    b = torch.full((na, d_out, rank), float("inf"), dtype=t, device="cuda")
+    s = torch.full((na,), float("nan"), device="cuda")
+    at = torch.tensor(ids, device="cuda")
+    a[at], b[at], s[at] = few_a.cuda(), few_b.cuda(), few_s.cuda()
+    small = torch.full((n,), -1, dtype=torch.int32)
+    for k, i in enumerate(ids):
+        small[ad == i] = k
+    p = binding.Projection(w.cuda(), a, b, s)
+    want, mag = exact_project(x, w, few_a, few_b, few_s, small)
+    y = p.project(x.cuda(), ad.cuda())
+    close(y, want, (sum_err(d_in) + sum_err(rank)) * mag + half(F32) * want.abs(), "y")
+    assert torch.equal(y, p.project(x.cuda(), ad.cuda())), "not the same bits again"
+    dx, da, db = p.backward(x.cuda(), ad.cuda(), dy.cuda())
+    gone = torch.ones(na, dtype=torch.bool, device="cuda")
+    gone[at] = False
+    assert not da[gone].any() and not db[gone].any()
+    # the projection that has these adapters alone
+    q = binding.Projection(w.cuda(), few_a.cuda(), few_b.cuda(), few_s.cuda())
+    mags = binding.Projection(w.abs().cuda(), few_a.abs().cuda(), few_b.abs().cuda(), few_s.cuda()).backward(x.abs().cuda(), small.cuda(), dy.abs().cuda())
+    err = 2 * (sum_err(n) + sum_err(d_in) + sum_err(d_out) + half(t))
+    for u, v, m in zip((dx, da[at], db[at]), q.backward(x.cuda(), small.cuda(), dy.cuda()), mags):
+        close(u, v.double().cpu(), err * 1.01 * m.double().cpu(), "gradient")

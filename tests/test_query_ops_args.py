@@ -228,3 +228,12 @@ def test_workspaces_do_not_grow_with_the_product_of_batch_and_table():
                     sums = max(8 * 4 * n * d, GB)
                     parts = 16 * n * (v // 256 // 16 + 64) if qt == 0 else 0
                     assert 0 < back <= 17 * GB + 3 * rows + sums + parts, (dtype, v, d, n, grad, back / GB)
+
+
+def test_workspaces_of_projections_grow_with_the_adapters_that_a_batch_can_have():
+    # 300 rows have at most 300 adapters, however many there are
+    lib = binding.load()
+    for dtype in (0, 1):
+        for f in (lib.rairs_project_workspace_bytes, lib.rairs_project_backward_workspace_bytes):
+            few, many = (f(C.byref(projection(d_in=1024, d_out=4096, rank=16, n_adapters=na, dtype=dtype)), C.c_int64(300)) for na in (300, 4096))
+            assert 0 < few <= many <= few + (1 << 20), (dtype, few, many)
