@@ -348,7 +348,9 @@ int rairs_pq_encode(const float *d_codebook, int d, int M, const float *d_vector
  * calls that may overlap.  Calls with workspaces and outputs of their own may overlap on any streams,
  * and all of them may be captured into a graph.  Inputs and outputs must not overlap in memory.
  * Row strides (ld_...) are in elements and at least the row's length.  Results do not depend on the
- * order in which workgroups run: the same call gives the same bits.
+ * order in which workgroups run: the same call gives the same bits.  A product of rows
+ * of which one has an infinity is not finite, but whether an infinity or NaN goes by the size of the call: in large ones
+ * fp32 rows go through the matrix cores in pieces, and infinity times a piece that is zero is NaN.
  */
 enum { RAIRS_F32 = 0, RAIRS_BF16 = 1, RAIRS_U8 = 2 };
 #define RAIRS_MAX_RANK 128          /* of an adapter */
@@ -456,7 +458,8 @@ int rairs_logprob(const rairs_table_t *t, const void *d_q, int64_t ld_q, int q_d
  *                     then be NULL too)
  * n <= RAIRS_MAX_GRAD_ROWS (parts of a larger batch one after the other; d_dtable is the parts' sum).
  * A target that is none or that the mask hides passes no gradient; a row that passes none at all (dlogp
- * and dentropy 0) may hold anything and gets zeros.
+ * and dentropy 0) may hold anything and gets zeros.  But a row of the table that some query sees and that is not finite
+ * reaches the gradients of all queries, and a query that passes a gradient and is not finite those of all rows.
  */
 size_t rairs_logprob_backward_workspace_bytes(const rairs_table_t *t, int64_t n, int q_dtype, int table_grad);
 int rairs_logprob_backward(const rairs_table_t *t, const void *d_q, int64_t ld_q, int q_dtype, int64_t n, const int64_t *d_targets,
