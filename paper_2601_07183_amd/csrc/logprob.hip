@@ -795,12 +795,12 @@ struct GradArgs {
 
 // G = scale (dlogp (1[v = t] - p) - dentropy p (log p + H)) in registers, in NP bf16 pieces: two for bf16 rows (16 bits: at
 // most 2^-16 of a value, so that a gradient is off by its own rounding and little else; one piece would be half the work of
-// both products, 1.8 ms instead of 3.0 for 4,095 x 65,537 x 1024, and 2.3e-3 off instead of 1.7e-3) or three (fp32), written for the
+// both products, 1.8 ms instead of 2.9 for 4,095 x 65,537 x 1024, and 2.3e-3 off instead of 1.7e-3) or three (fp32), written for the
 // products with the table (rows of queries) and with the queries (rows of the table).  Both sum over what
 // they have in common with the operand beside them, so their columns lie in the order that a wave holds
 // them in (ORDER_TABLE, ORDER_QUERIES): a lane's values are 32 or 8 bytes in a row, the lanes of a row 128.
-// (4,095 x 65,537 x 1024 bf16: 710 us in runs of tiles, 795 a tile at a time; the product alone would take 400, and 1.1 GB
-// of G are written in between.)
+// (4,095 x 65,537 x 1024 bf16: 960 us, of which the product alone would take 400 and 2.1 GB of G are written, 4.4 TB/s beside it;
+// with the pieces in planes of their own 957, but the products that read them 1,088 each instead of 1,038.)
 template <int NP, bool ENT>
 struct GradEpi {
     GradArgs a;
@@ -885,8 +885,8 @@ struct GradEpi {
                 }
             }
             if constexpr (NP == 2) {
-                // both pieces of a value in one register, where the value was (beside them they would not fit a wave's with the
-                // largest tile), and written by one copy of the code
+                // both pieces of a value in one register, where the value was: beside them they would not fit a wave's with the
+                // largest tile
 #pragma unroll
                 for (int i = 0; i < 4; i++)
 #pragma unroll
@@ -896,20 +896,18 @@ struct GradEpi {
                             const float x = acc.v[4 * b + i][j][r], hi = (float)(__bf16)x;
                             acc.v[4 * b + i][j][r] = __builtin_bit_cast(float, (v2bf){(__bf16)(x - hi), (__bf16)hi});
                         }
-#pragma unroll 1
-                for (int u = 0; u < 2; u++) {
-                    const uint32_t half = u ? 0x05040100u : 0x07060302u;      // of two registers: the upper halves are first pieces
-                    const auto pair = [&](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), half); };
-                    write<T>(
-                        u, p0 + 64 * b, q0, lane,
-                        [&](int i, int j) {
-                            const v4f x = acc.v[4 * b + i][j];
-                            return (v2u){pair(x[0], x[1]), pair(x[2], x[3])};
-                        },
-                        [&](int i, int r) {
-                            return (v2u){pair(acc.v[4 * b + i][0][r], acc.v[4 * b + i][1][r]), pair(acc.v[4 * b + i][2][r], acc.v[4 * b + i][3][r])};
-                        });
-                }
+                const auto pair = [](int u, float x, float y) {      // of two registers: the upper halves are first pieces
+                    return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), u ? 0x05040100u : 0x07060302u);
+                };
+                write<T, 2>(
+                    0, p0 + 64 * b, q0, lane,
+                    [&](int u, int i, int j) {
+                        const v4f x = acc.v[4 * b + i][j];
+                        return (v2u){pair(u, x[0], x[1]), pair(u, x[2], x[3])};
+                    },
+                    [&](int u, int i, int r) {
+                        return (v2u){pair(u, acc.v[4 * b + i][0][r], acc.v[4 * b + i][1][r]), pair(u, acc.v[4 * b + i][2][r], acc.v[4 * b + i][3][r])};
+                    });
             } else {
                 // pieces, one after the other: rounded off what is left
 #pragma unroll 1
@@ -924,9 +922,9 @@ struct GradEpi {
                                 o[i][j][r] = (__bf16)acc.v[4 * b + i][j][r];
                                 acc.v[4 * b + i][j][r] -= (float)o[i][j][r];
                             }
-                    write<T>(
-                        u, p0 + 64 * b, q0, lane, [&](int i, int j) { return __builtin_bit_cast(v2u, o[i][j]); },
-                        [&](int i, int r) { return __builtin_bit_cast(v2u, (v4bf){o[i][0][r], o[i][1][r], o[i][2][r], o[i][3][r]}); });
+                    write<T, 1>(
+                        u, p0 + 64 * b, q0, lane, [&](int, int i, int j) { return __builtin_bit_cast(v2u, o[i][j]); },
+                        [&](int, int i, int r) { return __builtin_bit_cast(v2u, (v4bf){o[i][0][r], o[i][1][r], o[i][2][r], o[i][3][r]}); });
                 }
             }
         }
@@ -939,28 +937,32 @@ struct GradEpi {
         if constexpr (NP == 3) return fmaf(z - st.m[j], a.scale, -st.lse[j]);
         else return z * a.scale - st.lse[j];
     }
-    // piece u of 64 x 64 values: by_row(i, j) a query's four, by_col(i, r) a row's
-    template <class T, class R, class C>
-    __device__ __forceinline__ void write(int u, int p, int q0, int lane, const R &by_row, const C &by_col) const
+    // pieces u0 .. u0 + U - 1 of 64 x 64 values: by_row(u, i, j) a query's four, by_col(u, i, r) a row's.  (The pieces of a line
+    // follow each other)
+    template <class T, int U, class R, class C>
+    __device__ __forceinline__ void write(int u0, int p, int q0, int lane, const R &by_row, const C &by_col) const
     {
         const int h = lane >> 4, c = lane & 15;
         if (a.g)
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 const int q = q0 + 16 * j + c;
-                __bf16 *to = a.g + (int64_t)q * a.gto.ld + (int64_t)(p / 32 + h / 2) * a.gto.block + u * a.gto.piece + 16 * (h & 1);
-                if (q < a.n) {
-                    *(v4u *)to = __builtin_shufflevector(by_row(0, j), by_row(1, j), 0, 1, 2, 3);
-                    *(v4u *)(to + 8) = __builtin_shufflevector(by_row(2, j), by_row(3, j), 0, 1, 2, 3);
-                }
+                __bf16 *to = a.g + (int64_t)q * a.gto.ld + (int64_t)(p / 32 + h / 2) * a.gto.block + u0 * a.gto.piece + 16 * (h & 1);
+                if (q < a.n)
+#pragma unroll
+                    for (int u = 0; u < U; u++) {
+                        *(v4u *)(to + 32 * u) = __builtin_shufflevector(by_row(u, 0, j), by_row(u, 1, j), 0, 1, 2, 3);
+                        *(v4u *)(to + 32 * u + 8) = __builtin_shufflevector(by_row(u, 2, j), by_row(u, 3, j), 0, 1, 2, 3);
+                    }
             }
         if (a.gt)
 #pragma unroll
             for (int i = 0; i < 4; i++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    __bf16 *to = a.gt + (int64_t)(p + 16 * i + 4 * h + r) * a.gtto.ld + (q0 / 32 + c / 8) * a.gtto.block + u * a.gtto.piece + 4 * (c & 7);
-                    *(v2u *)to = by_col(i, r);
+                    __bf16 *to = a.gt + (int64_t)(p + 16 * i + 4 * h + r) * a.gtto.ld + (q0 / 32 + c / 8) * a.gtto.block + u0 * a.gtto.piece + 4 * (c & 7);
+#pragma unroll
+                    for (int u = 0; u < U; u++) *(v2u *)(to + 32 * u) = by_col(u, i, r);
                 }
     }
 };
@@ -1285,7 +1287,7 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
 {
     const int np = dtype_pieces(a.qtype), tp = dtype_pieces(a.ttype);
     const int gp = np == 3 ? 3 : 2;                                   // pieces of the logits' gradient
-    const bool threes = tp == 3, again = np == 3;
+    const bool threes = tp == 3, twos = gp == 2, again = np == 3;
     const int64_t kpad = pad_to(a.d, threes ? 32 : ROWPROD_K), npad = pad_to(a.n, ROWPROD_K), dpad = pad_to(a.d, 4);
     const bool need_dt = a.dtable != nullptr, need_dq = a.dq != nullptr;
     // bytes of a row of the table: G both ways, the row as it lies and turned
@@ -1403,34 +1405,44 @@ int rairs_run_logprob_backward(const LogprobArgs &a, void *ws, size_t *bytes, hi
         ga.rows = rows_stats;
         ga.lse = a.lse_in; ga.entropy = a.entropy_in; ga.dlogp = a.dlogp; ga.dentropy = a.dentropy;
         ga.g = g; ga.gt = gt;
-        ga.gto = pack_layout(a.n, cpad, threes); ga.gtto = pack_layout(cpad, npad, threes);
+        ga.gto = twos ? pack_twos(cpad) : pack_layout(a.n, cpad, threes);
+        ga.gtto = twos ? pack_twos(npad) : pack_layout(cpad, npad, threes);
         const bool ent = a.dentropy != nullptr;
         if (np == 3) rc = ent ? grad_launch<3, true>(rp, ga, threes, s) : grad_launch<3, false>(rp, ga, threes, s);
         else rc = ent ? grad_launch<2, true>(rp, ga, threes, s) : grad_launch<2, false>(rp, ga, threes, s);
         if (rc) return rc;
+        // (products of G with pieces of a table or of queries)
+        const auto sums_of = [&](RowProd &rp, int pieces, int64_t values) {
+            if (!twos) return rowprod_sums(rp, pieces, gp, values);
+            rowprod_pieces(rp, 1, 1);
+            rp.ksteps = (int)(values / 32);
+        };
+        const auto launch = [&](RowProd &rp, const StoreEpi &e) {
+            return threes ? rowprod_launch_any<ROW_THREES>(rp, e, s) : twos ? rowprod_launch_any<ROW_TWOS>(rp, e, s) : rowprod_launch_any(rp, e, s);
+        };
         RowProd pq = {}, pt = {};
         StoreEpi eq = {}, et = {};
         if (need_dq) {
             const PackLayout tto = pack_layout(a.d, cpad, threes);
-            rowprod_sums(pq, tp, gp, cpad);
+            sums_of(pq, tp, cpad);
             pq.P = RowOperand{tcols, tto.ld, tto.piece, a.d, nullptr, nullptr};
-            pq.Q = RowOperand{g, ga.gto.ld, ga.gto.piece, a.n, nullptr, nullptr};
+            pq.Q = RowOperand{g, ga.gto.ld, twos ? 0 : ga.gto.piece, a.n, nullptr, nullptr};
             pq.splits = (int)splits;
             eq = StoreEpi{sums, dpad, a.n * dpad, a.d, a.n, nullptr, 0, v0 > 0};
         }
         if (need_dt) {
-            rowprod_sums(pt, np, gp, npad);
+            sums_of(pt, np, npad);
             pt.P = RowOperand{qcols, qto.ld, qto.piece, a.d, nullptr, nullptr};
-            pt.Q = RowOperand{gt, ga.gtto.ld, ga.gtto.piece, rows, nullptr, nullptr};
+            pt.Q = RowOperand{gt, ga.gtto.ld, twos ? 0 : ga.gtto.piece, rows, nullptr, nullptr};
             et = StoreEpi{(char *)a.dtable + v0 * a.lddt * dtype_width(a.ttype), a.lddt, 0, a.d, rows, nullptr, a.ttype == RAIRS_BF16, 0};
         }
         // (both of small tiles: side by side; fp32 1,000 x 1,024 x 96 22.5 us, one after the other 26.6)
         if (need_dq && need_dt && rowprod_size(a.d, a.n, (int)splits) == 0 && rowprod_size(a.d, rows) == 0) {
-            if ((rc = threes ? rowprod_launch_pair<TileU, ROW_THREES>(pq, eq, pt, et, s) : rowprod_launch_pair<TileS>(pq, eq, pt, et, s))) return rc;
+            if ((rc = threes ? rowprod_launch_pair<TileU, ROW_THREES>(pq, eq, pt, et, s) : rowprod_launch_pair<TileS, ROW_TWOS>(pq, eq, pt, et, s))) return rc;
             continue;
         }
-        if (need_dq && (rc = threes ? rowprod_launch_any<ROW_THREES>(pq, eq, s) : rowprod_launch_any(pq, eq, s))) return rc;
-        if (need_dt && (rc = threes ? rowprod_launch_any<ROW_THREES>(pt, et, s) : rowprod_launch_any(pt, et, s))) return rc;
+        if (need_dq && (rc = launch(pq, eq))) return rc;
+        if (need_dt && (rc = launch(pt, et))) return rc;
     }
     if (need_dq) {
         hipLaunchKernelGGL(join_splits_kernel, dim3(capped(a.n * dpad / 4)), dim3(WG), 0, s, sums, (int)splits, a.n, a.d,

@@ -30,6 +30,8 @@ static inline PackLayout pack_layout(int64_t rows, int64_t kpad, bool threes)
 {
     return threes ? PackLayout{3 * kpad, 32, 96} : PackLayout{kpad, rows * kpad, 32};
 }
+// two pieces together in every 32 values
+static inline PackLayout pack_twos(int64_t kpad) { return PackLayout{2 * kpad, 32, 64}; }
 // rows of a matrix as bf16 pieces with rows of kpad values, zero from `cols` on (and where live says so)
 // (perm: row r is src's row perm[r]; flags[i], if given: cleared if `clear`, else set if piece i + 1 of any value is
 // not zero)

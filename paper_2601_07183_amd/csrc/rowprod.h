@@ -11,6 +11,9 @@
 // with adapters: 49 us, 66 as six sums one after the other).  The products with smaller factors have sums of their own, added at the end, so that they
 // do not round the large one's.
 //
+// Rows of bf16 against values in two pieces ("twos": the gradient of the logits) go by steps of 32 values too, with both
+// pieces of Q in LDS and P once.
+//
 // Small products of fp32 rows take the rows as they are and the fp32 matrix instruction (a sixteenth of the
 // bf16 rate, against six products of pieces and the packing): lengths, strides and steps are then counted in
 // units of two bytes all the same, so that a step is 32 values.
@@ -35,7 +38,7 @@ typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 
 // Rows of bf16 pieces: value k of piece i of row r at p[i * piece + r * ld + k]; ld a multiple of 8, below
 // 2^22, p 16-byte aligned, k up to a multiple of ROWPROD_K readable (zero beyond the row).  Rows of fp32: units of
-// two bytes in place of values.  Threes: 32 values of piece 0, of piece 1, of piece 2, then the next 32 values.
+// two bytes in place of values.  Threes: 32 values of piece 0, of piece 1, of piece 2, then the next 32 values; twos likewise.
 struct RowOperand {
     const __bf16 *p;
     int64_t ld, piece;
@@ -123,45 +126,47 @@ struct RowAcc {
     float nrm[T::PT];               // ROW_NORM: this lane's part of the squared norm of row 16 i + (lane & 15) of P
 };
 
-// with adapters; fp32 rows; norms wanted; three pieces together
-enum { ROW_ADAPT = 1, ROW_F32 = 2, ROW_NORM = 4, ROW_THREES = 8 };
+// with adapters; fp32 rows; norms wanted; three pieces together; two pieces of Q together
+enum { ROW_ADAPT = 1, ROW_F32 = 2, ROW_NORM = 4, ROW_THREES = 8, ROW_TWOS = 16 };
 // bytes of one LDS buffer, loads that every wave makes for it
 template <class T, int FLAGS>
 struct RowStep {
-    static constexpr bool THREES = FLAGS & ROW_THREES;
-    static constexpr int BYTES = THREES ? T::BYTES * 3 / 2 : T::BYTES, LOADS = THREES ? T::LEAST * 3 / 2 : T::LEAST;
+    static constexpr bool THREES = FLAGS & ROW_THREES, TWOS = FLAGS & ROW_TWOS;
+    static constexpr int PL = TWOS ? T::LP / 2 : T::LP, PB = TWOS ? 64 : 128;             // loads of P, bytes of a row of P
+    static constexpr int BYTES = THREES ? T::BYTES * 3 / 2 : T::BP * PB + T::BQ * 128, LOADS = THREES ? T::LEAST * 3 / 2 : T::LEAST - T::LP + PL;
     static constexpr int LP2 = THREES ? T::LP / 2 : 1, LQ2 = THREES ? T::LQ / 2 : 1;      // loads of third pieces
     static constexpr int WAVES = T::NT == 256 && T::ST * BYTES > 80 * 1024 ? 1 : 2;       // per SIMD: four waves that have a CU to themselves
     static_assert(!THREES || (!T::SOME_Q && T::LP % 2 == 0 && T::LQ % 2 == 0), "");
+    static_assert(!TWOS || (!THREES && T::LP % 2 == 0), "");
 };
 
-// Threes in LDS: pieces 0 and 1 of a row as any row's 128 bytes, then the third pieces, two rows to 128 bytes: slot s of
-// pair r holds chunk s ^ (r & 3) of the two.
+// Threes in LDS: pieces 0 and 1 of a row as any row's 128 bytes, then the third pieces (`at` bytes into the row's), two rows to
+// 128 bytes: slot s of pair r holds chunk s ^ (r & 3) of the two.
 template <class T, int L>
-static __device__ __forceinline__ void rowprod_thirds(int64_t r0, int64_t rows, int64_t ld, int tid, uint32_t (&o)[L], int64_t (&row)[L])
+static __device__ __forceinline__ void rowprod_thirds(int64_t r0, int64_t rows, int64_t ld, int tid, uint32_t (&o)[L], int64_t (&row)[L], int at = 128)
 {
     const uint32_t last = (uint32_t)(rows - 1 - r0 < 0x7FFFFFFF ? rows - 1 - r0 : 0x7FFFFFFF);
 #pragma unroll
     for (int i = 0; i < L; i++) {
         const uint32_t pair = i * (T::NT / 8) + (tid >> 3), x = (tid & 7) ^ (pair & 3), r = 2 * pair + (x >> 2);
         row[i] = r0 + r;
-        o[i] = (r < last ? r : last) * (uint32_t)(ld * 2) + 128 + (x & 3) * 16;
+        o[i] = (r < last ? r : last) * (uint32_t)(ld * 2) + at + (x & 3) * 16;
     }
 }
 
 // one step's 16-byte chunks of both operands, straight into LDS: a row's place is a 32-bit offset from an
 // address that the workgroup shares
-template <class T>
-static __device__ __forceinline__ void rowprod_fetch(char *buf, const char *pb, const uint32_t (&po)[T::LP], const char *qb,
+template <class T, int PL>
+static __device__ __forceinline__ void rowprod_fetch(char *buf, const char *pb, const uint32_t (&po)[PL], const char *qb,
                                                      const uint32_t (&qo)[T::LQ], int wave)
 {
 #pragma unroll
-    for (int i = 0; i < T::LP; i++)
+    for (int i = 0; i < PL; i++)
         __builtin_amdgcn_global_load_lds((global_void *)(pb + po[i]), (lds_void *)(buf + (i * T::NT + wave * 64) * 16), 16, 0, 0);
     if (!T::SOME_Q || wave * 64 < T::BQ * 8)                          // uniform
 #pragma unroll
         for (int i = 0; i < T::LQ; i++)
-            __builtin_amdgcn_global_load_lds((global_void *)(qb + qo[i]), (lds_void *)(buf + T::BP * 128 + (i * T::NT + wave * 64) * 16), 16,
+            __builtin_amdgcn_global_load_lds((global_void *)(qb + qo[i]), (lds_void *)(buf + (PL * T::NT + i * T::NT + wave * 64) * 16), 16,
                                              0, 0);
 }
 
@@ -269,6 +274,33 @@ static __device__ __forceinline__ void rowprod_step_threes(const char *buf, int 
     mul(a1, b0, low);
 }
 
+// One step of twos: 32 values, of P once and of Q in both pieces, each value of P against two of Q.
+template <class T, class F>
+static __device__ __forceinline__ void rowprod_step_twos(const char *buf, int wp, int wq, int lane, RowAcc<T> &acc, const F &fetch)
+{
+    const int r = lane & 15, h = lane >> 4;
+    const char *pa = buf + wp * T::PT * 1024 + ((4 * (r & 1) + h) ^ ((r >> 1) & 3)) * 16 + (r >> 1) * 128;
+    const char *qa = buf + T::BP * 64 + wq * T::QT * 2048 + r * 128;
+    v8bf a[T::PT], b[T::QT];
+#pragma unroll
+    for (int i = 0; i < T::PT; i++) a[i] = *(const v8bf *)(pa + i * 1024);
+#pragma unroll
+    for (int u = 1; u >= 0; u--) {                                    // (the smaller products first)
+#pragma unroll
+        for (int j = 0; j < T::QT; j++) b[j] = *(const v8bf *)(qa + j * 2048 + ((4 * u + h) ^ (r & 7)) * 16);
+#pragma unroll
+        for (int x = 0; x < T::PT * T::QT; x++) {
+            if (u == 1 && x == T::PT * T::QT / 2) {
+                __builtin_amdgcn_sched_barrier(0);
+                fetch();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const int i = T::PT >= T::QT ? x % T::PT : x / T::QT, j = T::PT >= T::QT ? x / T::PT : x % T::QT;
+            acc.v[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc.v[i][j], 0, 0, 0);
+        }
+    }
+}
+
 // A workgroup's q tile and run of p tiles.  Workgroups are handed out round robin over the eight XCDs, each with
 // its own L2 cache: one XCD takes consecutive ids, and ids go over a band of q tiles, then to the next run, so that
 // what runs on an XCD at a time is about a square of tiles, whose rows its cache fetches once.
@@ -311,9 +343,11 @@ static __device__ __forceinline__ void rowprod_rows(int64_t r0, int64_t rows, in
 template <class T, class Epi, int FLAGS>
 static __device__ __forceinline__ void rowprod_run_tiles(const RowProd &a, const Epi &epi, uint32_t block)
 {
-    constexpr bool ADAPT = FLAGS & ROW_ADAPT, THREES = FLAGS & ROW_THREES;
+    constexpr bool ADAPT = FLAGS & ROW_ADAPT, THREES = FLAGS & ROW_THREES, TWOS = FLAGS & ROW_TWOS;
+    static_assert(!TWOS || !ADAPT, "");
     constexpr int BYTES = RowStep<T, FLAGS>::BYTES, LP2 = RowStep<T, FLAGS>::LP2, LQ2 = RowStep<T, FLAGS>::LQ2;
-    constexpr int STEP = THREES ? 192 : ROWPROD_K * 2;                // bytes of a row per step
+    constexpr int STEP = THREES ? 192 : ROWPROD_K * 2, PSTEP = TWOS ? 64 : STEP;          // bytes of a row per step, of P's
+    constexpr int PL = RowStep<T, FLAGS>::PL;
     extern __shared__ __align__(16) char rowprod_lds[];
     int run, qt, split;
     if (!rowprod_tile(a, block, run, qt, split)) return;
@@ -324,8 +358,16 @@ static __device__ __forceinline__ void rowprod_run_tiles(const RowProd &a, const
 
     // what is fetched, a step at a time, ahead of what is multiplied: the run's tiles one after the other, then (the run is
     // one tile) the adapters of the tile's rows
-    uint32_t po[T::LP], qo[T::LQ];
-    rowprod_rows<T>((int64_t)t0 * T::BP, a.P.rows, a.P.ld, tid, po);
+    uint32_t po[PL], qo[T::LQ];
+    const auto place_p = [&](int tile) {
+        if constexpr (TWOS) {
+            int64_t row[PL];
+            rowprod_thirds<T>((int64_t)tile * T::BP, a.P.rows, a.P.ld, tid, po, row, 0);
+        } else {
+            rowprod_rows<T>((int64_t)tile * T::BP, a.P.rows, a.P.ld, tid, po);
+        }
+    };
+    place_p(t0);
     const char *pb = (const char *)(a.P.p + (int64_t)t0 * T::BP * a.P.ld), *qb = (const char *)a.Q.p;
     const uint32_t chunk = ((tid & 7) ^ ((tid >> 3) & 7)) * 16;
     if (a.Q.perm) {
@@ -395,7 +437,7 @@ static __device__ __forceinline__ void rowprod_run_tiles(const RowProd &a, const
         if constexpr (ADAPT) base = f_tile < t1;
         if (base) {
             const int64_t ps = (sp >> (4 * seg)) & 15, qs = (sq >> (4 * seg)) & 15;
-            const char *pk = pb + ps * a.P.piece * 2 + (int64_t)k * STEP, *qk = qb + qs * a.Q.piece * 2 + (int64_t)k * STEP;
+            const char *pk = pb + ps * a.P.piece * 2 + (int64_t)k * PSTEP, *qk = qb + qs * a.Q.piece * 2 + (int64_t)k * STEP;
             rowprod_fetch<T>(f_buf, pk, po, qk, qo, wave);
             if constexpr (THREES) {
                 rowprod_fetch_thirds<T>(f_buf + T::BYTES, pk, po3, wave);
@@ -411,7 +453,7 @@ static __device__ __forceinline__ void rowprod_run_tiles(const RowProd &a, const
                         f_step = s0; seg = seg0; k = k0;
                         pb += (int64_t)T::BP * a.P.ld * 2;
                         if (f_tile + 1 == a.ptiles) {
-                            rowprod_rows<T>((int64_t)f_tile * T::BP, a.P.rows, a.P.ld, tid, po);
+                            place_p(f_tile);
                             if constexpr (THREES) rowprod_thirds<T>((int64_t)f_tile * T::BP, a.P.rows, a.P.ld, tid, po3, prow3);
                         }
                     } else if (!ADAPT || f_ad < 0) {
@@ -484,6 +526,7 @@ static __device__ __forceinline__ void rowprod_run_tiles(const RowProd &a, const
             // (this also says that every wave is past the step before, whose buffer the next fetch writes)
             rowprod_landed<(T::ST - 2) * RowStep<T, FLAGS>::LOADS>();
             if constexpr (THREES) rowprod_step_threes<T>(buf, wp, wq, lane, acc, low, fetch);
+            else if constexpr (TWOS) rowprod_step_twos<T>(buf, wp, wq, lane, acc, fetch);
             else rowprod_step<T, FLAGS>(buf, wp, wq, lane, acc, fetch);
             buf = buf == rowprod_lds + (T::ST - 1) * BYTES ? rowprod_lds : buf + BYTES;
             done++;
