@@ -115,6 +115,10 @@ typedef RowTile<4, 1, 4, 1, 4> TileF1;      // 256 x 16
 typedef RowTile<4, 2, 4, 1, 4> TileF2;      // 256 x 32
 typedef RowTile<4, 4, 4, 1, 3> TileF4;      // 256 x 64
 static inline int64_t rowprod_tiles(int64_t p, int64_t q, int side) { return ((p + side - 1) / side) * ((q + side - 1) / side); }
+// The size by the workgroups there are for 256 CUs, measured on either side of both limits (rows x K x columns, us, large / middle /
+// small, bf16; fp32 in three pieces): 8,191 x 1000 x 2048, 256 tiles of 256, 50 / 68 / 84; 170 / 189 / 231.  4,096 x 1000 x 2048, 128 of
+// them, 46 / 42 / 50; 92 / 100 / 126 (three pieces' large tile is half that size: 256 x 128 would still do).  2,999 x 1000 x 960, 192
+// tiles of 128, 42 / 27 / 28; 83 / 55 / 62.  1,024 x 1000 x 1024, 64 of them, 37 / 21 / 16; 79 / 51 / 34.
 static inline int rowprod_size(int64_t p, int64_t q, int splits = 1)
 {
     return rowprod_tiles(p, q, 256) * splits >= 200 ? 2 : rowprod_tiles(p, q, 128) * splits >= 160 ? 1 : 0;
