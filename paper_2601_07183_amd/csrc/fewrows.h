@@ -1,8 +1,9 @@
 // Products of a few rows with many that lie otherwise than rowprod.h's tiles need them (any stride, alignment and
 // length; bytes), and products that are small altogether: a wave takes 16 PT of the many rows and all of the few,
 // and both operands go from memory straight into the matrix instruction's registers.  A load costs a cache access for
-// each lane's row, which is what bounds these calls (16 queries against 131,071 x 1024 bf16: 83 us, by tiles 71; 1M x 128
-// fp32 and one query: 126 us, by tiles 119); the few come from the caches.  A lane holds 16 bytes of a row
+// each lane's row, which is what bounds these calls (16 queries against 131,071 x 1024 bf16: 80 us, by tiles 65; 64 queries
+// against 1M x 128 fp32: 321 us, by tiles 279; 1M x 128 bytes, which have no tiles here: 80 us for one query, 100 for 16, 237
+// for 64); the few come from the caches.  A lane holds 16 bytes of a row
 // per load, so that four lanes read 64 consecutive bytes of it, and the four loads in flight a line.
 //
 // bf16 rows use the 16 x 16 x 32 instruction, fp32 rows the fp32 one (16 x 16 x 4: 64 operations a cycle

@@ -1033,8 +1033,8 @@ static unsigned capped(int64_t threads) { return (unsigned)std::min<int64_t>((th
 // ---- launches ----------------------------------------------------------------------------------------
 
 // Up to here a tile has all of the queries, so that the table is read once and as it is, and a query is finished by a
-// whole workgroup.  So / by the larger tiles, us: 64 queries, 131,071 x 1024 bf16 74 / 133, 1M x 128 fp32 275 / 609; one
-// query 66 / 131 and 134 / 594.
+// whole workgroup.  So / by the larger tiles, us: 64 queries, 131,071 x 1024 bf16 72 / 133, 1M x 128 fp32 279 / 619, bytes
+// 237 / 283; one query 64 / 125, 125 / 596 and 81 / 279.
 #define FEW_ROWS 64
 
 static int lies_vec(const void *p, int dtype, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld * dtype_width(dtype) % 16 == 0; }

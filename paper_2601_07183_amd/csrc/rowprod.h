@@ -109,7 +109,7 @@ typedef RowTile<4, 4, 4, 2, 2> TileT;       // 256 x 128, 8 waves: what threes h
 typedef RowTile<2, 2, 2, 2, 3> TileU;       // 64 x 64: and for TileS (two workgroups a CU)
 typedef RowTile<4, 4, 2, 2, 2> TileW;       // 128 x 128, 4 waves: 64 x 64 to a wave, for epilogues that want that
 // few queries, whose rows' loads are what counts: about 100 KB of them on the way in a workgroup that has a CU to
-// itself (two workgroups with half of that each: the same time).  1M x 128 fp32 and one query: 92 us, 5.6 TB/s, with the
+// itself (two workgroups with half of that each: the same time).  1M x 128 fp32 and one query: 94 us, 5.5 TB/s, with the
 // norms; 131,071 x 1024 bf16 and 16 queries: 46 us, 5.8 TB/s.
 typedef RowTile<4, 1, 4, 1, 4> TileF1;      // 256 x 16
 typedef RowTile<4, 2, 4, 1, 4> TileF2;      // 256 x 32
