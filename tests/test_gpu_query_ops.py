@@ -1145,3 +1145,61 @@ def test_far_more_adapters_than_rows(n, d_in, d_out, rank, na, mix, t):
     err = 2 * (sum_err(n) + sum_err(d_in) + sum_err(d_out) + half(t))
     for u, v, m in zip((dx, da[at], db[at]), q.backward(x.cuda(), small.cuda(), dy.cuda()), mags):
         close(u, v.double().cpu(), err * 1.01 * m.double().cpu(), "gradient")
+
+
+@pytest.mark.parametrize("tt", [F32, BF16, U8])
+@pytest.mark.parametrize("n,v,d", [(6, 333, 40), (100, 700, 64), (300, 20_000, 72)])
+@pytest.mark.parametrize("pad,offset", [(1, 0), (16, 0), (0, 3)])
+def test_logprob_backward_of_strided_rows_and_of_one_side_alone(n, v, d, pad, offset, tt):
+    q, table, targets, scale, mask = logprob_data(n, v, d, tt, n + d, "shared")
+    da, db = torch.randn(n, generator=gen(1)).cuda(), torch.randn(n, generator=gen(2)).cuda()
+    words, tg = pack(mask), targets.cuda()
+    r = binding.logprob(q.cuda(), table.cuda(), tg, scale=scale, live=words)
+    kw = dict(scale=scale, live=words, entropy=r.entropy, dentropy=db)
+    dq, dt = binding.logprob_backward(q.cuda(), table.cuda(), tg, r.lse, da, table_grad=tt != U8, **kw)
+    got = binding.logprob_backward(strided(q, pad, offset), strided(table, pad, offset), tg, r.lse, da, table_grad=tt != U8, **kw)
+    # (where rows lie decides how they are read, not what is multiplied)
+    assert torch.equal(got[0], dq) and (dt is None or torch.equal(got[1], dt))
+    only = binding.logprob_backward(q.cuda(), table.cuda(), tg, r.lse, da, **kw)
+    assert only[1] is None
+    w = exact_logprob(q, table, targets, scale, mask, 1)
+    _, _, mag, T = exact_backward(q, table, targets, scale, mask, da.cpu(), db.cpu(), w)
+    # (without the table's gradient a sum may be cut otherwise)
+    close(only[0], dq.double().cpu(), 2 * (sum_err(v) * (mag @ T.abs()) + half(q.dtype) * dq.double().cpu().abs()), "dq alone")
+    if tt != U8:
+        only = binding.logprob_backward(q.cuda(), table.cuda(), tg, r.lse, da, q_grad=False, table_grad=True, **kw)
+        assert only[0] is None
+        close(only[1], dt.double().cpu(), 2 * (sum_err(n) * (mag.t() @ q.double().abs()) + half(tt) * dt.double().cpu().abs()), "dtable alone")
+
+
+def test_calls_that_overlap_on_two_streams():
+    # two chains at once, each with workspaces and results of its own, give what they give one after the other
+    def make(seed, t):
+        g = gen(seed)
+        x, w, a, b, s, ad = projection_data(700, 96, 64, 8, 40, t, seed)
+        table = torch.randn(30_000, 64, generator=g).to(t).cuda()
+        targets = torch.randint(0, 30_000, (700,), generator=g).cuda()
+        da = torch.randn(700, generator=g).cuda()
+        p = binding.Projection(w.cuda(), a.cuda(), b.cuda(), s.cuda())
+        x, ad = x.cuda(), ad.cuda()
+
+        def chain(stream=None):
+            y = p.project(x, ad, out_dtype=t, stream=stream)
+            r = binding.logprob(y, table, targets, scale=0.2, top=6, stream=stream)
+            dy, dt = binding.logprob_backward(y, table, targets, r.lse, da, scale=0.2, table_grad=True, stream=stream)
+            return (y, *r, dy, dt, *p.backward(x, ad, dy, stream=stream))
+
+        return chain
+
+    chains = [make(3, F32), make(4, BF16)]
+    want = [c() for c in chains]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i in (0, 1):
+            got[i].append(chains[i](streams[i]))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for one in got[i]:
+            assert all(torch.equal(u, v) for u, v in zip(one, want[i]))
