@@ -1165,7 +1165,7 @@ int rairs_run_project_backward(const ProjectArgs &g, void *ws, size_t *bytes, hi
         if ((rc = rairs_launch_clear_rows(g.db, p.n_adapters, (int64_t)p.rank * p.d_out, (int64_t)p.rank * p.d_out, p.dtype, s))) return rc;
     }
     if (!g.dx || g.n == 0) return RAIRS_OK;
-    rowprod_sums(rp, np, np, opad);
+    rowprod_sums(rp, np, np, bf ? opad : pad_to(p.d_out, 32));        // (as far as the batch's rows are laid out)
     if (!use && (rc = rairs_launch_pack(jobs, s))) return rc;
     if (!use && (rc = rairs_launch_pack_cols(p.W, p.dtype, p.d_in, p.d_out, p.d_in, nullptr, ORDER_SAME, wt, opad, wto, s))) return rc;
     rp.P = RowOperand{wt, wto.ld, 0, p.d_in, nullptr, nullptr};

@@ -1203,3 +1203,44 @@ def test_calls_that_overlap_on_two_streams():
     for i in (0, 1):
         for one in got[i]:
             assert all(torch.equal(u, v) for u, v in zip(one, want[i]))
+
+
+@pytest.fixture
+def scratch_of_nan(monkeypatch):
+    """Workspaces whose every byte is 255: NaN as fp32 and bf16, -1 as a word."""
+    def workspace(need, device):
+        ws = torch.full((max(need, 1),), 255, dtype=U8, device=device)
+        return ws, C.c_void_p(ws.data_ptr() if need else 0), C.c_size_t(need)
+
+    monkeypatch.setattr(binding, "_workspace", workspace)
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n,d_in,d_out,rank,na", [(3, 96, 32, 2, 8), (70, 40, 1, 3, 4), (300, 65, 200, 17, 9), (300, 32, 65, 8, 900), (2100, 200, 33, 4, 3), (20_000, 7, 32, 3, 4)])
+def test_projections_do_not_read_what_the_scratch_held(n, d_in, d_out, rank, na, t, scratch_of_nan):
+    x, w, a, b, s, ad = projection_data(n, d_in, d_out, rank, na, t, n + d_out)
+    dy = torch.randn(n, d_out, generator=gen(n)).to(t)
+    # a row that is not finite leaves the gradients of the rows beside it alone, also where rows are filled up
+    dy[n // 2] = float("inf")
+    x[n // 2] = float("nan")
+    ad[n // 2] = -1
+    p = binding.Projection(w.cuda(), a.cuda(), b.cuda(), s.cuda())
+    keep = torch.arange(n, device="cuda") != n // 2
+    for adapter in (ad.cuda(), None):
+        y = p.project(x.cuda(), adapter)
+        dx, da, db = p.backward(x.cuda(), adapter, dy.cuda())
+        assert y[keep].isfinite().all() and dx[keep].isfinite().all() and not dx[~keep].isfinite().any()
+        assert da.isfinite().all() and db.isfinite().all()
+
+
+@pytest.mark.parametrize("tt", [F32, BF16, U8])
+@pytest.mark.parametrize("n,v,d,top,live", [(1, 5, 1, 3, None), (6, 333, 33, 9, "shared"), (64, 1000, 96, 5, "rows"), (65, 129, 1, 10, None),
+                                            (130, 700, 65, 64, "shared"), (300, 20_000, 40, 1, "rows"), (520, 26_000, 24, 2, None)])
+def test_log_probabilities_do_not_read_what_the_scratch_held(n, v, d, top, live, tt, scratch_of_nan):
+    q, table, targets, scale, mask = logprob_data(n, v, d, tt, n + v + d, live)
+    words, tg, da = pack(mask), targets.cuda(), torch.randn(n, generator=gen(1)).cuda()
+    r = binding.logprob(q.cuda(), table.cuda(), tg, scale=scale, top=top, live=words)
+    check_logprob(r, exact_logprob(q, table, targets, scale, mask, top), v, top)
+    dq, dt = binding.logprob_backward(q.cuda(), table.cuda(), tg, r.lse, da, scale=scale, live=words, entropy=r.entropy, dentropy=da,
+                                      table_grad=tt != U8)
+    assert dq.isfinite().all() and (dt is None or dt.isfinite().all())
